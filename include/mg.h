@@ -206,6 +206,116 @@ mg_status mg_prefill(mg_ctx* ctx, int n_items, const int32_t* tokens, const int3
 mg_status mg_advance(mg_ctx* ctx, int B, const int32_t* emitted, int32_t* tokens, int32_t* positions,
                      void* stream);
 
+/* ---- (5) batch planning and an 8-bit paged K/V cache -------------------------------------
+ *
+ * For serving programs whose decode is bound by the bytes of the K/V cache: the cache of a
+ * layer at one byte a value, with the append that quantises into it, the attention that reads
+ * it, and the plan of a batch's pages and slots.  None of these calls needs a context; they
+ * keep no state, allocate nothing, and can be captured into a HIP graph (a replay reads the
+ * lengths, tables and slots that the device buffers then hold).  Calls on different streams may
+ * run at once where they write different buffers (pages, workspaces and outputs).
+ *
+ * A page holds 16 positions.  Slot = page * 16 + position % 16.  The cache of one layer:
+ *   codes  [n_pages][Hkv][K|V][16 * hd]  e4m3 values (OCP: 4 exponent bits, 3 mantissa bits,
+ *          largest 448, no infinity, 0x7f / 0xff NaN)
+ *   scales [n_pages][Hkv][K|V]           b = 0..255; a code stands for its value * 2^(b - 127)
+ * so one scale serves 16 positions of one KV head.  Order inside a page of a head, chosen so
+ * that a wave reads matrix operands as contiguous 1 KiB runs:
+ *   K: position t, feature d = 64 h + 16 g + j at byte ((h * 4 + g) * 16 + t) * 16 + j
+ *   V: position t = 4 g + i, feature d = 64 h + 16 c + m at byte ((h * 4 + g) * 16 + m) * 16 + 4 c + i
+ * A value read back is exact in bf16.  A zeroed pool is an empty cache. */
+typedef struct {
+    uint8_t* codes;   /* [device], 16-byte aligned */
+    uint8_t* scales;  /* [device] */
+    int32_t n_pages;  /* 1..2^27 - 1 */
+    int32_t n_kv_heads;
+    int32_t head_dim; /* 64 or 128 */
+} mg_kv8_cache;
+
+/* Bytes of the two buffers of one layer (0 if the shape is unsupported). */
+size_t mg_kv8_code_bytes(int n_pages, int n_kv_heads, int head_dim);
+size_t mg_kv8_scale_bytes(int n_pages, int n_kv_heads, int head_dim);
+
+/* Pages, slots and per-token lists of a batch from its requests' lengths, in one launch.
+ * Row b holds ctx_len[b] positions and asks for n_new[b] more.  It is valid when both are >= 0
+ * and their sum fits its page-table row (16 * max_pages_per_row positions).  Rows are admitted
+ * in order: a valid row is admitted when the new pages of all valid rows up to and including it
+ * are at most *n_free and their new tokens at most max_tokens (the first that does not fit stops
+ * the rows behind it; an invalid row stops nobody).  Every admitted row gets pages for positions
+ * ctx_len[b] .. ctx_len[b] + n_new[b] - 1: those it lacks are taken from the end of
+ * free_pages[0 .. *n_free) in row order and written to its entries of page_table; all other
+ * entries are left as they were.
+ *   cu_new [B + 1]: tokens of the admitted rows before row b;  lens [B]: positions after the call
+ *   (ctx_len[b] where not admitted, 0 where that is negative);  admitted [B] 0 or 1;
+ *   positions, rows, slots [max_tokens]: of every new token, row by row, positions ascending
+ *   (the item lists of mg_prefill; the slots of mg_kv8_append), -1 behind the last;
+ *   *n_left: free pages that remain, so that free_pages[0 .. *n_left) is the next call's list.
+ * free_pages must be distinct pages that no row holds.  1 <= B <= 1024.  All pointers [device];
+ * n_left must not be n_free, nor lens be ctx_len (blocks of the launch read one while others
+ * write): MG_ERR_ARG. */
+mg_status mg_batch_plan(int B, int max_pages_per_row, const int32_t* ctx_len, const int32_t* n_new,
+                        const int32_t* free_pages, const int32_t* n_free, int max_tokens, int32_t* page_table,
+                        int32_t* cu_new, int32_t* lens, int32_t* admitted, int32_t* positions, int32_t* rows,
+                        int32_t* slots, int32_t* n_left, void* stream);
+
+/* Quantises the K (after RoPE) and V rows of n_tokens tokens into the cache.  Token t's row is
+ * k + t * k_stride values (bf16 [Hkv][hd]; likewise v) and goes to slots[t]; a slot outside the
+ * cache (the plan's -1) is skipped.  Tokens of one page must stand together, in ascending slots
+ * without gaps (as the plan lists them); a page that two separate runs of one call write ends
+ * with one of them.  For a page and head, with need = the least b in [16, 254] with
+ * amax <= 448 * 2^(b - 127) over the finite values that the call writes there:
+ *   - a run that begins at the page's position 0, or a page whose scale is 0, starts anew: scale =
+ *     need, the page's other positions become 0;
+ *   - else scale = max(old scale, need); when it grows the page's other positions are rounded
+ *     once more, to the new scale.
+ * A code is the nearest e4m3 value, ties to even; a value that is not finite becomes NaN.  The
+ * outcome depends neither on the split of a page's tokens over calls nor on the launch, except
+ * where a value falls below its scale's normal range (2^-6) and is rounded again as it grows.
+ * k, v 16-byte aligned [device], strides multiples of 8 and >= Hkv * hd. */
+mg_status mg_kv8_append(const mg_kv8_cache* cache, int n_tokens, const uint16_t* k, int64_t k_stride,
+                        const uint16_t* v, int64_t v_stride, const int32_t* slots, void* stream);
+
+/* The values of n slots as bf16 rows (exact): slot slots[i]'s K [Hkv][hd] at k + i * k_stride and V
+ * likewise; either of k, v may be NULL.  Rows of slots outside the cache are left as they were.
+ * For handing a request's cache to the bf16 pool or to another program.  Alignment and strides as
+ * in mg_kv8_append. */
+mg_status mg_kv8_read(const mg_kv8_cache* cache, int n, const int32_t* slots, uint16_t* k, int64_t k_stride,
+                      uint16_t* v, int64_t v_stride, void* stream);
+
+/* Attention of a batch's new tokens over the cache.  Row b has the tokens cu_new[b] ..
+ * cu_new[b + 1] - 1 of q (cu_new NULL: token b alone), the last of them at position lens[b] - 1, so
+ * its token i of n stands at p = lens[b] - n + i; their own K/V are in the cache already.  A token sees
+ * the positions j <= p, j > p - window (window > 0), whose page-table entry is a page of the cache
+ * (entries outside 0 .. n_pages - 1 are holes).  With s_j = scale * q . k_j, or softcap *
+ * tanh(scale * q . k_j / softcap) where softcap > 0: out = sum_j softmax(s)_j v_j, rounded once to bf16; a
+ * token that sees nothing gets zeros.  A NaN in a position that a token does not see has no effect
+ * on it.  Query head h reads KV head h / (Hq / Hkv).  Rows without tokens and rows of out behind
+ * the last token are left as they were.
+ * Sums are fp32; a probability enters the product with V as two bf16 terms (16 bits) where a row
+ * has few query rows, and as one (8 bits, as V's own rounding point) in longer chunks. */
+typedef struct {
+    int32_t n_rows, n_tokens;
+    int32_t n_q_heads;         /* a multiple of n_kv_heads, at most 16 times it */
+    int32_t max_new;           /* at least the most tokens of any row (a row with more is the caller's error) */
+    int32_t max_len;           /* host bound on lens, for the launch's shape only (0: the page table's capacity) */
+    int32_t max_pages_per_row; /* page-table row stride */
+    int32_t window;            /* 0: every earlier position */
+    float scale;               /* 0: 1 / sqrt(head_dim) */
+    float softcap;             /* 0: none */
+    const uint16_t* q;         /* [device] bf16 [n_tokens][Hq][hd], token stride q_stride values */
+    int64_t q_stride;
+    uint16_t* out;             /* [device] as q, token stride out_stride; must not overlap q */
+    int64_t out_stride;
+    const int32_t* page_table; /* [device] [n_rows][max_pages_per_row] */
+    const int32_t* lens;       /* [device] [n_rows] */
+    const int32_t* cu_new;     /* [device] [n_rows + 1], or NULL */
+} mg_kv8_attn_args;
+/* Bytes of workspace the call needs on the current device (host logic; 0 also where the arguments
+ * are refused).  The workspace holds nothing between calls. */
+size_t mg_kv8_attention_workspace_bytes(const mg_kv8_cache* cache, const mg_kv8_attn_args* args);
+mg_status mg_kv8_attention(const mg_kv8_cache* cache, const mg_kv8_attn_args* args, void* workspace,
+                           size_t workspace_bytes, void* stream);
+
 /* ---- measurement hooks (used by the benchmark; not part of the method) ---- */
 
 enum {

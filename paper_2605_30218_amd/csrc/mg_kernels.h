@@ -205,6 +205,43 @@ hipError_t launch_repair(int n_host, const int32_t* n_dev, int cap, const int32_
                          int32_t* n_repaired, int action, hipStream_t s);
 hipError_t launch_advance(int B, const int32_t* emitted, int32_t* tokens, int32_t* positions, hipStream_t s);
 
+// ---------------------------------------------------------------- 8-bit paged K/V cache
+// The cache of one layer as the kernels see it (include/mg.h has the layout).
+struct Kv8 {
+    uint8_t* codes;
+    uint8_t* scales;
+    int n_pages, Hkv, hd;
+};
+// B rows' pages, slots and token lists from their lengths (k_plan.hip)
+struct PlanArgs {
+    int B, maxp, max_tokens;
+    const int32_t *ctx, *n_new, *free_pages, *n_free;
+    int32_t *page_table, *cu_new, *lens, *admitted, *positions, *rows, *slots, *n_left;
+};
+constexpr int PLAN_MAXB = 1024;
+hipError_t launch_batch_plan(const PlanArgs& a, hipStream_t s);
+// append and read (k_kv8.hip); strides in values
+hipError_t launch_kv8_append(const Kv8& c, int n, const uint16_t* k, int64_t ks, const uint16_t* v, int64_t vs,
+                             const int32_t* slots, hipStream_t s);
+hipError_t launch_kv8_read(const Kv8& c, int n, const int32_t* slots, uint16_t* k, int64_t ks, uint16_t* v, int64_t vs,
+                           hipStream_t s);
+// attention over the cache (k_attn_kv8.hip)
+struct Kv8AttnArgs {
+    Kv8 c;
+    int B, T, Hq, G;            // rows, query tokens, query heads, query heads per KV head
+    int max_new, max_len, maxp; // host bounds on a row's tokens and positions; page-table row stride
+    int window;                 // 0: none
+    float scale, cap, inv_cap;  // cap 0: none
+    const uint16_t* q;
+    uint16_t* out;
+    int64_t q_stride, out_stride;
+    const int32_t *page_table, *lens, *cu_new;
+    int n_cu;
+    float* part;                // split partials (kv8_attention_ws_bytes)
+};
+size_t kv8_attention_ws_bytes(const Kv8AttnArgs& a);
+hipError_t launch_kv8_attention(const Kv8AttnArgs& a, hipStream_t s);
+
 // element-wise numerics probes used by the tests
 hipError_t launch_copy16(int64_t n16, const void* src, void* dst, hipStream_t s);
 // streaming read of n16 16-byte words; sink receives read_stream_blocks() words

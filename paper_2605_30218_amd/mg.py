@@ -6,6 +6,7 @@ device pointers.  load() raises when the library is missing: there is no fallbac
 """
 from __future__ import annotations
 
+import collections
 import ctypes as C
 import os
 
@@ -38,6 +39,19 @@ class MgModelCfg(C.Structure):
                [(n, C.c_int32) for n in ("page_size", "max_batch", "max_pages_per_row", "n_pages", "max_prefill")]
 
 
+class MgKv8Cache(C.Structure):
+    _fields_ = [("codes", C.c_void_p), ("scales", C.c_void_p), ("n_pages", C.c_int32), ("n_kv_heads", C.c_int32),
+                ("head_dim", C.c_int32)]
+
+
+class MgKv8AttnArgs(C.Structure):
+    _fields_ = [(n, C.c_int32) for n in ("n_rows", "n_tokens", "n_q_heads", "max_new", "max_len",
+                                         "max_pages_per_row", "window")] + \
+               [("scale", C.c_float), ("softcap", C.c_float), ("q", C.c_void_p), ("q_stride", C.c_int64),
+                ("out", C.c_void_p), ("out_stride", C.c_int64), ("page_table", C.c_void_p), ("lens", C.c_void_p),
+                ("cu_new", C.c_void_p)]
+
+
 # name -> (restype, argtypes); the set of C-ABI symbols the binding uses
 P, I, F, I64, SZ = C.c_void_p, C.c_int, C.c_float, C.c_int64, C.c_size_t
 SIGNATURES = {
@@ -57,6 +71,13 @@ SIGNATURES = {
     "mg_verify_rows_mfma": (I, [P, I, P, P, P, P, P, P, P, P]),
     "mg_prefill": (I, [P, I, P, P, P, P, P]),
     "mg_advance": (I, [P, I, P, P, P, P]),
+    "mg_kv8_code_bytes": (SZ, [I, I, I]),
+    "mg_kv8_scale_bytes": (SZ, [I, I, I]),
+    "mg_batch_plan": (I, [I, I, P, P, P, P, I, P, P, P, P, P, P, P, P, P]),
+    "mg_kv8_append": (I, [P, I, P, I64, P, I64, P, P]),
+    "mg_kv8_read": (I, [P, I, P, P, I64, P, I64, P]),
+    "mg_kv8_attention_workspace_bytes": (SZ, [P, P]),
+    "mg_kv8_attention": (I, [P, P, P, SZ, P]),
     "mg_profile_begin": (I, [P, I, I]),
     "mg_profile_end": (I, [P, I, P, P, P, P]),
     "mg_op_copy": (I, [I64, P, P, P]),
@@ -240,6 +261,133 @@ def margin_gate_noalloc(B, V, logits, protected_mask, tau, top1, margin, gate, g
     _check("mg_margin_gate_noalloc", load().mg_margin_gate_noalloc(
         int(B), int(V), _ptr(logits), _ptr(protected_mask), float(tau), _ptr(top1), _ptr(margin), _ptr(gate),
         _ptr(gated_rows), _ptr(n_gated), _stream(stream)))
+
+
+# ---------------------------------------------------------------- batch plan and 8-bit K/V cache
+
+BatchPlan = collections.namedtuple("BatchPlan", "cu_new lens admitted positions rows slots n_left")
+
+
+def _need(ok, what):
+    if not ok:
+        raise ValueError(what)
+
+
+def _ints(name, t, device, numel=None):
+    """An int32 tensor of the call's device, contiguous, with the given number of values."""
+    _need(t.dtype is torch.int32 and t.device == device and t.is_contiguous(),
+          f"{name}: a contiguous int32 tensor on {device} is needed, got {t.dtype} on {t.device}")
+    _need(numel is None or t.numel() == numel, f"{name}: {t.numel()} values, {numel} needed")
+    return t.data_ptr()
+
+
+def _on(device, stream):
+    """The stream to enqueue on: the given one, or the device's current one."""
+    _need(device.type == "cuda", f"tensors on the GPU are needed, got {device}")
+    return (torch.cuda.current_stream(device) if stream is None else stream).cuda_stream
+
+
+def batch_plan(ctx_len, n_new, free_pages, n_free, page_table, max_tokens, out=None, stream=None):
+    """mg_batch_plan: pages, slots and per-token lists of a batch from its requests' lengths.  All
+    tensors int32 on one GPU: ctx_len, n_new [B], free_pages [any], n_free [1] (the count in use),
+    page_table [B, max_pages] (updated in place).  out: a BatchPlan to write into, whose tensors the
+    caller keeps (a captured step), or None for new ones."""
+    dev = ctx_len.device
+    _need(page_table.dim() == 2, "page_table: [B, max_pages] is needed")
+    B, maxp = page_table.shape
+    M = int(max_tokens)
+    args = (_ints("ctx_len", ctx_len, dev, B), _ints("n_new", n_new, dev, B), _ints("free_pages", free_pages, dev),
+            _ints("n_free", n_free, dev, 1), M, _ints("page_table", page_table, dev))
+    _need(0 <= M <= 1 << 30, f"max_tokens {M}")
+    s = _on(dev, stream)
+    if out is None:
+        # one allocation: positions, rows, slots, cu_new, lens, admitted, n_left
+        buf = torch.empty(3 * M + 3 * B + 2, dtype=torch.int32, device=dev)
+        pos, row, slot, cu, lens, adm, left = buf.split_with_sizes([M, M, M, B + 1, B, B, 1])
+        out = BatchPlan(cu, lens, adm, pos, row, slot, left)
+    po = [_ints(n, t, dev, k) for n, t, k in zip(BatchPlan._fields, out, (B + 1, B, B, M, M, M, 1))]
+    with torch.cuda.device(dev):
+        _check("mg_batch_plan", load().mg_batch_plan(B, maxp, *args, *po, s))
+    return out
+
+
+def _kv8(codes, scales):
+    """The MgKv8Cache of a layer's codes [n_pages, Hkv, 2, 16 hd] and scales [n_pages, Hkv, 2]."""
+    _need(codes.dtype is torch.uint8 and scales.dtype is torch.uint8 and codes.is_contiguous() and
+          scales.is_contiguous() and codes.device == scales.device, "codes and scales: contiguous uint8 of one device")
+    _need(codes.dim() == 4 and codes.shape[2] == 2 and scales.shape == codes.shape[:3],
+          f"codes {tuple(codes.shape)}, scales {tuple(scales.shape)}: [n_pages, Hkv, 2, 16 hd] and [n_pages, Hkv, 2]")
+    return MgKv8Cache(codes.data_ptr(), scales.data_ptr(), codes.shape[0], codes.shape[1], codes.shape[3] // 16)
+
+
+def kv8_empty(n_pages, n_kv_heads, head_dim, device="cuda"):
+    """An empty 8-bit cache of one layer: (codes, scales)."""
+    nb = load().mg_kv8_code_bytes(n_pages, n_kv_heads, head_dim)
+    if nb == 0:
+        raise MgError("mg_kv8_code_bytes", -2)
+    return (torch.zeros((n_pages, n_kv_heads, 2, 16 * head_dim), dtype=torch.uint8, device=device),
+            torch.zeros((n_pages, n_kv_heads, 2), dtype=torch.uint8, device=device))
+
+
+def _rows16(name, t, n, heads, hd, device):
+    """bf16 rows [n, heads, hd] (or their bits as int16), each row contiguous: (pointer, stride)."""
+    _need(t.dtype in (torch.bfloat16, torch.int16) and t.device == device, f"{name}: bf16 on {device} is needed")
+    _need(t.shape == (n, heads, hd) and (n == 0 or (t.stride(2) == 1 and (heads == 1 or t.stride(1) == hd))),
+          f"{name}: [{n}, {heads}, {hd}] with contiguous rows is needed, got {tuple(t.shape)} strides {t.stride()}")
+    return t.data_ptr(), (t.stride(0) if n > 1 else heads * hd)
+
+
+def kv8_append(codes, scales, k, v, slots, stream=None):
+    """mg_kv8_append: K (after RoPE) and V rows [n, Hkv, hd] quantised into the cache at slots [n]."""
+    c = _kv8(codes, scales)
+    dev, n = codes.device, slots.numel()
+    kp, ks = _rows16("k", k, n, c.n_kv_heads, c.head_dim, dev)
+    vp, vs = _rows16("v", v, n, c.n_kv_heads, c.head_dim, dev)
+    sl, s = _ints("slots", slots, dev), _on(dev, stream)
+    with torch.cuda.device(dev):
+        _check("mg_kv8_append", load().mg_kv8_append(C.byref(c), n, kp, ks, vp, vs, sl, s))
+
+
+def kv8_read(codes, scales, slots, k_out=None, v_out=None, stream=None):
+    """mg_kv8_read: the values of slots [n] as bf16 rows (k, v), each [n, Hkv, hd].  Rows of slots
+    outside the cache are not written: in a new tensor they hold anything."""
+    c = _kv8(codes, scales)
+    dev, n = codes.device, slots.numel()
+    new = [torch.empty((n, c.n_kv_heads, c.head_dim), dtype=torch.bfloat16, device=dev) if t is None else t
+           for t in (k_out, v_out)]
+    (kp, ks), (vp, vs) = (_rows16(m, t, n, c.n_kv_heads, c.head_dim, dev) for m, t in zip(("k_out", "v_out"), new))
+    sl, s = _ints("slots", slots, dev), _on(dev, stream)
+    with torch.cuda.device(dev):
+        _check("mg_kv8_read", load().mg_kv8_read(C.byref(c), n, sl, kp, ks, vp, vs, s))
+    return new[0], new[1]
+
+
+def kv8_attention(codes, scales, q, page_table, lens, cu_new=None, max_new=1, max_len=0, scale=None, window=0,
+                  softcap=0.0, out=None, workspace=None, stream=None):
+    """mg_kv8_attention: q [T, Hq, hd] attends over the cache's positions of its rows -> out [T, Hq, hd]
+    bf16.  Tokens behind the last row's are not written: in a new tensor they hold anything.
+    workspace: a uint8 tensor of kv8_attention_workspace_bytes, or None to take one per call."""
+    c = _kv8(codes, scales)
+    dev = codes.device
+    _need(q.dim() == 3 and page_table.dim() == 2, "q [T, Hq, hd] and page_table [B, max_pages] are needed")
+    T, Hq, hd = q.shape
+    B, maxp = page_table.shape
+    _need(hd == c.head_dim, f"q: head_dim {hd}, the cache's is {c.head_dim}")
+    if out is None:
+        out = torch.empty((T, Hq, hd), dtype=q.dtype, device=dev)
+    qp, qs = _rows16("q", q, T, Hq, hd, dev)
+    op, os_ = _rows16("out", out, T, Hq, hd, dev)
+    a = MgKv8AttnArgs(B, T, Hq, int(max_new), int(max_len), maxp, int(window), 0.0 if scale is None else float(scale),
+                      float(softcap), qp, qs, op, os_, _ints("page_table", page_table, dev),
+                      _ints("lens", lens, dev, B), None if cu_new is None else _ints("cu_new", cu_new, dev, B + 1))
+    s, lib = _on(dev, stream), load()
+    with torch.cuda.device(dev):
+        need = lib.mg_kv8_attention_workspace_bytes(C.byref(c), C.byref(a))
+        if workspace is None and need:
+            workspace = torch.empty(need, dtype=torch.uint8, device=dev)
+        _check("mg_kv8_attention", lib.mg_kv8_attention(C.byref(c), C.byref(a), _ptr(workspace),
+                                                        0 if workspace is None else workspace.numel(), s))
+    return out
 
 
 # ---------------------------------------------------------------- op-level calls (tests)

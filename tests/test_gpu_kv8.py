@@ -1,0 +1,514 @@
+"""The batch plan and the 8-bit paged K/V cache (GPU) against their definitions in float64 and Python
+integers (_kv8_ref.py): plan, append and read bit for bit, attention within the bound that its roundings
+give."""
+import numpy as np
+import pytest
+import torch
+
+import _kv8_ref as ref
+from _gpu_common import dev_i32
+from paper_2605_30218_amd import mg, synth
+from paper_2605_30218_amd.runtime import prefill_rows
+
+pytestmark = pytest.mark.gpu
+
+
+# ---------------------------------------------------------------- the plan
+
+
+def run_plan(ctx, new, free, n_free, table, max_tokens):
+    pt = dev_i32(table)
+    p = mg.batch_plan(dev_i32(ctx), dev_i32(new), dev_i32(free), dev_i32([n_free]), pt, max_tokens)
+    got = {k: v.cpu().numpy() for k, v in p._asdict().items()}
+    return got | {"table": pt.cpu().numpy()}
+
+
+def check_plan(ctx, new, free, n_free, table, max_tokens):
+    got, want = run_plan(ctx, new, free, n_free, table, max_tokens), ref.plan(ctx, new, free, n_free, table, max_tokens)
+    for k in want:
+        np.testing.assert_array_equal(got[k], np.asarray(want[k], np.int32).reshape(got[k].shape), err_msg=k)
+    return got
+
+
+def tables(rng, ctx, maxp, spare):
+    """A page table for the contexts (rows interleaved in the pool) and the free pages."""
+    held = [max(0, min(maxp, -(-int(c) // 16))) for c in ctx]
+    pool = rng.permutation(sum(held) + spare).astype(np.int32)
+    t = np.full((len(ctx), maxp), -1, np.int32)
+    o = 0
+    for b, k in enumerate(held):
+        t[b, :k] = pool[o:o + k]
+        o += k
+    return t, pool[o:]
+
+
+@pytest.mark.parametrize("B,hi,new_hi", [(1, 0, 1), (1, 500, 1), (3, 40, 40), (64, 700, 1), (255, 200, 90),
+                                         (256, 100, 3), (257, 64, 17), (1024, 60, 20)])
+def test_plan_matches_the_definition(B, hi, new_hi):
+    rng = np.random.RandomState(B)
+    ctx, new = rng.randint(0, hi + 1, B), rng.randint(0, new_hi + 1, B)
+    maxp = -(-(hi + new_hi) // 16) + 1
+    table, free = tables(rng, ctx, maxp, 8 * B + 4 * B * (new_hi // 16 + 1))
+    got = check_plan(ctx, new, free, len(free), table, int(new.sum()) + 300)
+    assert got["admitted"].all()
+
+
+@pytest.mark.parametrize("what", ["pages", "tokens", "neither", "no_pages", "no_tokens", "invalid"])
+def test_plan_stops_at_the_first_row_that_does_not_fit(what):
+    rng = np.random.RandomState(5)
+    B = 300
+    ctx, new = rng.randint(0, 200, B), rng.randint(0, 60, B)
+    new[::7] = 0
+    table, free = tables(rng, ctx, 20, 2000)
+    n_free, most = len(free), int(new.sum())
+    if what == "pages":
+        n_free = 217
+    if what == "tokens":
+        most = int(new[:123].sum()) + 1
+    if what == "no_pages":
+        n_free = -3
+    if what == "no_tokens":
+        most = 0
+    if what == "invalid":  # past the table row, negative: skipped, nobody behind waits for them
+        ctx[3], new[10], ctx[20], new[299], ctx[40] = 5000, -1, -4, 2 ** 31 - 1, 2 ** 31 - 1
+    got = check_plan(ctx, new, free, n_free, table, most)
+    assert got["admitted"].any() != (what == "nothing")
+
+
+def test_plan_feeds_the_prefill():
+    """The plan's token lists drive mg_prefill to the cache that prefill_rows leaves."""
+    shape, B = synth.TINY, 5
+    lens = [33, 16, 1, 50, 17]
+    prompts = synth.make_prompts(B, [n + 1 for n in lens], shape.vocab, seed=3)
+    rng = np.random.RandomState(0)
+    n_pages = 16
+    plan = run_plan([0] * B, lens, rng.permutation(n_pages), n_pages, np.full((B, 4), -1), sum(lens))
+    w = synth.make_weights(shape, seed=0)
+    pools = []
+    for direct in (False, True):
+        eng = mg.Engine(shape, w, B, 4, n_pages)
+        if direct:
+            tok = np.concatenate([p[:-1] for p in prompts])
+            eng.prefill(sum(lens), dev_i32(tok), dev_i32(plan["positions"]), dev_i32(plan["rows"]), dev_i32(plan["table"]))
+        else:
+            prefill_rows(eng, prompts, plan["table"])
+        torch.cuda.synchronize()
+        pools.append(eng.kv_pool.cpu().numpy())
+        eng.close()
+    np.testing.assert_array_equal(*pools)
+
+
+# ---------------------------------------------------------------- append and read
+
+
+def rows_bf16(rng, shape, std=1.0):
+    return torch.as_tensor(rng.randn(*shape) * std).to(torch.bfloat16)
+
+
+def check_append(codes, scales, k, v, slots, want):
+    mg.kv8_append(codes, scales, k.cuda(), v.cuda(), dev_i32(slots))
+    want.append(ref.bf16(k), ref.bf16(v), slots)
+    got = ref.RefCache.of(codes, scales)
+    np.testing.assert_array_equal(got.byte, want.byte)
+    np.testing.assert_array_equal(got.val, want.val)
+
+
+def noisy_cache(rng, n_pages, hkv, hd):
+    """A cache of random codes (no NaN) under random scales."""
+    codes, scales = mg.kv8_empty(n_pages, hkv, hd)
+    c = rng.randint(0, 256, codes.shape).astype(np.uint8)
+    c[(c & 127) == 127] = 0x40
+    codes.copy_(torch.as_tensor(c))
+    scales.copy_(torch.as_tensor(rng.randint(115, 124, scales.shape).astype(np.uint8)))
+    return codes, scales
+
+
+@pytest.mark.parametrize("hkv,hd", [(1, 64), (2, 64), (8, 128), (3, 128)])
+@pytest.mark.parametrize("piece", [1, 5, 16, 37])
+def test_append_token_by_token_and_in_runs(hkv, hd, piece):
+    """Three requests' positions arrive in pieces; what the pool holds is what the definition gives."""
+    rng = np.random.RandomState(hd + piece)
+    codes, scales = noisy_cache(rng, 9, hkv, hd)
+    want = ref.RefCache.of(codes, scales)
+    pages = rng.permutation(9).reshape(3, 3)
+    for p0 in range(0, 41, piece):
+        slots = [pages[r, p // 16] * 16 + p % 16 for r in range(3) for p in range(p0, min(p0 + piece, 41))]
+        slots = np.array(slots + [-1, 9 * 16, -5], np.int32)
+        std = 0.3 * 2.0 ** (p0 / 10)  # later positions are larger: the scales grow
+        k, v = (rows_bf16(rng, (len(slots), hkv, hd), std) for _ in range(2))
+        check_append(codes, scales, k, v, slots, want)
+
+
+def test_every_bf16_value_is_coded_as_defined():
+    """All 2^16 bf16 values, 256 of one sign and exponent region a page, both sides."""
+    hd, n = 128, 65536 // (16 * 128)
+    codes, scales = mg.kv8_empty(n, 1, hd)
+    bits = np.arange(65536).astype(np.uint16)
+    x = torch.as_tensor(bits.view(np.int16)).view(torch.bfloat16).reshape(n * 16, 1, hd)
+    perm = np.random.RandomState(0).permutation(65536)
+    y = x.reshape(-1)[torch.as_tensor(perm)].reshape(n * 16, 1, hd)
+    check_append(codes, scales, x, y, np.arange(n * 16, dtype=np.int32), ref.RefCache.of(codes, scales))
+
+
+@pytest.mark.parametrize("scale", [1e-38, 1e-30, 1e-3, 1e30, 3e38])
+def test_append_of_extreme_values(scale):
+    rng = np.random.RandomState(2)
+    codes, scales = mg.kv8_empty(3, 2, 64)
+    want = ref.RefCache.of(codes, scales)
+    x = torch.as_tensor(np.clip(rng.randn(20, 2, 64) * scale, -3.38e38, 3.38e38)).to(torch.bfloat16)
+    x[3, 0, 5], x[4, 1, 6], x[5, 0, 7] = float("nan"), float("inf"), -float("inf")
+    x[6] = 0.0
+    x[7, 1] = float("nan")
+    for i, j in ((0, 3), (3, 4), (4, 20)):
+        check_append(codes, scales, x[i:j], x[i:j].flip(2), np.arange(i, j, dtype=np.int32), want)
+
+
+def test_append_reads_strided_rows_and_leaves_other_pages():
+    rng = np.random.RandomState(3)
+    hkv, hd = 4, 128
+    codes, scales = noisy_cache(rng, 6, hkv, hd)
+    want = ref.RefCache.of(codes, scales)
+    qkv = rows_bf16(rng, (11, 28 + 2 * hkv, hd)).cuda()
+    slots = np.array([35, 36, 37, 80, 81, 82, 83, 3, 4, 5, 6], np.int32)
+    before = codes.clone(), scales.clone()
+    check_append(codes, scales, qkv[:, 28:32], qkv[:, 32:], slots, want)
+    for page in (1, 3, 4):
+        assert torch.equal(codes[page], before[0][page]) and torch.equal(scales[page], before[1][page])
+
+
+@pytest.mark.parametrize("hkv,hd,n", [(1, 64, 1), (8, 128, 77), (3, 64, 200), (2, 128, 16)])
+def test_read_gives_every_slot_exactly(hkv, hd, n):
+    rng = np.random.RandomState(n)
+    codes, scales = noisy_cache(rng, 13, hkv, hd)
+    want = ref.RefCache.of(codes, scales)
+    slots = rng.randint(0, 13 * 16, n).astype(np.int32)  # any order, some twice
+    if n > 100:
+        slots[50:150] = np.arange(30, 130)
+    k, v = mg.kv8_read(codes, scales, dev_i32(slots))
+    for got, exp in zip((k, v), want.read(slots)):
+        np.testing.assert_array_equal(ref.bf16(got), exp)
+
+
+def test_read_leaves_rows_of_slots_outside_the_cache():
+    rng = np.random.RandomState(1)
+    codes, scales = noisy_cache(rng, 2, 2, 64)
+    slots = np.array([-1, 5, 32, 31, 2 ** 30], np.int32)
+    k, v = (torch.full((5, 2, 72), 7.0, dtype=torch.bfloat16, device="cuda")[:, :, :64] for _ in range(2))
+    k, v = (torch.full((5, 3, 64), 7.0, dtype=torch.bfloat16, device="cuda")[:, :2] for _ in range(2))
+    mg.kv8_read(codes, scales, dev_i32(slots), k, v)
+    want = ref.RefCache.of(codes, scales).read([5, 31])
+    for got, exp in zip((k, v), want):
+        got = ref.bf16(got)
+        np.testing.assert_array_equal(got[[1, 3]], exp)
+        assert (got[[0, 2, 4]] == 7.0).all()
+
+
+# ---------------------------------------------------------------- attention
+
+
+def filled(rng, n_pages, hkv, hd, std=1.0):
+    codes, scales = mg.kv8_empty(n_pages, hkv, hd)
+    n = 16 * n_pages
+    k = rows_bf16(rng, (n, hkv, hd), std) * torch.as_tensor(np.exp(0.4 * rng.randn(hkv, hd))).to(torch.bfloat16)
+    mg.kv8_append(codes, scales, k.cuda(), rows_bf16(rng, (n, hkv, hd)).cuda(), dev_i32(np.arange(n)))
+    return codes, scales
+
+
+def few(new, G):
+    """Whether a row's query rows are few: a probability then keeps 16 bits."""
+    return max(new) * G <= 16
+
+
+class Batch:
+    """Rows of lengths lens with new tokens each, over a filled cache."""
+
+    def __init__(self, lens, new, hq, hkv, hd, seed=0, spare=1):
+        rng = np.random.RandomState(seed)
+        self.lens, self.new = np.asarray(lens), np.asarray(new)
+        self.table, free = tables(rng, self.lens, max(1, -(-int(max(self.lens.max(), 1)) // 16)) + spare, 3)
+        self.codes, self.scales = filled(rng, max(1, int(self.table.max()) + 1 + len(free)), hkv, hd)
+        self.cu = np.concatenate([[0], np.cumsum(self.new)])
+        self.q = rows_bf16(rng, (int(self.cu[-1]), hq, hd))
+        self.hd, self.G = hd, hq // hkv
+
+    def run(self, **kw):
+        return mg.kv8_attention(self.codes, self.scales, self.q.cuda(), dev_i32(self.table), dev_i32(self.lens),
+                                cu_new=dev_i32(self.cu), max_new=max(1, int(self.new.max())), **kw)
+
+    def check(self, got=None, **kw):
+        got = self.run(**kw) if got is None else got
+        kw.pop("max_len", None)
+        kw["scale"] = kw.get("scale") or 1 / np.sqrt(self.hd)
+        out, bound = ref.attention(ref.RefCache.of(self.codes, self.scales), ref.bf16(self.q), self.table, self.lens,
+                                   self.cu, p_bits=16 if few(self.new, self.G) else 8, **kw)
+        got = ref.bf16(got)
+        np.testing.assert_array_equal(np.isnan(got), np.isnan(out))
+        worst = np.nanmax(np.abs(got - out) / np.where(bound > 0, bound, 1e-38)) if out.size else 0.0
+        assert worst <= 1.0, f"{worst} of the bound"
+        return got
+
+
+HEADS = [(32, 8, 128), (40, 8, 128), (28, 4, 128), (4, 2, 64), (8, 8, 64), (16, 1, 128), (3, 1, 64), (12, 1, 64)]
+
+
+@pytest.mark.parametrize("hq,hkv,hd", HEADS)
+def test_single_tokens(hq, hkv, hd):
+    Batch([1, 2, 15, 16, 17, 31, 33, 100, 257, 600], [1] * 10, hq, hkv, hd).check()
+
+
+@pytest.mark.parametrize("hq,hkv,hd", [(4, 2, 64), (28, 4, 128)])
+@pytest.mark.parametrize("lens", [[5000], [1], [2049, 64, 3], [700] * 40, [16] * 100, [1023, 1024, 1025]])
+def test_single_tokens_of_other_batches(hq, hkv, hd, lens):
+    Batch(lens, [1] * len(lens), hq, hkv, hd, seed=len(lens)).check()
+
+
+@pytest.mark.parametrize("hq,hkv,hd", HEADS)
+@pytest.mark.parametrize("n", [2, 3, 4, 7])
+def test_few_tokens(hq, hkv, hd, n):
+    Batch([n, n + 1, 40, 333, 1500], [n] * 5, hq, hkv, hd, seed=n).check()
+
+
+@pytest.mark.parametrize("hq,hkv,hd", HEADS)
+@pytest.mark.parametrize("ctx,new", [([0, 0], [33, 130]), ([17, 500], [200, 64]), ([300], [129])])
+def test_chunks(hq, hkv, hd, ctx, new):
+    Batch(np.add(ctx, new), new, hq, hkv, hd, seed=sum(new)).check()
+
+
+@pytest.mark.parametrize("hq,hkv,hd", [(32, 8, 128), (4, 2, 64)])
+def test_mixed_batches_with_empty_rows(hq, hkv, hd):
+    new = [1, 70, 0, 1, 5, 1, 0, 300, 2, 1]
+    ctx = [40, 0, 50, 0, 900, 333, 0, 200, 15, 1000]
+    Batch(np.add(ctx, new), new, hq, hkv, hd).check()
+
+
+@pytest.mark.parametrize("window", [1, 7, 16, 100, 2000])
+@pytest.mark.parametrize("new", [[1, 1, 1, 1], [3, 1, 2, 4], [150, 1, 90, 20]])
+def test_window(window, new):
+    Batch(np.add([300, 5, 0, 1000], new), new, 8, 2, 128, seed=window).check(window=window)
+
+
+@pytest.mark.parametrize("cap", [0.5, 20.0, 50.0])
+@pytest.mark.parametrize("new", [[1, 1, 1], [80, 1, 3]])
+def test_softcap_and_scale(cap, new):
+    b = Batch(np.add([300, 5, 70], new), new, 8, 2, 64, seed=3)
+    b.check(softcap=cap)
+    b.check(softcap=cap, scale=0.3, window=50)
+
+
+@pytest.mark.parametrize("new", [[1, 1], [5, 1], [100, 40]])
+def test_large_scores(new):
+    """Scores of some hundreds: all but a few weights are zero."""
+    Batch(np.add([300, 64], new), new, 8, 2, 128, seed=4).check(scale=3.0)
+
+
+@pytest.mark.parametrize("new", [[1, 1, 1, 1], [20, 2, 33, 4]])
+def test_rows_that_see_nothing(new):
+    """No positions, fewer positions than tokens, all pages unmapped, lengths past the table."""
+    b = Batch([200, 64, 50, 130], new, 4, 2, 64, seed=5, spare=0)
+    b.lens = np.array([0, min(1, new[1] - 1), 50, 10 ** 6])
+    b.table[2] = -1
+    got = b.check()
+    assert (got[:b.cu[1]] == 0).all() and (got[b.cu[2]:b.cu[3]] == 0).all()
+
+
+@pytest.mark.parametrize("new", [[1, 1, 1], [6, 1, 2], [120, 1, 3]])
+@pytest.mark.parametrize("window", [0, 90])
+def test_holes_in_the_page_table(new, window):
+    b = Batch(np.add([333, 500, 20], new), new, 8, 2, 128, seed=6)
+    b.table[0, 3:6] = -1
+    b.table[0, 9] = 10 ** 6
+    b.table[1, 0::2] = -7
+    b.table[1, 31:] = -1
+    b.check(window=window)
+
+
+@pytest.mark.parametrize("hd", [64, 128])
+@pytest.mark.parametrize("new", [[1, 1, 1], [4, 2, 3], [100, 1, 65]])
+@pytest.mark.parametrize("window", [0, 40])
+def test_nan_reaches_only_who_sees_it(hd, new, window):
+    """NaN in K or V of single positions: behind the length, outside the window, later than a token."""
+    b = Batch(np.add([50, 77, 200], new), new, 4, 2, hd, seed=7)
+    flat = b.codes.view(-1, 2, 2, 16 * hd)
+
+    def poison(row, pos, head, side, d):
+        flat[int(b.table[row, pos // 16]), head, side, int(ref.byte_index(hd, side)[pos % 16, d])] = 0x7f
+
+    L = b.lens
+    poison(0, int(L[0]) - 1, 0, 1, 3)          # the last position, seen by the last token alone
+    poison(0, 2, 1, 1, 5)
+    for side in (0, 1):
+        if L[1] % 16:
+            poison(1, int(L[1]), 1, side, 9)   # behind the length, on a mapped page
+    poison(2, 150, 0, 0, 1)
+    poison(2, int(L[2]) - new[2] // 2 - 1, 1, 1, 40)
+    got = b.check(window=window)
+    assert np.isnan(got).any() and not np.isnan(got).all()
+
+
+def test_nan_and_infinity_in_a_query_stay_in_its_row():
+    for new in ([1, 1, 1], [40, 1, 30]):
+        b = Batch(np.add([50, 77, 200], new), new, 4, 2, 64, seed=8)
+        clean = ref.bf16(b.run())
+        b.q[b.cu[1] - 1, 2, 7] = float("nan")
+        got = ref.bf16(b.run())
+        assert np.isnan(got[b.cu[1] - 1, 2]).all()
+        got[b.cu[1] - 1, 2] = clean[b.cu[1] - 1, 2]
+        np.testing.assert_array_equal(got, clean)
+
+
+def test_strided_rows_and_rows_behind_the_last_token():
+    new = [1, 20, 1]
+    b = Batch(np.add([50, 77, 200], new), new, 4, 2, 64, seed=9)
+    T = int(b.cu[-1])
+    wide = torch.zeros((T + 3, 8, 64), dtype=torch.bfloat16, device="cuda")
+    wide[:T, :4] = b.q.cuda()
+    out = torch.full((T + 3, 6, 64), 7.0, dtype=torch.bfloat16, device="cuda")
+    mg.kv8_attention(b.codes, b.scales, wide[:, :4], dev_i32(b.table), dev_i32(b.lens), cu_new=dev_i32(b.cu),
+                     max_new=20, out=out[:, :4])
+    b.check(out[:T, :4])
+    assert (out[T:] == 7.0).all() and (out[:, 4:] == 7.0).all()
+
+
+def test_without_token_offsets_every_row_has_one():
+    b = Batch([3, 70, 200], [1, 1, 1], 8, 2, 128, seed=10)
+    got = mg.kv8_attention(b.codes, b.scales, b.q.cuda(), dev_i32(b.table), dev_i32(b.lens))
+    b.check(got)
+
+
+@pytest.mark.parametrize("max_len", [1, 64, 5000])
+def test_max_len_shapes_the_launch_only(max_len):
+    for new in ([1, 1], [40, 1]):
+        Batch(np.add([700, 130], new), new, 8, 2, 128, seed=11).check(max_len=max_len)
+
+
+@pytest.mark.parametrize("new", [1, 40])
+def test_offsets_past_32_bits(new):
+    """Pages behind 4 GiB of codes."""
+    hkv, hd, n_pages = 8, 128, 140000
+    codes, scales = mg.kv8_empty(n_pages, hkv, hd)
+    assert codes.numel() > 1 << 32
+    rng = np.random.RandomState(12)
+    L = 100 + new
+    table = np.array([n_pages - 1 - np.arange(10)], np.int32)
+    slots = np.array([table[0, p // 16] * 16 + p % 16 for p in range(L)], np.int32)
+    k, v, q = (rows_bf16(rng, (n, h, hd)) for n, h in ((L, hkv), (L, hkv), (new, 32)))
+    mg.kv8_append(codes, scales, k.cuda(), v.cuda(), dev_i32(slots))
+    got = mg.kv8_attention(codes, scales, q.cuda(), dev_i32(table), dev_i32([L]), cu_new=dev_i32([0, new]), max_new=new)
+    back = mg.kv8_read(codes, scales, dev_i32(slots))
+    small = ref.RefCache(10, hkv, hd)
+    t2 = np.arange(10, dtype=np.int32)[None]
+    s2 = np.arange(L)
+    small.append(ref.bf16(k), ref.bf16(v), s2)
+    for a, b in zip(back, small.read(s2)):
+        np.testing.assert_array_equal(ref.bf16(a), b)
+    out, bound = ref.attention(small, ref.bf16(q), t2, [L], [0, new], 1 / np.sqrt(hd), p_bits=16 if few([new], 4) else 8)
+    assert (np.abs(ref.bf16(got) - out) <= bound).all()
+
+
+def test_same_call_twice_gives_the_same_bits():
+    new = [1, 300, 4, 1]
+    b = Batch(np.add([900, 20, 700, 5000], new), new, 32, 8, 128, seed=13)
+    one = b.run()
+    for _ in range(3):
+        assert torch.equal(one, b.run())
+
+
+def test_a_row_does_not_depend_on_the_rows_beside_it():
+    """Row 1 alone and among others, on the launch of the larger batch's bounds."""
+    new = [1, 40, 4]
+    b = Batch(np.add([900, 130, 700], new), new, 8, 2, 128, seed=14)
+    both = b.run()
+    alone = mg.kv8_attention(b.codes, b.scales, b.q[1:41].cuda(), dev_i32(b.table[1:2]), dev_i32(b.lens[1:2]),
+                             cu_new=dev_i32([0, 40]), max_new=40)
+    assert torch.equal(both[1:41], alone)
+
+
+# ---------------------------------------------------------------- together
+
+
+class Loop:
+    """A serving loop's state: requests whose tokens arrive chunk by chunk, on one set of buffers."""
+
+    def __init__(self, B, hq, hkv, hd, maxp, n_pages, most):
+        self.B, self.most = B, most
+        self.codes, self.scales = mg.kv8_empty(n_pages, hkv, hd)
+        z = lambda *s: torch.zeros(s, dtype=torch.int32, device="cuda")  # noqa: E731
+        self.ctx, self.new, self.table, self.n_free = z(B), z(B), z(B, maxp) - 1, z(1) + n_pages
+        self.free = dev_i32(np.random.RandomState(0).permutation(n_pages))
+        self.plan = mg.BatchPlan(z(B + 1), z(B), z(B), z(most), z(most), z(most), z(1))
+        bf = lambda h: torch.zeros((most, h, hd), dtype=torch.bfloat16, device="cuda")  # noqa: E731
+        self.q, self.k, self.v, self.out = bf(hq), bf(hkv), bf(hkv), bf(hq)
+        self.ws = torch.empty(1 << 24, dtype=torch.uint8, device="cuda")
+
+    def step(self):
+        mg.batch_plan(self.ctx, self.new, self.free, self.n_free, self.table, self.most, out=self.plan)
+        mg.kv8_append(self.codes, self.scales, self.k, self.v, self.plan.slots)
+        mg.kv8_attention(self.codes, self.scales, self.q, self.table, self.plan.lens, cu_new=self.plan.cu_new,
+                         max_new=self.most, out=self.out, workspace=self.ws)
+        self.ctx.copy_(self.plan.lens)
+        self.n_free.copy_(self.plan.n_left)
+
+
+STEPS = [[20, 0, 33], [1, 16, 1], [1, 1, 1], [1, 40, 0], [1, 1, 1], [2, 1, 30]]
+
+
+def drive(loop, step):
+    """The steps of STEPS through `step`, each checked against the definitions."""
+    rng = np.random.RandomState(1)
+    hkv, hd = loop.codes.shape[1], loop.codes.shape[3] // 16
+    want = ref.RefCache(loop.codes.shape[0], hkv, hd)
+    outs = []
+    for new in STEPS:
+        n = sum(new)
+        for t in (loop.q, loop.k, loop.v):
+            t.copy_(rows_bf16(rng, tuple(t.shape)))
+        loop.new.copy_(torch.as_tensor(new, dtype=torch.int32))
+        step()
+        torch.cuda.synchronize()
+        slots = loop.plan.slots.cpu().numpy()
+        assert (slots[:n] >= 0).all() and (slots[n:] == -1).all()
+        want.append(ref.bf16(loop.k), ref.bf16(loop.v), slots)
+        got = ref.RefCache.of(loop.codes, loop.scales)
+        np.testing.assert_array_equal(got.byte, want.byte)
+        np.testing.assert_array_equal(got.val, want.val)
+        cu = np.concatenate([[0], np.cumsum(new)])
+        out, bound = ref.attention(want, ref.bf16(loop.q)[:n], loop.table.cpu().numpy(), loop.ctx.cpu().numpy(), cu,
+                                   1 / np.sqrt(hd))
+        assert (np.abs(ref.bf16(loop.out)[:n] - out) <= bound).all()
+        outs.append(loop.out[:n].clone())
+    return outs
+
+
+def test_plan_append_attend_over_a_request_s_life():
+    loop = Loop(3, 8, 2, 128, 8, 24, 60)
+    drive(loop, loop.step)
+
+
+def test_a_captured_step_follows_its_buffers():
+    """One capture replayed over prompts and single tokens, on another stream than the buffers' own."""
+    eager = drive(*(lambda l: (l, l.step))(Loop(3, 8, 2, 128, 8, 24, 60)))
+    loop = Loop(3, 8, 2, 128, 8, 24, 60)
+    loop.step()  # nothing new: warms the library up and changes nothing
+    torch.cuda.synchronize()
+    g = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(g):
+        loop.step()
+    for a, b in zip(eager, drive(loop, g.replay)):
+        assert torch.equal(a, b)
+
+
+def test_two_streams_at_once():
+    """Two batches on streams of their own, interleaved, with a workspace each."""
+    bs = [Batch(np.add([900, 130, 700], [1, 1, 1]), [1, 1, 1], 8, 2, 128, seed=s) for s in (20, 21)]
+    alone = [b.run() for b in bs]
+    args = [(b.q.cuda(), dev_i32(b.table), dev_i32(b.lens)) for b in bs]
+    outs = [torch.zeros_like(a) for a in alone]
+    ws = [torch.empty(1 << 22, dtype=torch.uint8, device="cuda") for _ in bs]
+    torch.cuda.synchronize()
+    st = [torch.cuda.Stream() for _ in bs]
+    for _ in range(20):
+        for b, (q, t, l), o, w, s in zip(bs, args, outs, ws, st):
+            mg.kv8_attention(b.codes, b.scales, q, t, l, out=o, workspace=w, stream=s)
+    torch.cuda.synchronize()
+    for a, o in zip(alone, outs):
+        assert torch.equal(a, o)
