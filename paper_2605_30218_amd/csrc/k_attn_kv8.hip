@@ -1,7 +1,5 @@
-// k_attn_kv8.hip -- attention of a batch's new tokens over the 8-bit paged K/V cache.
-//
-// One wave per (token, query head): a pass over the positions that the token sees with the running
-// maximum, sum and output of the softmax, a lane holding hd / 64 features.
+// k_attn_kv8.hip -- attention of a batch's new tokens over the 8-bit paged K/V cache: one kernel (and
+// the joining of its splits) for rows of few query rows, one for longer chunks of tokens.
 #include <algorithm>
 
 #include "mg_device.h"
@@ -12,6 +10,7 @@ namespace mg {
 typedef __bf16 bf16x2_k8 __attribute__((ext_vector_type(2)));
 typedef __bf16 bf16x8_k8 __attribute__((ext_vector_type(8)));
 typedef float f32x4_k8 __attribute__((ext_vector_type(4)));
+typedef uint32_t u32x4_k8 __attribute__((ext_vector_type(4)));
 
 constexpr int K8_WAVES = 4;
 constexpr int K8_THREADS = 64 * K8_WAVES;
@@ -66,17 +65,203 @@ __device__ __forceinline__ int k8_active(int npg, int sp, int nsplit) {
     return min(nsplit, max(1, (npg + sp - 1) / sp));
 }
 
+// ---- one step: 32 positions (two pages) against NT tiles of 16 query rows
+// S^T[pos][c] = K[pos][:] . Q[c][:]: K is the A operand, straight from a page (the cache stores a head's
+// page in the order in which a wave's 16-byte reads give the operand registers), and column c of a
+// tile one query row, in lanes c, c + 16, c + 32, c + 48.
+// O^T[d][c] += V^T[d][pos] P^T[pos][c]: V is the A operand, likewise; the scores' registers, positions
+// 4 g .. 4 g + 3 of both pages in lane group g, are the B operand as they are.
+// So a row's maximum takes two exchanges between lanes, and its rescaling is a lane's own.  Codes become bf16 with
+// their page's scale in one instruction a pair, exactly.
+template <int HD, int NT>
+struct K8Acc {
+    float m[NT], l[NT];          // reference of the exponents (log2 units); sum over the lane's positions
+    f32x4_k8 o[NT][HD / 16];
+    __device__ __forceinline__ void clear() {
+#pragma unroll
+        for (int u = 0; u < NT; ++u) {
+            // below every finite score, and finite: exp2(masked - m) is 0 where nothing was seen yet
+            m[u] = -3.0e38f;
+            l[u] = 0.0f;
+#pragma unroll
+            for (int d = 0; d < HD / 16; ++d) o[u][d] = f32x4_k8{0.f, 0.f, 0.f, 0.f};
+        }
+    }
+};
+// what the kernels derive from the scale and the cap: the exponent is x * f with x a score as k8_scores
+// leaves it
+struct K8Soft {
+    float f, zin, cap2;
+};
+__device__ __forceinline__ K8Soft k8_soft(const Kv8AttnArgs& a) {
+    return K8Soft{a.cap > 0.0f ? 1.0f : a.scale * 1.4426950408889634f, a.scale * a.inv_cap * 2.8853900817779268f,
+                  a.cap * 1.4426950408889634f};
+}
+
+// scores: x[u][4 e + i] of position 16 e + 4 g + i of the step and column c of tile u
+template <int HD, int NT, bool CAP>
+__device__ __forceinline__ void k8_scores(const uint4 (&kb)[2][HD / 64], const float (&ksc)[2],
+                                          const uint4 (&qa)[NT][HD / 32], const K8Soft& so, float (&x)[NT][8]) {
+#pragma unroll
+    for (int e = 0; e < 2; ++e) {
+        f32x4_k8 acc[NT];
+#pragma unroll
+        for (int u = 0; u < NT; ++u) acc[u] = f32x4_k8{0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+        for (int h = 0; h < HD / 64; ++h)
+#pragma unroll
+            for (int st = 0; st < 2; ++st) {
+                const uint2 lo = k8_bf16x4(st ? kb[e][h].z : kb[e][h].x, ksc[e]);
+                const uint2 hi = k8_bf16x4(st ? kb[e][h].w : kb[e][h].y, ksc[e]);
+                const bf16x8_k8 A = __builtin_bit_cast(bf16x8_k8, make_uint4(lo.x, lo.y, hi.x, hi.y));
+#pragma unroll
+                for (int u = 0; u < NT; ++u)
+                    acc[u] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(A, __builtin_bit_cast(bf16x8_k8, qa[u][2 * h + st]), acc[u], 0, 0, 0);
+            }
+#pragma unroll
+        for (int u = 0; u < NT; ++u)
+#pragma unroll
+            for (int i = 0; i < 4; ++i)
+                // tanh(z) = 1 - 2 / (1 + e^2z)
+                x[u][4 * e + i] = CAP ? so.cap2 * (1.0f - 2.0f * __builtin_amdgcn_rcpf(1.0f + __builtin_amdgcn_exp2f(acc[u][i] * so.zin)))
+                                      : acc[u][i];
+    }
+}
+
+// Whether the token at position p sees the step's position i of this lane: j0 the step's first position,
+// mapped bit e whether page e is one of the cache's.
+__device__ __forceinline__ bool k8_sees(const K8Row& row, int window, int j0, int mapped, int g, int i, int p) {
+    const int j = j0 + 16 * (i >> 2) + 4 * g + (i & 3);
+    return ((mapped >> (i >> 2)) & 1) && j <= p && j < row.len && (!window || j > p - window);
+}
+
+// The online softmax of a step.  The reference m moves only when a score passes it by more than 2^8: a
+// probability is then at most 256, its bits are relative, and the exchanges between lanes and the
+// rescaling of the output are rare.  TERMS bf16 values stand for a probability: their sum is 2^-8 (1) or
+// 2^-16 (2) of itself off.
+template <int HD, int NT, int TERMS>
+__device__ __forceinline__ void k8_softmax(float (&x)[NT][8], float f, K8Acc<HD, NT>& acc, bf16x8_k8 (&p)[NT][TERMS]) {
+#pragma unroll
+    for (int u = 0; u < NT; ++u) {
+        const float mx = fmaxf(fmaxf(fmaxf(x[u][0], x[u][1]), fmaxf(x[u][2], x[u][3])),
+                               fmaxf(fmaxf(x[u][4], x[u][5]), fmaxf(x[u][6], x[u][7])));
+        if (__any(__builtin_fmaf(mx, f, -acc.m[u]) > 8.0f)) {
+            const float mn = fmaxf(acc.m[u], k8_col_max(mx) * f);
+            const float al = __builtin_amdgcn_exp2f(acc.m[u] - mn);
+            acc.m[u] = mn;
+            acc.l[u] *= al;
+#pragma unroll
+            for (int d = 0; d < HD / 16; ++d) acc.o[u][d] *= al;
+        }
+#pragma unroll
+        for (int i = 0; i < 8; ++i) {
+            x[u][i] = __builtin_amdgcn_exp2f(__builtin_fmaf(x[u][i], f, -acc.m[u]));
+            acc.l[u] += x[u][i];
+        }
+        uint32_t w[4];
+#pragma unroll
+        for (int i = 0; i < 4; ++i) w[i] = k8_pack(x[u][2 * i], x[u][2 * i + 1]);
+        p[u][0] = __builtin_bit_cast(bf16x8_k8, make_uint4(w[0], w[1], w[2], w[3]));
+        if constexpr (TERMS == 2) {
+            uint32_t v[4];
+#pragma unroll
+            for (int i = 0; i < 4; ++i) v[i] = k8_pack(x[u][2 * i] - bf_lo(w[i]), x[u][2 * i + 1] - bf_hi(w[i]));
+            p[u][1] = __builtin_bit_cast(bf16x8_k8, make_uint4(v[0], v[1], v[2], v[3]));
+        }
+    }
+}
+
+// A NaN code of V under a probability of zero: in a step whose columns do not all see all positions it
+// must reach the columns that see it and no other.  Takes the NaN codes out of vb and puts a NaN into the outputs
+// that see one, found by a product of the codes' and the columns' indicators.
+template <int HD, int NT>
+__device__ __forceinline__ void k8_mend_nan(uint4 (&vb)[2][HD / 64], K8Acc<HD, NT>& acc, const K8Row& row, int window,
+                                            int j0, int mapped, int g, const int (&pc)[NT]) {
+    uint32_t any = 0;
+#pragma unroll
+    for (int e = 0; e < 2; ++e)
+#pragma unroll
+        for (int h = 0; h < HD / 64; ++h)
+            any |= k8_nan_bytes(vb[e][h].x) | k8_nan_bytes(vb[e][h].y) | k8_nan_bytes(vb[e][h].z) | k8_nan_bytes(vb[e][h].w);
+    if (!__any(any != 0)) return;
+#pragma unroll
+    for (int u = 0; u < NT; ++u) {
+        uint32_t sw[4];
+#pragma unroll
+        for (int i = 0; i < 4; ++i)
+            sw[i] = (k8_sees(row, window, j0, mapped, g, 2 * i, pc[u]) ? 0x3f80u : 0u) |
+                    (k8_sees(row, window, j0, mapped, g, 2 * i + 1, pc[u]) ? 0x3f800000u : 0u);
+        const bf16x8_k8 S = __builtin_bit_cast(bf16x8_k8, make_uint4(sw[0], sw[1], sw[2], sw[3]));
+#pragma unroll
+        for (int h = 0; h < HD / 64; ++h)
+#pragma unroll
+            for (int q = 0; q < 4; ++q) {
+                uint32_t f[4];
+#pragma unroll
+                for (int e = 0; e < 2; ++e) {
+                    const uint32_t nb = k8_nan_bytes(q == 0 ? vb[e][h].x : q == 1 ? vb[e][h].y : q == 2 ? vb[e][h].z : vb[e][h].w);
+                    f[2 * e] = ((nb >> 7) & 1u) * 0x3f80u | ((nb >> 15) & 1u) * 0x3f800000u;
+                    f[2 * e + 1] = ((nb >> 23) & 1u) * 0x3f80u | (nb >> 31) * 0x3f800000u;
+                }
+                f32x4_k8 hit = f32x4_k8{0.f, 0.f, 0.f, 0.f};
+                hit = __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8_k8, make_uint4(f[0], f[1], f[2], f[3])), S, hit, 0, 0, 0);
+#pragma unroll
+                for (int i = 0; i < 4; ++i) acc.o[u][4 * h + q][i] = hit[i] > 0.0f ? __builtin_nanf("") : acc.o[u][4 * h + q][i];
+            }
+    }
+#pragma unroll
+    for (int e = 0; e < 2; ++e)
+#pragma unroll
+        for (int h = 0; h < HD / 64; ++h) {
+            vb[e][h].x &= ~((k8_nan_bytes(vb[e][h].x) >> 7) * 0xffu);
+            vb[e][h].y &= ~((k8_nan_bytes(vb[e][h].y) >> 7) * 0xffu);
+            vb[e][h].z &= ~((k8_nan_bytes(vb[e][h].z) >> 7) * 0xffu);
+            vb[e][h].w &= ~((k8_nan_bytes(vb[e][h].w) >> 7) * 0xffu);
+        }
+}
+
+template <int HD, int NT, int TERMS>
+__device__ __forceinline__ void k8_pv(const uint4 (&vb)[2][HD / 64], const float (&vsc)[2], const bf16x8_k8 (&p)[NT][TERMS],
+                                      K8Acc<HD, NT>& acc) {
+#pragma unroll
+    for (int h = 0; h < HD / 64; ++h)
+#pragma unroll
+        for (int q = 0; q < 4; ++q) {
+            const uint32_t w0 = q == 0 ? vb[0][h].x : q == 1 ? vb[0][h].y : q == 2 ? vb[0][h].z : vb[0][h].w;
+            const uint32_t w1 = q == 0 ? vb[1][h].x : q == 1 ? vb[1][h].y : q == 2 ? vb[1][h].z : vb[1][h].w;
+            const uint2 lo = k8_bf16x4(w0, vsc[0]), hi = k8_bf16x4(w1, vsc[1]);
+            const bf16x8_k8 A = __builtin_bit_cast(bf16x8_k8, make_uint4(lo.x, lo.y, hi.x, hi.y));
+#pragma unroll
+            for (int u = 0; u < NT; ++u)
+#pragma unroll
+                for (int t = 0; t < TERMS; ++t)
+                    acc.o[u][4 * h + q] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(A, p[u][t], acc.o[u][4 * h + q], 0, 0, 0);
+        }
+}
+
+// query rows rr0 + 16 u + c of a row's KV head (row rr: token rr / G, head rr % G of the group) as B operands, and
+// the positions of their tokens; columns past the row's last repeat its first
+template <int HD, int NT>
+__device__ __forceinline__ void k8_query(const Kv8AttnArgs& a, const K8Row& row, int kh, int rr0, int c, int g,
+                                         uint4 (&qa)[NT][HD / 32], int (&pc)[NT]) {
+#pragma unroll
+    for (int u = 0; u < NT; ++u) {
+        int rr = rr0 + 16 * u + c;
+        rr = rr < row.n * a.G ? rr : 0;
+        const uint16_t* qp = a.q + (int64_t)(row.t0 + rr / a.G) * a.q_stride + (size_t)(kh * a.G + rr % a.G) * HD;
+        pc[u] = row.p0 + rr / a.G;
+#pragma unroll
+        for (int h = 0; h < HD / 64; ++h) {
+            // operand slot (g, st) holds features 64 h + 16 g + 8 st ..
+            qa[u][2 * h] = *reinterpret_cast<const uint4*>(qp + 64 * h + 16 * g);
+            qa[u][2 * h + 1] = *reinterpret_cast<const uint4*>(qp + 64 * h + 16 * g + 8);
+        }
+    }
+}
+
 // Rows of few query rows (tokens times query heads of a KV head <= 16 NT): one block of 4 waves per
-// (row, KV head, split of the row's pages).
-// A wave takes every 4th step of two pages and keeps the running maximum, sum and output of its share:
-//   S^T[pos][c] = K[pos][:] . Q[c][:]      K the A operand, straight from the page: the cache stores a
-//       head's page in the order in which a wave's 16-byte loads give the operand registers;
-//   O^T[d][c] += V^T[d][pos] P^T[pos][c]   V the A operand, likewise; the scores' registers, positions
-//       4 g .. 4 g + 3 of both pages in lane group g, are the B operand as they are.
-// Column c of every product is one query row, in lanes c, c + 16, c + 32, c + 48, so its maximum is two
-// exchanges and its rescaling a lane's own.  Codes become bf16 with their page's scale in one
-// instruction a pair, exactly.  A probability is the sum of two bf16 terms (16 bits, 2^-16 of itself off),
-// one product each: the matrix cores have the time, the K/V stream is what bounds the kernel.
+// (row, KV head, split of the row's pages), a wave taking every 4th step of its pages.  The K/V stream
+// bounds it, so the matrix cores have the time for two terms of a probability.
 template <int HD, int NT, bool CAP>
 __global__ __launch_bounds__(K8_THREADS) __attribute__((amdgpu_waves_per_eu(NT == 1 ? 3 : 2))) void attn_kv8_few_kernel(Kv8AttnArgs a, int sp, int nsplit) {
     constexpr int H = HD / 64;        // 1 KiB runs of a page of K or V
@@ -97,32 +282,12 @@ __global__ __launch_bounds__(K8_THREADS) __attribute__((amdgpu_waves_per_eu(NT =
     __shared__ __attribute__((aligned(16))) float wo[K8_WAVES][16 * NT][OS];
     __shared__ float wm[K8_WAVES][16 * NT], wl[K8_WAVES][16 * NT];
 
-    // query rows: tile u's column c is row 16 u + c = token * G + head of the KV head's group
     uint4 qa[NT][2 * H];
-    int pc[NT];  // position of the column's token
-#pragma unroll
-    for (int u = 0; u < NT; ++u) {
-        const int rr = 16 * u + c, tok = rr / a.G;
-        const bool live = rr < row.n * a.G;
-        const uint16_t* qp = a.q + (int64_t)(row.t0 + (live ? tok : 0)) * a.q_stride + (size_t)(kh * a.G + (live ? rr % a.G : 0)) * HD;
-        pc[u] = row.p0 + (live ? tok : 0);
-#pragma unroll
-        for (int h = 0; h < H; ++h) {
-            // operand slot (g, st) holds features 64 h + 16 g + 8 st ..
-            qa[u][2 * h] = *reinterpret_cast<const uint4*>(qp + 64 * h + 16 * g);
-            qa[u][2 * h + 1] = *reinterpret_cast<const uint4*>(qp + 64 * h + 16 * g + 8);
-        }
-    }
-    const float sl2 = a.scale * 1.4426950408889634f;
-    float m[NT], l[NT];
-    f32x4_k8 o[NT][DT];
-#pragma unroll
-    for (int u = 0; u < NT; ++u) {
-        m[u] = -__builtin_inff();
-        l[u] = 0.0f;
-#pragma unroll
-        for (int d = 0; d < DT; ++d) o[u][d] = f32x4_k8{0.f, 0.f, 0.f, 0.f};
-    }
+    int pc[NT];
+    k8_query<HD, NT>(a, row, kh, 0, c, g, qa, pc);
+    const K8Soft so = k8_soft(a);
+    K8Acc<HD, NT> acc;
+    acc.clear();
     const int32_t* ptab = a.page_table + (size_t)r * a.maxp;
     const size_t head_bytes = (size_t)2 * 16 * HD;
     const uint8_t* base = a.c.codes + (size_t)kh * head_bytes;
@@ -134,7 +299,7 @@ __global__ __launch_bounds__(K8_THREADS) __attribute__((amdgpu_waves_per_eu(NT =
         if (id < 0 || id >= a.c.n_pages) id = -1;
         const uint32_t sc = id < 0 ? 0u : *reinterpret_cast<const uint16_t*>(a.c.scales + ((size_t)id * a.c.Hkv + kh) * 2);
         uint4 kb[2][H], vb[2][H];
-        // K (side 0) or V of step s, into the operand registers
+        // K (side 0) or V of step s, into the operand registers; a hole reads page 0, unseen
         auto fetch = [&](int s, int side, uint4 (&x)[2][H]) {
 #pragma unroll
             for (int e = 0; e < 2; ++e) {
@@ -151,152 +316,33 @@ __global__ __launch_bounds__(K8_THREADS) __attribute__((amdgpu_waves_per_eu(NT =
         for (int s = wave; s < steps; s += K8_WAVES) {
             const bool more = s + K8_WAVES < steps;
             float ksc[2], vsc[2];
-            bool hole = false;
+            int mapped = 0;
 #pragma unroll
             for (int e = 0; e < 2; ++e) {
                 const uint32_t b = (uint32_t)__builtin_amdgcn_readlane((int)sc, 2 * s + e);
                 ksc[e] = __uint_as_float((b & 0xffu) << 23);
                 vsc[e] = __uint_as_float((b >> 8) << 23);
-                hole |= __builtin_amdgcn_readlane(id, 2 * s + e) < 0;
+                mapped |= (__builtin_amdgcn_readlane(id, 2 * s + e) >= 0) << e;
             }
             const int j0 = 16 * (ch + 2 * s);
-            const bool edge = hole || j0 + 31 > row.p0 || j0 + 32 > row.len ||
+            const bool edge = mapped != 3 || j0 + 31 > row.p0 || j0 + 32 > row.len ||
                               (a.window && j0 <= row.p0 + row.n - 1 - a.window);
-            // scores, in log2 units: positions j0 + 16 e + 4 g + i of column c
             float x[NT][8];
-            uint32_t see[NT];
-#pragma unroll
-            for (int u = 0; u < NT; ++u) see[u] = 0xffu;
-#pragma unroll
-            for (int e = 0; e < 2; ++e) {
-                f32x4_k8 acc[NT];
-#pragma unroll
-                for (int u = 0; u < NT; ++u) acc[u] = f32x4_k8{0.f, 0.f, 0.f, 0.f};
-#pragma unroll
-                for (int h = 0; h < H; ++h)
-#pragma unroll
-                    for (int st = 0; st < 2; ++st) {
-                        const uint2 lo = k8_bf16x4(st ? kb[e][h].z : kb[e][h].x, ksc[e]);
-                        const uint2 hi = k8_bf16x4(st ? kb[e][h].w : kb[e][h].y, ksc[e]);
-                        const bf16x8_k8 A = __builtin_bit_cast(bf16x8_k8, make_uint4(lo.x, lo.y, hi.x, hi.y));
-#pragma unroll
-                        for (int u = 0; u < NT; ++u)
-                            acc[u] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(A, __builtin_bit_cast(bf16x8_k8, qa[u][2 * h + st]), acc[u], 0, 0, 0);
-                    }
-#pragma unroll
-                for (int u = 0; u < NT; ++u)
-#pragma unroll
-                    for (int i = 0; i < 4; ++i) {
-                        if (CAP) {
-                            // tanh(z) = 1 - 2 / (1 + e^2z)
-                            const float z = acc[u][i] * a.scale * a.inv_cap;
-                            const float t = 1.0f - 2.0f * __builtin_amdgcn_rcpf(1.0f + __builtin_amdgcn_exp2f(z * 2.8853900817779268f));
-                            x[u][4 * e + i] = t * (a.cap * 1.4426950408889634f);
-                        } else {
-                            x[u][4 * e + i] = acc[u][i] * sl2;
-                        }
-                    }
-            }
+            k8_scores<HD, NT, CAP>(kb, ksc, qa, so, x);
             __builtin_amdgcn_sched_barrier(0);
             if (more) fetch(s + K8_WAVES, 0, kb);  // its registers are free: in flight under the rest of the step
             __builtin_amdgcn_sched_barrier(0);
             if (edge) {
 #pragma unroll
-                for (int u = 0; u < NT; ++u) {
-                    see[u] = 0;
+                for (int u = 0; u < NT; ++u)
 #pragma unroll
-                    for (int i = 0; i < 8; ++i) {
-                        const int j = j0 + 16 * (i >> 2) + 4 * g + (i & 3);
-                        const bool mapped = __builtin_amdgcn_readlane(id, 2 * s + (i >> 2)) >= 0;
-                        const bool v = mapped && j <= pc[u] && j < row.len && (!a.window || j > pc[u] - a.window);
-                        x[u][i] = v ? x[u][i] : -__builtin_inff();
-                        see[u] |= (uint32_t)v << i;
-                    }
-                }
+                    for (int i = 0; i < 8; ++i)
+                        x[u][i] = k8_sees(row, a.window, j0, mapped, g, i, pc[u]) ? x[u][i] : -__builtin_inff();
             }
-            bf16x8_k8 ph[NT], pl[NT];
-#pragma unroll
-            for (int u = 0; u < NT; ++u) {
-                float mx = fmaxf(fmaxf(fmaxf(x[u][0], x[u][1]), fmaxf(x[u][2], x[u][3])),
-                                 fmaxf(fmaxf(x[u][4], x[u][5]), fmaxf(x[u][6], x[u][7])));
-                const float mn = fmaxf(m[u], k8_col_max(mx));
-                const float ms = mn == -__builtin_inff() ? 0.0f : mn;
-                const float al = __builtin_amdgcn_exp2f(m[u] - ms);
-                m[u] = mn;
-                float sum = 0.0f, lo[8];
-                uint32_t w[4];
-#pragma unroll
-                for (int i = 0; i < 8; ++i) {
-                    x[u][i] = __builtin_amdgcn_exp2f(x[u][i] - ms);
-                    sum += x[u][i];
-                }
-#pragma unroll
-                for (int i = 0; i < 4; ++i) {
-                    w[i] = k8_pack(x[u][2 * i], x[u][2 * i + 1]);
-                    lo[2 * i] = x[u][2 * i] - bf_lo(w[i]);
-                    lo[2 * i + 1] = x[u][2 * i + 1] - bf_hi(w[i]);
-                }
-                l[u] = l[u] * al + sum;
-                ph[u] = __builtin_bit_cast(bf16x8_k8, make_uint4(w[0], w[1], w[2], w[3]));
-                pl[u] = __builtin_bit_cast(bf16x8_k8, make_uint4(k8_pack(lo[0], lo[1]), k8_pack(lo[2], lo[3]),
-                                                                 k8_pack(lo[4], lo[5]), k8_pack(lo[6], lo[7])));
-                if (__any(al != 1.0f)) {
-#pragma unroll
-                    for (int d = 0; d < DT; ++d) o[u][d] *= al;
-                }
-            }
-            // a NaN code of V under a probability of zero: in a step whose columns do not all see all
-            // positions it must reach the columns that see it, and no other
-            if (edge) {
-                uint32_t any = 0;
-#pragma unroll
-                for (int e = 0; e < 2; ++e)
-#pragma unroll
-                    for (int h = 0; h < H; ++h)
-                        any |= k8_nan_bytes(vb[e][h].x) | k8_nan_bytes(vb[e][h].y) | k8_nan_bytes(vb[e][h].z) | k8_nan_bytes(vb[e][h].w);
-                if (__any(any != 0)) {
-#pragma unroll
-                    for (int h = 0; h < H; ++h)
-#pragma unroll
-                        for (int q = 0; q < 4; ++q) {
-                            uint32_t* w[2] = {reinterpret_cast<uint32_t*>(&vb[0][h]) + q, reinterpret_cast<uint32_t*>(&vb[1][h]) + q};
-                            uint32_t f[4];
-#pragma unroll
-                            for (int e = 0; e < 2; ++e) {
-                                const uint32_t nb = k8_nan_bytes(*w[e]);
-                                *w[e] &= ~((nb >> 7) * 0xffu);
-                                f[2 * e] = ((nb >> 7) & 1u) * 0x3f80u | ((nb >> 15) & 1u) * 0x3f800000u;
-                                f[2 * e + 1] = ((nb >> 23) & 1u) * 0x3f80u | (nb >> 31) * 0x3f800000u;
-                            }
-                            const bf16x8_k8 F = __builtin_bit_cast(bf16x8_k8, make_uint4(f[0], f[1], f[2], f[3]));
-#pragma unroll
-                            for (int u = 0; u < NT; ++u) {
-                                uint32_t sw[4];
-#pragma unroll
-                                for (int i = 0; i < 4; ++i)
-                                    sw[i] = ((see[u] >> (2 * i)) & 1u) * 0x3f80u | ((see[u] >> (2 * i + 1)) & 1u) * 0x3f800000u;
-                                f32x4_k8 hit = f32x4_k8{0.f, 0.f, 0.f, 0.f};
-                                hit = __builtin_amdgcn_mfma_f32_16x16x32_bf16(F, __builtin_bit_cast(bf16x8_k8, make_uint4(sw[0], sw[1], sw[2], sw[3])), hit, 0, 0, 0);
-#pragma unroll
-                                for (int i = 0; i < 4; ++i) o[u][4 * h + q][i] = hit[i] > 0.0f ? __builtin_nanf("") : o[u][4 * h + q][i];
-                            }
-                        }
-                }
-            }
-#pragma unroll
-            for (int h = 0; h < H; ++h)
-#pragma unroll
-                for (int q = 0; q < 4; ++q) {
-                    const uint32_t w0 = q == 0 ? vb[0][h].x : q == 1 ? vb[0][h].y : q == 2 ? vb[0][h].z : vb[0][h].w;
-                    const uint32_t w1 = q == 0 ? vb[1][h].x : q == 1 ? vb[1][h].y : q == 2 ? vb[1][h].z : vb[1][h].w;
-                    const uint2 lo = k8_bf16x4(w0, vsc[0]), hi = k8_bf16x4(w1, vsc[1]);
-                    const bf16x8_k8 A = __builtin_bit_cast(bf16x8_k8, make_uint4(lo.x, lo.y, hi.x, hi.y));
-#pragma unroll
-                    for (int u = 0; u < NT; ++u) {
-                        o[u][4 * h + q] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(A, ph[u], o[u][4 * h + q], 0, 0, 0);
-                        o[u][4 * h + q] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(A, pl[u], o[u][4 * h + q], 0, 0, 0);
-                    }
-                }
+            bf16x8_k8 p[NT][2];
+            k8_softmax<HD, NT, 2>(x, so.f, acc, p);
+            if (edge) k8_mend_nan<HD, NT>(vb, acc, row, a.window, j0, mapped, g, pc);
+            k8_pv<HD, NT, 2>(vb, vsc, p, acc);
             __builtin_amdgcn_sched_barrier(0);
             if (more) fetch(s + K8_WAVES, 1, vb);
         }
@@ -305,14 +351,14 @@ __global__ __launch_bounds__(K8_THREADS) __attribute__((amdgpu_waves_per_eu(NT =
     // the waves' shares join in LDS
 #pragma unroll
     for (int u = 0; u < NT; ++u) {
-        const float ls = k8_col_sum(l[u]);
+        const float ls = k8_col_sum(acc.l[u]);
         if (g == 0) {
-            wm[wave][16 * u + c] = m[u];
+            wm[wave][16 * u + c] = acc.m[u];
             wl[wave][16 * u + c] = ls;
         }
 #pragma unroll
         for (int d = 0; d < DT; ++d)
-            *reinterpret_cast<f32x4_k8*>(&wo[wave][16 * u + c][16 * d + 4 * g]) = o[u][d];
+            *reinterpret_cast<f32x4_k8*>(&wo[wave][16 * u + c][16 * d + 4 * g]) = acc.o[u][d];
     }
     __syncthreads();
     const int live = row.n * a.G;
@@ -321,12 +367,11 @@ __global__ __launch_bounds__(K8_THREADS) __attribute__((amdgpu_waves_per_eu(NT =
         float M = wm[0][rr];
 #pragma unroll
         for (int w = 1; w < K8_WAVES; ++w) M = fmaxf(M, wm[w][rr]);
-        const float Ms = M == -__builtin_inff() ? 0.0f : M;
         float L = 0.0f;
         f32x4_k8 O = f32x4_k8{0.f, 0.f, 0.f, 0.f};
 #pragma unroll
         for (int w = 0; w < K8_WAVES; ++w) {
-            const float f = __builtin_amdgcn_exp2f(wm[w][rr] - Ms);
+            const float f = __builtin_amdgcn_exp2f(wm[w][rr] - M);
             L += f * wl[w][rr];
             O += f * *reinterpret_cast<const f32x4_k8*>(&wo[w][rr][d]);
         }
@@ -366,7 +411,7 @@ __global__ __launch_bounds__(K8_THREADS) void attn_kv8_join_kernel(Kv8AttnArgs a
         const float2 ml = *reinterpret_cast<const float2*>(mls + 2 * at);
         const float ms = lane < act ? ml.x : -__builtin_inff();
         const float M = wave_max(ms);
-        const float f = lane < act ? __builtin_amdgcn_exp2f(ms - (M == -__builtin_inff() ? 0.0f : M)) : 0.0f;
+        const float f = lane < act ? __builtin_amdgcn_exp2f(ms - M) : 0.0f;
         const float L = wave_sum_fast(lane < act ? f * ml.y : 0.0f);
         const float inv = L == 0.0f ? 0.0f : ieee_div(1.0f, L);
         constexpr int PL = HD / 64;
@@ -383,6 +428,155 @@ __global__ __launch_bounds__(K8_THREADS) void attn_kv8_join_kernel(Kv8AttnArgs a
         uint16_t* out = a.out + (int64_t)(row.t0 + rr / a.G) * a.out_stride + (size_t)(kh * a.G + rr % a.G) * HD + PL * lane;
 #pragma unroll
         for (int e = 0; e < PL; ++e) out[e] = (uint16_t)f2bf(O[e] * inv);
+    }
+}
+
+// Rows of more query rows than 16 * few tiles: one block of 4 waves per (row, KV head, 64 NT query rows), the
+// tokens of a row's end first (they see the most), a wave holding NT tiles.  The block walks the
+// positions that its tokens see in stages of 4 pages, which go through a double buffer in LDS as codes: the
+// next stage is in flight in registers while one is used, and one barrier a stage parts them.
+constexpr int K8_STAGE = 4;  // pages a stage, one a wave to fetch
+template <int HD, int NT, bool CAP>
+__global__ __launch_bounds__(K8_THREADS) __attribute__((amdgpu_waves_per_eu(2))) void attn_kv8_chunk_kernel(Kv8AttnArgs a, int few) {
+    constexpr int H = HD / 64;
+    constexpr int ROWS = K8_WAVES * 16 * NT;
+    constexpr int PB = 2 * H * 64;  // 16-byte pieces of a page: K, then V
+    const int lane = threadIdx.x & 63, c = lane & 15, g = lane >> 4;
+    const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+    const int kh = blockIdx.x % a.c.Hkv;
+    // the row that holds this block's tile: rows' tile counts summed by the wave, 64 rows at a time
+    int t = blockIdx.x / a.c.Hkv, r = -1;
+    for (int b0 = 0; b0 < a.B && r < 0; b0 += 64) {
+        int k = 0;
+        if (b0 + lane < a.B) {
+            const int rows = (a.cu_new[b0 + lane + 1] - a.cu_new[b0 + lane]) * a.G;
+            k = rows > few ? (rows + ROWS - 1) / ROWS : 0;
+        }
+        int sum = k;
+#pragma unroll
+        for (int o = 1; o < 64; o <<= 1) {
+            const int v = __shfl_up(sum, o, 64);
+            if (lane >= o) sum += v;
+        }
+        const unsigned long long past = __ballot(sum > t);
+        if (past) {
+            const int at = __ffsll(past) - 1;
+            r = b0 + at;
+            // from the row's end
+            t = __builtin_amdgcn_readlane(sum, at) - 1 - t;
+        } else {
+            t -= __builtin_amdgcn_readlane(sum, 63);
+        }
+    }
+    if (r < 0) return;
+    r = __builtin_amdgcn_readfirstlane(r);
+    t = __builtin_amdgcn_readfirstlane(t);
+    const K8Row row = k8_row(a, r);
+    const int live = row.n * a.G;
+    if (t * ROWS >= live) return;
+    // the positions that the block's, and the wave's, tokens see
+    const int rr0 = t * ROWS + wave * (16 * NT);
+    const int bp0 = row.p0 + t * ROWS / a.G, bp1 = row.p0 + (min((t + 1) * ROWS, live) - 1) / a.G;
+    const int wp0 = row.p0 + min(rr0, live - 1) / a.G, wp1 = row.p0 + (min(rr0 + 16 * NT, live) - 1) / a.G;
+    const int pg0 = a.window ? max(0, min(bp0 - a.window + 1, row.len)) / 16 : 0;
+    const int pg1 = max(0, min(bp1 + 1, row.len) + 15) / 16;
+    const int stages = max(0, (pg1 - pg0 + K8_STAGE - 1) / K8_STAGE);
+
+    __shared__ u32x4_k8 tile[2][K8_STAGE][PB];
+
+    uint4 qa[NT][2 * H];
+    int pc[NT];
+    k8_query<HD, NT>(a, row, kh, rr0, c, g, qa, pc);
+    const K8Soft so = k8_soft(a);
+    K8Acc<HD, NT> acc;
+    acc.clear();
+    const int32_t* ptab = a.page_table + (size_t)r * a.maxp;
+    const size_t head_bytes = (size_t)2 * 16 * HD;
+    const uint8_t* base = a.c.codes + (size_t)kh * head_bytes;
+
+    int id = -1;        // lane i: page pg0 + 64 k + i, of the 64 that hold the stage fetched last
+    uint32_t sc = 0;    // and its scale bytes
+    u32x4_k8 nx[2 * H]; // the wave's page of the next stage
+    int nmap = 0;       // which of that stage's pages are the cache's
+    uint2 nsc;          // and the scale bytes of its pages, 16 bits each
+    auto fetch = [&](int st, u32x4_k8 (&nx)[2 * H], int& id, uint32_t& sc, int& nmap, uint2& nsc) {
+        const int at = st * K8_STAGE % K8_IDS;
+        if (at == 0) {
+            const int i = pg0 + st * K8_STAGE + lane;
+            id = i < pg1 ? ptab[i] : -1;
+            if (id < 0 || id >= a.c.n_pages) id = -1;
+            sc = id < 0 ? 0u : *reinterpret_cast<const uint16_t*>(a.c.scales + ((size_t)id * a.c.Hkv + kh) * 2);
+        }
+        nmap = 0;
+#pragma unroll
+        for (int e = 0; e < K8_STAGE; ++e) nmap |= (__builtin_amdgcn_readlane(id, at + e) >= 0) << e;
+        static_assert(K8_STAGE == 4, "four 16-bit scales in a uint2");
+        nsc.x = (uint32_t)__builtin_amdgcn_readlane((int)sc, at) | (uint32_t)__builtin_amdgcn_readlane((int)sc, at + 1) << 16;
+        nsc.y = (uint32_t)__builtin_amdgcn_readlane((int)sc, at + 2) | (uint32_t)__builtin_amdgcn_readlane((int)sc, at + 3) << 16;
+        const int pg = max(__builtin_amdgcn_readlane(id, at + wave), 0);
+        const u32x4_k8* p = reinterpret_cast<const u32x4_k8*>(base + (size_t)pg * a.c.Hkv * head_bytes) + lane;
+#pragma unroll
+        for (int h = 0; h < 2 * H; ++h) nx[h] = p[64 * h];
+    };
+    auto put = [&](int buf, const u32x4_k8 (&nx)[2 * H]) {
+#pragma unroll
+        for (int h = 0; h < 2 * H; ++h) tile[buf][wave][64 * h + lane] = nx[h];
+    };
+    if (stages) {
+        fetch(0, nx, id, sc, nmap, nsc);
+        put(0, nx);
+    }
+    for (int st = 0; st < stages; ++st) {
+        const int map = nmap;
+        const uint2 scl = nsc;
+        __syncthreads();
+        if (st + 1 < stages) fetch(st + 1, nx, id, sc, nmap, nsc);
+        const int jst = 16 * (pg0 + st * K8_STAGE);
+        for (int hf = 0; hf < K8_STAGE / 2; ++hf) {
+            const int j0 = jst + 32 * hf;
+            // nothing for this wave's tokens in these 32 positions
+            if (j0 > wp1 || (a.window && j0 + 31 <= wp0 - a.window)) continue;
+            const int mapped = (map >> (2 * hf)) & 3;
+            const bool edge = mapped != 3 || j0 + 31 > wp0 || j0 + 32 > row.len || (a.window && j0 <= wp1 - a.window);
+            const uint32_t scw = hf ? scl.y : scl.x;  // the scale bytes of the two pages: K, V, K, V
+            const float ksc[2] = {__uint_as_float((scw & 0xffu) << 23), __uint_as_float((scw >> 16 & 0xffu) << 23)};
+            const float vsc[2] = {__uint_as_float((scw >> 8 & 0xffu) << 23), __uint_as_float((scw >> 24) << 23)};
+            float x[NT][8];
+            uint4 kb[2][H], vb[2][H];
+#pragma unroll
+            for (int e = 0; e < 2; ++e)
+#pragma unroll
+                for (int h = 0; h < H; ++h) kb[e][h] = __builtin_bit_cast(uint4, tile[st & 1][2 * hf + e][64 * h + lane]);
+            k8_scores<HD, NT, CAP>(kb, ksc, qa, so, x);
+#pragma unroll
+            for (int e = 0; e < 2; ++e)
+#pragma unroll
+                for (int h = 0; h < H; ++h) vb[e][h] = __builtin_bit_cast(uint4, tile[st & 1][2 * hf + e][64 * (H + h) + lane]);
+            if (edge) {
+#pragma unroll
+                for (int u = 0; u < NT; ++u)
+#pragma unroll
+                    for (int i = 0; i < 8; ++i)
+                        x[u][i] = k8_sees(row, a.window, j0, mapped, g, i, pc[u]) ? x[u][i] : -__builtin_inff();
+            }
+            bf16x8_k8 p[NT][1];
+            k8_softmax<HD, NT, 1>(x, so.f, acc, p);
+            if (edge) k8_mend_nan<HD, NT>(vb, acc, row, a.window, j0, mapped, g, pc);
+            k8_pv<HD, NT, 1>(vb, vsc, p, acc);
+        }
+        if (st + 1 < stages) put((st + 1) & 1, nx);
+    }
+#pragma unroll
+    for (int u = 0; u < NT; ++u) {
+        const float L = k8_col_sum(acc.l[u]);
+        const float inv = L == 0.0f ? 0.0f : ieee_div(1.0f, L);
+        const int rr = rr0 + 16 * u + c;
+        if (rr >= live) continue;
+        uint16_t* out = a.out + (int64_t)(row.t0 + rr / a.G) * a.out_stride + (size_t)(kh * a.G + rr % a.G) * HD + 4 * g;
+#pragma unroll
+        for (int d = 0; d < HD / 16; ++d)
+            *reinterpret_cast<uint2*>(out + 16 * d) =
+                make_uint2(k8_pack(acc.o[u][d][0] * inv, acc.o[u][d][1] * inv), k8_pack(acc.o[u][d][2] * inv, acc.o[u][d][3] * inv));
     }
 }
 
@@ -426,65 +620,28 @@ static hipError_t k8_few(const Kv8AttnArgs& a, const K8Plan& p, hipStream_t s) {
     return hipGetLastError();
 }
 
-__global__ __launch_bounds__(256) void attn_kv8_kernel(Kv8AttnArgs a, int few) {
-    const int lane = threadIdx.x & 63;
-    const int64_t w = (int64_t)blockIdx.x * 4 + (threadIdx.x >> 6);
-    const int t = (int)(w / a.Hq), head = (int)(w % a.Hq), kh = head / a.G, hd = a.c.hd;
-    if (t >= a.T) return;
-    int r = t, t0 = t, n = 1;
-    if (a.cu_new) {
-        int lo = 0, hi = a.B;  // the last row that begins at or before t
-        while (hi - lo > 1) {
-            const int mid = (lo + hi) >> 1;
-            if (a.cu_new[mid] <= t) lo = mid; else hi = mid;
-        }
-        r = lo;
-        t0 = a.cu_new[r];
-        n = a.cu_new[r + 1] - t0;
-        if (t < t0 || t >= t0 + n) return;
-    }
-    if (n * a.G <= few) return;
-    const int len = min(a.lens[r], 16 * a.maxp), p = a.lens[r] - n + (t - t0);
-    const int j1 = min(p + 1, len), j0 = a.window ? max(0, p - a.window + 1) : 0;
-    const int per = hd / 64;
-    const uint16_t* q = a.q + t * a.q_stride + head * hd;
-    float qv[2], o[2] = {0.f, 0.f}, m = -__builtin_inff(), l = 0.f;
-    for (int e = 0; e < per; ++e) qv[e] = bf2f(q[64 * e + lane]) * a.scale;
-    for (int j = j0; j < j1; ++j) {
-        const int pg = a.page_table[(size_t)r * a.maxp + j / 16];
-        if (pg < 0 || pg >= a.c.n_pages) continue;
-        const size_t ph = ((size_t)pg * a.c.Hkv + kh) * 2;
-        const uint8_t* kp = a.c.codes + ph * (size_t)(16 * hd);
-        const uint8_t* vp = kp + 16 * hd;
-        const float ksc = __uint_as_float((uint32_t)a.c.scales[ph] << 23);
-        const float vsc = __uint_as_float((uint32_t)a.c.scales[ph + 1] << 23);
-        const int i = j % 16;
-        float s = 0.f, v[2];
-        for (int e = 0; e < per; ++e) {
-            const int d = 64 * e + lane;
-            s += qv[e] * __builtin_amdgcn_cvt_f32_fp8(kp[((d >> 4) * 16 + i) * 16 + (d & 15)], 0);
-            v[e] = __builtin_amdgcn_cvt_f32_fp8(vp[((e * 4 + (i >> 2)) * 16 + (d & 15)) * 16 + ((d >> 4) & 3) * 4 + (i & 3)], 0) * vsc;
-        }
-        s = wave_sum_fast(s) * ksc;
-        if (a.cap > 0.f) s = a.cap * (1.0f - 2.0f / (1.0f + expf(2.0f * (s * a.inv_cap))));
-        const float mn = fmaxf(m, s);
-        const float al = m == -__builtin_inff() ? 0.f : expf(m - mn), pr = expf(s - mn);
-        m = mn;
-        l = l * al + pr;
-        for (int e = 0; e < per; ++e) o[e] = o[e] * al + pr * v[e];
-    }
-    const float inv = l == 0.f ? 0.f : 1.0f / l;
-    for (int e = 0; e < per; ++e) a.out[t * a.out_stride + head * hd + 64 * e + lane] = (uint16_t)f2bf(o[e] * inv);
+constexpr int K8_CHUNK_TILES = 2;  // tiles of 16 query rows a wave of the chunk kernel holds
+
+template <int HD>
+static hipError_t k8_chunk(const Kv8AttnArgs& a, int few, hipStream_t s) {
+    constexpr int NT = K8_CHUNK_TILES, ROWS = K8_WAVES * 16 * NT;
+    // at most: every row's last tile may be partly empty
+    const int64_t tiles = (int64_t)a.T * a.G / ROWS + std::min(a.B, a.T);
+    const dim3 grid((unsigned)(tiles * a.c.Hkv));
+    if (a.cap > 0.0f)
+        hipLaunchKernelGGL((attn_kv8_chunk_kernel<HD, NT, true>), grid, dim3(K8_THREADS), 0, s, a, few);
+    else
+        hipLaunchKernelGGL((attn_kv8_chunk_kernel<HD, NT, false>), grid, dim3(K8_THREADS), 0, s, a, few);
+    return hipGetLastError();
 }
 
 hipError_t launch_kv8_attention(const Kv8AttnArgs& a, hipStream_t s) {
     const K8Plan p = k8_plan(a);
+    const int few = 16 * p.nt;
     const hipError_t e = a.c.hd == 128 ? (p.nt == 1 ? k8_few<128, 1>(a, p, s) : k8_few<128, 2>(a, p, s))
                                        : (p.nt == 1 ? k8_few<64, 1>(a, p, s) : k8_few<64, 2>(a, p, s));
-    if (e != hipSuccess || a.max_new * a.G <= 16 * p.nt) return e;
-    const int64_t waves = (int64_t)a.T * a.Hq;
-    hipLaunchKernelGGL(attn_kv8_kernel, dim3((unsigned)((waves + 3) / 4)), dim3(256), 0, s, a, 16 * p.nt);
-    return hipGetLastError();
+    if (e != hipSuccess || (int64_t)a.max_new * a.G <= few) return e;
+    return a.c.hd == 128 ? k8_chunk<128>(a, few, s) : k8_chunk<64>(a, few, s);
 }
 
 }  // namespace mg
