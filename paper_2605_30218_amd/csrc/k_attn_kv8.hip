@@ -393,42 +393,51 @@ __global__ __launch_bounds__(K8_THREADS) __attribute__((amdgpu_waves_per_eu(NT =
     }
 }
 
-// Joins the splits of attn_kv8_few_kernel in their order: one block per (row, KV head), a wave a query row.
+// Joins the splits of attn_kv8_few_kernel in their order: a wave per query row of a (row, KV head).
 template <int HD, int NT>
 __global__ __launch_bounds__(K8_THREADS) void attn_kv8_join_kernel(Kv8AttnArgs a, int sp, int nsplit) {
-    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
+    constexpr int PL = HD / 64;  // consecutive features of a lane
+    constexpr int AHEAD = 8;     // splits whose outputs are requested together, the first before their weights are known
+    const int lane = threadIdx.x & 63, rr = blockIdx.y * K8_WAVES + (threadIdx.x >> 6);
     const int kh = blockIdx.x % a.c.Hkv, r = blockIdx.x / a.c.Hkv;
     const K8Row row = k8_row(a, r);
-    const int live = row.n * a.G;
-    if (row.n <= 0 || live > 16 * NT) return;
+    if (row.n <= 0 || row.n * a.G > 16 * NT || rr >= row.n * a.G) return;
     const int act = k8_active(max(row.pgb - row.pga, 0), sp, nsplit);
     if (act == 1) return;
     const size_t first = ((size_t)r * a.c.Hkv + kh) * nsplit;
     const float* mls = a.part + (size_t)a.B * a.c.Hkv * nsplit * (16 * NT) * HD;
-    for (int rr = wave; rr < live; rr += K8_WAVES) {
-        // nsplit <= 64: lane s has split s
-        const size_t at = (first + min(lane, act - 1)) * (16 * NT) + rr;
-        const float2 ml = *reinterpret_cast<const float2*>(mls + 2 * at);
-        const float ms = lane < act ? ml.x : -__builtin_inff();
-        const float M = wave_max(ms);
-        const float f = lane < act ? __builtin_amdgcn_exp2f(ms - M) : 0.0f;
-        const float L = wave_sum_fast(lane < act ? f * ml.y : 0.0f);
-        const float inv = L == 0.0f ? 0.0f : ieee_div(1.0f, L);
-        constexpr int PL = HD / 64;
-        float O[PL];
+    const float* po = a.part + (first * (16 * NT) + rr) * HD + PL * lane;
+    using vec = float __attribute__((ext_vector_type(PL)));
+    vec v[AHEAD];
+    // nsplit <= 64: lane s has split s
+    const float2 ml = *reinterpret_cast<const float2*>(mls + 2 * ((first + min(lane, act - 1)) * (16 * NT) + rr));
 #pragma unroll
-        for (int e = 0; e < PL; ++e) O[e] = 0.0f;
-        const float* po = a.part + (first * (16 * NT) + rr) * HD + PL * lane;
-#pragma unroll 4
-        for (int s = 0; s < act; ++s) {
-            const float w = __shfl(f, s, 64);
+    for (int k = 0; k < AHEAD; ++k) v[k] = *reinterpret_cast<const vec*>(po + (size_t)min(k, act - 1) * (16 * NT) * HD);
+    const float M = wave_max(ml.x);
+    const float f = lane < act ? __builtin_amdgcn_exp2f(ml.x - M) : 0.0f;
+    const float L = wave_sum_fast(lane < act ? f * ml.y : 0.0f);
+    const float inv = L == 0.0f ? 0.0f : ieee_div(1.0f, L);
+    float O[PL];
 #pragma unroll
-            for (int e = 0; e < PL; ++e) O[e] += w * po[(size_t)s * (16 * NT) * HD + e];
+    for (int e = 0; e < PL; ++e) O[e] = 0.0f;
+    for (int s = 0; s < act; s += AHEAD) {
+        if (s) {
+#pragma unroll
+            for (int k = 0; k < AHEAD; ++k) v[k] = *reinterpret_cast<const vec*>(po + (size_t)min(s + k, act - 1) * (16 * NT) * HD);
         }
-        uint16_t* out = a.out + (int64_t)(row.t0 + rr / a.G) * a.out_stride + (size_t)(kh * a.G + rr % a.G) * HD + PL * lane;
 #pragma unroll
-        for (int e = 0; e < PL; ++e) out[e] = (uint16_t)f2bf(O[e] * inv);
+        for (int k = 0; k < AHEAD; ++k) {
+            if (s + k >= act) break;
+            const float w = __shfl(f, s + k, 64);
+#pragma unroll
+            for (int e = 0; e < PL; ++e) O[e] += w * v[k][e];
+        }
     }
+    uint16_t* out = a.out + (int64_t)(row.t0 + rr / a.G) * a.out_stride + (size_t)(kh * a.G + rr % a.G) * HD + PL * lane;
+    if constexpr (PL == 2)
+        *reinterpret_cast<uint32_t*>(out) = k8_pack(O[0] * inv, O[1] * inv);
+    else
+        out[0] = (uint16_t)f2bf(O[0] * inv);
 }
 
 // Rows of more query rows than 16 * few tiles: one block of 4 waves per (row, KV head, 64 NT query rows), the
@@ -616,7 +625,8 @@ static hipError_t k8_few(const Kv8AttnArgs& a, const K8Plan& p, hipStream_t s) {
     else
         hipLaunchKernelGGL((attn_kv8_few_kernel<HD, NT, false>), grid, dim3(K8_THREADS), 0, s, a, p.sp, p.nsplit);
     if (p.nsplit > 1)
-        hipLaunchKernelGGL((attn_kv8_join_kernel<HD, NT>), dim3(a.B * a.c.Hkv), dim3(K8_THREADS), 0, s, a, p.sp, p.nsplit);
+        hipLaunchKernelGGL((attn_kv8_join_kernel<HD, NT>), dim3(a.B * a.c.Hkv, (std::min(a.max_new * a.G, 16 * NT) + K8_WAVES - 1) / K8_WAVES),
+                           dim3(K8_THREADS), 0, s, a, p.sp, p.nsplit);
     return hipGetLastError();
 }
 

@@ -265,26 +265,52 @@ def margin_gate_noalloc(B, V, logits, protected_mask, tau, top1, margin, gate, g
 
 # ---------------------------------------------------------------- batch plan and 8-bit K/V cache
 
+# A decode step makes these calls once a layer, and their kernels take some microseconds: the checks are
+# plain comparisons, messages are made only when one fails, and the device is switched only when
+# the tensors are on another than the current one.
+
 BatchPlan = collections.namedtuple("BatchPlan", "cu_new lens admitted positions rows slots n_left")
+_BF16 = (torch.bfloat16, torch.int16)
+_raw_stream = torch._C._cuda_getCurrentRawStream if hasattr(torch._C, "_cuda_getCurrentRawStream") else None
 
 
-def _need(ok, what):
-    if not ok:
-        raise ValueError(what)
+def _refuse(name, t, want):
+    what = f"{t.dtype} {tuple(t.shape)} strides {t.stride()} on {t.device}" if isinstance(t, torch.Tensor) else repr(t)
+    raise ValueError(f"{name}: {want} is needed, got {what}")
 
 
 def _ints(name, t, device, numel=None):
-    """An int32 tensor of the call's device, contiguous, with the given number of values."""
-    _need(t.dtype is torch.int32 and t.device == device and t.is_contiguous(),
-          f"{name}: a contiguous int32 tensor on {device} is needed, got {t.dtype} on {t.device}")
-    _need(numel is None or t.numel() == numel, f"{name}: {t.numel()} values, {numel} needed")
+    """The address of an int32 tensor of the call's device, contiguous, with the given number of values."""
+    if t.dtype is not torch.int32 or t.device != device or not t.is_contiguous() or \
+            (numel is not None and t.numel() != numel):
+        _refuse(name, t, f"a contiguous int32 tensor of {'any' if numel is None else numel} values on {device}")
     return t.data_ptr()
 
 
-def _on(device, stream):
-    """The stream to enqueue on: the given one, or the device's current one."""
-    _need(device.type == "cuda", f"tensors on the GPU are needed, got {device}")
-    return (torch.cuda.current_stream(device) if stream is None else stream).cuda_stream
+def _call(name, device, stream, fn, *args):
+    """fn(*args, stream) on the tensors' device, on the given stream or the device's current one."""
+    if device.type != "cuda":
+        raise ValueError(f"{name}: tensors on the GPU are needed, got {device}")
+    if device.index != torch.cuda.current_device():
+        with torch.cuda.device(device):
+            return _call(name, device, stream, fn, *args)
+    if stream is not None:
+        s = stream.cuda_stream
+    elif _raw_stream is not None:
+        s = _raw_stream(device.index)
+    else:
+        s = torch.cuda.current_stream(device).cuda_stream
+    rc = fn(*args, s)
+    if rc != MG_OK:
+        raise MgError(name, rc)
+
+
+def _made(t, stream):
+    """A tensor that a call took from torch's allocator, which must not reuse it before the call's
+    own stream is done with it."""
+    if stream is not None:
+        t.record_stream(stream)
+    return t
 
 
 def batch_plan(ctx_len, n_new, free_pages, n_free, page_table, max_tokens, out=None, stream=None):
@@ -292,49 +318,54 @@ def batch_plan(ctx_len, n_new, free_pages, n_free, page_table, max_tokens, out=N
     tensors int32 on one GPU: ctx_len, n_new [B], free_pages [any], n_free [1] (the count in use),
     page_table [B, max_pages] (updated in place).  out: a BatchPlan to write into, whose tensors the
     caller keeps (a captured step), or None for new ones."""
-    dev = ctx_len.device
-    _need(page_table.dim() == 2, "page_table: [B, max_pages] is needed")
+    dev, M = ctx_len.device, int(max_tokens)
+    if page_table.dim() != 2:
+        _refuse("page_table", page_table, "[B, max_pages]")
+    if not 0 <= M <= 1 << 30:
+        _refuse("max_tokens", M, "0 .. 2^30")
     B, maxp = page_table.shape
-    M = int(max_tokens)
     args = (_ints("ctx_len", ctx_len, dev, B), _ints("n_new", n_new, dev, B), _ints("free_pages", free_pages, dev),
             _ints("n_free", n_free, dev, 1), M, _ints("page_table", page_table, dev))
-    _need(0 <= M <= 1 << 30, f"max_tokens {M}")
-    s = _on(dev, stream)
     if out is None:
-        # one allocation: positions, rows, slots, cu_new, lens, admitted, n_left
-        buf = torch.empty(3 * M + 3 * B + 2, dtype=torch.int32, device=dev)
-        pos, row, slot, cu, lens, adm, left = buf.split_with_sizes([M, M, M, B + 1, B, B, 1])
+        buf = _made(torch.empty(3 * M + 3 * B + 2, dtype=torch.int32, device=dev), stream)
+        cu, lens, adm, pos, row, slot, left = buf.split_with_sizes((B + 1, B, B, M, M, M, 1))
         out = BatchPlan(cu, lens, adm, pos, row, slot, left)
-    po = [_ints(n, t, dev, k) for n, t, k in zip(BatchPlan._fields, out, (B + 1, B, B, M, M, M, 1))]
-    with torch.cuda.device(dev):
-        _check("mg_batch_plan", load().mg_batch_plan(B, maxp, *args, *po, s))
+        at = buf.data_ptr()
+        lists = 3 * B + 1
+        ptrs = [at + 4 * k for k in (0, B + 1, 2 * B + 1, lists, lists + M, lists + 2 * M, lists + 3 * M)]
+    else:
+        ptrs = [_ints(n, t, dev, k) for n, t, k in zip(BatchPlan._fields, out, (B + 1, B, B, M, M, M, 1))]
+    _call("mg_batch_plan", dev, stream, load().mg_batch_plan, B, maxp, *args, *ptrs)
     return out
 
 
 def _kv8(codes, scales):
     """The MgKv8Cache of a layer's codes [n_pages, Hkv, 2, 16 hd] and scales [n_pages, Hkv, 2]."""
-    _need(codes.dtype is torch.uint8 and scales.dtype is torch.uint8 and codes.is_contiguous() and
-          scales.is_contiguous() and codes.device == scales.device, "codes and scales: contiguous uint8 of one device")
-    _need(codes.dim() == 4 and codes.shape[2] == 2 and scales.shape == codes.shape[:3],
-          f"codes {tuple(codes.shape)}, scales {tuple(scales.shape)}: [n_pages, Hkv, 2, 16 hd] and [n_pages, Hkv, 2]")
-    return MgKv8Cache(codes.data_ptr(), scales.data_ptr(), codes.shape[0], codes.shape[1], codes.shape[3] // 16)
+    shape = codes.shape
+    if codes.dtype is not torch.uint8 or len(shape) != 4 or shape[2] != 2 or not codes.is_contiguous():
+        _refuse("codes", codes, "contiguous uint8 [n_pages, Hkv, 2, 16 hd]")
+    if scales.dtype is not torch.uint8 or scales.shape != shape[:3] or not scales.is_contiguous() or \
+            scales.device != codes.device:
+        _refuse("scales", scales, f"contiguous uint8 [n_pages, Hkv, 2] for codes {tuple(shape)} on {codes.device}")
+    return MgKv8Cache(codes.data_ptr(), scales.data_ptr(), shape[0], shape[1], shape[3] // 16)
 
 
 def kv8_empty(n_pages, n_kv_heads, head_dim, device="cuda"):
     """An empty 8-bit cache of one layer: (codes, scales)."""
-    nb = load().mg_kv8_code_bytes(n_pages, n_kv_heads, head_dim)
-    if nb == 0:
+    if load().mg_kv8_code_bytes(n_pages, n_kv_heads, head_dim) == 0:
         raise MgError("mg_kv8_code_bytes", -2)
     return (torch.zeros((n_pages, n_kv_heads, 2, 16 * head_dim), dtype=torch.uint8, device=device),
             torch.zeros((n_pages, n_kv_heads, 2), dtype=torch.uint8, device=device))
 
 
 def _rows16(name, t, n, heads, hd, device):
-    """bf16 rows [n, heads, hd] (or their bits as int16), each row contiguous: (pointer, stride)."""
-    _need(t.dtype in (torch.bfloat16, torch.int16) and t.device == device, f"{name}: bf16 on {device} is needed")
-    _need(t.shape == (n, heads, hd) and (n == 0 or (t.stride(2) == 1 and (heads == 1 or t.stride(1) == hd))),
-          f"{name}: [{n}, {heads}, {hd}] with contiguous rows is needed, got {tuple(t.shape)} strides {t.stride()}")
-    return t.data_ptr(), (t.stride(0) if n > 1 else heads * hd)
+    """(address, stride) of bf16 rows [n, heads, hd] (or their bits as int16), each row contiguous."""
+    if t.dtype not in _BF16 or t.device != device or t.shape != (n, heads, hd):
+        _refuse(name, t, f"bf16 [{n}, {heads}, {hd}] on {device}")
+    st = t.stride()
+    if n and (st[2] != 1 or (heads > 1 and st[1] != hd)):
+        _refuse(name, t, "rows [heads, head_dim] without gaps")
+    return t.data_ptr(), (st[0] if n > 1 else heads * hd)
 
 
 def kv8_append(codes, scales, k, v, slots, stream=None):
@@ -343,9 +374,7 @@ def kv8_append(codes, scales, k, v, slots, stream=None):
     dev, n = codes.device, slots.numel()
     kp, ks = _rows16("k", k, n, c.n_kv_heads, c.head_dim, dev)
     vp, vs = _rows16("v", v, n, c.n_kv_heads, c.head_dim, dev)
-    sl, s = _ints("slots", slots, dev), _on(dev, stream)
-    with torch.cuda.device(dev):
-        _check("mg_kv8_append", load().mg_kv8_append(C.byref(c), n, kp, ks, vp, vs, sl, s))
+    _call("mg_kv8_append", dev, stream, load().mg_kv8_append, C.byref(c), n, kp, ks, vp, vs, _ints("slots", slots, dev))
 
 
 def kv8_read(codes, scales, slots, k_out=None, v_out=None, stream=None):
@@ -353,40 +382,45 @@ def kv8_read(codes, scales, slots, k_out=None, v_out=None, stream=None):
     outside the cache are not written: in a new tensor they hold anything."""
     c = _kv8(codes, scales)
     dev, n = codes.device, slots.numel()
-    new = [torch.empty((n, c.n_kv_heads, c.head_dim), dtype=torch.bfloat16, device=dev) if t is None else t
-           for t in (k_out, v_out)]
-    (kp, ks), (vp, vs) = (_rows16(m, t, n, c.n_kv_heads, c.head_dim, dev) for m, t in zip(("k_out", "v_out"), new))
-    sl, s = _ints("slots", slots, dev), _on(dev, stream)
-    with torch.cuda.device(dev):
-        _check("mg_kv8_read", load().mg_kv8_read(C.byref(c), n, sl, kp, ks, vp, vs, s))
-    return new[0], new[1]
+    if k_out is None:
+        k_out = _made(torch.empty((n, c.n_kv_heads, c.head_dim), dtype=torch.bfloat16, device=dev), stream)
+    if v_out is None:
+        v_out = _made(torch.empty((n, c.n_kv_heads, c.head_dim), dtype=torch.bfloat16, device=dev), stream)
+    kp, ks = _rows16("k_out", k_out, n, c.n_kv_heads, c.head_dim, dev)
+    vp, vs = _rows16("v_out", v_out, n, c.n_kv_heads, c.head_dim, dev)
+    _call("mg_kv8_read", dev, stream, load().mg_kv8_read, C.byref(c), n, _ints("slots", slots, dev), kp, ks, vp, vs)
+    return k_out, v_out
 
 
 def kv8_attention(codes, scales, q, page_table, lens, cu_new=None, max_new=1, max_len=0, scale=None, window=0,
                   softcap=0.0, out=None, workspace=None, stream=None):
     """mg_kv8_attention: q [T, Hq, hd] attends over the cache's positions of its rows -> out [T, Hq, hd]
     bf16.  Tokens behind the last row's are not written: in a new tensor they hold anything.
-    workspace: a uint8 tensor of kv8_attention_workspace_bytes, or None to take one per call."""
+    workspace: a contiguous uint8 tensor that no other call in flight uses, or None to take one per
+    call."""
     c = _kv8(codes, scales)
     dev = codes.device
-    _need(q.dim() == 3 and page_table.dim() == 2, "q [T, Hq, hd] and page_table [B, max_pages] are needed")
+    if q.dim() != 3 or q.shape[2] != c.head_dim:
+        _refuse("q", q, f"[T, Hq, {c.head_dim}]")
+    if page_table.dim() != 2:
+        _refuse("page_table", page_table, "[B, max_pages]")
     T, Hq, hd = q.shape
     B, maxp = page_table.shape
-    _need(hd == c.head_dim, f"q: head_dim {hd}, the cache's is {c.head_dim}")
     if out is None:
-        out = torch.empty((T, Hq, hd), dtype=q.dtype, device=dev)
+        out = _made(torch.empty((T, Hq, hd), dtype=q.dtype, device=dev), stream)
     qp, qs = _rows16("q", q, T, Hq, hd, dev)
     op, os_ = _rows16("out", out, T, Hq, hd, dev)
-    a = MgKv8AttnArgs(B, T, Hq, int(max_new), int(max_len), maxp, int(window), 0.0 if scale is None else float(scale),
-                      float(softcap), qp, qs, op, os_, _ints("page_table", page_table, dev),
-                      _ints("lens", lens, dev, B), None if cu_new is None else _ints("cu_new", cu_new, dev, B + 1))
-    s, lib = _on(dev, stream), load()
-    with torch.cuda.device(dev):
-        need = lib.mg_kv8_attention_workspace_bytes(C.byref(c), C.byref(a))
-        if workspace is None and need:
-            workspace = torch.empty(need, dtype=torch.uint8, device=dev)
-        _check("mg_kv8_attention", lib.mg_kv8_attention(C.byref(c), C.byref(a), _ptr(workspace),
-                                                        0 if workspace is None else workspace.numel(), s))
+    a = MgKv8AttnArgs(B, T, Hq, max_new, max_len, maxp, window, 0.0 if scale is None else scale, softcap, qp, qs, op,
+                      os_, _ints("page_table", page_table, dev), _ints("lens", lens, dev, B),
+                      None if cu_new is None else _ints("cu_new", cu_new, dev, B + 1))
+    cp, ap, lib = C.byref(c), C.byref(a), load()
+    if workspace is None:
+        need = lib.mg_kv8_attention_workspace_bytes(cp, ap)
+        workspace = _made(torch.empty(need, dtype=torch.uint8, device=dev), stream) if need else None
+    elif workspace.dtype is not torch.uint8 or workspace.device != dev or not workspace.is_contiguous():
+        _refuse("workspace", workspace, f"contiguous uint8 on {dev}")
+    ws, n = (None, 0) if workspace is None else (workspace.data_ptr(), workspace.numel())
+    _call("mg_kv8_attention", dev, stream, lib.mg_kv8_attention, cp, ap, ws, n)
     return out
 
 
