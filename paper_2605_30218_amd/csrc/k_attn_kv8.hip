@@ -262,8 +262,8 @@ __device__ __forceinline__ void k8_query(const Kv8AttnArgs& a, const K8Row& row,
 // Rows of few query rows (tokens times query heads of a KV head <= 16 NT): one block of 4 waves per
 // (row, KV head, split of the row's pages), a wave taking every 4th step of its pages.  The K/V stream
 // bounds it, so the matrix cores have the time for two terms of a probability.
-template <int HD, int NT, bool CAP>
-__global__ __launch_bounds__(K8_THREADS) __attribute__((amdgpu_waves_per_eu(NT == 1 ? 3 : 2))) void attn_kv8_few_kernel(Kv8AttnArgs a, int sp, int nsplit) {
+template <int HD, int NT, int WAVES, bool CAP>
+__global__ __launch_bounds__(64 * WAVES) __attribute__((amdgpu_waves_per_eu(NT == 1 ? (WAVES > 8 ? 4 : WAVES > 4 ? 2 : 3) : 2))) void attn_kv8_few_kernel(Kv8AttnArgs a, int sp, int nsplit) {
     constexpr int H = HD / 64;        // 1 KiB runs of a page of K or V
     constexpr int DT = HD / 16;       // output tiles
     constexpr int OS = HD + 4;        // padded row of O in LDS
@@ -279,8 +279,8 @@ __global__ __launch_bounds__(K8_THREADS) __attribute__((amdgpu_waves_per_eu(NT =
     const int per = ((npg + act - 1) / act + 1) & ~1;
     const int pg0 = row.pga + split * per, pg1 = split == act - 1 ? row.pgb : min(row.pgb, pg0 + per);
 
-    __shared__ __attribute__((aligned(16))) float wo[K8_WAVES][16 * NT][OS];
-    __shared__ float wm[K8_WAVES][16 * NT], wl[K8_WAVES][16 * NT];
+    __shared__ __attribute__((aligned(16))) float wo[WAVES][16 * NT][OS];
+    __shared__ float wm[WAVES][16 * NT], wl[WAVES][16 * NT];
 
     uint4 qa[NT][2 * H];
     int pc[NT];
@@ -306,15 +306,16 @@ __global__ __launch_bounds__(K8_THREADS) __attribute__((amdgpu_waves_per_eu(NT =
                 const int pg = max(__builtin_amdgcn_readlane(id, 2 * s + e), 0);
                 const uint8_t* p = base + (size_t)pg * a.c.Hkv * head_bytes + side * (16 * HD);
 #pragma unroll
-                for (int h = 0; h < H; ++h) x[e][h] = *reinterpret_cast<const uint4*>(p + h * 1024 + lane * 16);
+                for (int h = 0; h < H; ++h)
+                    x[e][h] = __builtin_bit_cast(uint4, __builtin_nontemporal_load(reinterpret_cast<const u32x4_k8*>(p + h * 1024 + lane * 16)));
             }
         };
         if (wave < steps) {
             fetch(wave, 0, kb);
             fetch(wave, 1, vb);
         }
-        for (int s = wave; s < steps; s += K8_WAVES) {
-            const bool more = s + K8_WAVES < steps;
+        for (int s = wave; s < steps; s += WAVES) {
+            const bool more = s + WAVES < steps;
             float ksc[2], vsc[2];
             int mapped = 0;
 #pragma unroll
@@ -330,7 +331,7 @@ __global__ __launch_bounds__(K8_THREADS) __attribute__((amdgpu_waves_per_eu(NT =
             float x[NT][8];
             k8_scores<HD, NT, CAP>(kb, ksc, qa, so, x);
             __builtin_amdgcn_sched_barrier(0);
-            if (more) fetch(s + K8_WAVES, 0, kb);  // its registers are free: in flight under the rest of the step
+            if (more) fetch(s + WAVES, 0, kb);  // its registers are free: in flight under the rest of the step
             __builtin_amdgcn_sched_barrier(0);
             if (edge) {
 #pragma unroll
@@ -344,7 +345,7 @@ __global__ __launch_bounds__(K8_THREADS) __attribute__((amdgpu_waves_per_eu(NT =
             if (edge) k8_mend_nan<HD, NT>(vb, acc, row, a.window, j0, mapped, g, pc);
             k8_pv<HD, NT, 2>(vb, vsc, p, acc);
             __builtin_amdgcn_sched_barrier(0);
-            if (more) fetch(s + K8_WAVES, 1, vb);
+            if (more) fetch(s + WAVES, 1, vb);
         }
     }
 
@@ -362,15 +363,15 @@ __global__ __launch_bounds__(K8_THREADS) __attribute__((amdgpu_waves_per_eu(NT =
     }
     __syncthreads();
     const int live = row.n * a.G;
-    for (int i = threadIdx.x; i < live * (HD / 4); i += K8_THREADS) {
+    for (int i = threadIdx.x; i < live * (HD / 4); i += 64 * WAVES) {
         const int rr = i / (HD / 4), d = i % (HD / 4) * 4;
         float M = wm[0][rr];
 #pragma unroll
-        for (int w = 1; w < K8_WAVES; ++w) M = fmaxf(M, wm[w][rr]);
+        for (int w = 1; w < WAVES; ++w) M = fmaxf(M, wm[w][rr]);
         float L = 0.0f;
         f32x4_k8 O = f32x4_k8{0.f, 0.f, 0.f, 0.f};
 #pragma unroll
-        for (int w = 0; w < K8_WAVES; ++w) {
+        for (int w = 0; w < WAVES; ++w) {
             const float f = __builtin_amdgcn_exp2f(wm[w][rr] - M);
             L += f * wl[w][rr];
             O += f * *reinterpret_cast<const f32x4_k8*>(&wo[w][rr][d]);
@@ -589,14 +590,23 @@ __global__ __launch_bounds__(K8_THREADS) __attribute__((amdgpu_waves_per_eu(2)))
     }
 }
 
-// The launch of rows of few query rows: tiles a block holds, pages a split, splits of a row.
+// The launch of rows of few query rows: tiles and waves of a block, pages of a split, splits of a row.
+// Measured on graphs of calls, 32 query heads over 8 KV heads of 128, us:
+//   - rows are split until two blocks a CU are there (three: 64 rows of 512..768, 512 blocks without a split,
+//     18 -> 24, as the join is a launch of its own; 23 rows of four tokens 25 -> 31);
+//   - a split takes at most 128 pages (64: 32 rows of 4096..16384 122 -> 125, 128 ragged rows 60.4 -> 59.2;
+//     256: 122 -> 134);
+//   - where the blocks of unsplit rows fit the device at once and a row has few pages, one block of 8
+//     waves takes a row whole: one row of 512 7.1 -> 6.3, 32 rows of 512 12.1 -> 9.8; at 64 pages one row
+//     7.9 -> 9.7, but 32 rows 17.0 -> 14.7, so up to 32 pages, or 64 where the blocks are half of the CUs.
 struct K8Plan {
-    int nt, sp, nsplit;
+    int nt, waves, sp, nsplit;
 };
-constexpr int K8_MIN_PAGES = 8;    // pages a split takes at least: a step of every wave
-constexpr int K8_MAX_PAGES = 64;
+constexpr int K8_MIN_PAGES = 8;  // pages a split takes at least: a step of every wave
+constexpr int K8_MAX_PAGES = 128;
 constexpr int K8_MAX_SPLITS = 64;
-constexpr int K8_BLOCKS_PER_CU = 3;
+constexpr int K8_BLOCKS_PER_CU = 2;
+constexpr int K8_WHOLE_PAGES = 32;
 static K8Plan k8_plan(const Kv8AttnArgs& a) {
     K8Plan p;
     p.nt = a.max_new * a.G <= 16 ? 1 : 2;
@@ -604,9 +614,14 @@ static K8Plan k8_plan(const Kv8AttnArgs& a) {
     if (a.window) len = std::min<int64_t>(len, (int64_t)a.window + a.max_new + 15);
     const int64_t pages = std::max<int64_t>(1, (len + 15) / 16);
     const int64_t blocks = (int64_t)a.B * a.c.Hkv;
-    const int64_t want = std::max<int64_t>(1, (K8_BLOCKS_PER_CU * a.n_cu + blocks - 1) / blocks);
+    const int64_t want = std::max<int64_t>(1, (K8_BLOCKS_PER_CU * a.n_cu + blocks / 2) / blocks);
     int64_t sp = std::min<int64_t>(K8_MAX_PAGES, std::max<int64_t>(K8_MIN_PAGES, (pages + want - 1) / want));
     sp = std::max(sp, (pages + K8_MAX_SPLITS - 1) / K8_MAX_SPLITS);
+    p.waves = K8_WAVES;
+    if (p.nt == 1 && blocks <= a.n_cu && pages <= (2 * blocks >= a.n_cu ? 2 : 1) * K8_WHOLE_PAGES) {
+        p.waves = 2 * K8_WAVES;
+        sp = pages;
+    }
     p.sp = (int)sp;
     p.nsplit = (int)((pages + sp - 1) / sp);
     return p;
@@ -617,15 +632,24 @@ size_t kv8_attention_ws_bytes(const Kv8AttnArgs& a) {
     return p.nsplit == 1 ? 0 : (size_t)a.B * a.c.Hkv * p.nsplit * (16 * p.nt) * (a.c.hd + 2) * sizeof(float);
 }
 
-template <int HD, int NT>
-static hipError_t k8_few(const Kv8AttnArgs& a, const K8Plan& p, hipStream_t s) {
+template <int HD, int NT, int WAVES>
+static void k8_few_launch(const Kv8AttnArgs& a, const K8Plan& p, hipStream_t s) {
     const dim3 grid((unsigned)((int64_t)a.B * a.c.Hkv * p.nsplit));
     if (a.cap > 0.0f)
-        hipLaunchKernelGGL((attn_kv8_few_kernel<HD, NT, true>), grid, dim3(K8_THREADS), 0, s, a, p.sp, p.nsplit);
+        hipLaunchKernelGGL((attn_kv8_few_kernel<HD, NT, WAVES, true>), grid, dim3(64 * WAVES), 0, s, a, p.sp, p.nsplit);
     else
-        hipLaunchKernelGGL((attn_kv8_few_kernel<HD, NT, false>), grid, dim3(K8_THREADS), 0, s, a, p.sp, p.nsplit);
+        hipLaunchKernelGGL((attn_kv8_few_kernel<HD, NT, WAVES, false>), grid, dim3(64 * WAVES), 0, s, a, p.sp, p.nsplit);
+}
+
+template <int HD, int NT>
+static hipError_t k8_few(const Kv8AttnArgs& a, const K8Plan& p, hipStream_t s) {
+    if (NT == 1 && p.waves == 2 * K8_WAVES)
+        k8_few_launch<HD, 1, 2 * K8_WAVES>(a, p, s);
+    else
+        k8_few_launch<HD, NT, K8_WAVES>(a, p, s);
     if (p.nsplit > 1)
-        hipLaunchKernelGGL((attn_kv8_join_kernel<HD, NT>), dim3(a.B * a.c.Hkv, (std::min(a.max_new * a.G, 16 * NT) + K8_WAVES - 1) / K8_WAVES),
+        hipLaunchKernelGGL((attn_kv8_join_kernel<HD, NT>),
+                           dim3(a.B * a.c.Hkv, (std::min(a.max_new * a.G, 16 * NT) + K8_WAVES - 1) / K8_WAVES),
                            dim3(K8_THREADS), 0, s, a, p.sp, p.nsplit);
     return hipGetLastError();
 }

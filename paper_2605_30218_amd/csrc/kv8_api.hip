@@ -2,6 +2,8 @@
 // then one launcher each.  See include/mg.h for the contract.
 #include <math.h>
 
+#include <atomic>
+
 #include "../../include/mg.h"
 #include "mg_kernels.h"
 
@@ -25,10 +27,17 @@ bool rows_ok(const mg_kv8_cache* c, const void* p, int64_t stride) {
 }
 mg_status status_of(hipError_t e) { return e == hipSuccess ? MG_OK : MG_ERR_HIP; }
 
+// compute units of the current device, looked up once a device (256 where that fails)
 int cu_count() {
+    constexpr int MAX_DEVICES = 64;
+    static std::atomic<int> known[MAX_DEVICES];
     int dev = 0, n = 0;
-    if (hipGetDevice(&dev) != hipSuccess) return 256;
-    if (hipDeviceGetAttribute(&n, hipDeviceAttributeMultiprocessorCount, dev) != hipSuccess || n <= 0) return 256;
+    if (hipGetDevice(&dev) != hipSuccess || dev < 0 || dev >= MAX_DEVICES) return 256;
+    n = known[dev].load(std::memory_order_relaxed);
+    if (n == 0) {
+        if (hipDeviceGetAttribute(&n, hipDeviceAttributeMultiprocessorCount, dev) != hipSuccess || n <= 0) return 256;
+        known[dev].store(n, std::memory_order_relaxed);
+    }
     return n;
 }
 
