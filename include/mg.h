@@ -226,7 +226,7 @@ mg_status mg_advance(mg_ctx* ctx, int B, const int32_t* emitted, int32_t* tokens
  * A value read back is exact in bf16.  A zeroed pool is an empty cache. */
 typedef struct {
     uint8_t* codes;   /* [device], 16-byte aligned */
-    uint8_t* scales;  /* [device] */
+    uint8_t* scales;  /* [device], 2-byte aligned */
     int32_t n_pages;  /* 1..2^27 - 1 */
     int32_t n_kv_heads;
     int32_t head_dim; /* 64 or 128 */

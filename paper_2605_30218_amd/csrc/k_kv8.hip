@@ -12,115 +12,204 @@ namespace mg {
 constexpr int KV8_PAGE = 16;
 constexpr int KV8_MIN_BYTE = 16;  // 2^(16 - 127) times the least code, 2^-9, is still normal in bf16
 
-__device__ __forceinline__ size_t k8_off(int t, int d) { return (size_t)((((d >> 4) * 16) + t) * 16 + (d & 15)); }
-__device__ __forceinline__ size_t v8_off(int t, int d) {
-    return (size_t)((((d >> 6) * 4 + (t >> 2)) * 16 + (d & 15)) * 16 + ((d >> 4) & 3) * 4 + (t & 3));
-}
+typedef float f32x2_q8 __attribute__((ext_vector_type(2)));
 
 __device__ __forceinline__ bool finite_bf(uint32_t h) { return (h & 0x7f80u) != 0x7f80u; }
+// magnitude bits of the larger finite value of a bf16 pair
+__device__ __forceinline__ uint32_t top_of(uint32_t pair) {
+    const uint32_t a = pair & 0x7fffu, b = (pair >> 16) & 0x7fffu;
+    return max(a < 0x7f80u ? a : 0u, b < 0x7f80u ? b : 0u);
+}
 // scale byte that a finite magnitude (bf16 bits without the sign) needs: 448 = 1.75 * 2^8
 __device__ __forceinline__ int need_byte(uint32_t mag) {
     const int b = (int)(mag >> 7) - 8 + ((mag & 0x7fu) > 0x60u);
     return max(b, KV8_MIN_BYTE);
 }
-// one bf16 value as a code of scale byte b
-__device__ __forceinline__ uint32_t quant(uint32_t h, int b) {
-    if (!finite_bf(h)) return 0x7fu;
-    const float x = bf2f(h) * __uint_as_float((uint32_t)(254 - b) << 23);
-    return (uint32_t)__builtin_amdgcn_cvt_pk_fp8_f32(x, 0.0f, 0, false) & 0xffu;
+// four bf16 values (two pairs) as codes: inv = 2^(127 - b)
+__device__ __forceinline__ uint32_t quant4(uint32_t lo, uint32_t hi, float inv) {
+    int w = __builtin_amdgcn_cvt_pk_fp8_f32(finite_bf(lo) ? bf_lo(lo) * inv : 0.0f, finite_bf(lo >> 16) ? bf_hi(lo) * inv : 0.0f, 0, false);
+    w = __builtin_amdgcn_cvt_pk_fp8_f32(finite_bf(hi) ? bf_lo(hi) * inv : 0.0f, finite_bf(hi >> 16) ? bf_hi(hi) * inv : 0.0f, w, true);
+    return (uint32_t)w | (finite_bf(lo) ? 0u : 0x7fu) | (finite_bf(lo >> 16) ? 0u : 0x7f00u) |
+           (finite_bf(hi) ? 0u : 0x7f0000u) | (finite_bf(hi >> 16) ? 0u : 0x7f000000u);
 }
-// a code of one scale as a code of a larger one (shift: 2^(old - new)); no shift: empty
-__device__ __forceinline__ uint32_t requant(uint32_t c, float shift) {
-    return (uint32_t)__builtin_amdgcn_cvt_pk_fp8_f32(__builtin_amdgcn_cvt_f32_fp8((int)c, 0) * shift, 0.0f, 0, false) &
-           0xffu;
+// four codes of one scale as codes of a larger one (shift = 2^(old - new))
+__device__ __forceinline__ uint32_t requant4(uint32_t c, float shift) {
+    const f32x2_q8 a = __builtin_amdgcn_cvt_pk_f32_fp8((int)c, false), b = __builtin_amdgcn_cvt_pk_f32_fp8((int)c, true);
+    int w = __builtin_amdgcn_cvt_pk_fp8_f32(a.x * shift, a.y * shift, 0, false);
+    return (uint32_t)__builtin_amdgcn_cvt_pk_fp8_f32(b.x * shift, b.y * shift, w, true);
 }
 
-// One wave per (token, KV head); the wave of the first token of a page's run does the run.
+// One wave per (token, KV head); the wave of the first token of a page's run does the run, so one wave alone
+// writes a page of a head.  Lane (g, m) holds K's position m, features 64 h + 16 g .., and V's positions
+// 4 g .. 4 g + 3, features 64 h + 16 c + m: 16-byte pieces of the page, whose words it writes whole.  All that
+// a run may need is requested at once: its rows, its scales and, where it begins inside a page, the page.
+// What bounds it: a call of single tokens its three memory round trips (slots, rows, stores), a prompt's call the
+// bytes.
+template <int HD>
 __global__ __launch_bounds__(256) void kv8_append_kernel(Kv8 c, int n, const uint16_t* __restrict__ k, int64_t ks,
                                                          const uint16_t* __restrict__ v, int64_t vs,
                                                          const int32_t* __restrict__ slots) {
-    const int lane = threadIdx.x & 63;
+    constexpr int H = HD / 64;
+    const int lane = threadIdx.x & 63, m = lane & 15, g = lane >> 4;
     const int64_t w = (int64_t)blockIdx.x * 4 + (threadIdx.x >> 6);
-    const int t0 = (int)(w / c.Hkv), h = (int)(w % c.Hkv);
+    const int t0 = (int)(w / c.Hkv), h0 = (int)(w % c.Hkv);
     if (t0 >= n) return;
-    const int64_t n_slots = (int64_t)c.n_pages * KV8_PAGE;
-    const int s0 = slots[t0];
-    if (s0 < 0 || s0 >= n_slots) return;
+    // lanes 0..15: the slots from the token on; lane 16: the one before it
+    const int at = lane < 16 ? t0 + lane : t0 - 1;
+    const int sl = at >= 0 && at < n && lane <= 16 ? slots[at] : -1;
+    const int s0 = __builtin_amdgcn_readfirstlane(sl);
+    if (s0 < 0 || s0 >= (int64_t)c.n_pages * KV8_PAGE) return;
     const int o = s0 % KV8_PAGE;
-    if (o > 0 && t0 > 0 && slots[t0 - 1] == s0 - 1) return;
-    int cnt = 1;
-    while (o + cnt < KV8_PAGE && t0 + cnt < n && slots[t0 + cnt] == s0 + cnt) ++cnt;
-    const int hd = c.hd, pg = s0 / KV8_PAGE;
-    for (int side = 0; side < 2; ++side) {
-        const uint16_t* x = (side ? v + (int64_t)t0 * vs : k + (int64_t)t0 * ks) + h * hd;
-        const int64_t xs = side ? vs : ks;
-        const size_t ph = ((size_t)pg * c.Hkv + h) * 2 + side;
-        uint8_t* page = c.codes + ph * (size_t)(KV8_PAGE * hd);
-        uint32_t top = 0;
-        for (int i = 0; i < cnt; ++i)
-            for (int d = lane; d < hd; d += 64) {
-                const uint32_t e = x[i * xs + d];
-                if (finite_bf(e)) top = max(top, e & 0x7fffu);
-            }
+    if (o > 0 && __builtin_amdgcn_readlane(sl, 16) == s0 - 1) return;
+    const unsigned long long run = __ballot(lane < KV8_PAGE - o && sl == s0 + lane);
+    const int end = o + __ffsll(~run) - 1;  // the run's positions in the page: [o, end)
+
+    const size_t ph = ((size_t)(s0 / KV8_PAGE) * c.Hkv + h0) * 2;
+    uint8_t* page = c.codes + ph * (size_t)(KV8_PAGE * HD);
+    uint4 kx[H][2], old[2][H];
+    uint32_t vx[H][4][2];  // [h][c]: positions 4 g, 4 g + 1 and 4 g + 2, 4 g + 3
+    const bool mine = m >= o && m < end;
+    const uint16_t* kr = k + (int64_t)(t0 + (mine ? m - o : 0)) * ks + (size_t)h0 * HD;
+    const uint16_t* vr = v + (int64_t)t0 * vs + (size_t)h0 * HD + m;
+    uint32_t ob = 0;
+    if (o) ob = *reinterpret_cast<const uint16_t*>(c.scales + ph);
 #pragma unroll
-        for (int m = 32; m >= 1; m >>= 1) top = max(top, (uint32_t)__shfl_xor((int)top, m, 64));
-        const int old = o == 0 ? 0 : c.scales[ph];
-        const int b = max(old, need_byte(top));
-        if (b != old) {
-            const float shift = __uint_as_float((uint32_t)max(127 + old - b, 0) << 23);
-            for (int t = 0; t < KV8_PAGE; ++t) {
-                if (t >= o && t < o + cnt) continue;
-                for (int d = lane; d < hd; d += 64) {
-                    uint8_t* p = page + (side ? v8_off(t, d) : k8_off(t, d));
-                    *p = old ? (uint8_t)requant(*p, shift) : 0;
-                }
-            }
-            if (lane == 0) c.scales[ph] = (uint8_t)b;
+    for (int h = 0; h < H; ++h) {
+        kx[h][0] = kx[h][1] = make_uint4(0, 0, 0, 0);
+        if (mine) {
+            kx[h][0] = *reinterpret_cast<const uint4*>(kr + 64 * h + 16 * g);
+            kx[h][1] = *reinterpret_cast<const uint4*>(kr + 64 * h + 16 * g + 8);
         }
-        for (int i = 0; i < cnt; ++i)
-            for (int d = lane; d < hd; d += 64)
-                page[side ? v8_off(o + i, d) : k8_off(o + i, d)] = (uint8_t)quant(x[i * xs + d], b);
+#pragma unroll
+        for (int q = 0; q < 4; ++q) vx[h][q][0] = vx[h][q][1] = 0;
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+            const int t = 4 * g + i;
+            if (t >= o && t < end) {
+#pragma unroll
+                for (int q = 0; q < 4; ++q)
+                    vx[h][q][i >> 1] |= (uint32_t)vr[(t - o) * vs + 64 * h + 16 * q] << (16 * (i & 1));
+            }
+        }
+        old[0][h] = old[1][h] = make_uint4(0, 0, 0, 0);
+        if (o) {
+            old[0][h] = *reinterpret_cast<const uint4*>(page + h * 1024 + lane * 16);
+            old[1][h] = *reinterpret_cast<const uint4*>(page + (H + h) * 1024 + lane * 16);
+        }
+    }
+    uint32_t tk = 0, tv = 0;
+#pragma unroll
+    for (int h = 0; h < H; ++h) {
+#pragma unroll
+        for (int e = 0; e < 2; ++e) {
+            tk = max(max(tk, max(top_of(kx[h][e].x), top_of(kx[h][e].y))), max(top_of(kx[h][e].z), top_of(kx[h][e].w)));
+#pragma unroll
+            for (int q = 0; q < 4; ++q) tv = max(tv, top_of(vx[h][q][e]));
+        }
+    }
+#pragma unroll
+    for (int x = 32; x >= 1; x >>= 1) {
+        tk = max(tk, (uint32_t)__shfl_xor((int)tk, x, 64));
+        tv = max(tv, (uint32_t)__shfl_xor((int)tv, x, 64));
+    }
+#pragma unroll
+    for (int side = 0; side < 2; ++side) {
+        const int was = (int)(side ? ob >> 8 : ob & 0xffu);  // 0: the page starts anew
+        const int b = max(was, need_byte(side ? tv : tk));
+        const float inv = __uint_as_float((uint32_t)(254 - b) << 23);
+        const float shift = __uint_as_float((uint32_t)max(127 + was - b, 0) << 23);
+        // positions of this lane's pieces that the run writes, as a byte mask of a word of V or all of K's piece
+        uint32_t keep = 0;
+#pragma unroll
+        for (int i = 0; i < 4; ++i) keep |= 4 * g + i >= o && 4 * g + i < end ? 0u : 0xffu << (8 * i);
+        if (side == 0) keep = mine ? 0u : 0xffffffffu;
+        const bool store = b != was || keep != 0xffffffffu;  // else none of the piece changes
+#pragma unroll
+        for (int h = 0; h < H; ++h) {
+            uint32_t nw[4], ow[4] = {old[side][h].x, old[side][h].y, old[side][h].z, old[side][h].w};
+#pragma unroll
+            for (int q = 0; q < 4; ++q) {
+                if (side)
+                    nw[q] = quant4(vx[h][q][0], vx[h][q][1], inv);
+                else
+                    nw[q] = quant4(q & 1 ? kx[h][q >> 1].z : kx[h][q >> 1].x, q & 1 ? kx[h][q >> 1].w : kx[h][q >> 1].y, inv);
+                const uint32_t kept = was == 0 ? 0u : b != was ? requant4(ow[q], shift) : ow[q];
+                nw[q] = (nw[q] & ~keep) | (kept & keep);
+            }
+            if (store) *reinterpret_cast<uint4*>(page + (side * H + h) * 1024 + lane * 16) = make_uint4(nw[0], nw[1], nw[2], nw[3]);
+        }
+        if (lane == 0 && b != was) c.scales[ph + side] = (uint8_t)b;
     }
 }
 
 hipError_t launch_kv8_append(const Kv8& c, int n, const uint16_t* k, int64_t ks, const uint16_t* v, int64_t vs,
                              const int32_t* slots, hipStream_t s) {
-    const int64_t waves = (int64_t)n * c.Hkv;
-    hipLaunchKernelGGL(kv8_append_kernel, dim3((unsigned)((waves + 3) / 4)), dim3(256), 0, s, c, n, k, ks, v, vs,
-                       slots);
+    const dim3 grid((unsigned)(((int64_t)n * c.Hkv + 3) / 4));
+    if (c.hd == 128)
+        hipLaunchKernelGGL(kv8_append_kernel<128>, grid, dim3(256), 0, s, c, n, k, ks, v, vs, slots);
+    else
+        hipLaunchKernelGGL(kv8_append_kernel<64>, grid, dim3(256), 0, s, c, n, k, ks, v, vs, slots);
     return hipGetLastError();
 }
 
-// One wave per (slot, KV head).
+// One wave per (four slots of the list, KV head), 16 lanes a slot.  K: lane m has the 16-byte piece of features
+// 16 m ..; V: lane m the pieces of features 16 c + m, whose words hold four positions (the four slots of a
+// wave mostly), of which it takes its own.
+template <int HD>
 __global__ __launch_bounds__(256) void kv8_read_kernel(Kv8 c, int n, const int32_t* __restrict__ slots,
                                                        uint16_t* __restrict__ k, int64_t ks, uint16_t* __restrict__ v,
                                                        int64_t vs) {
-    const int lane = threadIdx.x & 63;
+    constexpr int H = HD / 64;
+    const int lane = threadIdx.x & 63, m = lane & 15;
     const int64_t w = (int64_t)blockIdx.x * 4 + (threadIdx.x >> 6);
-    const int64_t i = w / c.Hkv;
-    const int h = (int)(w % c.Hkv);
+    const int64_t i = w / c.Hkv * 4 + (lane >> 4);
+    const int h0 = (int)(w % c.Hkv);
     if (i >= n) return;
     const int s0 = slots[i];
     if (s0 < 0 || s0 >= (int64_t)c.n_pages * KV8_PAGE) return;
-    const int t = s0 % KV8_PAGE, hd = c.hd;
-    for (int side = 0; side < 2; ++side) {
-        uint16_t* out = side ? v : k;
-        if (!out) continue;
-        out += i * (side ? vs : ks) + h * hd;
-        const size_t ph = ((size_t)(s0 / KV8_PAGE) * c.Hkv + h) * 2 + side;
-        const uint8_t* page = c.codes + ph * (size_t)(KV8_PAGE * hd);
-        const float scale = __uint_as_float((uint32_t)c.scales[ph] << 23);
-        for (int d = lane; d < hd; d += 64) {
-            const uint32_t e = page[side ? v8_off(t, d) : k8_off(t, d)];
-            out[d] = (uint16_t)f2bf(__builtin_amdgcn_cvt_f32_fp8((int)e, 0) * scale);
+    const int t = s0 % KV8_PAGE;
+    const size_t ph = ((size_t)(s0 / KV8_PAGE) * c.Hkv + h0) * 2;
+    const uint8_t* page = c.codes + ph * (size_t)(KV8_PAGE * HD);
+    const uint32_t sc = *reinterpret_cast<const uint16_t*>(c.scales + ph);
+    uint4 kp = make_uint4(0, 0, 0, 0), vp[H];
+    if (k && m < HD / 16) kp = *reinterpret_cast<const uint4*>(page + (m * 16 + t) * 16);
+#pragma unroll
+    for (int h = 0; h < H; ++h)
+        if (v) vp[h] = *reinterpret_cast<const uint4*>(page + ((H + h) * 4 + (t >> 2)) * 256 + m * 16);
+    if (k && m < HD / 16) {
+        const float f = __uint_as_float((sc & 0xffu) << 23);
+        const uint32_t q[4] = {kp.x, kp.y, kp.z, kp.w};
+        uint32_t o[8];
+#pragma unroll
+        for (int e = 0; e < 4; ++e) {
+            const f32x2_q8 a = __builtin_amdgcn_cvt_pk_f32_fp8((int)q[e], false), b = __builtin_amdgcn_cvt_pk_f32_fp8((int)q[e], true);
+            o[2 * e] = pack_bf2(a.x * f, a.y * f);
+            o[2 * e + 1] = pack_bf2(b.x * f, b.y * f);
+        }
+        uint4* out = reinterpret_cast<uint4*>(k + i * ks + (size_t)h0 * HD + 16 * m);
+        out[0] = make_uint4(o[0], o[1], o[2], o[3]);
+        out[1] = make_uint4(o[4], o[5], o[6], o[7]);
+    }
+    if (v) {
+        const float f = __uint_as_float((sc >> 8) << 23);
+        uint16_t* out = v + i * vs + (size_t)h0 * HD + m;
+#pragma unroll
+        for (int h = 0; h < H; ++h) {
+            const uint32_t q[4] = {vp[h].x, vp[h].y, vp[h].z, vp[h].w};
+#pragma unroll
+            for (int e = 0; e < 4; ++e)
+                out[64 * h + 16 * e] = (uint16_t)f2bf(__builtin_amdgcn_cvt_f32_fp8((int)(q[e] >> (8 * (t & 3))), 0) * f);
         }
     }
 }
 
 hipError_t launch_kv8_read(const Kv8& c, int n, const int32_t* slots, uint16_t* k, int64_t ks, uint16_t* v, int64_t vs,
                            hipStream_t s) {
-    const int64_t waves = (int64_t)n * c.Hkv;
-    hipLaunchKernelGGL(kv8_read_kernel, dim3((unsigned)((waves + 3) / 4)), dim3(256), 0, s, c, n, slots, k, ks, v, vs);
+    const dim3 grid((unsigned)((((int64_t)n + 3) / 4 * c.Hkv + 3) / 4));
+    if (c.hd == 128)
+        hipLaunchKernelGGL(kv8_read_kernel<128>, grid, dim3(256), 0, s, c, n, slots, k, ks, v, vs);
+    else
+        hipLaunchKernelGGL(kv8_read_kernel<64>, grid, dim3(256), 0, s, c, n, slots, k, ks, v, vs);
     return hipGetLastError();
 }
 

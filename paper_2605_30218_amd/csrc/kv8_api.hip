@@ -18,7 +18,7 @@ bool dims_ok(int n_pages, int n_kv_heads, int head_dim) {
 bool aligned(const void* p, size_t n) { return reinterpret_cast<uintptr_t>(p) % n == 0; }
 // MG_OK, or why the cache is refused
 mg_status cache_status(const mg_kv8_cache* c) {
-    if (!c || !c->codes || !c->scales || !aligned(c->codes, 16)) return MG_ERR_ARG;
+    if (!c || !c->codes || !c->scales || !aligned(c->codes, 16) || !aligned(c->scales, 2)) return MG_ERR_ARG;
     return dims_ok(c->n_pages, c->n_kv_heads, c->head_dim) ? MG_OK : MG_ERR_SHAPE;
 }
 Kv8 view(const mg_kv8_cache* c) { return Kv8{c->codes, c->scales, c->n_pages, c->n_kv_heads, c->head_dim}; }

@@ -34,6 +34,7 @@ def test_sizes():
 
 
 @pytest.mark.parametrize("kw,rc", [(dict(codes=None), ARG), (dict(scales=None), ARG), (dict(codes=P + 8), ARG),
+                                   (dict(scales=P + 1), ARG),
                                    (dict(n_pages=0), SHAPE), (dict(n_pages=1 << 27), SHAPE), (dict(hkv=0), SHAPE),
                                    (dict(hd=96), SHAPE), (dict(hd=256), SHAPE)])
 def test_caches_that_are_refused(kw, rc):
