@@ -12,6 +12,10 @@ namespace mg {
 constexpr int KV8_PAGE = 16;
 constexpr int KV8_MIN_BYTE = 16;  // 2^(16 - 127) times the least code, 2^-9, is still normal in bf16
 
+// Tokens of a wave's window where a call has more than KV8_MANY (token, KV head) pairs, else 1
+constexpr int KV8_WINDOW = 16;
+constexpr int KV8_MANY = 2048;
+
 typedef float f32x2_q8 __attribute__((ext_vector_type(2)));
 
 __device__ __forceinline__ bool finite_bf(uint32_t h) { return (h & 0x7f80u) != 0x7f80u; }
@@ -39,31 +43,16 @@ __device__ __forceinline__ uint32_t requant4(uint32_t c, float shift) {
     return (uint32_t)__builtin_amdgcn_cvt_pk_fp8_f32(b.x * shift, b.y * shift, w, true);
 }
 
-// One wave per (token, KV head); the wave of the first token of a page's run does the run, so one wave alone
-// writes a page of a head.  Lane (g, m) holds K's position m, features 64 h + 16 g .., and V's positions
-// 4 g .. 4 g + 3, features 64 h + 16 c + m: 16-byte pieces of the page, whose words it writes whole.  All that
-// a run may need is requested at once: its rows, its scales and, where it begins inside a page, the page.
-// What bounds it: a call of single tokens its three memory round trips (slots, rows, stores), a prompt's call the
-// bytes.
+// The run of tokens t0 .. on a page: positions [o, end) of the page of slot s0, KV head h0, by one wave.  Lane (g, m)
+// holds K's position m, features 64 h + 16 g .., and V's positions 4 g .. 4 g + 3, features 64 h + 16 c + m:
+// 16-byte pieces of the page, whose words it writes whole.  All that a run may need is requested at once:
+// its rows, its scales and, where it begins inside a page, the page.
 template <int HD>
-__global__ __launch_bounds__(256) void kv8_append_kernel(Kv8 c, int n, const uint16_t* __restrict__ k, int64_t ks,
-                                                         const uint16_t* __restrict__ v, int64_t vs,
-                                                         const int32_t* __restrict__ slots) {
+__device__ __forceinline__ void append_run(const Kv8& c, int t0, int s0, int o, int end, int h0, int lane,
+                                           const uint16_t* __restrict__ k, int64_t ks, const uint16_t* __restrict__ v,
+                                           int64_t vs) {
     constexpr int H = HD / 64;
-    const int lane = threadIdx.x & 63, m = lane & 15, g = lane >> 4;
-    const int64_t w = (int64_t)blockIdx.x * 4 + (threadIdx.x >> 6);
-    const int t0 = (int)(w / c.Hkv), h0 = (int)(w % c.Hkv);
-    if (t0 >= n) return;
-    // lanes 0..15: the slots from the token on; lane 16: the one before it
-    const int at = lane < 16 ? t0 + lane : t0 - 1;
-    const int sl = at >= 0 && at < n && lane <= 16 ? slots[at] : -1;
-    const int s0 = __builtin_amdgcn_readfirstlane(sl);
-    if (s0 < 0 || s0 >= (int64_t)c.n_pages * KV8_PAGE) return;
-    const int o = s0 % KV8_PAGE;
-    if (o > 0 && __builtin_amdgcn_readlane(sl, 16) == s0 - 1) return;
-    const unsigned long long run = __ballot(lane < KV8_PAGE - o && sl == s0 + lane);
-    const int end = o + __ffsll(~run) - 1;  // the run's positions in the page: [o, end)
-
+    const int m = lane & 15, g = lane >> 4;
     const size_t ph = ((size_t)(s0 / KV8_PAGE) * c.Hkv + h0) * 2;
     uint8_t* page = c.codes + ph * (size_t)(KV8_PAGE * HD);
     uint4 kx[H][2], old[2][H];
@@ -142,13 +131,131 @@ __global__ __launch_bounds__(256) void kv8_append_kernel(Kv8 c, int n, const uin
     }
 }
 
+// Up to four runs of one token each, 16 lanes a run: position sl of the lane's run (-1: none), its token t, KV head h0.
+// A lane holds hd / 16 features of K and of V.  The page itself is only touched where the scale grows, by the whole
+// wave, before the token's own bytes are written.
+template <int HD>
+__device__ __forceinline__ void append_singles(const Kv8& c, int t, int sl, int h0, int lane, const uint16_t* __restrict__ k,
+                                               int64_t ks, const uint16_t* __restrict__ v, int64_t vs) {
+    constexpr int H = HD / 64, F = HD / 16;
+    const int m = lane & 15, o = sl % KV8_PAGE;
+    const bool live = sl >= 0;
+    const size_t ph = ((size_t)(live ? sl / KV8_PAGE : 0) * c.Hkv + h0) * 2;
+    uint8_t* page = c.codes + ph * (size_t)(KV8_PAGE * HD);
+    uint32_t x[2][F / 2];
+    uint32_t ob = 0;
+#pragma unroll
+    for (int i = 0; i < F / 2; ++i) x[0][i] = x[1][i] = 0;
+    if (live) {
+        const uint32_t* kr = reinterpret_cast<const uint32_t*>(k + (int64_t)t * ks + (size_t)h0 * HD) + m * (F / 2);
+        const uint32_t* vr = reinterpret_cast<const uint32_t*>(v + (int64_t)t * vs + (size_t)h0 * HD) + m * (F / 2);
+#pragma unroll
+        for (int i = 0; i < F / 2; ++i) {
+            x[0][i] = kr[i];
+            x[1][i] = vr[i];
+        }
+        if (o) ob = *reinterpret_cast<const uint16_t*>(c.scales + ph);
+    }
+    int b[2];
+#pragma unroll
+    for (int side = 0; side < 2; ++side) {
+        uint32_t top = 0;
+#pragma unroll
+        for (int i = 0; i < F / 2; ++i) top = max(top, top_of(x[side][i]));
+#pragma unroll
+        for (int e = 8; e >= 1; e >>= 1) top = max(top, (uint32_t)__shfl_xor((int)top, e, 64));
+        const int was = (int)(side ? ob >> 8 : ob & 0xffu);
+        b[side] = max(was, need_byte(top));
+        unsigned long long grows = __ballot(live && b[side] != was && m == 0);
+        if (grows) {
+            while (grows) {
+                const int l0 = __ffsll(grows) - 1;
+                grows &= grows - 1;
+                const int w0 = __builtin_amdgcn_readlane(was, l0), s0 = __builtin_amdgcn_readlane(sl, l0);
+                const float shift = __uint_as_float((uint32_t)max(127 + w0 - __builtin_amdgcn_readlane(b[side], l0), 0) << 23);
+                uint4* p = reinterpret_cast<uint4*>(c.codes + (((size_t)(s0 / KV8_PAGE) * c.Hkv + h0) * 2 + side) * (size_t)(KV8_PAGE * HD)) + lane;
+#pragma unroll
+                for (int h = 0; h < H; ++h) {
+                    uint4 q = make_uint4(0, 0, 0, 0);
+                    if (w0) {
+                        q = p[64 * h];
+                        q = make_uint4(requant4(q.x, shift), requant4(q.y, shift), requant4(q.z, shift), requant4(q.w, shift));
+                    }
+                    p[64 * h] = q;
+                }
+            }
+            // the pages are written before the tokens' bytes, which other lanes write
+            asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
+        }
+        if (live && b[side] != was && m == 0) c.scales[ph + side] = (uint8_t)b[side];
+    }
+    if (!live) return;
+    const float ik = __uint_as_float((uint32_t)(254 - b[0]) << 23), iv = __uint_as_float((uint32_t)(254 - b[1]) << 23);
+    uint8_t* kd = page + ((m * F / 16) * 16 + o) * 16 + m * F % 16;
+#pragma unroll
+    for (int i = 0; i < F / 4; ++i) {
+        reinterpret_cast<uint32_t*>(kd)[i] = quant4(x[0][2 * i], x[0][2 * i + 1], ik);
+        const uint32_t q = quant4(x[1][2 * i], x[1][2 * i + 1], iv);
+#pragma unroll
+        for (int e = 0; e < 4; ++e) {
+            const int d = m * F + 4 * i + e;
+            page[KV8_PAGE * HD + (((d >> 6) * 4 + (o >> 2)) * 16 + (d & 15)) * 16 + ((d >> 4) & 3) * 4 + (o & 3)] = (uint8_t)(q >> (8 * e));
+        }
+    }
+}
+
+// One wave per (window of W tokens, KV head): it does the runs that begin in its window, so one wave alone
+// writes a page of a head; with windows of several tokens four runs of one token at a time, the others one
+// after the other.
+template <int HD, bool MANY>
+__global__ __launch_bounds__(256) void kv8_append_kernel(Kv8 c, int n, const uint16_t* __restrict__ k, int64_t ks,
+                                                         const uint16_t* __restrict__ v, int64_t vs,
+                                                         const int32_t* __restrict__ slots) {
+    constexpr int W = MANY ? KV8_WINDOW : 1;
+    const int lane = threadIdx.x & 63;
+    const int64_t w = (int64_t)blockIdx.x * 4 + __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+    const int64_t base = w / c.Hkv * W;
+    const int h0 = (int)(w % c.Hkv);
+    if (base >= n) return;
+    // lane l: the slot of token base - 1 + l, to the end of a run that begins with the window's last token
+    const int64_t at = base - 1 + lane;
+    const int sl = at >= 0 && at < n && lane <= W + KV8_PAGE - 1 ? slots[at] : -1;
+    const bool in = sl >= 0 && sl < (int64_t)c.n_pages * KV8_PAGE;
+    const int before = __shfl_up(sl, 1, 64), after = __shfl_down(sl, 1, 64);
+    const bool begins = lane >= 1 && lane <= W && in && (sl % KV8_PAGE == 0 || before != sl - 1);
+    const bool single = MANY && begins && (sl % KV8_PAGE == KV8_PAGE - 1 || after != sl + 1);
+    unsigned long long ones = __ballot(single), first = __ballot(begins && !single);
+    while (ones) {
+        int l0 = 0;
+        bool have = false;
+#pragma unroll
+        for (int r = 0; r < 4; ++r) {  // lane group r takes the r-th run that is left
+            if (ones && (lane >> 4) == r) {
+                l0 = __ffsll(ones) - 1;
+                have = true;
+            }
+            ones &= ones - 1;
+        }
+        const int s0 = __shfl(sl, l0, 64);
+        append_singles<HD>(c, (int)base - 1 + l0, have ? s0 : -1, h0, lane, k, ks, v, vs);
+    }
+    while (first) {
+        const int l0 = __ffsll(first) - 1;
+        first &= first - 1;
+        const int s0 = __builtin_amdgcn_readlane(sl, l0), o = s0 % KV8_PAGE, i = lane - l0;
+        const unsigned long long run = __ballot(i >= 0 && i < KV8_PAGE - o && sl == s0 + i) >> l0;
+        append_run<HD>(c, (int)base - 1 + l0, s0, o, o + __ffsll(~run) - 1, h0, lane, k, ks, v, vs);
+    }
+}
+
 hipError_t launch_kv8_append(const Kv8& c, int n, const uint16_t* k, int64_t ks, const uint16_t* v, int64_t vs,
                              const int32_t* slots, hipStream_t s) {
-    const dim3 grid((unsigned)(((int64_t)n * c.Hkv + 3) / 4));
-    if (c.hd == 128)
-        hipLaunchKernelGGL(kv8_append_kernel<128>, grid, dim3(256), 0, s, c, n, k, ks, v, vs, slots);
-    else
-        hipLaunchKernelGGL(kv8_append_kernel<64>, grid, dim3(256), 0, s, c, n, k, ks, v, vs, slots);
+    const bool many = (int64_t)n * c.Hkv > KV8_MANY;
+    const int W = many ? KV8_WINDOW : 1;
+    const dim3 grid((unsigned)((((int64_t)n + W - 1) / W * c.Hkv + 3) / 4));
+    auto f = c.hd == 128 ? (many ? kv8_append_kernel<128, true> : kv8_append_kernel<128, false>)
+                         : (many ? kv8_append_kernel<64, true> : kv8_append_kernel<64, false>);
+    hipLaunchKernelGGL(f, grid, dim3(256), 0, s, c, n, k, ks, v, vs, slots);
     return hipGetLastError();
 }
 

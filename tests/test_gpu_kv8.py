@@ -139,6 +139,24 @@ def test_append_token_by_token_and_in_runs(hkv, hd, piece):
         check_append(codes, scales, k, v, slots, want)
 
 
+@pytest.mark.parametrize("hkv,hd", [(8, 128), (9, 64)])
+def test_append_of_many_requests_at_once(hkv, hd):
+    """Calls of some hundred requests, most with one token, some with a few or with more than a page."""
+    rng = np.random.RandomState(hkv)
+    B, n_pages = 260, 260 * 6
+    codes, scales = noisy_cache(rng, n_pages, hkv, hd)
+    want = ref.RefCache.of(codes, scales)
+    pages, ctx = rng.permutation(n_pages).reshape(B, 6), rng.randint(0, 33, B)
+    for call in range(2):
+        new = np.where(rng.rand(B) < 0.8, 1, rng.randint(0, 30, B))
+        slots = np.array([pages[r, p // 16] * 16 + p % 16 for r in range(B) for p in range(ctx[r], ctx[r] + new[r])] +
+                         [-1, n_pages * 16], np.int32)
+        assert len(slots) * hkv > 2048
+        k, v = (rows_bf16(rng, (len(slots), hkv, hd), 0.2 * 4.0 ** call) for _ in range(2))
+        check_append(codes, scales, k, v, slots, want)
+        ctx = ctx + new
+
+
 def test_every_bf16_value_is_coded_as_defined():
     """All 2^16 bf16 values, 256 of one sign and exponent region a page, both sides."""
     hd, n = 128, 65536 // (16 * 128)
