@@ -10,6 +10,7 @@ namespace mg {
 typedef __bf16 bf16x2_k8 __attribute__((ext_vector_type(2)));
 typedef __bf16 bf16x8_k8 __attribute__((ext_vector_type(8)));
 typedef float f32x4_k8 __attribute__((ext_vector_type(4)));
+typedef uint32_t u32x2_k8 __attribute__((ext_vector_type(2)));
 typedef uint32_t u32x4_k8 __attribute__((ext_vector_type(4)));
 
 constexpr int K8_WAVES = 4;
@@ -28,6 +29,16 @@ __device__ __forceinline__ uint32_t k8_pack(float lo, float hi) {
     v.x = (__bf16)lo;
     v.y = (__bf16)hi;
     return __builtin_bit_cast(uint32_t, v);
+}
+// 16 bytes at a wave-uniform address and a lane's own offset; the address stays in scalar registers
+__device__ __forceinline__ uint64_t k8_uniform(const uint8_t* p) {
+    uint64_t u = reinterpret_cast<uint64_t>(p);
+    asm("" : "+s"(u));
+    return u;
+}
+__device__ __forceinline__ u32x4_k8 k8_load(uint64_t p, uint32_t off) {
+    typedef const __attribute__((address_space(1))) char* gptr;
+    return *reinterpret_cast<const __attribute__((address_space(1))) u32x4_k8*>(reinterpret_cast<gptr>(p) + off);
 }
 // high bit of every byte that is a NaN code
 __device__ __forceinline__ uint32_t k8_nan_bytes(uint32_t w) { return ((w & 0x7f7f7f7fu) + 0x01010101u) & 0x80808080u; }
@@ -98,6 +109,13 @@ __device__ __forceinline__ K8Soft k8_soft(const Kv8AttnArgs& a) {
                   a.cap * 1.4426950408889634f};
 }
 
+// a product q . k as a score: itself, or capped, in log2 units
+template <bool CAP>
+__device__ __forceinline__ float k8_score(float s, const K8Soft& so) {
+    // tanh(z) = 1 - 2 / (1 + e^2z)
+    return CAP ? so.cap2 * (1.0f - 2.0f * __builtin_amdgcn_rcpf(1.0f + __builtin_amdgcn_exp2f(s * so.zin))) : s;
+}
+
 // scores: x[u][4 e + i] of position 16 e + 4 g + i of the step and column c of tile u
 template <int HD, int NT, bool CAP>
 __device__ __forceinline__ void k8_scores(const uint4 (&kb)[2][HD / 64], const float (&ksc)[2],
@@ -121,10 +139,7 @@ __device__ __forceinline__ void k8_scores(const uint4 (&kb)[2][HD / 64], const f
 #pragma unroll
         for (int u = 0; u < NT; ++u)
 #pragma unroll
-            for (int i = 0; i < 4; ++i)
-                // tanh(z) = 1 - 2 / (1 + e^2z)
-                x[u][4 * e + i] = CAP ? so.cap2 * (1.0f - 2.0f * __builtin_amdgcn_rcpf(1.0f + __builtin_amdgcn_exp2f(acc[u][i] * so.zin)))
-                                      : acc[u][i];
+            for (int i = 0; i < 4; ++i) x[u][4 * e + i] = k8_score<CAP>(acc[u][i], so);
     }
 }
 
@@ -143,19 +158,25 @@ template <int HD, int NT, int TERMS>
 __device__ __forceinline__ void k8_softmax(float (&x)[NT][8], float f, K8Acc<HD, NT>& acc, bf16x8_k8 (&p)[NT][TERMS]) {
 #pragma unroll
     for (int u = 0; u < NT; ++u) {
-        const float mx = fmaxf(fmaxf(fmaxf(x[u][0], x[u][1]), fmaxf(x[u][2], x[u][3])),
-                               fmaxf(fmaxf(x[u][4], x[u][5]), fmaxf(x[u][6], x[u][7])));
-        if (__any(__builtin_fmaf(mx, f, -acc.m[u]) > 8.0f)) {
+        float y[8];
+#pragma unroll
+        for (int i = 0; i < 8; ++i) y[i] = __builtin_fmaf(x[u][i], f, -acc.m[u]);
+        const float my = fmaxf(fmaxf(fmaxf(y[0], y[1]), fmaxf(y[2], y[3])), fmaxf(fmaxf(y[4], y[5]), fmaxf(y[6], y[7])));
+        if (__any(my > 8.0f)) {
+            const float mx = fmaxf(fmaxf(fmaxf(x[u][0], x[u][1]), fmaxf(x[u][2], x[u][3])),
+                                   fmaxf(fmaxf(x[u][4], x[u][5]), fmaxf(x[u][6], x[u][7])));
             const float mn = fmaxf(acc.m[u], k8_col_max(mx) * f);
             const float al = __builtin_amdgcn_exp2f(acc.m[u] - mn);
             acc.m[u] = mn;
             acc.l[u] *= al;
 #pragma unroll
             for (int d = 0; d < HD / 16; ++d) acc.o[u][d] *= al;
+#pragma unroll
+            for (int i = 0; i < 8; ++i) y[i] = __builtin_fmaf(x[u][i], f, -mn);
         }
 #pragma unroll
         for (int i = 0; i < 8; ++i) {
-            x[u][i] = __builtin_amdgcn_exp2f(__builtin_fmaf(x[u][i], f, -acc.m[u]));
+            x[u][i] = __builtin_amdgcn_exp2f(y[i]);
             acc.l[u] += x[u][i];
         }
         uint32_t w[4];
@@ -443,14 +464,16 @@ __global__ __launch_bounds__(K8_THREADS) void attn_kv8_join_kernel(Kv8AttnArgs a
 
 // Rows of more query rows than 16 * few tiles: one block of 4 waves per (row, KV head, 64 NT query rows), the
 // tokens of a row's end first (they see the most), a wave holding NT tiles.  The block walks the
-// positions that its tokens see in stages of 4 pages, which go through a double buffer in LDS as codes: the
-// next stage is in flight in registers while one is used, and one barrier a stage parts them.
-constexpr int K8_STAGE = 4;  // pages a stage, one a wave to fetch
+// positions that its tokens see in stages of 4 pages, which go through a double buffer in LDS as bf16 matrix
+// operands: a wave fetches and converts K or V of two pages, so that a code is converted once a block and an
+// operand is one read for NT products.  The next stage is in flight in registers while one is used, and one barrier a
+// stage parts them.
+constexpr int K8_STAGE = 4;  // pages a stage: K or V of two by each wave
+// one 16-byte operand per lane of an LDS stage: [pair][side][k]; side 0: K, k = (page, h, half); side 1: V, k = (h, tile)
 template <int HD, int NT, bool CAP>
 __global__ __launch_bounds__(K8_THREADS) __attribute__((amdgpu_waves_per_eu(2))) void attn_kv8_chunk_kernel(Kv8AttnArgs a, int few) {
-    constexpr int H = HD / 64;
+    constexpr int H = HD / 64, DT = HD / 16;
     constexpr int ROWS = K8_WAVES * 16 * NT;
-    constexpr int PB = 2 * H * 64;  // 16-byte pieces of a page: K, then V
     const int lane = threadIdx.x & 63, c = lane & 15, g = lane >> 4;
     const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
     const int kh = blockIdx.x % a.c.Hkv;
@@ -492,7 +515,10 @@ __global__ __launch_bounds__(K8_THREADS) __attribute__((amdgpu_waves_per_eu(2)))
     const int pg1 = max(0, min(bp1 + 1, row.len) + 15) / 16;
     const int stages = max(0, (pg1 - pg0 + K8_STAGE - 1) / K8_STAGE);
 
-    __shared__ u32x4_k8 tile[2][K8_STAGE][PB];
+    // operands of two stages, 16 bytes a lane: [stage][pair of pages][K: (page, h, half); V: output tile]
+    __shared__ u32x4_k8 tile[2][2][2][4 * H][64];
+    __shared__ uint32_t nan_at[2][2][2][64];  // NaN codes of V: bits 4 d .. of a lane: output tile d's four positions of a page
+    __shared__ int nan_any[2][2];
 
     uint4 qa[NT][2 * H];
     int pc[NT];
@@ -500,81 +526,208 @@ __global__ __launch_bounds__(K8_THREADS) __attribute__((amdgpu_waves_per_eu(2)))
     const K8Soft so = k8_soft(a);
     K8Acc<HD, NT> acc;
     acc.clear();
+    uint32_t nan_out[NT];  // bit 4 d + i: output i of tile d saw a NaN of V
+#pragma unroll
+    for (int u = 0; u < NT; ++u) nan_out[u] = 0;
     const int32_t* ptab = a.page_table + (size_t)r * a.maxp;
     const size_t head_bytes = (size_t)2 * 16 * HD;
-    const uint8_t* base = a.c.codes + (size_t)kh * head_bytes;
+    const int pair = wave >> 1, side = wave & 1;  // what the wave fetches: K (side 0) or V of two of a stage's pages
+    const uint8_t* base = a.c.codes + (size_t)kh * head_bytes + side * (16 * HD);
 
-    int id = -1;        // lane i: page pg0 + 64 k + i, of the 64 that hold the stage fetched last
-    uint32_t sc = 0;    // and its scale bytes
-    u32x4_k8 nx[2 * H]; // the wave's page of the next stage
-    int nmap = 0;       // which of that stage's pages are the cache's
-    uint2 nsc;          // and the scale bytes of its pages, 16 bits each
-    auto fetch = [&](int st, u32x4_k8 (&nx)[2 * H], int& id, uint32_t& sc, int& nmap, uint2& nsc) {
+    // lane i: page pg0 + 64 k + i of the table (-1: not one of the cache's, or past the block's) and its scale
+    // bytes, of the 64 that hold the stage fetched last and of the next 64
+    auto page_id = [&](int i) { return i < pg1 ? *reinterpret_cast<const int32_t*>(reinterpret_cast<const char*>(ptab) + 4u * (uint32_t)i) : -1; };
+    auto valid = [&](int v) { return v < 0 || v >= a.c.n_pages ? -1 : v; };
+    auto scales = [&](int v) {
+        return v < 0 ? 0u : (uint32_t) * reinterpret_cast<const uint16_t*>(a.c.scales + ((size_t)v * a.c.Hkv + kh) * 2);
+    };
+    int id = valid(page_id(pg0 + lane)), idn = page_id(pg0 + K8_IDS + lane);
+    uint32_t sc = scales(id), scn = 0;
+    // codes of the stages after the current one, their scales, and which of their pages are the cache's
+    u32x4_k8 nx[2][2][H];
+    float nsc[2][2];
+    int map[2] = {0, 0};
+    auto fetch = [&](int st, u32x4_k8 (&x)[2][H], float (&xs)[2], int& m, int& id, uint32_t& sc, int& idn, uint32_t& scn) {
         const int at = st * K8_STAGE % K8_IDS;
-        if (at == 0) {
-            const int i = pg0 + st * K8_STAGE + lane;
-            id = i < pg1 ? ptab[i] : -1;
-            if (id < 0 || id >= a.c.n_pages) id = -1;
-            sc = id < 0 ? 0u : *reinterpret_cast<const uint16_t*>(a.c.scales + ((size_t)id * a.c.Hkv + kh) * 2);
+        if (at == 0 && st) {
+            id = idn;
+            sc = scn;
+            idn = page_id(pg0 + st * K8_STAGE + K8_IDS + lane);
         }
-        nmap = 0;
+        if (at == K8_IDS / 2) {  // halfway: the next ids are there, their scales are requested
+            idn = valid(idn);
+            scn = scales(idn);
+        }
+        m = 0;
 #pragma unroll
-        for (int e = 0; e < K8_STAGE; ++e) nmap |= (__builtin_amdgcn_readlane(id, at + e) >= 0) << e;
-        static_assert(K8_STAGE == 4, "four 16-bit scales in a uint2");
-        nsc.x = (uint32_t)__builtin_amdgcn_readlane((int)sc, at) | (uint32_t)__builtin_amdgcn_readlane((int)sc, at + 1) << 16;
-        nsc.y = (uint32_t)__builtin_amdgcn_readlane((int)sc, at + 2) | (uint32_t)__builtin_amdgcn_readlane((int)sc, at + 3) << 16;
-        const int pg = max(__builtin_amdgcn_readlane(id, at + wave), 0);
-        const u32x4_k8* p = reinterpret_cast<const u32x4_k8*>(base + (size_t)pg * a.c.Hkv * head_bytes) + lane;
+        for (int e = 0; e < K8_STAGE; ++e) m |= (__builtin_amdgcn_readlane(id, at + e) >= 0) << e;
 #pragma unroll
-        for (int h = 0; h < 2 * H; ++h) nx[h] = p[64 * h];
+        for (int e = 0; e < 2; ++e) {
+            xs[e] = __uint_as_float(((uint32_t)__builtin_amdgcn_readlane((int)sc, at + 2 * pair + e) >> (8 * side) & 0xffu) << 23);
+            const int pg = max(__builtin_amdgcn_readlane(id, at + 2 * pair + e), 0);
+            const uint64_t p = k8_uniform(base + (size_t)pg * a.c.Hkv * head_bytes);
+#pragma unroll
+            for (int h = 0; h < H; ++h) x[e][h] = k8_load(p, h * 1024u + lane * 16u);
+        }
     };
-    auto put = [&](int buf, const u32x4_k8 (&nx)[2 * H]) {
+    auto put = [&](int buf, const u32x4_k8 (&x)[2][H], const float (&xs)[2]) {
+        u32x4_k8(*to)[64] = tile[buf][pair][side];
+        if (side) {
+            uint32_t any = 0;
 #pragma unroll
-        for (int h = 0; h < 2 * H; ++h) tile[buf][wave][64 * h + lane] = nx[h];
+            for (int e = 0; e < 2; ++e)
+#pragma unroll
+                for (int h = 0; h < H; ++h)
+#pragma unroll
+                    for (int q = 0; q < 4; ++q) any |= k8_nan_bytes(x[e][h][q]);
+            const bool some = __any(any != 0);
+            if (lane == 0) nan_any[buf][pair] = some;
+#pragma unroll
+            for (int h = 0; h < H; ++h)
+#pragma unroll
+                for (int q = 0; q < 4; ++q) {
+                    const uint2 lo = k8_bf16x4(x[0][h][q], xs[0]), hi = k8_bf16x4(x[1][h][q], xs[1]);
+                    to[4 * h + q][lane] = u32x4_k8{lo.x, lo.y, hi.x, hi.y};
+                }
+            if (some) {  // NaN codes are noted, and their operands become 0
+                uint32_t at[2] = {0, 0};
+#pragma unroll
+                for (int h = 0; h < H; ++h)
+#pragma unroll
+                    for (int q = 0; q < 4; ++q) {
+                        u32x4_k8 w = to[4 * h + q][lane];
+#pragma unroll
+                        for (int e = 0; e < 2; ++e) {
+                            const uint32_t b = k8_nan_bytes(x[e][h][q]) >> 7;  // bits 0, 8, 16, 24
+                            at[e] |= ((b | b >> 7 | b >> 14 | b >> 21) & 15u) << (4 * (4 * h + q));
+                            w[2 * e] &= ~((b & 1u) * 0xffffu | (b >> 8 & 1u) * 0xffff0000u);
+                            w[2 * e + 1] &= ~((b >> 16 & 1u) * 0xffffu | (b >> 24) * 0xffff0000u);
+                        }
+                        to[4 * h + q][lane] = w;
+                    }
+                nan_at[buf][pair][0][lane] = at[0];
+                nan_at[buf][pair][1][lane] = at[1];
+            }
+        } else {
+#pragma unroll
+            for (int e = 0; e < 2; ++e)
+#pragma unroll
+                for (int h = 0; h < H; ++h)
+#pragma unroll
+                    for (int q = 0; q < 4; q += 2) {
+                        const uint2 lo = k8_bf16x4(x[e][h][q], xs[e]), hi = k8_bf16x4(x[e][h][q + 1], xs[e]);
+                        to[(e * H + h) * 2 + (q >> 1)][lane] = u32x4_k8{lo.x, lo.y, hi.x, hi.y};
+                    }
+        }
     };
+    int now = 0;
     if (stages) {
-        fetch(0, nx, id, sc, nmap, nsc);
-        put(0, nx);
+        fetch(0, nx[0], nsc[0], map[0], id, sc, idn, scn);
+        now = map[0];
+        fetch(1, nx[1], nsc[1], map[1], id, sc, idn, scn);
+        put(0, nx[0], nsc[0]);
     }
-    for (int st = 0; st < stages; ++st) {
-        const int map = nmap;
-        const uint2 scl = nsc;
+    for (int st2 = 0; st2 < stages; st2 += 2) {
+#pragma unroll
+      for (int ph = 0; ph < 2; ++ph) {
+        const int st = st2 + ph;  // (one past the last where their count is odd: nothing in it is seen)
         __syncthreads();
-        if (st + 1 < stages) fetch(st + 1, nx, id, sc, nmap, nsc);
-        const int jst = 16 * (pg0 + st * K8_STAGE);
+        fetch(st + 2, nx[ph], nsc[ph], map[ph], id, sc, idn, scn);  // (past the last: page 0, unused)
+        // K's operands of the first 32 positions; V's are requested before the softmax and K's of the second 32
+        // before V's product, so that an operand is waited for only where its latency has passed under other work
+        bf16x8_k8 kf[4 * H], vf[DT];
+#pragma unroll
+        for (int k = 0; k < 4 * H; ++k) kf[k] = __builtin_bit_cast(bf16x8_k8, tile[ph][0][0][k][lane]);
+        const int bad[2] = {nan_any[ph][0], nan_any[ph][1]};
+        __builtin_amdgcn_sched_barrier(0);
+#pragma unroll
         for (int hf = 0; hf < K8_STAGE / 2; ++hf) {
-            const int j0 = jst + 32 * hf;
-            // nothing for this wave's tokens in these 32 positions
-            if (j0 > wp1 || (a.window && j0 + 31 <= wp0 - a.window)) continue;
-            const int mapped = (map >> (2 * hf)) & 3;
+            const int j0 = 16 * (pg0 + st * K8_STAGE) + 32 * hf;
+            // whether there is anything for this wave's tokens in these 32 positions
+            const bool any = st < stages && j0 <= wp1 && !(a.window && j0 + 31 <= wp0 - a.window);
+            const int mapped = now >> (2 * hf) & 3;
             const bool edge = mapped != 3 || j0 + 31 > wp0 || j0 + 32 > row.len || (a.window && j0 <= wp1 - a.window);
-            const uint32_t scw = hf ? scl.y : scl.x;  // the scale bytes of the two pages: K, V, K, V
-            const float ksc[2] = {__uint_as_float((scw & 0xffu) << 23), __uint_as_float((scw >> 16 & 0xffu) << 23)};
-            const float vsc[2] = {__uint_as_float((scw >> 8 & 0xffu) << 23), __uint_as_float((scw >> 24) << 23)};
             float x[NT][8];
-            uint4 kb[2][H], vb[2][H];
+            if (hf == 1) {
 #pragma unroll
-            for (int e = 0; e < 2; ++e)
+                for (int k = 2 * H; k < 4 * H; ++k) kf[k] = __builtin_bit_cast(bf16x8_k8, tile[ph][1][0][k][lane]);
+                __builtin_amdgcn_sched_barrier(0);
+            }
 #pragma unroll
-                for (int h = 0; h < H; ++h) kb[e][h] = __builtin_bit_cast(uint4, tile[st & 1][2 * hf + e][64 * h + lane]);
-            k8_scores<HD, NT, CAP>(kb, ksc, qa, so, x);
+            for (int e = 0; e < 2; ++e) {
+                f32x4_k8 s[NT];
 #pragma unroll
-            for (int e = 0; e < 2; ++e)
+                for (int u = 0; u < NT; ++u) s[u] = f32x4_k8{0.f, 0.f, 0.f, 0.f};
 #pragma unroll
-                for (int h = 0; h < H; ++h) vb[e][h] = __builtin_bit_cast(uint4, tile[st & 1][2 * hf + e][64 * (H + h) + lane]);
-            if (edge) {
+                for (int k = 0; k < 2 * H; ++k)
+#pragma unroll
+                    for (int u = 0; u < NT; ++u)
+                        s[u] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(kf[e * 2 * H + k], __builtin_bit_cast(bf16x8_k8, qa[u][k]), s[u], 0, 0, 0);
 #pragma unroll
                 for (int u = 0; u < NT; ++u)
 #pragma unroll
-                    for (int i = 0; i < 8; ++i)
-                        x[u][i] = k8_sees(row, a.window, j0, mapped, g, i, pc[u]) ? x[u][i] : -__builtin_inff();
+                    for (int i = 0; i < 4; ++i) x[u][4 * e + i] = k8_score<CAP>(s[u][i], so);
             }
+            __builtin_amdgcn_sched_barrier(0);
+#pragma unroll
+            for (int d = 0; d < DT; ++d) vf[d] = __builtin_bit_cast(bf16x8_k8, tile[ph][hf][1][d][lane]);
+            __builtin_amdgcn_sched_barrier(0);
             bf16x8_k8 p[NT][1];
-            k8_softmax<HD, NT, 1>(x, so.f, acc, p);
-            if (edge) k8_mend_nan<HD, NT>(vb, acc, row, a.window, j0, mapped, g, pc);
-            k8_pv<HD, NT, 1>(vb, vsc, p, acc);
+            if (any) {
+                if (edge) {
+#pragma unroll
+                    for (int u = 0; u < NT; ++u)
+#pragma unroll
+                        for (int i = 0; i < 8; ++i)
+                            x[u][i] = k8_sees(row, a.window, j0, mapped, g, i, pc[u]) ? x[u][i] : -__builtin_inff();
+                }
+                k8_softmax<HD, NT, 1>(x, so.f, acc, p);
+            }
+            if (any && bad[hf]) {
+                // NaN codes of V went into the tile as 0: a product of the codes' and the columns' indicators finds the
+                // outputs that see one, which become NaN at the end
+                const uint32_t n0 = nan_at[ph][hf][0][lane], n1 = nan_at[ph][hf][1][lane];
+                u32x4_k8 sw[NT];
+#pragma unroll
+                for (int u = 0; u < NT; ++u)
+#pragma unroll
+                    for (int i = 0; i < 4; ++i)
+                        sw[u][i] = (k8_sees(row, a.window, j0, mapped, g, 2 * i, pc[u]) ? 0x3f80u : 0u) |
+                                   (k8_sees(row, a.window, j0, mapped, g, 2 * i + 1, pc[u]) ? 0x3f800000u : 0u);
+#pragma unroll
+                for (int d = 0; d < DT; ++d) {
+                    __builtin_amdgcn_sched_barrier(0);
+                    u32x4_k8 f;
+#pragma unroll
+                    for (int i = 0; i < 4; ++i) {
+                        const uint32_t b = (i < 2 ? n0 : n1) >> (4 * d + 2 * (i & 1));
+                        f[i] = (b & 1u ? 0x3f80u : 0u) | (b & 2u ? 0x3f800000u : 0u);
+                    }
+#pragma unroll
+                    for (int u = 0; u < NT; ++u) {
+                        f32x4_k8 hit = f32x4_k8{0.f, 0.f, 0.f, 0.f};
+                        hit = __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8_k8, f), __builtin_bit_cast(bf16x8_k8, sw[u]), hit, 0, 0, 0);
+#pragma unroll
+                        for (int i = 0; i < 4; ++i) nan_out[u] |= (hit[i] > 0.0f ? 1u : 0u) << (4 * d + i);
+                    }
+                }
+            }
+            __builtin_amdgcn_sched_barrier(0);
+            if (hf == 0) {  // (the second page's when V's registers are free)
+#pragma unroll
+                for (int k = 0; k < 2 * H; ++k) kf[k] = __builtin_bit_cast(bf16x8_k8, tile[ph][1][0][k][lane]);
+            }
+            __builtin_amdgcn_sched_barrier(0);
+            if (!any) continue;
+#pragma unroll
+            for (int d = 0; d < DT; ++d) {
+#pragma unroll
+                for (int u = 0; u < NT; ++u) acc.o[u][d] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(vf[d], p[u][0], acc.o[u][d], 0, 0, 0);
+            }
         }
-        if (st + 1 < stages) put((st + 1) & 1, nx);
+        put(ph ^ 1, nx[ph ^ 1], nsc[ph ^ 1]);
+        now = map[ph ^ 1];
+      }
     }
 #pragma unroll
     for (int u = 0; u < NT; ++u) {
@@ -584,7 +737,12 @@ __global__ __launch_bounds__(K8_THREADS) __attribute__((amdgpu_waves_per_eu(2)))
         if (rr >= live) continue;
         uint16_t* out = a.out + (int64_t)(row.t0 + rr / a.G) * a.out_stride + (size_t)(kh * a.G + rr % a.G) * HD + 4 * g;
 #pragma unroll
-        for (int d = 0; d < HD / 16; ++d)
+        for (int d = 0; d < DT; ++d)
+#pragma unroll
+            for (int i = 0; i < 4; ++i)
+                if (nan_out[u] >> (4 * d + i) & 1u) acc.o[u][d][i] = __builtin_nanf("");
+#pragma unroll
+        for (int d = 0; d < DT; ++d)
             *reinterpret_cast<uint2*>(out + 16 * d) =
                 make_uint2(k8_pack(acc.o[u][d][0] * inv, acc.o[u][d][1] * inv), k8_pack(acc.o[u][d][2] * inv, acc.o[u][d][3] * inv));
     }
