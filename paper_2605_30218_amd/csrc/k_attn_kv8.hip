@@ -150,19 +150,28 @@ __device__ __forceinline__ bool k8_sees(const K8Row& row, int window, int j0, in
     return ((mapped >> (i >> 2)) & 1) && j <= p && j < row.len && (!window || j > p - window);
 }
 
-// The online softmax of a step.  The reference m moves only when a score passes it by more than 2^8: a
-// probability is then at most 256, its bits are relative, and the exchanges between lanes and the
-// rescaling of the output are rare.  TERMS bf16 values stand for a probability: their sum is 2^-8 (1) or
-// 2^-16 (2) of itself off.
+// The online softmax of a step.  The reference m moves only when a row's probabilities of the step would sum to more than
+// K8_MOVE on a lane: their bits are relative, and the exchanges between lanes and the rescaling of the
+// output are rare (the sums, which are needed anyway, tell; a reference far too low makes infinities, which are
+// more).  TERMS bf16 values stand for a probability: their sum is 2^-8 (1) or 2^-16 (2) of itself off.
+constexpr float K8_MOVE = 4096.0f;
 template <int HD, int NT, int TERMS>
-__device__ __forceinline__ void k8_softmax(float (&x)[NT][8], float f, K8Acc<HD, NT>& acc, bf16x8_k8 (&p)[NT][TERMS]) {
+__device__ __forceinline__ void k8_softmax(const float (&x)[NT][8], float f, K8Acc<HD, NT>& acc, bf16x8_k8 (&p)[NT][TERMS]) {
+    float y[NT][8], t[NT];
+    bool move = false;
+    auto probs = [&](int u) {
+#pragma unroll
+        for (int i = 0; i < 8; ++i) y[u][i] = __builtin_amdgcn_exp2f(__builtin_fmaf(x[u][i], f, -acc.m[u]));
+        t[u] = ((y[u][0] + y[u][1]) + (y[u][2] + y[u][3])) + ((y[u][4] + y[u][5]) + (y[u][6] + y[u][7]));
+    };
 #pragma unroll
     for (int u = 0; u < NT; ++u) {
-        float y[8];
+        probs(u);
+        move |= t[u] > K8_MOVE;
+    }
+    if (__any(move)) {
 #pragma unroll
-        for (int i = 0; i < 8; ++i) y[i] = __builtin_fmaf(x[u][i], f, -acc.m[u]);
-        const float my = fmaxf(fmaxf(fmaxf(y[0], y[1]), fmaxf(y[2], y[3])), fmaxf(fmaxf(y[4], y[5]), fmaxf(y[6], y[7])));
-        if (__any(my > 8.0f)) {
+        for (int u = 0; u < NT; ++u) {
             const float mx = fmaxf(fmaxf(fmaxf(x[u][0], x[u][1]), fmaxf(x[u][2], x[u][3])),
                                    fmaxf(fmaxf(x[u][4], x[u][5]), fmaxf(x[u][6], x[u][7])));
             const float mn = fmaxf(acc.m[u], k8_col_max(mx) * f);
@@ -171,22 +180,20 @@ __device__ __forceinline__ void k8_softmax(float (&x)[NT][8], float f, K8Acc<HD,
             acc.l[u] *= al;
 #pragma unroll
             for (int d = 0; d < HD / 16; ++d) acc.o[u][d] *= al;
-#pragma unroll
-            for (int i = 0; i < 8; ++i) y[i] = __builtin_fmaf(x[u][i], f, -mn);
+            probs(u);
         }
+    }
 #pragma unroll
-        for (int i = 0; i < 8; ++i) {
-            x[u][i] = __builtin_amdgcn_exp2f(y[i]);
-            acc.l[u] += x[u][i];
-        }
+    for (int u = 0; u < NT; ++u) {
+        acc.l[u] += t[u];
         uint32_t w[4];
 #pragma unroll
-        for (int i = 0; i < 4; ++i) w[i] = k8_pack(x[u][2 * i], x[u][2 * i + 1]);
+        for (int i = 0; i < 4; ++i) w[i] = k8_pack(y[u][2 * i], y[u][2 * i + 1]);
         p[u][0] = __builtin_bit_cast(bf16x8_k8, make_uint4(w[0], w[1], w[2], w[3]));
         if constexpr (TERMS == 2) {
             uint32_t v[4];
 #pragma unroll
-            for (int i = 0; i < 4; ++i) v[i] = k8_pack(x[u][2 * i] - bf_lo(w[i]), x[u][2 * i + 1] - bf_hi(w[i]));
+            for (int i = 0; i < 4; ++i) v[i] = k8_pack(y[u][2 * i] - bf_lo(w[i]), y[u][2 * i + 1] - bf_hi(w[i]));
             p[u][1] = __builtin_bit_cast(bf16x8_k8, make_uint4(v[0], v[1], v[2], v[3]));
         }
     }
@@ -415,26 +422,19 @@ __global__ __launch_bounds__(64 * WAVES) __attribute__((amdgpu_waves_per_eu(NT =
     }
 }
 
-// Joins the splits of attn_kv8_few_kernel in their order: a wave per query row of a (row, KV head).
-template <int HD, int NT>
-__global__ __launch_bounds__(K8_THREADS) void attn_kv8_join_kernel(Kv8AttnArgs a, int sp, int nsplit) {
+// One query row's splits joined in their order by a wave: outputs at po + s * so, reference and sum of split s in lane s's
+// ml (act <= 64).
+template <int HD>
+__device__ __forceinline__ void k8_join(const float* po, size_t so, const float* pml, size_t sml, int act, uint16_t* out) {
     constexpr int PL = HD / 64;  // consecutive features of a lane
     constexpr int AHEAD = 8;     // splits whose outputs are requested together, the first before their weights are known
-    const int lane = threadIdx.x & 63, rr = blockIdx.y * K8_WAVES + (threadIdx.x >> 6);
-    const int kh = blockIdx.x % a.c.Hkv, r = blockIdx.x / a.c.Hkv;
-    const K8Row row = k8_row(a, r);
-    if (row.n <= 0 || row.n * a.G > 16 * NT || rr >= row.n * a.G) return;
-    const int act = k8_active(max(row.pgb - row.pga, 0), sp, nsplit);
-    if (act == 1) return;
-    const size_t first = ((size_t)r * a.c.Hkv + kh) * nsplit;
-    const float* mls = a.part + (size_t)a.B * a.c.Hkv * nsplit * (16 * NT) * HD;
-    const float* po = a.part + (first * (16 * NT) + rr) * HD + PL * lane;
+    const int lane = threadIdx.x & 63;
     using vec = float __attribute__((ext_vector_type(PL)));
     vec v[AHEAD];
-    // nsplit <= 64: lane s has split s
-    const float2 ml = *reinterpret_cast<const float2*>(mls + 2 * ((first + min(lane, act - 1)) * (16 * NT) + rr));
+    const float2 ml = *reinterpret_cast<const float2*>(pml + (size_t)min(lane, act - 1) * sml);
+    po += PL * lane;
 #pragma unroll
-    for (int k = 0; k < AHEAD; ++k) v[k] = *reinterpret_cast<const vec*>(po + (size_t)min(k, act - 1) * (16 * NT) * HD);
+    for (int k = 0; k < AHEAD; ++k) v[k] = *reinterpret_cast<const vec*>(po + (size_t)min(k, act - 1) * so);
     const float M = wave_max(ml.x);
     const float f = lane < act ? __builtin_amdgcn_exp2f(ml.x - M) : 0.0f;
     const float L = wave_sum_fast(lane < act ? f * ml.y : 0.0f);
@@ -445,7 +445,7 @@ __global__ __launch_bounds__(K8_THREADS) void attn_kv8_join_kernel(Kv8AttnArgs a
     for (int s = 0; s < act; s += AHEAD) {
         if (s) {
 #pragma unroll
-            for (int k = 0; k < AHEAD; ++k) v[k] = *reinterpret_cast<const vec*>(po + (size_t)min(s + k, act - 1) * (16 * NT) * HD);
+            for (int k = 0; k < AHEAD; ++k) v[k] = *reinterpret_cast<const vec*>(po + (size_t)min(s + k, act - 1) * so);
         }
 #pragma unroll
         for (int k = 0; k < AHEAD; ++k) {
@@ -455,31 +455,40 @@ __global__ __launch_bounds__(K8_THREADS) void attn_kv8_join_kernel(Kv8AttnArgs a
             for (int e = 0; e < PL; ++e) O[e] += w * v[k][e];
         }
     }
-    uint16_t* out = a.out + (int64_t)(row.t0 + rr / a.G) * a.out_stride + (size_t)(kh * a.G + rr % a.G) * HD + PL * lane;
+    out += PL * lane;
     if constexpr (PL == 2)
         *reinterpret_cast<uint32_t*>(out) = k8_pack(O[0] * inv, O[1] * inv);
     else
         out[0] = (uint16_t)f2bf(O[0] * inv);
 }
+__device__ __forceinline__ uint16_t* k8_out(const Kv8AttnArgs& a, const K8Row& row, int kh, int rr) {
+    return a.out + (int64_t)(row.t0 + rr / a.G) * a.out_stride + (size_t)(kh * a.G + rr % a.G) * a.c.hd;
+}
 
-// Rows of more query rows than 16 * few tiles: one block of 4 waves per (row, KV head, 64 NT query rows), the
-// tokens of a row's end first (they see the most), a wave holding NT tiles.  The block walks the
-// positions that its tokens see in stages of 4 pages, which go through a double buffer in LDS as bf16 matrix
-// operands: a wave fetches and converts K or V of two pages, so that a code is converted once a block and an
-// operand is one read for NT products.  The next stage is in flight in registers while one is used, and one barrier a
-// stage parts them.
-constexpr int K8_STAGE = 4;  // pages a stage: K or V of two by each wave
-// one 16-byte operand per lane of an LDS stage: [pair][side][k]; side 0: K, k = (page, h, half); side 1: V, k = (h, tile)
-template <int HD, int NT, bool CAP>
-__global__ __launch_bounds__(K8_THREADS) __attribute__((amdgpu_waves_per_eu(2))) void attn_kv8_chunk_kernel(Kv8AttnArgs a, int few) {
-    constexpr int H = HD / 64, DT = HD / 16;
-    constexpr int ROWS = K8_WAVES * 16 * NT;
-    const int lane = threadIdx.x & 63, c = lane & 15, g = lane >> 4;
-    const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
-    const int kh = blockIdx.x % a.c.Hkv;
-    // the row that holds this block's tile: rows' tile counts summed by the wave, 64 rows at a time
-    int t = blockIdx.x / a.c.Hkv, r = -1;
-    for (int b0 = 0; b0 < a.B && r < 0; b0 += 64) {
+// Joins the splits of attn_kv8_few_kernel: a wave per query row of a (row, KV head).
+template <int HD, int NT>
+__global__ __launch_bounds__(K8_THREADS) void attn_kv8_join_kernel(Kv8AttnArgs a, int sp, int nsplit) {
+    const int rr = blockIdx.y * K8_WAVES + (threadIdx.x >> 6);
+    const int kh = blockIdx.x % a.c.Hkv, r = blockIdx.x / a.c.Hkv;
+    const K8Row row = k8_row(a, r);
+    if (row.n <= 0 || row.n * a.G > 16 * NT || rr >= row.n * a.G) return;
+    const int act = k8_active(max(row.pgb - row.pga, 0), sp, nsplit);
+    if (act == 1) return;
+    const size_t first = ((size_t)r * a.c.Hkv + kh) * nsplit * (16 * NT) + rr;
+    const float* ml = a.part + (size_t)a.B * a.c.Hkv * nsplit * (16 * NT) * HD;
+    k8_join<HD>(a.part + first * HD, (size_t)(16 * NT) * HD, ml + 2 * first, 2 * 16 * NT, act, k8_out(a, row, kh, rr));
+}
+
+// Tile `index` of the rows of more than `few` query rows, their tiles of ROWS query rows counted row by row: the row, and the
+// tile in it from its end (the last tokens see the most); r < 0 behind the last.  Tile counts are summed by
+// the wave, 64 rows at a time.
+struct K8Tile {
+    int r, t;
+};
+template <int ROWS>
+__device__ __forceinline__ K8Tile k8_tile(const Kv8AttnArgs& a, int few, int index) {
+    const int lane = threadIdx.x & 63;
+    for (int b0 = 0; b0 < a.B; b0 += 64) {
         int k = 0;
         if (b0 + lane < a.B) {
             const int rows = (a.cu_new[b0 + lane + 1] - a.cu_new[b0 + lane]) * a.G;
@@ -491,34 +500,64 @@ __global__ __launch_bounds__(K8_THREADS) __attribute__((amdgpu_waves_per_eu(2)))
             const int v = __shfl_up(sum, o, 64);
             if (lane >= o) sum += v;
         }
-        const unsigned long long past = __ballot(sum > t);
+        const unsigned long long past = __ballot(sum > index);
         if (past) {
-            const int at = __ffsll(past) - 1;
-            r = b0 + at;
-            // from the row's end
-            t = __builtin_amdgcn_readlane(sum, at) - 1 - t;
-        } else {
-            t -= __builtin_amdgcn_readlane(sum, 63);
+            const int at = __builtin_amdgcn_readfirstlane(__ffsll(past) - 1);
+            return K8Tile{b0 + at, __builtin_amdgcn_readlane(sum, at) - 1 - index};
         }
+        index -= __builtin_amdgcn_readlane(sum, 63);
     }
-    if (r < 0) return;
-    r = __builtin_amdgcn_readfirstlane(r);
-    t = __builtin_amdgcn_readfirstlane(t);
+    return K8Tile{-1, 0};
+}
+constexpr int K8_STAGE = 4;       // pages a stage of the chunk kernel, one a wave to fetch
+constexpr int K8_MIN_STAGES = 4;  // stages a split of a tile takes at least
+// The pages that tile t's tokens see, the stages of four pages they make and the splits that share these.
+struct K8Span {
+    int pg0, pg1, stages, act;
+};
+template <int ROWS>
+__device__ __forceinline__ K8Span k8_span(const Kv8AttnArgs& a, const K8Row& row, int t, int nsplit) {
+    const int p0 = row.p0 + t * ROWS / a.G, p1 = row.p0 + (min((t + 1) * ROWS, row.n * a.G) - 1) / a.G;
+    K8Span x;
+    x.pg0 = a.window ? max(0, min(p0 - a.window + 1, row.len)) / 16 : 0;
+    x.pg1 = max(0, min(p1 + 1, row.len) + 15) / 16;
+    x.stages = max(0, (x.pg1 - x.pg0 + K8_STAGE - 1) / K8_STAGE);
+    x.act = max(1, min(nsplit, x.stages / K8_MIN_STAGES));
+    return x;
+}
+
+// Rows of more query rows than 16 * few tiles: one block of 4 waves per (row, KV head, 64 NT query rows), the
+// tokens of a row's end first (they see the most), a wave holding NT tiles.  The block walks the
+// positions that its tokens see in stages of 4 pages, which go through a double buffer in LDS as bf16 matrix
+// operands: a wave fetches and converts K or V of two pages, so that a code is converted once a block and an
+// operand is one read for NT products.  The next stage is in flight in registers while one is used, and one barrier a
+// stage parts them.
+template <int HD, int NT, bool CAP>
+__global__ __launch_bounds__(K8_THREADS) __attribute__((amdgpu_waves_per_eu(2))) void attn_kv8_chunk_kernel(Kv8AttnArgs a, int few, int nsplit, float* part) {
+    constexpr int H = HD / 64, DT = HD / 16;
+    constexpr int ROWS = K8_WAVES * 16 * NT;
+    const int lane = threadIdx.x & 63, c = lane & 15, g = lane >> 4;
+    const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+    const int kh = blockIdx.x % a.c.Hkv;
+    const int split = blockIdx.x / a.c.Hkv % nsplit, index = blockIdx.x / a.c.Hkv / nsplit;
+    const K8Tile at = k8_tile<ROWS>(a, few, index);
+    if (at.r < 0) return;
+    const int r = __builtin_amdgcn_readfirstlane(at.r), t = __builtin_amdgcn_readfirstlane(at.t);
     const K8Row row = k8_row(a, r);
     const int live = row.n * a.G;
     if (t * ROWS >= live) return;
-    // the positions that the block's, and the wave's, tokens see
+    K8Span span = k8_span<ROWS>(a, row, t, nsplit);
+    if (split >= span.act) return;
+    const int st0 = span.stages * split / span.act, stages = span.stages * (split + 1) / span.act - st0;
+    const int pg0 = span.pg0 + st0 * K8_STAGE, pg1 = min(span.pg1, pg0 + stages * K8_STAGE);
+    // the positions of the wave's tokens
     const int rr0 = t * ROWS + wave * (16 * NT);
-    const int bp0 = row.p0 + t * ROWS / a.G, bp1 = row.p0 + (min((t + 1) * ROWS, live) - 1) / a.G;
     const int wp0 = row.p0 + min(rr0, live - 1) / a.G, wp1 = row.p0 + (min(rr0 + 16 * NT, live) - 1) / a.G;
-    const int pg0 = a.window ? max(0, min(bp0 - a.window + 1, row.len)) / 16 : 0;
-    const int pg1 = max(0, min(bp1 + 1, row.len) + 15) / 16;
-    const int stages = max(0, (pg1 - pg0 + K8_STAGE - 1) / K8_STAGE);
 
     // operands of two stages, 16 bytes a lane: [stage][pair of pages][K: (page, h, half); V: output tile]
-    __shared__ u32x4_k8 tile[2][2][2][4 * H][64];
-    __shared__ uint32_t nan_at[2][2][2][64];  // NaN codes of V: bits 4 d .. of a lane: output tile d's four positions of a page
-    __shared__ int nan_any[2][2];
+    __shared__ __attribute__((aligned(16))) uint32_t tile[2][2][2][4 * H][64][4];
+    __shared__ uint32_t nan_at[2][K8_STAGE][64];  // NaN codes of V: bits 4 d .. of a lane: output tile d's four positions of a page
+    __shared__ int nan_any[2][K8_STAGE];
 
     uint4 qa[NT][2 * H];
     int pc[NT];
@@ -531,128 +570,116 @@ __global__ __launch_bounds__(K8_THREADS) __attribute__((amdgpu_waves_per_eu(2)))
     for (int u = 0; u < NT; ++u) nan_out[u] = 0;
     const int32_t* ptab = a.page_table + (size_t)r * a.maxp;
     const size_t head_bytes = (size_t)2 * 16 * HD;
-    const int pair = wave >> 1, side = wave & 1;  // what the wave fetches: K (side 0) or V of two of a stage's pages
-    const uint8_t* base = a.c.codes + (size_t)kh * head_bytes + side * (16 * HD);
+    const uint8_t* base = a.c.codes + (size_t)kh * head_bytes;
 
-    // lane i: page pg0 + 64 k + i of the table (-1: not one of the cache's, or past the block's) and its scale
-    // bytes, of the 64 that hold the stage fetched last and of the next 64
-    auto page_id = [&](int i) { return i < pg1 ? *reinterpret_cast<const int32_t*>(reinterpret_cast<const char*>(ptab) + 4u * (uint32_t)i) : -1; };
-    auto valid = [&](int v) { return v < 0 || v >= a.c.n_pages ? -1 : v; };
-    auto scales = [&](int v) {
+    // lane i: page pg0 + 64 k + i of the table, of the 64 that hold the stage fetched last: its place, its scales and
+    // (mapped) whether it is one of the cache's and the block's; and the id and scale bytes of the next 64's
+    auto page_id = [&](int i) {
+        const int v = i < pg1 ? *reinterpret_cast<const int32_t*>(reinterpret_cast<const char*>(ptab) + 4u * (uint32_t)i) : -1;
+        return v;
+    };
+    auto scale_bytes = [&](int v) {
         return v < 0 ? 0u : (uint32_t) * reinterpret_cast<const uint16_t*>(a.c.scales + ((size_t)v * a.c.Hkv + kh) * 2);
     };
-    int id = valid(page_id(pg0 + lane)), idn = page_id(pg0 + K8_IDS + lane);
-    uint32_t sc = scales(id), scn = 0;
-    // codes of the stages after the current one, their scales, and which of their pages are the cache's
-    u32x4_k8 nx[2][2][H];
-    float nsc[2][2];
-    int map[2] = {0, 0};
-    auto fetch = [&](int st, u32x4_k8 (&x)[2][H], float (&xs)[2], int& m, int& id, uint32_t& sc, int& idn, uint32_t& scn) {
+    int idn = page_id(pg0 + lane);
+    idn = idn < 0 || idn >= a.c.n_pages ? -1 : idn;
+    uint32_t scn = scale_bytes(idn);
+    uint64_t place = 0, mapped64 = 0;
+    uint32_t kscale = 0, vscale = 0;
+    // the wave's page of the next stage: K, V, their scales, and which of the stage's pages are mapped
+    u32x4_k8 nx[2][H];
+    float nsc[2];
+    int map = 0;
+    auto fetch = [&](int st, u32x4_k8 (&x)[2][H], float (&xs)[2], int& m, int& idn, uint32_t& scn, uint64_t& place,
+                     uint64_t& mapped64, uint32_t& kscale, uint32_t& vscale) {
         const int at = st * K8_STAGE % K8_IDS;
-        if (at == 0 && st) {
-            id = idn;
-            sc = scn;
+        if (at == 0) {
+            place = (uint64_t)max(idn, 0) * a.c.Hkv * head_bytes;
+            mapped64 = __ballot(idn >= 0);
+            kscale = (scn & 0xffu) << 23;
+            vscale = scn >> 8 << 23;
             idn = page_id(pg0 + st * K8_STAGE + K8_IDS + lane);
         }
         if (at == K8_IDS / 2) {  // halfway: the next ids are there, their scales are requested
-            idn = valid(idn);
-            scn = scales(idn);
+            idn = idn < 0 || idn >= a.c.n_pages ? -1 : idn;
+            scn = scale_bytes(idn);
         }
-        m = 0;
+        m = (int)(mapped64 >> at) & 15;
+        const int mine = at + wave;
+        xs[0] = __uint_as_float((uint32_t)__builtin_amdgcn_readlane((int)kscale, mine));
+        xs[1] = __uint_as_float((uint32_t)__builtin_amdgcn_readlane((int)vscale, mine));
+        const uint64_t off = (uint32_t)__builtin_amdgcn_readlane((int)(uint32_t)place, mine) |
+                             (uint64_t)(uint32_t)__builtin_amdgcn_readlane((int)(place >> 32), mine) << 32;
+        const uint64_t p = k8_uniform(base + off);
 #pragma unroll
-        for (int e = 0; e < K8_STAGE; ++e) m |= (__builtin_amdgcn_readlane(id, at + e) >= 0) << e;
-#pragma unroll
-        for (int e = 0; e < 2; ++e) {
-            xs[e] = __uint_as_float(((uint32_t)__builtin_amdgcn_readlane((int)sc, at + 2 * pair + e) >> (8 * side) & 0xffu) << 23);
-            const int pg = max(__builtin_amdgcn_readlane(id, at + 2 * pair + e), 0);
-            const uint64_t p = k8_uniform(base + (size_t)pg * a.c.Hkv * head_bytes);
-#pragma unroll
-            for (int h = 0; h < H; ++h) x[e][h] = k8_load(p, h * 1024u + lane * 16u);
-        }
+        for (int h = 0; h < 2 * H; ++h) x[h / H][h % H] = k8_load(p, h * 1024u + lane * 16u);
     };
     auto put = [&](int buf, const u32x4_k8 (&x)[2][H], const float (&xs)[2]) {
-        u32x4_k8(*to)[64] = tile[buf][pair][side];
-        if (side) {
-            uint32_t any = 0;
+        const int pair = wave >> 1, e = wave & 1;
+        uint32_t any = 0;
 #pragma unroll
-            for (int e = 0; e < 2; ++e)
+        for (int h = 0; h < H; ++h)
 #pragma unroll
-                for (int h = 0; h < H; ++h)
+            for (int q = 0; q < 4; ++q) any |= (x[1][h][q] & 0x7f7f7f7fu) + 0x01010101u;
+        const bool some = __any((any & 0x80808080u) != 0);
+        if (lane == 0) nan_any[buf][wave] = some;
+        uint32_t at = 0;
 #pragma unroll
-                    for (int q = 0; q < 4; ++q) any |= k8_nan_bytes(x[e][h][q]);
-            const bool some = __any(any != 0);
-            if (lane == 0) nan_any[buf][pair] = some;
+        for (int h = 0; h < H; ++h)
+#pragma unroll
+            for (int q = 0; q < 4; q += 2) {
+                const uint2 lo = k8_bf16x4(x[0][h][q], xs[0]), hi = k8_bf16x4(x[0][h][q + 1], xs[0]);
+                *reinterpret_cast<u32x4_k8*>(tile[buf][pair][0][(e * H + h) * 2 + (q >> 1)][lane]) = u32x4_k8{lo.x, lo.y, hi.x, hi.y};
+            }
+#pragma unroll
+        for (int h = 0; h < H; ++h)
+#pragma unroll
+            for (int q = 0; q < 4; ++q) {
+                const uint2 w = k8_bf16x4(x[1][h][q], xs[1]);
+                *reinterpret_cast<u32x2_k8*>(&tile[buf][pair][1][4 * h + q][lane][2 * e]) = u32x2_k8{w.x, w.y};
+            }
+        if (some) {  // NaN codes are noted, and their operands become 0
 #pragma unroll
             for (int h = 0; h < H; ++h)
 #pragma unroll
                 for (int q = 0; q < 4; ++q) {
-                    const uint2 lo = k8_bf16x4(x[0][h][q], xs[0]), hi = k8_bf16x4(x[1][h][q], xs[1]);
-                    to[4 * h + q][lane] = u32x4_k8{lo.x, lo.y, hi.x, hi.y};
+                    const uint32_t b = k8_nan_bytes(x[1][h][q]) >> 7;  // bits 0, 8, 16, 24
+                    at |= ((b | b >> 7 | b >> 14 | b >> 21) & 15u) << (4 * (4 * h + q));
+                    uint32_t* w = &tile[buf][pair][1][4 * h + q][lane][2 * e];
+                    w[0] &= ~((b & 1u) * 0xffffu | (b >> 8 & 1u) * 0xffff0000u);
+                    w[1] &= ~((b >> 16 & 1u) * 0xffffu | (b >> 24) * 0xffff0000u);
                 }
-            if (some) {  // NaN codes are noted, and their operands become 0
-                uint32_t at[2] = {0, 0};
-#pragma unroll
-                for (int h = 0; h < H; ++h)
-#pragma unroll
-                    for (int q = 0; q < 4; ++q) {
-                        u32x4_k8 w = to[4 * h + q][lane];
-#pragma unroll
-                        for (int e = 0; e < 2; ++e) {
-                            const uint32_t b = k8_nan_bytes(x[e][h][q]) >> 7;  // bits 0, 8, 16, 24
-                            at[e] |= ((b | b >> 7 | b >> 14 | b >> 21) & 15u) << (4 * (4 * h + q));
-                            w[2 * e] &= ~((b & 1u) * 0xffffu | (b >> 8 & 1u) * 0xffff0000u);
-                            w[2 * e + 1] &= ~((b >> 16 & 1u) * 0xffffu | (b >> 24) * 0xffff0000u);
-                        }
-                        to[4 * h + q][lane] = w;
-                    }
-                nan_at[buf][pair][0][lane] = at[0];
-                nan_at[buf][pair][1][lane] = at[1];
-            }
-        } else {
-#pragma unroll
-            for (int e = 0; e < 2; ++e)
-#pragma unroll
-                for (int h = 0; h < H; ++h)
-#pragma unroll
-                    for (int q = 0; q < 4; q += 2) {
-                        const uint2 lo = k8_bf16x4(x[e][h][q], xs[e]), hi = k8_bf16x4(x[e][h][q + 1], xs[e]);
-                        to[(e * H + h) * 2 + (q >> 1)][lane] = u32x4_k8{lo.x, lo.y, hi.x, hi.y};
-                    }
+            nan_at[buf][wave][lane] = at;
         }
     };
     int now = 0;
     if (stages) {
-        fetch(0, nx[0], nsc[0], map[0], id, sc, idn, scn);
-        now = map[0];
-        fetch(1, nx[1], nsc[1], map[1], id, sc, idn, scn);
-        put(0, nx[0], nsc[0]);
+        fetch(0, nx, nsc, map, idn, scn, place, mapped64, kscale, vscale);
+        put(0, nx, nsc);
     }
-    for (int st2 = 0; st2 < stages; st2 += 2) {
-#pragma unroll
-      for (int ph = 0; ph < 2; ++ph) {
-        const int st = st2 + ph;  // (one past the last where their count is odd: nothing in it is seen)
+    for (int st = 0; st < stages; ++st) {
+        const int buf = st & 1;
+        now = map;
         __syncthreads();
-        fetch(st + 2, nx[ph], nsc[ph], map[ph], id, sc, idn, scn);  // (past the last: page 0, unused)
         // K's operands of the first 32 positions; V's are requested before the softmax and K's of the second 32
         // before V's product, so that an operand is waited for only where its latency has passed under other work
         bf16x8_k8 kf[4 * H], vf[DT];
+        auto read_k = [&](int hf, bf16x8_k8 (&kf)[4 * H]) {
 #pragma unroll
-        for (int k = 0; k < 4 * H; ++k) kf[k] = __builtin_bit_cast(bf16x8_k8, tile[ph][0][0][k][lane]);
-        const int bad[2] = {nan_any[ph][0], nan_any[ph][1]};
+            for (int k = 0; k < 4 * H; ++k) kf[k] = *reinterpret_cast<const bf16x8_k8*>(tile[buf][hf][0][k][lane]);
+        };
+        read_k(0, kf);
+        const int bad[2] = {nan_any[buf][0] | nan_any[buf][1], nan_any[buf][2] | nan_any[buf][3]};
         __builtin_amdgcn_sched_barrier(0);
+        if (st + 1 < stages) fetch(st + 1, nx, nsc, map, idn, scn, place, mapped64, kscale, vscale);
 #pragma unroll
         for (int hf = 0; hf < K8_STAGE / 2; ++hf) {
             const int j0 = 16 * (pg0 + st * K8_STAGE) + 32 * hf;
             // whether there is anything for this wave's tokens in these 32 positions
-            const bool any = st < stages && j0 <= wp1 && !(a.window && j0 + 31 <= wp0 - a.window);
+            const bool any = j0 <= wp1 && !(a.window && j0 + 31 <= wp0 - a.window);
             const int mapped = now >> (2 * hf) & 3;
             const bool edge = mapped != 3 || j0 + 31 > wp0 || j0 + 32 > row.len || (a.window && j0 <= wp1 - a.window);
             float x[NT][8];
-            if (hf == 1) {
-#pragma unroll
-                for (int k = 2 * H; k < 4 * H; ++k) kf[k] = __builtin_bit_cast(bf16x8_k8, tile[ph][1][0][k][lane]);
-                __builtin_amdgcn_sched_barrier(0);
-            }
 #pragma unroll
             for (int e = 0; e < 2; ++e) {
                 f32x4_k8 s[NT];
@@ -670,7 +697,7 @@ __global__ __launch_bounds__(K8_THREADS) __attribute__((amdgpu_waves_per_eu(2)))
             }
             __builtin_amdgcn_sched_barrier(0);
 #pragma unroll
-            for (int d = 0; d < DT; ++d) vf[d] = __builtin_bit_cast(bf16x8_k8, tile[ph][hf][1][d][lane]);
+            for (int d = 0; d < DT; ++d) vf[d] = *reinterpret_cast<const bf16x8_k8*>(tile[buf][hf][1][d][lane]);
             __builtin_amdgcn_sched_barrier(0);
             bf16x8_k8 p[NT][1];
             if (any) {
@@ -686,7 +713,8 @@ __global__ __launch_bounds__(K8_THREADS) __attribute__((amdgpu_waves_per_eu(2)))
             if (any && bad[hf]) {
                 // NaN codes of V went into the tile as 0: a product of the codes' and the columns' indicators finds the
                 // outputs that see one, which become NaN at the end
-                const uint32_t n0 = nan_at[ph][hf][0][lane], n1 = nan_at[ph][hf][1][lane];
+                const uint32_t n0 = nan_any[buf][2 * hf] ? nan_at[buf][2 * hf][lane] : 0u;
+                const uint32_t n1 = nan_any[buf][2 * hf + 1] ? nan_at[buf][2 * hf + 1][lane] : 0u;
                 u32x4_k8 sw[NT];
 #pragma unroll
                 for (int u = 0; u < NT; ++u)
@@ -708,26 +736,24 @@ __global__ __launch_bounds__(K8_THREADS) __attribute__((amdgpu_waves_per_eu(2)))
                         f32x4_k8 hit = f32x4_k8{0.f, 0.f, 0.f, 0.f};
                         hit = __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8_k8, f), __builtin_bit_cast(bf16x8_k8, sw[u]), hit, 0, 0, 0);
 #pragma unroll
-                        for (int i = 0; i < 4; ++i) nan_out[u] |= (hit[i] > 0.0f ? 1u : 0u) << (4 * d + i);
+                        for (int i = 0; i < 4; ++i) {
+                            uint32_t one = hit[i] > 0.0f ? 1u : 0u;
+                            asm("" : "+v"(one));  // (shifted, not chosen from 32 constants that would take registers)
+                            nan_out[u] |= one << (4 * d + i);
+                        }
                     }
                 }
             }
             __builtin_amdgcn_sched_barrier(0);
-            if (hf == 0) {  // (the second page's when V's registers are free)
-#pragma unroll
-                for (int k = 0; k < 2 * H; ++k) kf[k] = __builtin_bit_cast(bf16x8_k8, tile[ph][1][0][k][lane]);
-            }
+            if (hf == 0) read_k(1, kf);
             __builtin_amdgcn_sched_barrier(0);
             if (!any) continue;
 #pragma unroll
-            for (int d = 0; d < DT; ++d) {
+            for (int d = 0; d < DT; ++d)
 #pragma unroll
                 for (int u = 0; u < NT; ++u) acc.o[u][d] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(vf[d], p[u][0], acc.o[u][d], 0, 0, 0);
-            }
         }
-        put(ph ^ 1, nx[ph ^ 1], nsc[ph ^ 1]);
-        now = map[ph ^ 1];
-      }
+        if (st + 1 < stages) put(buf ^ 1, nx, nsc);
     }
 #pragma unroll
     for (int u = 0; u < NT; ++u) {
@@ -741,11 +767,39 @@ __global__ __launch_bounds__(K8_THREADS) __attribute__((amdgpu_waves_per_eu(2)))
 #pragma unroll
             for (int i = 0; i < 4; ++i)
                 if (nan_out[u] >> (4 * d + i) & 1u) acc.o[u][d][i] = __builtin_nanf("");
+        if (span.act > 1) {
+            const size_t pr = ((size_t)(index * a.c.Hkv + kh) * nsplit + split) * ROWS + wave * (16 * NT) + 16 * u + c;
+#pragma unroll
+            for (int d = 0; d < DT; ++d) *reinterpret_cast<f32x4_k8*>(part + pr * HD + 16 * d + 4 * g) = acc.o[u][d];
+            if (g == 0) {
+                float* ml = part + (size_t)(gridDim.x / nsplit) * nsplit * ROWS * HD + 2 * pr;
+                ml[0] = acc.m[u];
+                ml[1] = L;
+            }
+            continue;
+        }
 #pragma unroll
         for (int d = 0; d < DT; ++d)
             *reinterpret_cast<uint2*>(out + 16 * d) =
                 make_uint2(k8_pack(acc.o[u][d][0] * inv, acc.o[u][d][1] * inv), k8_pack(acc.o[u][d][2] * inv, acc.o[u][d][3] * inv));
     }
+}
+
+// Joins the splits of attn_kv8_chunk_kernel: a wave per query row of a (tile, KV head).
+template <int HD, int NT>
+__global__ __launch_bounds__(K8_THREADS) void attn_kv8_chunk_join_kernel(Kv8AttnArgs a, int few, int nsplit, const float* part) {
+    constexpr int ROWS = K8_WAVES * 16 * NT;
+    const int kh = blockIdx.x % a.c.Hkv, index = blockIdx.x / a.c.Hkv;
+    const K8Tile at = k8_tile<ROWS>(a, few, index);
+    if (at.r < 0) return;
+    const K8Row row = k8_row(a, at.r);
+    const int i = blockIdx.y * K8_WAVES + (threadIdx.x >> 6), rr = at.t * ROWS + i;
+    if (rr >= row.n * a.G) return;
+    const int act = k8_span<ROWS>(a, row, at.t, nsplit).act;
+    if (act == 1) return;
+    const size_t first = (size_t)blockIdx.x * nsplit * ROWS + i;
+    const float* ml = part + (size_t)gridDim.x * nsplit * ROWS * HD;
+    k8_join<HD>(part + first * HD, (size_t)ROWS * HD, ml + 2 * first, 2 * ROWS, act, k8_out(a, row, kh, rr));
 }
 
 // The launch of rows of few query rows: tiles and waves of a block, pages of a split, splits of a row.
@@ -765,12 +819,17 @@ constexpr int K8_MAX_PAGES = 128;
 constexpr int K8_MAX_SPLITS = 64;
 constexpr int K8_BLOCKS_PER_CU = 2;
 constexpr int K8_WHOLE_PAGES = 32;
+constexpr int K8_CHUNK_BLOCKS_PER_CU = 4;
+// pages that a group of `tokens` neighbouring tokens of a row sees at most, by the host's bounds
+static int64_t k8_pages(const Kv8AttnArgs& a, int64_t tokens) {
+    int64_t len = a.max_len;
+    if (a.window) len = std::min<int64_t>(len, (int64_t)a.window + tokens + 15);
+    return std::max<int64_t>(1, (len + 15) / 16);
+}
 static K8Plan k8_plan(const Kv8AttnArgs& a) {
     K8Plan p;
-    p.nt = a.max_new * a.G <= 16 ? 1 : 2;
-    int64_t len = a.max_len;
-    if (a.window) len = std::min<int64_t>(len, (int64_t)a.window + a.max_new + 15);
-    const int64_t pages = std::max<int64_t>(1, (len + 15) / 16);
+    p.nt = (int64_t)a.max_new * a.G <= 16 ? 1 : 2;
+    const int64_t pages = k8_pages(a, std::min(a.max_new, 16 * p.nt / a.G));
     const int64_t blocks = (int64_t)a.B * a.c.Hkv;
     const int64_t want = std::max<int64_t>(1, (K8_BLOCKS_PER_CU * a.n_cu + blocks / 2) / blocks);
     int64_t sp = std::min<int64_t>(K8_MAX_PAGES, std::max<int64_t>(K8_MIN_PAGES, (pages + want - 1) / want));
@@ -785,9 +844,33 @@ static K8Plan k8_plan(const Kv8AttnArgs& a) {
     return p;
 }
 
+constexpr int K8_CHUNK_TILES = 2;  // tiles of 16 query rows a wave of the chunk kernel holds
+constexpr int K8_CHUNK_ROWS = K8_WAVES * 16 * K8_CHUNK_TILES;
+// The launch of the longer rows: tiles (at most: every row's last one may be partly empty) and splits of a tile.
+struct K8Chunks {
+    int64_t tiles;
+    int nsplit;
+};
+static K8Chunks k8_chunks(const Kv8AttnArgs& a, const K8Plan& p) {
+    K8Chunks c{0, 1};
+    if ((int64_t)a.max_new * a.G <= 16 * p.nt) return c;
+    c.tiles = (int64_t)a.T * a.G / K8_CHUNK_ROWS + std::min(a.B, a.T);
+    const int64_t blocks = c.tiles * a.c.Hkv;
+    const int64_t stages = (k8_pages(a, std::min(a.max_new, K8_CHUNK_ROWS / a.G + 1)) + K8_STAGE - 1) / K8_STAGE;
+    const int64_t most = std::min<int64_t>(K8_MAX_SPLITS, std::max<int64_t>(1, stages / K8_MIN_STAGES));
+    c.nsplit = (int)std::min<int64_t>(most, std::max<int64_t>(1, K8_CHUNK_BLOCKS_PER_CU * a.n_cu / blocks));
+    return c;
+}
+
+static size_t k8_few_floats(const Kv8AttnArgs& a, const K8Plan& p) {
+    return p.nsplit == 1 ? 0 : (size_t)a.B * a.c.Hkv * p.nsplit * (16 * p.nt) * (a.c.hd + 2);
+}
+static size_t k8_chunk_floats(const Kv8AttnArgs& a, const K8Chunks& c) {
+    return c.nsplit == 1 ? 0 : (size_t)c.tiles * a.c.Hkv * c.nsplit * K8_CHUNK_ROWS * (a.c.hd + 2);
+}
 size_t kv8_attention_ws_bytes(const Kv8AttnArgs& a) {
     const K8Plan p = k8_plan(a);
-    return p.nsplit == 1 ? 0 : (size_t)a.B * a.c.Hkv * p.nsplit * (16 * p.nt) * (a.c.hd + 2) * sizeof(float);
+    return (k8_few_floats(a, p) + k8_chunk_floats(a, k8_chunks(a, p))) * sizeof(float);
 }
 
 template <int HD, int NT, int WAVES>
@@ -812,28 +895,29 @@ static hipError_t k8_few(const Kv8AttnArgs& a, const K8Plan& p, hipStream_t s) {
     return hipGetLastError();
 }
 
-constexpr int K8_CHUNK_TILES = 2;  // tiles of 16 query rows a wave of the chunk kernel holds
-
 template <int HD>
-static hipError_t k8_chunk(const Kv8AttnArgs& a, int few, hipStream_t s) {
-    constexpr int NT = K8_CHUNK_TILES, ROWS = K8_WAVES * 16 * NT;
-    // at most: every row's last tile may be partly empty
-    const int64_t tiles = (int64_t)a.T * a.G / ROWS + std::min(a.B, a.T);
-    const dim3 grid((unsigned)(tiles * a.c.Hkv));
+static hipError_t k8_chunk(const Kv8AttnArgs& a, const K8Plan& p, const K8Chunks& c, hipStream_t s) {
+    constexpr int NT = K8_CHUNK_TILES;
+    const int few = 16 * p.nt;
+    float* part = a.part + k8_few_floats(a, p);
+    const dim3 grid((unsigned)(c.tiles * a.c.Hkv * c.nsplit));
     if (a.cap > 0.0f)
-        hipLaunchKernelGGL((attn_kv8_chunk_kernel<HD, NT, true>), grid, dim3(K8_THREADS), 0, s, a, few);
+        hipLaunchKernelGGL((attn_kv8_chunk_kernel<HD, NT, true>), grid, dim3(K8_THREADS), 0, s, a, few, c.nsplit, part);
     else
-        hipLaunchKernelGGL((attn_kv8_chunk_kernel<HD, NT, false>), grid, dim3(K8_THREADS), 0, s, a, few);
+        hipLaunchKernelGGL((attn_kv8_chunk_kernel<HD, NT, false>), grid, dim3(K8_THREADS), 0, s, a, few, c.nsplit, part);
+    if (c.nsplit > 1)
+        hipLaunchKernelGGL((attn_kv8_chunk_join_kernel<HD, NT>), dim3((unsigned)(c.tiles * a.c.Hkv), K8_CHUNK_ROWS / K8_WAVES),
+                           dim3(K8_THREADS), 0, s, a, few, c.nsplit, part);
     return hipGetLastError();
 }
 
 hipError_t launch_kv8_attention(const Kv8AttnArgs& a, hipStream_t s) {
     const K8Plan p = k8_plan(a);
-    const int few = 16 * p.nt;
+    const K8Chunks c = k8_chunks(a, p);
     const hipError_t e = a.c.hd == 128 ? (p.nt == 1 ? k8_few<128, 1>(a, p, s) : k8_few<128, 2>(a, p, s))
                                        : (p.nt == 1 ? k8_few<64, 1>(a, p, s) : k8_few<64, 2>(a, p, s));
-    if (e != hipSuccess || (int64_t)a.max_new * a.G <= few) return e;
-    return a.c.hd == 128 ? k8_chunk<128>(a, few, s) : k8_chunk<64>(a, few, s);
+    if (e != hipSuccess || c.tiles == 0) return e;
+    return a.c.hd == 128 ? k8_chunk<128>(a, p, c, s) : k8_chunk<64>(a, p, c, s);
 }
 
 }  // namespace mg

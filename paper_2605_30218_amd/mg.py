@@ -392,27 +392,40 @@ def kv8_read(codes, scales, slots, k_out=None, v_out=None, stream=None):
     return k_out, v_out
 
 
-def kv8_attention(codes, scales, q, page_table, lens, cu_new=None, max_new=1, max_len=0, scale=None, window=0,
-                  softcap=0.0, out=None, workspace=None, stream=None):
-    """mg_kv8_attention: q [T, Hq, hd] attends over the cache's positions of its rows -> out [T, Hq, hd]
-    bf16.  Tokens behind the last row's are not written: in a new tensor they hold anything.
-    workspace: a contiguous uint8 tensor that no other call in flight uses, or None to take one per
-    call."""
-    c = _kv8(codes, scales)
-    dev = codes.device
+def _attn_args(c, q, page_table, lens, cu_new, max_new, max_len, scale, window, softcap, out, dev):
     if q.dim() != 3 or q.shape[2] != c.head_dim:
         _refuse("q", q, f"[T, Hq, {c.head_dim}]")
     if page_table.dim() != 2:
         _refuse("page_table", page_table, "[B, max_pages]")
     T, Hq, hd = q.shape
     B, maxp = page_table.shape
-    if out is None:
-        out = _made(torch.empty((T, Hq, hd), dtype=q.dtype, device=dev), stream)
     qp, qs = _rows16("q", q, T, Hq, hd, dev)
     op, os_ = _rows16("out", out, T, Hq, hd, dev)
-    a = MgKv8AttnArgs(B, T, Hq, max_new, max_len, maxp, window, 0.0 if scale is None else scale, softcap, qp, qs, op,
-                      os_, _ints("page_table", page_table, dev), _ints("lens", lens, dev, B),
-                      None if cu_new is None else _ints("cu_new", cu_new, dev, B + 1))
+    return MgKv8AttnArgs(B, T, Hq, max_new, max_len, maxp, window, 0.0 if scale is None else scale, softcap, qp, qs, op,
+                         os_, _ints("page_table", page_table, dev), _ints("lens", lens, dev, B),
+                         None if cu_new is None else _ints("cu_new", cu_new, dev, B + 1))
+
+
+def kv8_attention_workspace_bytes(codes, scales, q, page_table, lens, cu_new=None, max_new=1, max_len=0, window=0):
+    """mg_kv8_attention_workspace_bytes of the call with these arguments (no device work): for a program
+    that keeps a workspace, as one that captures its step does."""
+    c = _kv8(codes, scales)
+    a = _attn_args(c, q, page_table, lens, cu_new, max_new, max_len, None, window, 0.0, q, codes.device)
+    with torch.cuda.device(codes.device):
+        return load().mg_kv8_attention_workspace_bytes(C.byref(c), C.byref(a))
+
+
+def kv8_attention(codes, scales, q, page_table, lens, cu_new=None, max_new=1, max_len=0, scale=None, window=0,
+                  softcap=0.0, out=None, workspace=None, stream=None):
+    """mg_kv8_attention: q [T, Hq, hd] attends over the cache's positions of its rows -> out [T, Hq, hd]
+    bf16.  Tokens behind the last row's are not written: in a new tensor they hold anything.
+    workspace: a contiguous uint8 tensor of kv8_attention_workspace_bytes that no other call in flight
+    uses, or None to take one per call."""
+    c = _kv8(codes, scales)
+    dev = codes.device
+    if out is None:
+        out = _made(torch.empty(q.shape, dtype=q.dtype, device=dev), stream)
+    a = _attn_args(c, q, page_table, lens, cu_new, max_new, max_len, scale, window, softcap, out, dev)
     cp, ap, lib = C.byref(c), C.byref(a), load()
     if workspace is None:
         need = lib.mg_kv8_attention_workspace_bytes(cp, ap)

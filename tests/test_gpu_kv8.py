@@ -456,7 +456,9 @@ class Loop:
         self.plan = mg.BatchPlan(z(B + 1), z(B), z(B), z(most), z(most), z(most), z(1))
         bf = lambda h: torch.zeros((most, h, hd), dtype=torch.bfloat16, device="cuda")  # noqa: E731
         self.q, self.k, self.v, self.out = bf(hq), bf(hkv), bf(hkv), bf(hq)
-        self.ws = torch.empty(1 << 24, dtype=torch.uint8, device="cuda")
+        self.ws = torch.empty(max(1, mg.kv8_attention_workspace_bytes(
+            self.codes, self.scales, self.q, self.table, self.plan.lens, cu_new=self.plan.cu_new, max_new=most)),
+            dtype=torch.uint8, device="cuda")
 
     def step(self):
         mg.batch_plan(self.ctx, self.new, self.free, self.n_free, self.table, self.most, out=self.plan)
@@ -521,7 +523,8 @@ def test_two_streams_at_once():
     alone = [b.run() for b in bs]
     args = [(b.q.cuda(), dev_i32(b.table), dev_i32(b.lens)) for b in bs]
     outs = [torch.zeros_like(a) for a in alone]
-    ws = [torch.empty(1 << 22, dtype=torch.uint8, device="cuda") for _ in bs]
+    ws = [torch.empty(mg.kv8_attention_workspace_bytes(b.codes, b.scales, *a), dtype=torch.uint8, device="cuda")
+          for b, a in zip(bs, args)]
     torch.cuda.synchronize()
     st = [torch.cuda.Stream() for _ in bs]
     for _ in range(20):
