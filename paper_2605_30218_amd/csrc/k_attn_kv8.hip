@@ -32,9 +32,10 @@ __device__ __forceinline__ uint32_t k8_pack(float lo, float hi) {
 }
 // 16 bytes at a wave-uniform address and a lane's own offset; the address stays in scalar registers
 __device__ __forceinline__ uint64_t k8_uniform(const uint8_t* p) {
-    uint64_t u = reinterpret_cast<uint64_t>(p);
-    asm("" : "+s"(u));
-    return u;
+    const uint64_t u = reinterpret_cast<uint64_t>(p);
+    uint32_t lo = __builtin_amdgcn_readfirstlane((uint32_t)u), hi = __builtin_amdgcn_readfirstlane((uint32_t)(u >> 32));
+    asm("" : "+s"(lo), "+s"(hi));
+    return lo | (uint64_t)hi << 32;
 }
 __device__ __forceinline__ u32x4_k8 k8_load(uint64_t p, uint32_t off) {
     typedef const __attribute__((address_space(1))) char* gptr;
@@ -287,18 +288,22 @@ __device__ __forceinline__ void k8_query(const Kv8AttnArgs& a, const K8Row& row,
     }
 }
 
-// Rows of few query rows (tokens times query heads of a KV head <= 16 NT): one block of 4 waves per
-// (row, KV head, split of the row's pages), a wave taking every 4th step of its pages.  The K/V stream
+// Rows of few query rows (tokens times query heads of a KV head <= 16 NT): one block per (row, KV head,
+// split of the row's pages), a wave taking every WAVES-th step of its pages.  The K/V stream
 // bounds it, so the matrix cores have the time for two terms of a probability.
+template <int HD, int NT, int WAVES>
+struct K8FewShared {
+    float o[WAVES][16 * NT][HD + 4];  // (padded rows)
+    float m[WAVES][16 * NT], l[WAVES][16 * NT];
+};
 template <int HD, int NT, int WAVES, bool CAP>
-__global__ __launch_bounds__(64 * WAVES) __attribute__((amdgpu_waves_per_eu(NT == 1 ? (WAVES > 8 ? 4 : WAVES > 4 ? 2 : 3) : 2))) void attn_kv8_few_kernel(Kv8AttnArgs a, int sp, int nsplit) {
+__device__ __forceinline__ void k8_few_block(const Kv8AttnArgs& a, int sp, int nsplit, int block, K8FewShared<HD, NT, WAVES>& sh) {
     constexpr int H = HD / 64;        // 1 KiB runs of a page of K or V
     constexpr int DT = HD / 16;       // output tiles
-    constexpr int OS = HD + 4;        // padded row of O in LDS
     const int lane = threadIdx.x & 63, c = lane & 15, g = lane >> 4;
     const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
-    const int kh = blockIdx.x % a.c.Hkv;
-    const int r = blockIdx.x / a.c.Hkv % a.B, split = blockIdx.x / a.c.Hkv / a.B;
+    const int kh = block % a.c.Hkv;
+    const int r = block / a.c.Hkv % a.B, split = block / a.c.Hkv / a.B;
     const K8Row row = k8_row(a, r);
     if (row.n <= 0 || row.n * a.G > 16 * NT) return;
     const int npg = max(row.pgb - row.pga, 0);
@@ -306,9 +311,6 @@ __global__ __launch_bounds__(64 * WAVES) __attribute__((amdgpu_waves_per_eu(NT =
     if (split >= act) return;
     const int per = ((npg + act - 1) / act + 1) & ~1;
     const int pg0 = row.pga + split * per, pg1 = split == act - 1 ? row.pgb : min(row.pgb, pg0 + per);
-
-    __shared__ __attribute__((aligned(16))) float wo[WAVES][16 * NT][OS];
-    __shared__ float wm[WAVES][16 * NT], wl[WAVES][16 * NT];
 
     uint4 qa[NT][2 * H];
     int pc[NT];
@@ -382,27 +384,27 @@ __global__ __launch_bounds__(64 * WAVES) __attribute__((amdgpu_waves_per_eu(NT =
     for (int u = 0; u < NT; ++u) {
         const float ls = k8_col_sum(acc.l[u]);
         if (g == 0) {
-            wm[wave][16 * u + c] = acc.m[u];
-            wl[wave][16 * u + c] = ls;
+            sh.m[wave][16 * u + c] = acc.m[u];
+            sh.l[wave][16 * u + c] = ls;
         }
 #pragma unroll
         for (int d = 0; d < DT; ++d)
-            *reinterpret_cast<f32x4_k8*>(&wo[wave][16 * u + c][16 * d + 4 * g]) = acc.o[u][d];
+            *reinterpret_cast<f32x4_k8*>(&sh.o[wave][16 * u + c][16 * d + 4 * g]) = acc.o[u][d];
     }
     __syncthreads();
     const int live = row.n * a.G;
     for (int i = threadIdx.x; i < live * (HD / 4); i += 64 * WAVES) {
         const int rr = i / (HD / 4), d = i % (HD / 4) * 4;
-        float M = wm[0][rr];
+        float M = sh.m[0][rr];
 #pragma unroll
-        for (int w = 1; w < WAVES; ++w) M = fmaxf(M, wm[w][rr]);
+        for (int w = 1; w < WAVES; ++w) M = fmaxf(M, sh.m[w][rr]);
         float L = 0.0f;
         f32x4_k8 O = f32x4_k8{0.f, 0.f, 0.f, 0.f};
 #pragma unroll
         for (int w = 0; w < WAVES; ++w) {
-            const float f = __builtin_amdgcn_exp2f(wm[w][rr] - M);
-            L += f * wl[w][rr];
-            O += f * *reinterpret_cast<const f32x4_k8*>(&wo[w][rr][d]);
+            const float f = __builtin_amdgcn_exp2f(sh.m[w][rr] - M);
+            L += f * sh.l[w][rr];
+            O += f * *reinterpret_cast<const f32x4_k8*>(&sh.o[w][rr][d]);
         }
         const int64_t tok = row.t0 + rr / a.G;
         const int head = kh * a.G + rr % a.G;
@@ -420,6 +422,13 @@ __global__ __launch_bounds__(64 * WAVES) __attribute__((amdgpu_waves_per_eu(NT =
             }
         }
     }
+}
+
+template <int HD, int NT, int WAVES, bool CAP>
+__global__ __launch_bounds__(64 * WAVES) __attribute__((amdgpu_waves_per_eu(NT == 2 || WAVES > 4 ? 2 : 3))) void attn_kv8_few_kernel(
+    Kv8AttnArgs a, int sp, int nsplit) {
+    __shared__ __attribute__((aligned(16))) K8FewShared<HD, NT, WAVES> sh;
+    k8_few_block<HD, NT, WAVES, CAP>(a, sp, nsplit, blockIdx.x, sh);
 }
 
 // One query row's splits joined in their order by a wave: outputs at po + s * so, reference and sum of split s in lane s's
@@ -465,11 +474,12 @@ __device__ __forceinline__ uint16_t* k8_out(const Kv8AttnArgs& a, const K8Row& r
     return a.out + (int64_t)(row.t0 + rr / a.G) * a.out_stride + (size_t)(kh * a.G + rr % a.G) * a.c.hd;
 }
 
-// Joins the splits of attn_kv8_few_kernel: a wave per query row of a (row, KV head).
+// Joins the splits of rows of few query rows: a wave per query row of a (row, KV head); block: its index, of ROWB blocks a
+// (row, KV head).
 template <int HD, int NT>
-__global__ __launch_bounds__(K8_THREADS) void attn_kv8_join_kernel(Kv8AttnArgs a, int sp, int nsplit) {
-    const int rr = blockIdx.y * K8_WAVES + (threadIdx.x >> 6);
-    const int kh = blockIdx.x % a.c.Hkv, r = blockIdx.x / a.c.Hkv;
+__device__ __forceinline__ void k8_few_join(const Kv8AttnArgs& a, int sp, int nsplit, int block, int rowb) {
+    const int rr = block % rowb * K8_WAVES + (threadIdx.x >> 6);
+    const int kh = block / rowb % a.c.Hkv, r = block / rowb / a.c.Hkv;
     const K8Row row = k8_row(a, r);
     if (row.n <= 0 || row.n * a.G > 16 * NT || rr >= row.n * a.G) return;
     const int act = k8_active(max(row.pgb - row.pga, 0), sp, nsplit);
@@ -477,6 +487,10 @@ __global__ __launch_bounds__(K8_THREADS) void attn_kv8_join_kernel(Kv8AttnArgs a
     const size_t first = ((size_t)r * a.c.Hkv + kh) * nsplit * (16 * NT) + rr;
     const float* ml = a.part + (size_t)a.B * a.c.Hkv * nsplit * (16 * NT) * HD;
     k8_join<HD>(a.part + first * HD, (size_t)(16 * NT) * HD, ml + 2 * first, 2 * 16 * NT, act, k8_out(a, row, kh, rr));
+}
+template <int HD, int NT>
+__global__ __launch_bounds__(K8_THREADS) void attn_kv8_join_kernel(Kv8AttnArgs a, int sp, int nsplit, int rowb) {
+    k8_few_join<HD, NT>(a, sp, nsplit, blockIdx.x, rowb);
 }
 
 // Tile `index` of the rows of more than `few` query rows, their tiles of ROWS query rows counted row by row: the row, and the
@@ -511,6 +525,8 @@ __device__ __forceinline__ K8Tile k8_tile(const Kv8AttnArgs& a, int few, int ind
 }
 constexpr int K8_STAGE = 4;       // pages a stage of the chunk kernel, one a wave to fetch
 constexpr int K8_MIN_STAGES = 4;  // stages a split of a tile takes at least
+constexpr int K8_CHUNK_TILES = 2; // tiles of 16 query rows a wave of a chunk's block holds
+constexpr int K8_CHUNK_ROWS = K8_WAVES * 16 * K8_CHUNK_TILES;
 // The pages that tile t's tokens see, the stages of four pages they make and the splits that share these.
 struct K8Span {
     int pg0, pg1, stages, act;
@@ -526,20 +542,37 @@ __device__ __forceinline__ K8Span k8_span(const Kv8AttnArgs& a, const K8Row& row
     return x;
 }
 
-// Rows of more query rows than 16 * few tiles: one block of 4 waves per (row, KV head, 64 NT query rows), the
-// tokens of a row's end first (they see the most), a wave holding NT tiles.  The block walks the
-// positions that its tokens see in stages of 4 pages, which go through a double buffer in LDS as bf16 matrix
-// operands: a wave fetches and converts K or V of two pages, so that a code is converted once a block and an
-// operand is one read for NT products.  The next stage is in flight in registers while one is used, and one barrier a
-// stage parts them.
+// Rows of more query rows: one block of 8 waves per (row, KV head, 64 NT query rows, split of the positions that these see),
+// the tokens of a row's end first (they see the most).  The waves form two groups of four; a wave holds NT
+// tiles of query rows, the same in both groups, and each group takes half of the block's positions in stages of 4
+// pages, which go through a double buffer of the group's in LDS as bf16 matrix operands: a wave fetches and
+// converts one page, so that a code is converted once a group and an operand is one read for NT products.  The
+// next stage is in flight in registers while one is used, and one barrier a stage parts them.  A wave alone
+// on its SIMD leaves it idle for more than half of a stage (LDS reads, the chain from scores to probabilities): the
+// two groups fill each other's gaps, and halve the time of the longest block.
+constexpr int K8_GROUPS = 2;
+constexpr int K8_CHUNK_THREADS = K8_GROUPS * K8_THREADS;
+template <int HD>
+struct K8ChunkShared {
+    // operands of two stages, 16 bytes a lane: [stage][pair of pages][K: (page, h, half); V: output tile]
+    uint32_t tile[K8_GROUPS][2][2][2][HD / 16][64][4];
+    uint32_t nan_at[K8_GROUPS][2][K8_STAGE][64];  // NaN codes of V: bits 4 d .. of a lane: output tile d's four positions of a page
+    int nan_any[K8_GROUPS][2][K8_STAGE];
+};
 template <int HD, int NT, bool CAP>
-__global__ __launch_bounds__(K8_THREADS) __attribute__((amdgpu_waves_per_eu(2))) void attn_kv8_chunk_kernel(Kv8AttnArgs a, int few, int nsplit, float* part) {
+__device__ __forceinline__ void k8_chunk_block(const Kv8AttnArgs& a, int few, int tiles, int nsplit, float* part, int block,
+                                               K8ChunkShared<HD>& sh) {
     constexpr int H = HD / 64, DT = HD / 16;
     constexpr int ROWS = K8_WAVES * 16 * NT;
+    static_assert(NT * DT * 4 * K8_THREADS <= sizeof(sh.tile) / K8_GROUPS / 4, "a group's outputs fit its tiles");
     const int lane = threadIdx.x & 63, c = lane & 15, g = lane >> 4;
-    const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
-    const int kh = blockIdx.x % a.c.Hkv;
-    const int split = blockIdx.x / a.c.Hkv % nsplit, index = blockIdx.x / a.c.Hkv / nsplit;
+    const int group = __builtin_amdgcn_readfirstlane(threadIdx.x / K8_THREADS);
+    const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6) % K8_WAVES;
+    const int kh = block % a.c.Hkv;
+    uint32_t(*tile)[2][2][DT][64][4] = sh.tile[group];
+    uint32_t(*nan_at)[K8_STAGE][64] = sh.nan_at[group];
+    int(*nan_any)[K8_STAGE] = sh.nan_any[group];
+    const int split = block / a.c.Hkv % nsplit, index = block / a.c.Hkv / nsplit;
     const K8Tile at = k8_tile<ROWS>(a, few, index);
     if (at.r < 0) return;
     const int r = __builtin_amdgcn_readfirstlane(at.r), t = __builtin_amdgcn_readfirstlane(at.t);
@@ -548,16 +581,13 @@ __global__ __launch_bounds__(K8_THREADS) __attribute__((amdgpu_waves_per_eu(2)))
     if (t * ROWS >= live) return;
     K8Span span = k8_span<ROWS>(a, row, t, nsplit);
     if (split >= span.act) return;
-    const int st0 = span.stages * split / span.act, stages = span.stages * (split + 1) / span.act - st0;
+    // the block's stages, and the group's of them; most: those of the group that has more
+    const int b0 = span.stages * split / span.act, b1 = span.stages * (split + 1) / span.act, half = (b0 + b1 + 1) / 2;
+    const int st0 = group ? half : b0, stages = (group ? b1 : half) - st0, most = half - b0;
     const int pg0 = span.pg0 + st0 * K8_STAGE, pg1 = min(span.pg1, pg0 + stages * K8_STAGE);
     // the positions of the wave's tokens
     const int rr0 = t * ROWS + wave * (16 * NT);
     const int wp0 = row.p0 + min(rr0, live - 1) / a.G, wp1 = row.p0 + (min(rr0 + 16 * NT, live) - 1) / a.G;
-
-    // operands of two stages, 16 bytes a lane: [stage][pair of pages][K: (page, h, half); V: output tile]
-    __shared__ __attribute__((aligned(16))) uint32_t tile[2][2][2][4 * H][64][4];
-    __shared__ uint32_t nan_at[2][K8_STAGE][64];  // NaN codes of V: bits 4 d .. of a lane: output tile d's four positions of a page
-    __shared__ int nan_any[2][K8_STAGE];
 
     uint4 qa[NT][2 * H];
     int pc[NT];
@@ -572,45 +602,39 @@ __global__ __launch_bounds__(K8_THREADS) __attribute__((amdgpu_waves_per_eu(2)))
     const size_t head_bytes = (size_t)2 * 16 * HD;
     const uint8_t* base = a.c.codes + (size_t)kh * head_bytes;
 
-    // lane i: page pg0 + 64 k + i of the table, of the 64 that hold the stage fetched last: its place, its scales and
-    // (mapped) whether it is one of the cache's and the block's; and the id and scale bytes of the next 64's
+    // lane i: page pg0 + 64 k + i of the table (-1: not one of the cache's, or past the group's), of the 64 that hold the
+    // stage fetched last, and its scale bytes; and the next 64's
     auto page_id = [&](int i) {
-        const int v = i < pg1 ? *reinterpret_cast<const int32_t*>(reinterpret_cast<const char*>(ptab) + 4u * (uint32_t)i) : -1;
-        return v;
+        return i < pg1 ? *reinterpret_cast<const int32_t*>(reinterpret_cast<const char*>(ptab) + 4u * (uint32_t)i) : -1;
     };
+    auto valid = [&](int v) { return v < 0 || v >= a.c.n_pages ? -1 : v; };
     auto scale_bytes = [&](int v) {
         return v < 0 ? 0u : (uint32_t) * reinterpret_cast<const uint16_t*>(a.c.scales + ((size_t)v * a.c.Hkv + kh) * 2);
     };
-    int idn = page_id(pg0 + lane);
-    idn = idn < 0 || idn >= a.c.n_pages ? -1 : idn;
-    uint32_t scn = scale_bytes(idn);
-    uint64_t place = 0, mapped64 = 0;
-    uint32_t kscale = 0, vscale = 0;
+    int id = -1, idn = valid(page_id(pg0 + lane));
+    uint32_t sc = 0, scn = scale_bytes(idn);
     // the wave's page of the next stage: K, V, their scales, and which of the stage's pages are mapped
     u32x4_k8 nx[2][H];
     float nsc[2];
     int map = 0;
-    auto fetch = [&](int st, u32x4_k8 (&x)[2][H], float (&xs)[2], int& m, int& idn, uint32_t& scn, uint64_t& place,
-                     uint64_t& mapped64, uint32_t& kscale, uint32_t& vscale) {
+    const size_t page_bytes = (size_t)a.c.Hkv * head_bytes;
+    auto fetch = [&](int st, u32x4_k8 (&x)[2][H], float (&xs)[2], int& m, int& id, uint32_t& sc, int& idn, uint32_t& scn) {
         const int at = st * K8_STAGE % K8_IDS;
         if (at == 0) {
-            place = (uint64_t)max(idn, 0) * a.c.Hkv * head_bytes;
-            mapped64 = __ballot(idn >= 0);
-            kscale = (scn & 0xffu) << 23;
-            vscale = scn >> 8 << 23;
+            id = idn;
+            sc = scn;
             idn = page_id(pg0 + st * K8_STAGE + K8_IDS + lane);
         }
         if (at == K8_IDS / 2) {  // halfway: the next ids are there, their scales are requested
-            idn = idn < 0 || idn >= a.c.n_pages ? -1 : idn;
+            idn = valid(idn);
             scn = scale_bytes(idn);
         }
-        m = (int)(mapped64 >> at) & 15;
+        m = (int)(__ballot(id >= 0) >> at) & 15;
         const int mine = at + wave;
-        xs[0] = __uint_as_float((uint32_t)__builtin_amdgcn_readlane((int)kscale, mine));
-        xs[1] = __uint_as_float((uint32_t)__builtin_amdgcn_readlane((int)vscale, mine));
-        const uint64_t off = (uint32_t)__builtin_amdgcn_readlane((int)(uint32_t)place, mine) |
-                             (uint64_t)(uint32_t)__builtin_amdgcn_readlane((int)(place >> 32), mine) << 32;
-        const uint64_t p = k8_uniform(base + off);
+        const uint32_t b = (uint32_t)__builtin_amdgcn_readlane((int)sc, mine);
+        xs[0] = __uint_as_float((b & 0xffu) << 23);
+        xs[1] = __uint_as_float(b >> 8 << 23);
+        const uint64_t p = k8_uniform(base + (size_t)max(__builtin_amdgcn_readlane(id, mine), 0) * page_bytes);
 #pragma unroll
         for (int h = 0; h < 2 * H; ++h) x[h / H][h % H] = k8_load(p, h * 1024u + lane * 16u);
     };
@@ -654,24 +678,26 @@ __global__ __launch_bounds__(K8_THREADS) __attribute__((amdgpu_waves_per_eu(2)))
     };
     int now = 0;
     if (stages) {
-        fetch(0, nx, nsc, map, idn, scn, place, mapped64, kscale, vscale);
+        fetch(0, nx, nsc, map, id, sc, idn, scn);
         put(0, nx, nsc);
     }
-    for (int st = 0; st < stages; ++st) {
+    for (int st = 0; st < most; ++st) {
         const int buf = st & 1;
         now = map;
         __syncthreads();
+        if (st < stages) {  // (else the last stage is the other group's alone)
         // K's operands of the first 32 positions; V's are requested before the softmax and K's of the second 32
         // before V's product, so that an operand is waited for only where its latency has passed under other work
         bf16x8_k8 kf[4 * H], vf[DT];
-        auto read_k = [&](int hf, bf16x8_k8 (&kf)[4 * H]) {
+        auto read_k = [&](int hf, int e, bf16x8_k8 (&kf)[4 * H]) {
 #pragma unroll
-            for (int k = 0; k < 4 * H; ++k) kf[k] = *reinterpret_cast<const bf16x8_k8*>(tile[buf][hf][0][k][lane]);
+            for (int k = 2 * H * e; k < 2 * H * (e + 1); ++k) kf[k] = *reinterpret_cast<const bf16x8_k8*>(tile[buf][hf][0][k][lane]);
         };
-        read_k(0, kf);
+        read_k(0, 0, kf);
+        read_k(0, 1, kf);
         const int bad[2] = {nan_any[buf][0] | nan_any[buf][1], nan_any[buf][2] | nan_any[buf][3]};
         __builtin_amdgcn_sched_barrier(0);
-        if (st + 1 < stages) fetch(st + 1, nx, nsc, map, idn, scn, place, mapped64, kscale, vscale);
+        if (st + 1 < stages) fetch(st + 1, nx, nsc, map, id, sc, idn, scn);
 #pragma unroll
         for (int hf = 0; hf < K8_STAGE / 2; ++hf) {
             const int j0 = 16 * (pg0 + st * K8_STAGE) + 32 * hf;
@@ -679,6 +705,10 @@ __global__ __launch_bounds__(K8_THREADS) __attribute__((amdgpu_waves_per_eu(2)))
             const bool any = j0 <= wp1 && !(a.window && j0 + 31 <= wp0 - a.window);
             const int mapped = now >> (2 * hf) & 3;
             const bool edge = mapped != 3 || j0 + 31 > wp0 || j0 + 32 > row.len || (a.window && j0 <= wp1 - a.window);
+            if (hf == 1) {
+                read_k(1, 1, kf);
+                __builtin_amdgcn_sched_barrier(0);
+            }
             float x[NT][8];
 #pragma unroll
             for (int e = 0; e < 2; ++e) {
@@ -713,28 +743,31 @@ __global__ __launch_bounds__(K8_THREADS) __attribute__((amdgpu_waves_per_eu(2)))
             if (any && bad[hf]) {
                 // NaN codes of V went into the tile as 0: a product of the codes' and the columns' indicators finds the
                 // outputs that see one, which become NaN at the end
-                const uint32_t n0 = nan_any[buf][2 * hf] ? nan_at[buf][2 * hf][lane] : 0u;
-                const uint32_t n1 = nan_any[buf][2 * hf + 1] ? nan_at[buf][2 * hf + 1][lane] : 0u;
-                u32x4_k8 sw[NT];
+                // (tile by tile of query rows, the codes' indicators made anew for each: 32 registers less)
 #pragma unroll
-                for (int u = 0; u < NT; ++u)
+                for (int u = 0; u < NT; ++u) {
+                    uint32_t n[2];
+#pragma unroll
+                    for (int e = 0; e < 2; ++e) {
+                        n[e] = nan_any[buf][2 * hf + e] ? nan_at[buf][2 * hf + e][lane] : 0u;
+                        asm("" : "+v"(n[e]));
+                    }
+                    u32x4_k8 sw;
 #pragma unroll
                     for (int i = 0; i < 4; ++i)
-                        sw[u][i] = (k8_sees(row, a.window, j0, mapped, g, 2 * i, pc[u]) ? 0x3f80u : 0u) |
-                                   (k8_sees(row, a.window, j0, mapped, g, 2 * i + 1, pc[u]) ? 0x3f800000u : 0u);
+                        sw[i] = (k8_sees(row, a.window, j0, mapped, g, 2 * i, pc[u]) ? 0x3f80u : 0u) |
+                                (k8_sees(row, a.window, j0, mapped, g, 2 * i + 1, pc[u]) ? 0x3f800000u : 0u);
 #pragma unroll
-                for (int d = 0; d < DT; ++d) {
-                    __builtin_amdgcn_sched_barrier(0);
-                    u32x4_k8 f;
+                    for (int d = 0; d < DT; ++d) {
+                        __builtin_amdgcn_sched_barrier(0);
+                        u32x4_k8 f;
 #pragma unroll
-                    for (int i = 0; i < 4; ++i) {
-                        const uint32_t b = (i < 2 ? n0 : n1) >> (4 * d + 2 * (i & 1));
-                        f[i] = (b & 1u ? 0x3f80u : 0u) | (b & 2u ? 0x3f800000u : 0u);
-                    }
-#pragma unroll
-                    for (int u = 0; u < NT; ++u) {
+                        for (int i = 0; i < 4; ++i) {
+                            const uint32_t b = n[i >> 1] >> (4 * d + 2 * (i & 1));
+                            f[i] = (b & 1u ? 0x3f80u : 0u) | (b & 2u ? 0x3f800000u : 0u);
+                        }
                         f32x4_k8 hit = f32x4_k8{0.f, 0.f, 0.f, 0.f};
-                        hit = __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8_k8, f), __builtin_bit_cast(bf16x8_k8, sw[u]), hit, 0, 0, 0);
+                        hit = __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8_k8, f), __builtin_bit_cast(bf16x8_k8, sw), hit, 0, 0, 0);
 #pragma unroll
                         for (int i = 0; i < 4; ++i) {
                             uint32_t one = hit[i] > 0.0f ? 1u : 0u;
@@ -745,7 +778,7 @@ __global__ __launch_bounds__(K8_THREADS) __attribute__((amdgpu_waves_per_eu(2)))
                 }
             }
             __builtin_amdgcn_sched_barrier(0);
-            if (hf == 0) read_k(1, kf);
+            if (hf == 0) read_k(1, 0, kf);  // (the second page's when V's registers are free)
             __builtin_amdgcn_sched_barrier(0);
             if (!any) continue;
 #pragma unroll
@@ -754,30 +787,56 @@ __global__ __launch_bounds__(K8_THREADS) __attribute__((amdgpu_waves_per_eu(2)))
                 for (int u = 0; u < NT; ++u) acc.o[u][d] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(vf[d], p[u][0], acc.o[u][d], 0, 0, 0);
         }
         if (st + 1 < stages) put(buf ^ 1, nx, nsc);
+        }
     }
+    // the second group's outputs join the first's, through its own tiles
 #pragma unroll
     for (int u = 0; u < NT; ++u) {
-        const float L = k8_col_sum(acc.l[u]);
-        const float inv = L == 0.0f ? 0.0f : ieee_div(1.0f, L);
-        const int rr = rr0 + 16 * u + c;
-        if (rr >= live) continue;
-        uint16_t* out = a.out + (int64_t)(row.t0 + rr / a.G) * a.out_stride + (size_t)(kh * a.G + rr % a.G) * HD + 4 * g;
+        acc.l[u] = k8_col_sum(acc.l[u]);
 #pragma unroll
         for (int d = 0; d < DT; ++d)
 #pragma unroll
             for (int i = 0; i < 4; ++i)
                 if (nan_out[u] >> (4 * d + i) & 1u) acc.o[u][d][i] = __builtin_nanf("");
+    }
+    __syncthreads();
+    f32x4_k8* other = reinterpret_cast<f32x4_k8*>(sh.tile[1]) + wave * (NT * DT * 64) + lane;
+    float* other_ml = reinterpret_cast<float*>(sh.tile[0]) + wave * (2 * NT * 64) + lane;
+    if (group) {
+#pragma unroll
+        for (int u = 0; u < NT; ++u) {
+            other_ml[2 * u * 64] = acc.m[u];
+            other_ml[(2 * u + 1) * 64] = acc.l[u];
+#pragma unroll
+            for (int d = 0; d < DT; ++d) other[(u * DT + d) * 64] = acc.o[u][d];
+        }
+    }
+    __syncthreads();
+    if (group) return;
+#pragma unroll
+    for (int u = 0; u < NT; ++u) {
+        const float m1 = other_ml[2 * u * 64], M = fmaxf(acc.m[u], m1);
+        const float f0 = __builtin_amdgcn_exp2f(acc.m[u] - M), f1 = __builtin_amdgcn_exp2f(m1 - M);
+        acc.m[u] = M;
+        acc.l[u] = acc.l[u] * f0 + other_ml[(2 * u + 1) * 64] * f1;
+#pragma unroll
+        for (int d = 0; d < DT; ++d) acc.o[u][d] = acc.o[u][d] * f0 + other[(u * DT + d) * 64] * f1;
+        const float L = acc.l[u];
+        const float inv = L == 0.0f ? 0.0f : ieee_div(1.0f, L);
+        const int rr = rr0 + 16 * u + c;
+        if (rr >= live) continue;
         if (span.act > 1) {
             const size_t pr = ((size_t)(index * a.c.Hkv + kh) * nsplit + split) * ROWS + wave * (16 * NT) + 16 * u + c;
 #pragma unroll
             for (int d = 0; d < DT; ++d) *reinterpret_cast<f32x4_k8*>(part + pr * HD + 16 * d + 4 * g) = acc.o[u][d];
             if (g == 0) {
-                float* ml = part + (size_t)(gridDim.x / nsplit) * nsplit * ROWS * HD + 2 * pr;
+                float* ml = part + (size_t)tiles * a.c.Hkv * nsplit * ROWS * HD + 2 * pr;
                 ml[0] = acc.m[u];
                 ml[1] = L;
             }
             continue;
         }
+        uint16_t* out = k8_out(a, row, kh, rr) + 4 * g;
 #pragma unroll
         for (int d = 0; d < DT; ++d)
             *reinterpret_cast<uint2*>(out + 16 * d) =
@@ -785,21 +844,44 @@ __global__ __launch_bounds__(K8_THREADS) __attribute__((amdgpu_waves_per_eu(2)))
     }
 }
 
-// Joins the splits of attn_kv8_chunk_kernel: a wave per query row of a (tile, KV head).
-template <int HD, int NT>
-__global__ __launch_bounds__(K8_THREADS) void attn_kv8_chunk_join_kernel(Kv8AttnArgs a, int few, int nsplit, const float* part) {
-    constexpr int ROWS = K8_WAVES * 16 * NT;
-    const int kh = blockIdx.x % a.c.Hkv, index = blockIdx.x / a.c.Hkv;
-    const K8Tile at = k8_tile<ROWS>(a, few, index);
-    if (at.r < 0) return;
-    const K8Row row = k8_row(a, at.r);
-    const int i = blockIdx.y * K8_WAVES + (threadIdx.x >> 6), rr = at.t * ROWS + i;
+// A call with longer rows: their blocks, then those of its rows of few query rows, in one launch.
+template <int HD, bool CAP>
+__global__ __launch_bounds__(K8_CHUNK_THREADS) __attribute__((amdgpu_waves_per_eu(2))) void attn_kv8_mixed_kernel(
+    Kv8AttnArgs a, int sp, int nsplit, int tiles, int csplit, float* cpart) {
+    union Shared {
+        K8ChunkShared<HD> chunk;
+        K8FewShared<HD, 1, K8_GROUPS * K8_WAVES> few;
+    };
+    __shared__ __attribute__((aligned(16))) Shared sh;
+    const int chunks = tiles * a.c.Hkv * csplit;
+    if ((int)blockIdx.x < chunks)
+        k8_chunk_block<HD, K8_CHUNK_TILES, CAP>(a, 16, tiles, csplit, cpart, blockIdx.x, sh.chunk);
+    else
+        k8_few_block<HD, 1, K8_GROUPS * K8_WAVES, CAP>(a, sp, nsplit, blockIdx.x - chunks, sh.few);
+}
+
+// Joins the splits of attn_kv8_mixed_kernel: blocks of its longer rows' tiles (csplit > 1), a wave per query row, then of the
+// others.
+template <int HD>
+__global__ __launch_bounds__(K8_THREADS) void attn_kv8_mixed_join_kernel(Kv8AttnArgs a, int sp, int nsplit, int rowb, int tiles,
+                                                                        int csplit, const float* cpart) {
+    constexpr int ROWS = K8_CHUNK_ROWS, RB = ROWS / K8_WAVES;
+    const int chunks = csplit > 1 ? tiles * a.c.Hkv * RB : 0;
+    if ((int)blockIdx.x >= chunks) {
+        k8_few_join<HD, 1>(a, sp, nsplit, blockIdx.x - chunks, rowb);
+        return;
+    }
+    const int at = blockIdx.x / RB, kh = at % a.c.Hkv;
+    const K8Tile tile = k8_tile<ROWS>(a, 16, at / a.c.Hkv);
+    if (tile.r < 0) return;
+    const K8Row row = k8_row(a, tile.r);
+    const int i = blockIdx.x % RB * K8_WAVES + (threadIdx.x >> 6), rr = tile.t * ROWS + i;
     if (rr >= row.n * a.G) return;
-    const int act = k8_span<ROWS>(a, row, at.t, nsplit).act;
+    const int act = k8_span<ROWS>(a, row, tile.t, csplit).act;
     if (act == 1) return;
-    const size_t first = (size_t)blockIdx.x * nsplit * ROWS + i;
-    const float* ml = part + (size_t)gridDim.x * nsplit * ROWS * HD;
-    k8_join<HD>(part + first * HD, (size_t)ROWS * HD, ml + 2 * first, 2 * ROWS, act, k8_out(a, row, kh, rr));
+    const size_t first = (size_t)at * csplit * ROWS + i;
+    const float* ml = cpart + (size_t)tiles * a.c.Hkv * csplit * ROWS * HD;
+    k8_join<HD>(cpart + first * HD, (size_t)ROWS * HD, ml + 2 * first, 2 * ROWS, act, k8_out(a, row, kh, rr));
 }
 
 // The launch of rows of few query rows: tiles and waves of a block, pages of a split, splits of a row.
@@ -812,14 +894,16 @@ __global__ __launch_bounds__(K8_THREADS) void attn_kv8_chunk_join_kernel(Kv8Attn
 //     waves takes a row whole: one row of 512 7.1 -> 6.3, 32 rows of 512 12.1 -> 9.8; at 64 pages one row
 //     7.9 -> 9.7, but 32 rows 17.0 -> 14.7, so up to 32 pages, or 64 where the blocks are half of the CUs.
 struct K8Plan {
-    int nt, waves, sp, nsplit;
+    int nt, waves, sp, nsplit;  // rows of few query rows: tiles and waves of a block, pages of a split, splits of a row
+    int64_t tiles;              // of 128 query rows, of the longer rows: at most (a row's last may be partly empty); 0: none
+    int csplit;                 // splits of such a tile
 };
 constexpr int K8_MIN_PAGES = 8;  // pages a split takes at least: a step of every wave
 constexpr int K8_MAX_PAGES = 128;
 constexpr int K8_MAX_SPLITS = 64;
 constexpr int K8_BLOCKS_PER_CU = 2;
 constexpr int K8_WHOLE_PAGES = 32;
-constexpr int K8_CHUNK_BLOCKS_PER_CU = 4;
+constexpr int K8_CHUNK_BLOCKS_PER_CU = 2;
 // pages that a group of `tokens` neighbouring tokens of a row sees at most, by the host's bounds
 static int64_t k8_pages(const Kv8AttnArgs& a, int64_t tokens) {
     int64_t len = a.max_len;
@@ -828,7 +912,9 @@ static int64_t k8_pages(const Kv8AttnArgs& a, int64_t tokens) {
 }
 static K8Plan k8_plan(const Kv8AttnArgs& a) {
     K8Plan p;
-    p.nt = (int64_t)a.max_new * a.G <= 16 ? 1 : 2;
+    const int64_t rows = (int64_t)a.max_new * a.G;
+    p.tiles = rows <= 32 ? 0 : (int64_t)a.T * a.G / K8_CHUNK_ROWS + std::min(a.B, a.T);
+    p.nt = rows <= 16 || p.tiles ? 1 : 2;
     const int64_t pages = k8_pages(a, std::min(a.max_new, 16 * p.nt / a.G));
     const int64_t blocks = (int64_t)a.B * a.c.Hkv;
     const int64_t want = std::max<int64_t>(1, (K8_BLOCKS_PER_CU * a.n_cu + blocks / 2) / blocks);
@@ -841,83 +927,64 @@ static K8Plan k8_plan(const Kv8AttnArgs& a) {
     }
     p.sp = (int)sp;
     p.nsplit = (int)((pages + sp - 1) / sp);
+    p.csplit = 1;
+    if (p.tiles) {
+        const int64_t stages = (k8_pages(a, std::min(a.max_new, K8_CHUNK_ROWS / a.G + 1)) + K8_STAGE - 1) / K8_STAGE;
+        const int64_t most = std::min<int64_t>(K8_MAX_SPLITS, std::max<int64_t>(1, stages / K8_MIN_STAGES));
+        p.csplit = (int)std::min<int64_t>(most, std::max<int64_t>(1, K8_CHUNK_BLOCKS_PER_CU * a.n_cu / (p.tiles * a.c.Hkv)));
+    }
     return p;
-}
-
-constexpr int K8_CHUNK_TILES = 2;  // tiles of 16 query rows a wave of the chunk kernel holds
-constexpr int K8_CHUNK_ROWS = K8_WAVES * 16 * K8_CHUNK_TILES;
-// The launch of the longer rows: tiles (at most: every row's last one may be partly empty) and splits of a tile.
-struct K8Chunks {
-    int64_t tiles;
-    int nsplit;
-};
-static K8Chunks k8_chunks(const Kv8AttnArgs& a, const K8Plan& p) {
-    K8Chunks c{0, 1};
-    if ((int64_t)a.max_new * a.G <= 16 * p.nt) return c;
-    c.tiles = (int64_t)a.T * a.G / K8_CHUNK_ROWS + std::min(a.B, a.T);
-    const int64_t blocks = c.tiles * a.c.Hkv;
-    const int64_t stages = (k8_pages(a, std::min(a.max_new, K8_CHUNK_ROWS / a.G + 1)) + K8_STAGE - 1) / K8_STAGE;
-    const int64_t most = std::min<int64_t>(K8_MAX_SPLITS, std::max<int64_t>(1, stages / K8_MIN_STAGES));
-    c.nsplit = (int)std::min<int64_t>(most, std::max<int64_t>(1, K8_CHUNK_BLOCKS_PER_CU * a.n_cu / blocks));
-    return c;
 }
 
 static size_t k8_few_floats(const Kv8AttnArgs& a, const K8Plan& p) {
     return p.nsplit == 1 ? 0 : (size_t)a.B * a.c.Hkv * p.nsplit * (16 * p.nt) * (a.c.hd + 2);
 }
-static size_t k8_chunk_floats(const Kv8AttnArgs& a, const K8Chunks& c) {
-    return c.nsplit == 1 ? 0 : (size_t)c.tiles * a.c.Hkv * c.nsplit * K8_CHUNK_ROWS * (a.c.hd + 2);
-}
 size_t kv8_attention_ws_bytes(const Kv8AttnArgs& a) {
     const K8Plan p = k8_plan(a);
-    return (k8_few_floats(a, p) + k8_chunk_floats(a, k8_chunks(a, p))) * sizeof(float);
+    const size_t chunk = p.csplit == 1 ? 0 : (size_t)p.tiles * a.c.Hkv * p.csplit * K8_CHUNK_ROWS * (a.c.hd + 2);
+    return (k8_few_floats(a, p) + chunk) * sizeof(float);
 }
 
 template <int HD, int NT, int WAVES>
-static void k8_few_launch(const Kv8AttnArgs& a, const K8Plan& p, hipStream_t s) {
+static void k8_launch_few(const Kv8AttnArgs& a, const K8Plan& p, hipStream_t s) {
     const dim3 grid((unsigned)((int64_t)a.B * a.c.Hkv * p.nsplit));
-    if (a.cap > 0.0f)
-        hipLaunchKernelGGL((attn_kv8_few_kernel<HD, NT, WAVES, true>), grid, dim3(64 * WAVES), 0, s, a, p.sp, p.nsplit);
-    else
-        hipLaunchKernelGGL((attn_kv8_few_kernel<HD, NT, WAVES, false>), grid, dim3(64 * WAVES), 0, s, a, p.sp, p.nsplit);
+    auto f = a.cap > 0.0f ? attn_kv8_few_kernel<HD, NT, WAVES, true> : attn_kv8_few_kernel<HD, NT, WAVES, false>;
+    hipLaunchKernelGGL(f, grid, dim3(64 * WAVES), 0, s, a, p.sp, p.nsplit);
 }
-
-template <int HD, int NT>
-static hipError_t k8_few(const Kv8AttnArgs& a, const K8Plan& p, hipStream_t s) {
-    if (NT == 1 && p.waves == 2 * K8_WAVES)
-        k8_few_launch<HD, 1, 2 * K8_WAVES>(a, p, s);
-    else
-        k8_few_launch<HD, NT, K8_WAVES>(a, p, s);
-    if (p.nsplit > 1)
-        hipLaunchKernelGGL((attn_kv8_join_kernel<HD, NT>),
-                           dim3(a.B * a.c.Hkv, (std::min(a.max_new * a.G, 16 * NT) + K8_WAVES - 1) / K8_WAVES),
-                           dim3(K8_THREADS), 0, s, a, p.sp, p.nsplit);
-    return hipGetLastError();
-}
-
 template <int HD>
-static hipError_t k8_chunk(const Kv8AttnArgs& a, const K8Plan& p, const K8Chunks& c, hipStream_t s) {
-    constexpr int NT = K8_CHUNK_TILES;
-    const int few = 16 * p.nt;
-    float* part = a.part + k8_few_floats(a, p);
-    const dim3 grid((unsigned)(c.tiles * a.c.Hkv * c.nsplit));
-    if (a.cap > 0.0f)
-        hipLaunchKernelGGL((attn_kv8_chunk_kernel<HD, NT, true>), grid, dim3(K8_THREADS), 0, s, a, few, c.nsplit, part);
-    else
-        hipLaunchKernelGGL((attn_kv8_chunk_kernel<HD, NT, false>), grid, dim3(K8_THREADS), 0, s, a, few, c.nsplit, part);
-    if (c.nsplit > 1)
-        hipLaunchKernelGGL((attn_kv8_chunk_join_kernel<HD, NT>), dim3((unsigned)(c.tiles * a.c.Hkv), K8_CHUNK_ROWS / K8_WAVES),
-                           dim3(K8_THREADS), 0, s, a, few, c.nsplit, part);
-    return hipGetLastError();
+static void k8_launch(const Kv8AttnArgs& a, const K8Plan& p, hipStream_t s) {
+    const int rowb = (int)(std::min<int64_t>((int64_t)a.max_new * a.G, 16 * p.nt) + K8_WAVES - 1) / K8_WAVES;
+    const int64_t few_joins = p.nsplit > 1 ? (int64_t)a.B * a.c.Hkv * rowb : 0;
+    if (p.tiles == 0) {
+        if (p.nt == 2)
+            k8_launch_few<HD, 2, K8_WAVES>(a, p, s);
+        else if (p.waves == K8_WAVES)
+            k8_launch_few<HD, 1, K8_WAVES>(a, p, s);
+        else
+            k8_launch_few<HD, 1, 2 * K8_WAVES>(a, p, s);
+        if (few_joins) {
+            auto f = p.nt == 2 ? attn_kv8_join_kernel<HD, 2> : attn_kv8_join_kernel<HD, 1>;
+            hipLaunchKernelGGL(f, dim3((unsigned)few_joins), dim3(K8_THREADS), 0, s, a, p.sp, p.nsplit, rowb);
+        }
+        return;
+    }
+    float* cpart = a.part + k8_few_floats(a, p);
+    const dim3 grid((unsigned)(p.tiles * a.c.Hkv * p.csplit + (int64_t)a.B * a.c.Hkv * p.nsplit));
+    auto f = a.cap > 0.0f ? attn_kv8_mixed_kernel<HD, true> : attn_kv8_mixed_kernel<HD, false>;
+    hipLaunchKernelGGL(f, grid, dim3(K8_CHUNK_THREADS), 0, s, a, p.sp, p.nsplit, (int)p.tiles, p.csplit, cpart);
+    const int64_t joins = few_joins + (p.csplit > 1 ? p.tiles * a.c.Hkv * (K8_CHUNK_ROWS / K8_WAVES) : 0);
+    if (joins)
+        hipLaunchKernelGGL(attn_kv8_mixed_join_kernel<HD>, dim3((unsigned)joins), dim3(K8_THREADS), 0, s, a, p.sp, p.nsplit,
+                           rowb, (int)p.tiles, p.csplit, cpart);
 }
 
 hipError_t launch_kv8_attention(const Kv8AttnArgs& a, hipStream_t s) {
     const K8Plan p = k8_plan(a);
-    const K8Chunks c = k8_chunks(a, p);
-    const hipError_t e = a.c.hd == 128 ? (p.nt == 1 ? k8_few<128, 1>(a, p, s) : k8_few<128, 2>(a, p, s))
-                                       : (p.nt == 1 ? k8_few<64, 1>(a, p, s) : k8_few<64, 2>(a, p, s));
-    if (e != hipSuccess || c.tiles == 0) return e;
-    return a.c.hd == 128 ? k8_chunk<128>(a, p, c, s) : k8_chunk<64>(a, p, c, s);
+    if (a.c.hd == 128)
+        k8_launch<128>(a, p, s);
+    else
+        k8_launch<64>(a, p, s);
+    return hipGetLastError();
 }
 
 }  // namespace mg
