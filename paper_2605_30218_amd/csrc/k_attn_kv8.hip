@@ -903,7 +903,8 @@ constexpr int K8_MAX_PAGES = 128;
 constexpr int K8_MAX_SPLITS = 64;
 constexpr int K8_BLOCKS_PER_CU = 2;
 constexpr int K8_WHOLE_PAGES = 32;
-constexpr int K8_CHUNK_BLOCKS_PER_CU = 2;
+constexpr int K8_MIXED_PAGES = 256;
+constexpr int K8_CHUNK_BLOCKS_PER_CU = 1;
 // pages that a group of `tokens` neighbouring tokens of a row sees at most, by the host's bounds
 static int64_t k8_pages(const Kv8AttnArgs& a, int64_t tokens) {
     int64_t len = a.max_len;
@@ -919,6 +920,7 @@ static K8Plan k8_plan(const Kv8AttnArgs& a) {
     const int64_t blocks = (int64_t)a.B * a.c.Hkv;
     const int64_t want = std::max<int64_t>(1, (K8_BLOCKS_PER_CU * a.n_cu + blocks / 2) / blocks);
     int64_t sp = std::min<int64_t>(K8_MAX_PAGES, std::max<int64_t>(K8_MIN_PAGES, (pages + want - 1) / want));
+    if (p.tiles) sp = std::min<int64_t>(K8_MIXED_PAGES, pages);
     sp = std::max(sp, (pages + K8_MAX_SPLITS - 1) / K8_MAX_SPLITS);
     p.waves = K8_WAVES;
     if (p.nt == 1 && blocks <= a.n_cu && pages <= (2 * blocks >= a.n_cu ? 2 : 1) * K8_WHOLE_PAGES) {

@@ -4,6 +4,8 @@
 // multiplying by one changes no mantissa, so a code is the nearest e4m3 value whatever the scale, a
 // growing scale moves the codes that stay in the normal range exactly, b is a byte, the largest of the bytes
 // that the tokens need is the byte that all of them need, and a value read back is exact in bf16.
+#include <type_traits>
+
 #include "mg_device.h"
 #include "mg_kernels.h"
 
@@ -17,25 +19,50 @@ constexpr int KV8_WINDOW = 16;
 constexpr int KV8_MANY = 2048;
 
 typedef float f32x2_q8 __attribute__((ext_vector_type(2)));
+typedef uint16_t u16x2_q8 __attribute__((ext_vector_type(2)));
+typedef __bf16 bf16x2_q8 __attribute__((ext_vector_type(2)));
 
-__device__ __forceinline__ bool finite_bf(uint32_t h) { return (h & 0x7f80u) != 0x7f80u; }
-// magnitude bits of the larger finite value of a bf16 pair
-__device__ __forceinline__ uint32_t top_of(uint32_t pair) {
-    const uint32_t a = pair & 0x7fffu, b = (pair >> 16) & 0x7fffu;
-    return max(a < 0x7f80u ? a : 0u, b < 0x7f80u ? b : 0u);
+// Largest magnitudes of bf16 pairs, as the pair of the two halves' maxima (bits without the sign order as
+// magnitudes do, those of infinities and NaN above all others).
+__device__ __forceinline__ uint32_t max2(uint32_t a, uint32_t b) {
+    return __builtin_bit_cast(uint32_t, __builtin_elementwise_max(__builtin_bit_cast(u16x2_q8, a), __builtin_bit_cast(u16x2_q8, b)));
+}
+__device__ __forceinline__ uint32_t mag2(uint32_t pair) { return pair & 0x7fff7fffu; }
+// the pair with 0 for what is not finite
+__device__ __forceinline__ uint32_t fin2(uint32_t pair) {
+    return pair & (((pair & 0x7f80u) != 0x7f80u ? 0xffffu : 0u) | ((pair & 0x7f800000u) != 0x7f800000u ? 0xffff0000u : 0u));
 }
 // scale byte that a finite magnitude (bf16 bits without the sign) needs: 448 = 1.75 * 2^8
 __device__ __forceinline__ int need_byte(uint32_t mag) {
     const int b = (int)(mag >> 7) - 8 + ((mag & 0x7fu) > 0x60u);
     return max(b, KV8_MIN_BYTE);
 }
-// four bf16 values (two pairs) as codes: inv = 2^(127 - b)
+// four finite bf16 values (two pairs) as codes: inv = 2^(127 - b)
 __device__ __forceinline__ uint32_t quant4(uint32_t lo, uint32_t hi, float inv) {
-    int w = __builtin_amdgcn_cvt_pk_fp8_f32(finite_bf(lo) ? bf_lo(lo) * inv : 0.0f, finite_bf(lo >> 16) ? bf_hi(lo) * inv : 0.0f, 0, false);
-    w = __builtin_amdgcn_cvt_pk_fp8_f32(finite_bf(hi) ? bf_lo(hi) * inv : 0.0f, finite_bf(hi >> 16) ? bf_hi(hi) * inv : 0.0f, w, true);
-    return (uint32_t)w | (finite_bf(lo) ? 0u : 0x7fu) | (finite_bf(lo >> 16) ? 0u : 0x7f00u) |
-           (finite_bf(hi) ? 0u : 0x7f0000u) | (finite_bf(hi >> 16) ? 0u : 0x7f000000u);
+    const int w = __builtin_amdgcn_cvt_pk_fp8_f32(bf_lo(lo) * inv, bf_hi(lo) * inv, 0, false);
+    return (uint32_t)__builtin_amdgcn_cvt_pk_fp8_f32(bf_lo(hi) * inv, bf_hi(hi) * inv, w, true);
 }
+// NaN codes of those that are not finite
+__device__ __forceinline__ uint32_t nan4(uint32_t lo, uint32_t hi) {
+    const uint32_t a = mag2(lo), b = mag2(hi);
+    return ((a & 0xffffu) >= 0x7f80u ? 0x7fu : 0u) | (a >= 0x7f800000u ? 0x7f00u : 0u) |
+           ((b & 0xffffu) >= 0x7f80u ? 0x7f0000u : 0u) | (b >= 0x7f800000u ? 0x7f000000u : 0u);
+}
+// four bf16 values as codes; ODD: some value of the wave's is not finite, and becomes NaN
+template <bool ODD>
+__device__ __forceinline__ uint32_t codes4(uint32_t lo, uint32_t hi, float inv) {
+    return ODD ? quant4(fin2(lo), fin2(hi), inv) | nan4(lo, hi) : quant4(lo, hi, inv);
+}
+// Per-lane maxima of K's and V's pairs as one pair over `lanes` lanes: K's in the low half, V's in the high
+template <int LANES>
+__device__ __forceinline__ uint32_t tops(uint32_t k, uint32_t v) {
+    const uint32_t kt = max(k & 0xffffu, k >> 16), vt = max(v & 0xffffu, v >> 16);
+    uint32_t t = kt | vt << 16;
+#pragma unroll
+    for (int x = LANES / 2; x >= 1; x >>= 1) t = max2(t, (uint32_t)__shfl_xor((int)t, x, 64));
+    return t;
+}
+__device__ __forceinline__ bool not_finite(uint32_t t) { return (t & 0xffffu) >= 0x7f80u || t >= 0x7f800000u; }
 // four codes of one scale as codes of a larger one (shift = 2^(old - new))
 __device__ __forceinline__ uint32_t requant4(uint32_t c, float shift) {
     const f32x2_q8 a = __builtin_amdgcn_cvt_pk_f32_fp8((int)c, false), b = __builtin_amdgcn_cvt_pk_f32_fp8((int)c, true);
@@ -86,25 +113,26 @@ __device__ __forceinline__ void append_run(const Kv8& c, int t0, int s0, int o, 
             old[1][h] = *reinterpret_cast<const uint4*>(page + (H + h) * 1024 + lane * 16);
         }
     }
-    uint32_t tk = 0, tv = 0;
+    auto maxima = [&](auto f) {
+        uint32_t mk = 0, mv = 0;
 #pragma unroll
-    for (int h = 0; h < H; ++h) {
+        for (int h = 0; h < H; ++h)
 #pragma unroll
-        for (int e = 0; e < 2; ++e) {
-            tk = max(max(tk, max(top_of(kx[h][e].x), top_of(kx[h][e].y))), max(top_of(kx[h][e].z), top_of(kx[h][e].w)));
+            for (int e = 0; e < 2; ++e) {
+                mk = max2(mk, max2(max2(mag2(f(kx[h][e].x)), mag2(f(kx[h][e].y))), max2(mag2(f(kx[h][e].z)), mag2(f(kx[h][e].w)))));
 #pragma unroll
-            for (int q = 0; q < 4; ++q) tv = max(tv, top_of(vx[h][q][e]));
-        }
-    }
-#pragma unroll
-    for (int x = 32; x >= 1; x >>= 1) {
-        tk = max(tk, (uint32_t)__shfl_xor((int)tk, x, 64));
-        tv = max(tv, (uint32_t)__shfl_xor((int)tv, x, 64));
-    }
+                for (int q = 0; q < 4; ++q) mv = max2(mv, mag2(f(vx[h][q][e])));
+            }
+        return tops<64>(mk, mv);
+    };
+    uint32_t top = maxima([](uint32_t x) { return x; });
+    const bool odd = not_finite(top);
+    if (odd) top = maxima([](uint32_t x) { return fin2(x); });
+    auto store = [&](auto is_odd) {
 #pragma unroll
     for (int side = 0; side < 2; ++side) {
         const int was = (int)(side ? ob >> 8 : ob & 0xffu);  // 0: the page starts anew
-        const int b = max(was, need_byte(side ? tv : tk));
+        const int b = max(was, need_byte(side ? top >> 16 : top & 0xffffu));
         const float inv = __uint_as_float((uint32_t)(254 - b) << 23);
         const float shift = __uint_as_float((uint32_t)max(127 + was - b, 0) << 23);
         // positions of this lane's pieces that the run writes, as a byte mask of a word of V or all of K's piece
@@ -119,9 +147,9 @@ __device__ __forceinline__ void append_run(const Kv8& c, int t0, int s0, int o, 
 #pragma unroll
             for (int q = 0; q < 4; ++q) {
                 if (side)
-                    nw[q] = quant4(vx[h][q][0], vx[h][q][1], inv);
+                    nw[q] = codes4<decltype(is_odd)::value>(vx[h][q][0], vx[h][q][1], inv);
                 else
-                    nw[q] = quant4(q & 1 ? kx[h][q >> 1].z : kx[h][q >> 1].x, q & 1 ? kx[h][q >> 1].w : kx[h][q >> 1].y, inv);
+                    nw[q] = codes4<decltype(is_odd)::value>(q & 1 ? kx[h][q >> 1].z : kx[h][q >> 1].x, q & 1 ? kx[h][q >> 1].w : kx[h][q >> 1].y, inv);
                 const uint32_t kept = was == 0 ? 0u : b != was ? requant4(ow[q], shift) : ow[q];
                 nw[q] = (nw[q] & ~keep) | (kept & keep);
             }
@@ -129,6 +157,11 @@ __device__ __forceinline__ void append_run(const Kv8& c, int t0, int s0, int o, 
         }
         if (lane == 0 && b != was) c.scales[ph + side] = (uint8_t)b;
     }
+    };
+    if (odd)
+        store(std::true_type{});
+    else
+        store(std::false_type{});
 }
 
 // Up to four runs of one token each, 16 lanes a run: position sl of the lane's run (-1: none), its token t, KV head h0.
@@ -156,16 +189,22 @@ __device__ __forceinline__ void append_singles(const Kv8& c, int t, int sl, int 
         }
         if (o) ob = *reinterpret_cast<const uint16_t*>(c.scales + ph);
     }
+    auto maxima = [&](auto f) {
+        uint32_t m[2] = {0, 0};
+#pragma unroll
+        for (int side = 0; side < 2; ++side)
+#pragma unroll
+            for (int i = 0; i < F / 2; ++i) m[side] = max2(m[side], mag2(f(x[side][i])));
+        return tops<16>(m[0], m[1]);
+    };
+    uint32_t top = maxima([](uint32_t v) { return v; });
+    const bool odd = __any(not_finite(top));
+    if (odd) top = maxima([](uint32_t v) { return fin2(v); });
     int b[2];
 #pragma unroll
     for (int side = 0; side < 2; ++side) {
-        uint32_t top = 0;
-#pragma unroll
-        for (int i = 0; i < F / 2; ++i) top = max(top, top_of(x[side][i]));
-#pragma unroll
-        for (int e = 8; e >= 1; e >>= 1) top = max(top, (uint32_t)__shfl_xor((int)top, e, 64));
         const int was = (int)(side ? ob >> 8 : ob & 0xffu);
-        b[side] = max(was, need_byte(top));
+        b[side] = max(was, need_byte(side ? top >> 16 : top & 0xffffu));
         unsigned long long grows = __ballot(live && b[side] != was && m == 0);
         if (grows) {
             while (grows) {
@@ -194,8 +233,8 @@ __device__ __forceinline__ void append_singles(const Kv8& c, int t, int sl, int 
     uint8_t* kd = page + ((m * F / 16) * 16 + o) * 16 + m * F % 16;
 #pragma unroll
     for (int i = 0; i < F / 4; ++i) {
-        reinterpret_cast<uint32_t*>(kd)[i] = quant4(x[0][2 * i], x[0][2 * i + 1], ik);
-        const uint32_t q = quant4(x[1][2 * i], x[1][2 * i + 1], iv);
+        reinterpret_cast<uint32_t*>(kd)[i] = odd ? codes4<true>(x[0][2 * i], x[0][2 * i + 1], ik) : codes4<false>(x[0][2 * i], x[0][2 * i + 1], ik);
+        const uint32_t q = odd ? codes4<true>(x[1][2 * i], x[1][2 * i + 1], iv) : codes4<false>(x[1][2 * i], x[1][2 * i + 1], iv);
 #pragma unroll
         for (int e = 0; e < 4; ++e) {
             const int d = m * F + 4 * i + e;
@@ -259,6 +298,11 @@ hipError_t launch_kv8_append(const Kv8& c, int n, const uint16_t* k, int64_t ks,
     return hipGetLastError();
 }
 
+// two of a word's codes times 2^(b - 127) (the float f) as a bf16 pair, exact
+template <bool HI>
+__device__ __forceinline__ uint32_t value2(uint32_t w, float f) {
+    return __builtin_bit_cast(uint32_t, (bf16x2_q8)__builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(w, f, HI));
+}
 // One wave per (four slots of the list, KV head), 16 lanes a slot.  K: lane m has the 16-byte piece of features
 // 16 m ..; V: lane m the pieces of features 16 c + m, whose words hold four positions (the four slots of a
 // wave mostly), of which it takes its own.
@@ -288,11 +332,7 @@ __global__ __launch_bounds__(256) void kv8_read_kernel(Kv8 c, int n, const int32
         const uint32_t q[4] = {kp.x, kp.y, kp.z, kp.w};
         uint32_t o[8];
 #pragma unroll
-        for (int e = 0; e < 4; ++e) {
-            const f32x2_q8 a = __builtin_amdgcn_cvt_pk_f32_fp8((int)q[e], false), b = __builtin_amdgcn_cvt_pk_f32_fp8((int)q[e], true);
-            o[2 * e] = pack_bf2(a.x * f, a.y * f);
-            o[2 * e + 1] = pack_bf2(b.x * f, b.y * f);
-        }
+        for (int e = 0; e < 8; ++e) o[e] = e & 1 ? value2<true>(q[e >> 1], f) : value2<false>(q[e >> 1], f);
         uint4* out = reinterpret_cast<uint4*>(k + i * ks + (size_t)h0 * HD + 16 * m);
         out[0] = make_uint4(o[0], o[1], o[2], o[3]);
         out[1] = make_uint4(o[4], o[5], o[6], o[7]);
@@ -300,12 +340,15 @@ __global__ __launch_bounds__(256) void kv8_read_kernel(Kv8 c, int n, const int32
     if (v) {
         const float f = __uint_as_float((sc >> 8) << 23);
         uint16_t* out = v + i * vs + (size_t)h0 * HD + m;
+        const uint32_t pick = (t & 3) * 0x0101u + 0x0400u;  // byte t % 4 of two words
 #pragma unroll
         for (int h = 0; h < H; ++h) {
-            const uint32_t q[4] = {vp[h].x, vp[h].y, vp[h].z, vp[h].w};
-#pragma unroll
-            for (int e = 0; e < 4; ++e)
-                out[64 * h + 16 * e] = (uint16_t)f2bf(__builtin_amdgcn_cvt_f32_fp8((int)(q[e] >> (8 * (t & 3))), 0) * f);
+            const uint32_t w = __builtin_amdgcn_perm(vp[h].y, vp[h].x, pick) & 0xffffu | __builtin_amdgcn_perm(vp[h].w, vp[h].z, pick) << 16;
+            const uint32_t lo = value2<false>(w, f), hi = value2<true>(w, f);
+            out[64 * h] = (uint16_t)lo;
+            out[64 * h + 16] = (uint16_t)(lo >> 16);
+            out[64 * h + 32] = (uint16_t)hi;
+            out[64 * h + 48] = (uint16_t)(hi >> 16);
         }
     }
 }
