@@ -271,7 +271,8 @@ mg_status mg_batch_plan(int B, int max_pages_per_row, const int32_t* ctx_len, co
  * A code is the nearest e4m3 value, ties to even; a value that is not finite becomes NaN.  The
  * outcome depends neither on the split of a page's tokens over calls nor on the launch, except
  * where a value falls below its scale's normal range (2^-6) and is rounded again as it grows.
- * k, v 16-byte aligned [device], strides multiples of 8 and >= Hkv * hd. */
+ * k, v 16-byte aligned [device], strides multiples of 8 and >= Hkv * hd; at most 2^26 (token, KV
+ * head) pairs a call. */
 mg_status mg_kv8_append(const mg_kv8_cache* cache, int n_tokens, const uint16_t* k, int64_t k_stride,
                         const uint16_t* v, int64_t v_stride, const int32_t* slots, void* stream);
 
@@ -291,8 +292,10 @@ mg_status mg_kv8_read(const mg_kv8_cache* cache, int n, const int32_t* slots, ui
  * token that sees nothing gets zeros.  A NaN in a position that a token does not see has no effect
  * on it.  Query head h reads KV head h / (Hq / Hkv).  Rows without tokens and rows of out behind
  * the last token are left as they were.
- * Sums are fp32; a probability enters the product with V as two bf16 terms (16 bits) where a row
- * has few query rows, and as one (8 bits, as V's own rounding point) in longer chunks. */
+ * Sums are fp32; a probability enters the product with V as two bf16 terms (16 bits) where a row has
+ * few query rows (tokens times query heads of a KV head: up to 16, or 32 where no row of the call has
+ * more), and as one (8 bits, as an output's) in longer chunks.  Calls whose launch would pass 2^22 blocks
+ * (some millions of rows, or of tokens) are refused: MG_ERR_ARG. */
 typedef struct {
     int32_t n_rows, n_tokens;
     int32_t n_q_heads;         /* a multiple of n_kv_heads, at most 16 times it */
@@ -300,7 +303,7 @@ typedef struct {
     int32_t max_len;           /* host bound on lens, for the launch's shape only (0: the page table's capacity) */
     int32_t max_pages_per_row; /* page-table row stride */
     int32_t window;            /* 0: every earlier position */
-    float scale;               /* 0: 1 / sqrt(head_dim) */
+    float scale;               /* 0: 1 / sqrt(head_dim); else at least 1e-30 */
     float softcap;             /* 0: none */
     const uint16_t* q;         /* [device] bf16 [n_tokens][Hq][hd], token stride q_stride values */
     int64_t q_stride;

@@ -980,6 +980,13 @@ static void k8_launch(const Kv8AttnArgs& a, const K8Plan& p, hipStream_t s) {
                            rowb, (int)p.tiles, p.csplit, cpart);
 }
 
+bool kv8_attention_fits(const Kv8AttnArgs& a) {
+    const K8Plan p = k8_plan(a);
+    constexpr int64_t most = 1 << 22;  // blocks of a launch
+    return p.tiles <= most && p.tiles * a.c.Hkv * p.csplit <= most && (int64_t)a.B * a.c.Hkv * p.nsplit <= most &&
+           (int64_t)a.B * a.c.Hkv * 8 + p.tiles * a.c.Hkv * (p.csplit > 1 ? K8_CHUNK_ROWS / K8_WAVES : 0) <= 2 * most;
+}
+
 hipError_t launch_kv8_attention(const Kv8AttnArgs& a, hipStream_t s) {
     const K8Plan p = k8_plan(a);
     if (a.c.hd == 128)

@@ -49,7 +49,8 @@ mg_status attn_args(const mg_kv8_cache* c, const mg_kv8_attn_args* g, Kv8AttnArg
         return MG_ERR_ARG;
     if (g->n_q_heads <= 0 || g->n_q_heads % c->n_kv_heads || g->n_q_heads / c->n_kv_heads > 16) return MG_ERR_SHAPE;
     if (g->max_new < 1 || g->max_len < 0 || g->window < 0) return MG_ERR_ARG;
-    if (!(g->scale >= 0.0f) || isinf(g->scale) || !(g->softcap >= 0.0f) || isinf(g->softcap)) return MG_ERR_ARG;
+    if (g->scale != 0.0f && !(g->scale >= 1e-30f)) return MG_ERR_ARG;
+    if (isinf(g->scale) || !(g->softcap >= 0.0f) || isinf(g->softcap)) return MG_ERR_ARG;
     if (g->softcap > 0.0f && isinf(1.0f / g->softcap)) return MG_ERR_ARG;
     const int64_t width = (int64_t)g->n_q_heads * c->head_dim;
     if (g->n_rows && g->n_tokens &&
@@ -79,6 +80,7 @@ mg_status attn_args(const mg_kv8_cache* c, const mg_kv8_attn_args* g, Kv8AttnArg
     a->cu_new = g->cu_new;
     a->n_cu = cu_count();
     a->part = nullptr;
+    if (a->B && a->T && !kv8_attention_fits(*a)) return MG_ERR_ARG;
     return MG_OK;
 }
 
@@ -113,7 +115,7 @@ mg_status mg_kv8_append(const mg_kv8_cache* cache, int n_tokens, const uint16_t*
                         const uint16_t* v, int64_t v_stride, const int32_t* slots, void* stream) {
     const mg_status st = cache_status(cache);
     if (st != MG_OK) return st;
-    if (n_tokens < 0) return MG_ERR_ARG;
+    if (n_tokens < 0 || (int64_t)n_tokens * cache->n_kv_heads > KV8_MOST_PAIRS) return MG_ERR_ARG;
     if (n_tokens == 0) return MG_OK;
     if (!k || !v || !slots || !rows_ok(cache, k, k_stride) || !rows_ok(cache, v, v_stride)) return MG_ERR_ARG;
     return status_of(launch_kv8_append(view(cache), n_tokens, k, k_stride, v, v_stride, slots,
@@ -124,7 +126,7 @@ mg_status mg_kv8_read(const mg_kv8_cache* cache, int n, const int32_t* slots, ui
                       uint16_t* v, int64_t v_stride, void* stream) {
     const mg_status st = cache_status(cache);
     if (st != MG_OK) return st;
-    if (n < 0) return MG_ERR_ARG;
+    if (n < 0 || (int64_t)n * cache->n_kv_heads > KV8_MOST_PAIRS) return MG_ERR_ARG;
     if (n == 0 || (!k && !v)) return MG_OK;
     if (!slots || (k && !rows_ok(cache, k, k_stride)) || (v && !rows_ok(cache, v, v_stride))) return MG_ERR_ARG;
     return status_of(launch_kv8_read(view(cache), n, slots, k, k_stride, v, v_stride,

@@ -221,6 +221,7 @@ struct PlanArgs {
 constexpr int PLAN_MAXB = 1024;
 hipError_t launch_batch_plan(const PlanArgs& a, hipStream_t s);
 // append and read (k_kv8.hip); strides in values
+constexpr int64_t KV8_MOST_PAIRS = 1 << 26;  // (token, KV head) pairs of a call
 hipError_t launch_kv8_append(const Kv8& c, int n, const uint16_t* k, int64_t ks, const uint16_t* v, int64_t vs,
                              const int32_t* slots, hipStream_t s);
 hipError_t launch_kv8_read(const Kv8& c, int n, const int32_t* slots, uint16_t* k, int64_t ks, uint16_t* v, int64_t vs,
@@ -240,6 +241,7 @@ struct Kv8AttnArgs {
     float* part;                // split partials (kv8_attention_ws_bytes)
 };
 size_t kv8_attention_ws_bytes(const Kv8AttnArgs& a);
+bool kv8_attention_fits(const Kv8AttnArgs& a);  // whether its launches are within the grid limits
 hipError_t launch_kv8_attention(const Kv8AttnArgs& a, hipStream_t s);
 
 // element-wise numerics probes used by the tests

@@ -48,7 +48,7 @@ def test_caches_that_are_refused(kw, rc):
 def test_rows_that_are_refused():
     lib, c = mg.load(), cache()
     ok = [1, P, 128, P, 128, P, None]
-    for i, bad in ((0, -1), (1, None), (1, P + 2), (2, 120), (2, 132), (2, -128), (3, None), (3, P + 8), (4, 0), (5, None)):
+    for i, bad in ((0, -1), (0, (1 << 25) + 1), (1, None), (1, P + 2), (2, 120), (2, 132), (2, -128), (3, None), (3, P + 8), (4, 0), (5, None)):
         assert lib.mg_kv8_append(C.byref(c), *[bad if k == i else x for k, x in enumerate(ok)]) == ARG, (i, bad)
     ok = [1, P, P, 128, P, 128, None]
     for i, bad in ((0, -1), (1, None), (2, P + 4), (3, 64), (4, P + 2), (5, 130)):
@@ -64,7 +64,8 @@ def test_rows_that_are_refused():
     (dict(n_rows=-1), ARG), (dict(n_tokens=-1), ARG), (dict(n_q_heads=5), SHAPE), (dict(n_q_heads=0), SHAPE),
     (dict(n_q_heads=34, q_stride=34 * 64, out_stride=34 * 64), SHAPE), (dict(max_new=0), ARG), (dict(max_len=-1), ARG),
     (dict(max_pages_per_row=0), ARG), (dict(max_pages_per_row=1 << 27), ARG), (dict(window=-1), ARG),
-    (dict(scale=-1.0), ARG), (dict(scale=math.nan), ARG), (dict(scale=math.inf), ARG), (dict(softcap=-2.0), ARG),
+    (dict(scale=-1.0), ARG), (dict(scale=1e-38), ARG), (dict(n_rows=1 << 30, n_tokens=1 << 30), ARG),
+    (dict(n_tokens=1 << 30, max_new=1 << 30), ARG), (dict(scale=math.nan), ARG), (dict(scale=math.inf), ARG), (dict(softcap=-2.0), ARG),
     (dict(softcap=math.nan), ARG), (dict(softcap=math.inf), ARG), (dict(softcap=1e-40), ARG), (dict(q=None), ARG),
     (dict(q=P + 2), ARG), (dict(q_stride=255), ARG), (dict(q_stride=248), ARG), (dict(out=None), ARG),
     (dict(out=P + 8), ARG), (dict(out_stride=260), ARG), (dict(page_table=None), ARG), (dict(lens=None), ARG),
@@ -73,6 +74,24 @@ def test_attention_arguments_that_are_refused(kw, rc):
     lib, c, a = mg.load(), cache(), attn(**kw)
     assert lib.mg_kv8_attention(C.byref(c), C.byref(a), P, 1 << 40, None) == rc
     assert lib.mg_kv8_attention_workspace_bytes(C.byref(c), C.byref(a)) == 0
+
+
+def test_workspace_follows_the_host_bounds():
+    """Splits are taken where rows are few and long, and a bound on the lengths saves them."""
+    lib = mg.load()
+    c = cache(n_pages=1 << 20, hkv=8, hd=128)
+
+    def need(**kw):
+        d = dict(n_rows=1, n_tokens=1, n_q_heads=32, max_new=1, max_pages_per_row=1024, q_stride=4096, out_stride=4096) | kw
+        return lib.mg_kv8_attention_workspace_bytes(C.byref(c), C.byref(attn(**d)))
+
+    assert need(max_len=512) == 0
+    one = need()
+    assert 0 < one < 64 << 20 and need(max_len=4096) <= one
+    assert need(window=256) == 0
+    assert need(n_rows=256, n_tokens=256, max_len=1024) == 0
+    assert 0 < need(n_tokens=64, max_new=64) < 256 << 20
+    assert need(n_tokens=8192, max_new=8192, max_len=2048) == 0
 
 
 def test_attention_of_nothing():
