@@ -223,7 +223,8 @@ mg_status mg_advance(mg_ctx* ctx, int B, const int32_t* emitted, int32_t* tokens
  * that a wave reads matrix operands as contiguous 1 KiB runs:
  *   K: position t, feature d = 64 h + 16 g + j at byte ((h * 4 + g) * 16 + t) * 16 + j
  *   V: position t = 4 g + i, feature d = 64 h + 16 c + m at byte ((h * 4 + g) * 16 + m) * 16 + 4 c + i
- * A value read back is exact in bf16.  A zeroed pool is an empty cache. */
+ * A value read back is exact in bf16 (but for codes that stand for 2^128, which finite values above
+ * 1.9375 * 2^127 round to: infinity).  A zeroed pool is an empty cache. */
 typedef struct {
     uint8_t* codes;   /* [device], 16-byte aligned */
     uint8_t* scales;  /* [device], 2-byte aligned */
@@ -261,8 +262,8 @@ mg_status mg_batch_plan(int B, int max_pages_per_row, const int32_t* ctx_len, co
 /* Quantises the K (after RoPE) and V rows of n_tokens tokens into the cache.  Token t's row is
  * k + t * k_stride values (bf16 [Hkv][hd]; likewise v) and goes to slots[t]; a slot outside the
  * cache (the plan's -1) is skipped.  Tokens of one page must stand together, in ascending slots
- * without gaps (as the plan lists them); a page that two separate runs of one call write ends
- * with one of them.  For a page and head, with need = the least b in [16, 254] with
+ * without gaps (as the plan lists them): of a page that two separate runs of one call write, the same
+ * slot twice among them, the content is undefined (of no other page).  For a page and head, with need = the least b in [16, 254] with
  * amax <= 448 * 2^(b - 127) over the finite values that the call writes there:
  *   - a run that begins at the page's position 0, or a page whose scale is 0, starts anew: scale =
  *     need, the page's other positions become 0;
@@ -294,17 +295,18 @@ mg_status mg_kv8_read(const mg_kv8_cache* cache, int n, const int32_t* slots, ui
  * the last token are left as they were.
  * Sums are fp32; a probability enters the product with V as two bf16 terms (16 bits) where a row has
  * few query rows (tokens times query heads of a KV head: up to 16, or 32 where no row of the call has
- * more), and as one (8 bits, as an output's) in longer chunks.  Calls whose launch would pass 2^22 blocks
- * (some millions of rows, or of tokens) are refused: MG_ERR_ARG. */
+ * more), and as one (8 bits, as an output's) in longer chunks.  The order of a row's sums follows the
+ * call's shape (rows, tokens, bounds) and the lengths, so the same call gives the same bits.  Calls whose
+ * launch would pass 2^22 blocks (some millions of rows, or of tokens) are refused: MG_ERR_ARG. */
 typedef struct {
     int32_t n_rows, n_tokens;
     int32_t n_q_heads;         /* a multiple of n_kv_heads, at most 16 times it */
     int32_t max_new;           /* at least the most tokens of any row (a row with more is the caller's error) */
     int32_t max_len;           /* host bound on lens, for the launch's shape only (0: the page table's capacity) */
-    int32_t max_pages_per_row; /* page-table row stride */
+    int32_t max_pages_per_row; /* page-table row stride, 1..2^26 */
     int32_t window;            /* 0: every earlier position */
-    float scale;               /* 0: 1 / sqrt(head_dim); else at least 1e-30 */
-    float softcap;             /* 0: none */
+    float scale;               /* 0: 1 / sqrt(head_dim); else 1e-15 .. 1e15 */
+    float softcap;             /* 0: none; else 1e-15 .. 1e15 */
     const uint16_t* q;         /* [device] bf16 [n_tokens][Hq][hd], token stride q_stride values */
     int64_t q_stride;
     uint16_t* out;             /* [device] as q, token stride out_stride; must not overlap q */

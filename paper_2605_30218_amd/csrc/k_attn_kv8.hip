@@ -61,12 +61,13 @@ struct K8Row {
     int len, p0;    // positions in reach of the page table; position of its first token
     int pga, pgb;   // pages that any of its tokens sees: [pga, pgb)
 };
+__device__ __forceinline__ int k8_token(const Kv8AttnArgs& a, int t) { return min(max(t, 0), a.T); }
 __device__ __forceinline__ K8Row k8_row(const Kv8AttnArgs& a, int r) {
     K8Row x;
-    x.t0 = a.cu_new ? min(max(a.cu_new[r], 0), a.T) : r;
-    x.n = (a.cu_new ? min(a.cu_new[r + 1], a.T) : r + 1) - x.t0;
-    const int len = a.lens[r];
-    x.len = min(max(len, 0), 16 * a.maxp);
+    x.t0 = a.cu_new ? k8_token(a, a.cu_new[r]) : r;
+    x.n = (a.cu_new ? k8_token(a, a.cu_new[r + 1]) : r + 1) - x.t0;
+    const int len = max(a.lens[r], 0);
+    x.len = min(len, 16 * a.maxp);
     x.p0 = len - x.n;
     x.pga = a.window ? max(0, min(x.p0 - a.window + 1, x.len)) / 16 : 0;
     x.pgb = (x.len + 15) / 16;
@@ -100,7 +101,7 @@ struct K8Acc {
         }
     }
 };
-// what the kernels derive from the scale and the cap: the exponent is x * f with x a score as k8_scores
+// what the kernels derive from the scale and the cap: the exponent is x * f with x a score as k8_score
 // leaves it
 struct K8Soft {
     float f, zin, cap2;
@@ -110,15 +111,27 @@ __device__ __forceinline__ K8Soft k8_soft(const Kv8AttnArgs& a) {
                   a.cap * 1.4426950408889634f};
 }
 
-// a product q . k as a score: itself, or capped, in log2 units
-template <bool CAP>
+// A product q . k as a score: itself, or capped, in log2 units.  tanh(z) = 1 - 2 / (1 + e^2z) is off by some 2^-23 whatever z, a
+// capped score by as much of the cap: up to K8_CAP_LARGE that is 2^-16, the accuracy of a two-term probability.  Larger caps
+// take z's series to z^7 below 1/8 (2^-29 of itself off), so that one far above the scores leaves them as they are; with
+// it for every cap, 24 rows of a mixed batch with a cap took 43 us instead of 36.
+enum { K8_UNCAPPED, K8_CAPPED, K8_CAPPED_LARGE };
+constexpr float K8_CAP_LARGE = 64.0f;
+template <int CAP>
 __device__ __forceinline__ float k8_score(float s, const K8Soft& so) {
-    // tanh(z) = 1 - 2 / (1 + e^2z)
-    return CAP ? so.cap2 * (1.0f - 2.0f * __builtin_amdgcn_rcpf(1.0f + __builtin_amdgcn_exp2f(s * so.zin))) : s;
+    if (CAP == K8_UNCAPPED) return s;
+    const float z2 = s * so.zin;  // 2 log2(e) z
+    float t = 1.0f - 2.0f * __builtin_amdgcn_rcpf(1.0f + __builtin_amdgcn_exp2f(z2));
+    if (CAP == K8_CAPPED_LARGE) {
+        const float z = z2 * 0.34657359027997264f, zz = z * z;
+        const float small = z * __builtin_fmaf(zz, __builtin_fmaf(zz, __builtin_fmaf(zz, -17.0f / 315.0f, 2.0f / 15.0f), -1.0f / 3.0f), 1.0f);
+        t = zz < 1.0f / 64.0f ? small : t;
+    }
+    return so.cap2 * t;
 }
 
 // scores: x[u][4 e + i] of position 16 e + 4 g + i of the step and column c of tile u
-template <int HD, int NT, bool CAP>
+template <int HD, int NT, int CAP>
 __device__ __forceinline__ void k8_scores(const uint4 (&kb)[2][HD / 64], const float (&ksc)[2],
                                           const uint4 (&qa)[NT][HD / 32], const K8Soft& so, float (&x)[NT][8]) {
 #pragma unroll
@@ -296,7 +309,7 @@ struct K8FewShared {
     float o[WAVES][16 * NT][HD + 4];  // (padded rows)
     float m[WAVES][16 * NT], l[WAVES][16 * NT];
 };
-template <int HD, int NT, int WAVES, bool CAP>
+template <int HD, int NT, int WAVES, int CAP>
 __device__ __forceinline__ void k8_few_block(const Kv8AttnArgs& a, int sp, int nsplit, int block, K8FewShared<HD, NT, WAVES>& sh) {
     constexpr int H = HD / 64;        // 1 KiB runs of a page of K or V
     constexpr int DT = HD / 16;       // output tiles
@@ -424,7 +437,7 @@ __device__ __forceinline__ void k8_few_block(const Kv8AttnArgs& a, int sp, int n
     }
 }
 
-template <int HD, int NT, int WAVES, bool CAP>
+template <int HD, int NT, int WAVES, int CAP>
 __global__ __launch_bounds__(64 * WAVES) __attribute__((amdgpu_waves_per_eu(NT == 2 || WAVES > 4 ? 2 : 3))) void attn_kv8_few_kernel(
     Kv8AttnArgs a, int sp, int nsplit) {
     __shared__ __attribute__((aligned(16))) K8FewShared<HD, NT, WAVES> sh;
@@ -505,7 +518,7 @@ __device__ __forceinline__ K8Tile k8_tile(const Kv8AttnArgs& a, int few, int ind
     for (int b0 = 0; b0 < a.B; b0 += 64) {
         int k = 0;
         if (b0 + lane < a.B) {
-            const int rows = (a.cu_new[b0 + lane + 1] - a.cu_new[b0 + lane]) * a.G;
+            const int rows = (k8_token(a, a.cu_new[b0 + lane + 1]) - k8_token(a, a.cu_new[b0 + lane])) * a.G;
             k = rows > few ? (rows + ROWS - 1) / ROWS : 0;
         }
         int sum = k;
@@ -559,7 +572,7 @@ struct K8ChunkShared {
     uint32_t nan_at[K8_GROUPS][2][K8_STAGE][64];  // NaN codes of V: bits 4 d .. of a lane: output tile d's four positions of a page
     int nan_any[K8_GROUPS][2][K8_STAGE];
 };
-template <int HD, int NT, bool CAP>
+template <int HD, int NT, int CAP>
 __device__ __forceinline__ void k8_chunk_block(const Kv8AttnArgs& a, int few, int tiles, int nsplit, float* part, int block,
                                                K8ChunkShared<HD>& sh) {
     constexpr int H = HD / 64, DT = HD / 16;
@@ -848,7 +861,7 @@ __device__ __forceinline__ void k8_chunk_block(const Kv8AttnArgs& a, int few, in
 }
 
 // A call with longer rows: their blocks, then those of its rows of few query rows, in one launch.
-template <int HD, bool CAP>
+template <int HD, int CAP>
 __global__ __launch_bounds__(K8_CHUNK_THREADS) __attribute__((amdgpu_waves_per_eu(2))) void attn_kv8_mixed_kernel(
     Kv8AttnArgs a, int sp, int nsplit, int tiles, int csplit, float* cpart) {
     union Shared {
@@ -953,7 +966,9 @@ size_t kv8_attention_ws_bytes(const Kv8AttnArgs& a) {
 template <int HD, int NT, int WAVES>
 static void k8_launch_few(const Kv8AttnArgs& a, const K8Plan& p, hipStream_t s) {
     const dim3 grid((unsigned)((int64_t)a.B * a.c.Hkv * p.nsplit));
-    auto f = a.cap > 0.0f ? attn_kv8_few_kernel<HD, NT, WAVES, true> : attn_kv8_few_kernel<HD, NT, WAVES, false>;
+    auto f = a.cap == 0.0f             ? attn_kv8_few_kernel<HD, NT, WAVES, K8_UNCAPPED>
+             : a.cap <= K8_CAP_LARGE ? attn_kv8_few_kernel<HD, NT, WAVES, K8_CAPPED>
+                                     : attn_kv8_few_kernel<HD, NT, WAVES, K8_CAPPED_LARGE>;
     hipLaunchKernelGGL(f, grid, dim3(64 * WAVES), 0, s, a, p.sp, p.nsplit);
 }
 template <int HD>
@@ -975,7 +990,9 @@ static void k8_launch(const Kv8AttnArgs& a, const K8Plan& p, hipStream_t s) {
     }
     float* cpart = a.part + k8_few_floats(a, p);
     const dim3 grid((unsigned)(p.tiles * a.c.Hkv * p.csplit + (int64_t)a.B * a.c.Hkv * p.nsplit));
-    auto f = a.cap > 0.0f ? attn_kv8_mixed_kernel<HD, true> : attn_kv8_mixed_kernel<HD, false>;
+    auto f = a.cap == 0.0f             ? attn_kv8_mixed_kernel<HD, K8_UNCAPPED>
+             : a.cap <= K8_CAP_LARGE ? attn_kv8_mixed_kernel<HD, K8_CAPPED>
+                                     : attn_kv8_mixed_kernel<HD, K8_CAPPED_LARGE>;
     hipLaunchKernelGGL(f, grid, dim3(K8_CHUNK_THREADS), 0, s, a, p.sp, p.nsplit, (int)p.tiles, p.csplit, cpart);
     const int64_t joins = few_joins + (p.csplit > 1 ? p.tiles * a.c.Hkv * (K8_CHUNK_ROWS / K8_WAVES) : 0);
     if (joins)
@@ -986,7 +1003,7 @@ static void k8_launch(const Kv8AttnArgs& a, const K8Plan& p, hipStream_t s) {
 bool kv8_attention_fits(const Kv8AttnArgs& a) {
     const K8Plan p = k8_plan(a);
     constexpr int64_t most = 1 << 22;  // blocks of a launch
-    return p.tiles <= most && p.tiles * a.c.Hkv * p.csplit <= most && (int64_t)a.B * a.c.Hkv * p.nsplit <= most &&
+    return (int64_t)a.T * a.G <= (1 << 29) && p.tiles * a.c.Hkv * p.csplit + (int64_t)a.B * a.c.Hkv * p.nsplit <= most &&
            (int64_t)a.B * a.c.Hkv * 8 + p.tiles * a.c.Hkv * (p.csplit > 1 ? K8_CHUNK_ROWS / K8_WAVES : 0) <= 2 * most;
 }
 

@@ -45,13 +45,13 @@ int cu_count() {
 mg_status attn_args(const mg_kv8_cache* c, const mg_kv8_attn_args* g, Kv8AttnArgs* a) {
     const mg_status st = cache_status(c);
     if (st != MG_OK) return st;
-    if (!g || g->n_rows < 0 || g->n_tokens < 0 || g->max_pages_per_row <= 0 || g->max_pages_per_row >= (1 << 27))
+    if (!g || g->n_rows < 0 || g->n_tokens < 0 || g->max_pages_per_row <= 0 || g->max_pages_per_row > (1 << 26))
         return MG_ERR_ARG;
     if (g->n_q_heads <= 0 || g->n_q_heads % c->n_kv_heads || g->n_q_heads / c->n_kv_heads > 16) return MG_ERR_SHAPE;
     if (g->max_new < 1 || g->max_len < 0 || g->window < 0) return MG_ERR_ARG;
-    if (g->scale != 0.0f && !(g->scale >= 1e-30f)) return MG_ERR_ARG;
-    if (isinf(g->scale) || !(g->softcap >= 0.0f) || isinf(g->softcap)) return MG_ERR_ARG;
-    if (g->softcap > 0.0f && isinf(1.0f / g->softcap)) return MG_ERR_ARG;
+    // (outside of this range their products with each other and with log2 e leave fp32's)
+    const auto factor = [](float f) { return f >= 1e-15f && f <= 1e15f; };
+    if ((g->scale != 0.0f && !factor(g->scale)) || (g->softcap != 0.0f && !factor(g->softcap))) return MG_ERR_ARG;
     const int64_t width = (int64_t)g->n_q_heads * c->head_dim;
     if (g->n_rows && g->n_tokens &&
         (!g->q || !g->out || !g->page_table || !g->lens || !aligned(g->q, 16) || !aligned(g->out, 16)))
@@ -67,7 +67,7 @@ mg_status attn_args(const mg_kv8_cache* c, const mg_kv8_attn_args* g, Kv8AttnArg
     a->max_new = g->max_new < g->n_tokens ? g->max_new : g->n_tokens;
     a->max_len = g->max_len && g->max_len < cap ? g->max_len : (int)cap;
     a->maxp = g->max_pages_per_row;
-    a->window = g->window;
+    a->window = g->window < cap ? g->window : 0;  // (one of the whole row's length hides nothing)
     a->scale = g->scale > 0.0f ? g->scale : (float)(1.0 / sqrt((double)c->head_dim));
     a->cap = g->softcap;
     a->inv_cap = g->softcap > 0.0f ? 1.0f / g->softcap : 0.0f;

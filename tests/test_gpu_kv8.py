@@ -299,7 +299,7 @@ def test_mixed_batches_with_empty_rows(hq, hkv, hd):
     Batch(np.add(ctx, new), new, hq, hkv, hd).check()
 
 
-@pytest.mark.parametrize("window", [1, 7, 16, 100, 2000])
+@pytest.mark.parametrize("window", [1, 7, 16, 100, 2000, 2 ** 31 - 1])
 @pytest.mark.parametrize("new", [[1, 1, 1, 1], [3, 1, 2, 4], [150, 1, 90, 20]])
 def test_window(window, new):
     Batch(np.add([300, 5, 0, 1000], new), new, 8, 2, 128, seed=window).check(window=window)
@@ -311,6 +311,12 @@ def test_softcap_and_scale(cap, new):
     b = Batch(np.add([300, 5, 70], new), new, 8, 2, 64, seed=3)
     b.check(softcap=cap)
     b.check(softcap=cap, scale=0.3, window=50)
+
+
+@pytest.mark.parametrize("cap", [300.0, 1e5, 1e15])
+@pytest.mark.parametrize("new", [[1, 1, 1], [80, 1, 3]])
+def test_a_cap_far_above_the_scores(cap, new):
+    Batch(np.add([300, 5, 70], new), new, 8, 2, 64, seed=9).check(softcap=cap)
 
 
 @pytest.mark.parametrize("new", [[1, 1], [5, 1], [100, 40]])

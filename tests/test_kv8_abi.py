@@ -64,7 +64,8 @@ def test_rows_that_are_refused():
     (dict(n_rows=-1), ARG), (dict(n_tokens=-1), ARG), (dict(n_q_heads=5), SHAPE), (dict(n_q_heads=0), SHAPE),
     (dict(n_q_heads=34, q_stride=34 * 64, out_stride=34 * 64), SHAPE), (dict(max_new=0), ARG), (dict(max_len=-1), ARG),
     (dict(max_pages_per_row=0), ARG), (dict(max_pages_per_row=1 << 27), ARG), (dict(window=-1), ARG),
-    (dict(scale=-1.0), ARG), (dict(scale=1e-38), ARG), (dict(n_rows=1 << 30, n_tokens=1 << 30), ARG),
+    (dict(scale=-1.0), ARG), (dict(scale=1e-38), ARG), (dict(scale=1e16), ARG), (dict(softcap=1e16), ARG),
+    (dict(max_pages_per_row=(1 << 26) + 1), ARG), (dict(n_rows=1 << 30, n_tokens=1 << 30), ARG),
     (dict(n_tokens=1 << 30, max_new=1 << 30), ARG), (dict(scale=math.nan), ARG), (dict(scale=math.inf), ARG), (dict(softcap=-2.0), ARG),
     (dict(softcap=math.nan), ARG), (dict(softcap=math.inf), ARG), (dict(softcap=1e-40), ARG), (dict(q=None), ARG),
     (dict(q=P + 2), ARG), (dict(q_stride=255), ARG), (dict(q_stride=248), ARG), (dict(out=None), ARG),
