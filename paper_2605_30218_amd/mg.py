@@ -267,7 +267,8 @@ def margin_gate_noalloc(B, V, logits, protected_mask, tau, top1, margin, gate, g
 
 # A decode step makes these calls once a layer, and their kernels take some microseconds: the checks are
 # plain comparisons, messages are made only when one fails, and the device is switched only when
-# the tensors are on another than the current one.
+# the tensors are on another than the current one.  As with torch's own operators, tensors that a call makes
+# belong to the stream it runs on: a program that then uses them on another one waits, and records them there.
 
 BatchPlan = collections.namedtuple("BatchPlan", "cu_new lens admitted positions rows slots n_left")
 _BF16 = (torch.bfloat16, torch.int16)
@@ -305,12 +306,13 @@ def _call(name, device, stream, fn, *args):
         raise MgError(name, rc)
 
 
-def _made(t, stream):
-    """A tensor that a call took from torch's allocator, which must not reuse it before the call's
-    own stream is done with it."""
-    if stream is not None:
-        t.record_stream(stream)
-    return t
+def _new(shape, dtype, device, stream):
+    """A tensor of torch's allocator that the call's stream may write: of that stream's own memory, which
+    neither earlier work of the current one still reads nor later work takes too soon."""
+    if stream is None:
+        return torch.empty(shape, dtype=dtype, device=device)
+    with torch.cuda.stream(stream):
+        return torch.empty(shape, dtype=dtype, device=device)
 
 
 def batch_plan(ctx_len, n_new, free_pages, n_free, page_table, max_tokens, out=None, stream=None):
@@ -327,7 +329,7 @@ def batch_plan(ctx_len, n_new, free_pages, n_free, page_table, max_tokens, out=N
     args = (_ints("ctx_len", ctx_len, dev, B), _ints("n_new", n_new, dev, B), _ints("free_pages", free_pages, dev),
             _ints("n_free", n_free, dev, 1), M, _ints("page_table", page_table, dev))
     if out is None:
-        buf = _made(torch.empty(3 * M + 3 * B + 2, dtype=torch.int32, device=dev), stream)
+        buf = _new(3 * M + 3 * B + 2, torch.int32, dev, stream)
         cu, lens, adm, pos, row, slot, left = buf.split_with_sizes((B + 1, B, B, M, M, M, 1))
         out = BatchPlan(cu, lens, adm, pos, row, slot, left)
         at = buf.data_ptr()
@@ -383,9 +385,9 @@ def kv8_read(codes, scales, slots, k_out=None, v_out=None, stream=None):
     c = _kv8(codes, scales)
     dev, n = codes.device, slots.numel()
     if k_out is None:
-        k_out = _made(torch.empty((n, c.n_kv_heads, c.head_dim), dtype=torch.bfloat16, device=dev), stream)
+        k_out = _new((n, c.n_kv_heads, c.head_dim), torch.bfloat16, dev, stream)
     if v_out is None:
-        v_out = _made(torch.empty((n, c.n_kv_heads, c.head_dim), dtype=torch.bfloat16, device=dev), stream)
+        v_out = _new((n, c.n_kv_heads, c.head_dim), torch.bfloat16, dev, stream)
     kp, ks = _rows16("k_out", k_out, n, c.n_kv_heads, c.head_dim, dev)
     vp, vs = _rows16("v_out", v_out, n, c.n_kv_heads, c.head_dim, dev)
     _call("mg_kv8_read", dev, stream, load().mg_kv8_read, C.byref(c), n, _ints("slots", slots, dev), kp, ks, vp, vs)
@@ -424,12 +426,12 @@ def kv8_attention(codes, scales, q, page_table, lens, cu_new=None, max_new=1, ma
     c = _kv8(codes, scales)
     dev = codes.device
     if out is None:
-        out = _made(torch.empty(q.shape, dtype=q.dtype, device=dev), stream)
+        out = _new(q.shape, q.dtype, dev, stream)
     a = _attn_args(c, q, page_table, lens, cu_new, max_new, max_len, scale, window, softcap, out, dev)
     cp, ap, lib = C.byref(c), C.byref(a), load()
     if workspace is None:
         need = lib.mg_kv8_attention_workspace_bytes(cp, ap)
-        workspace = _made(torch.empty(need, dtype=torch.uint8, device=dev), stream) if need else None
+        workspace = _new(need, torch.uint8, dev, stream) if need else None
     elif workspace.dtype is not torch.uint8 or workspace.device != dev or not workspace.is_contiguous():
         _refuse("workspace", workspace, f"contiguous uint8 on {dev}")
     ws, n = (None, 0) if workspace is None else (workspace.data_ptr(), workspace.numel())

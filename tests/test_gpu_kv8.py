@@ -539,3 +539,25 @@ def test_two_streams_at_once():
     torch.cuda.synchronize()
     for a, o in zip(alone, outs):
         assert torch.equal(a, o)
+
+
+def test_a_call_on_a_stream_makes_its_tensors_there():
+    """The current stream's allocator hands out memory that its queued work still writes: a call on another
+    stream must not take that for its result or its workspace."""
+    b = Batch([5000, 130], [1, 1], 8, 2, 128, seed=22)
+    want = b.run()
+    args = (b.codes, b.scales, b.q.cuda(), dev_i32(b.table), dev_i32(b.lens))
+    assert mg.kv8_attention_workspace_bytes(*args) > 0
+    x = torch.zeros(2048, 2048, device="cuda")
+    s = torch.cuda.Stream()
+    torch.cuda.synchronize()
+    for _ in range(10):
+        late = torch.empty_like(want)
+        for _ in range(20):
+            x.matmul(x)
+        late.fill_(9.0)
+        del late
+        got = mg.kv8_attention(*args, stream=s)
+        torch.cuda.synchronize()
+        assert torch.equal(got, want)
+        del got
