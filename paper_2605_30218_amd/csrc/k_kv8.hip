@@ -14,9 +14,13 @@ namespace mg {
 constexpr int KV8_PAGE = 16;
 constexpr int KV8_MIN_BYTE = 16;  // 2^(16 - 127) times the least code, 2^-9, is still normal in bf16
 
-// Tokens of a wave's window where a call has more than KV8_MANY (token, KV head) pairs, else 1
-constexpr int KV8_WINDOW = 16;
-constexpr int KV8_MANY = 2048;
+// Tokens of a wave's window: 1 up to KV8_FEW (token, KV head) pairs, 8 up to KV8_SOME, 16 above.  A window of several tokens
+// does its runs one after the other (single tokens four at a time), but its waves have work where a run is long: with
+// windows of one a run of 16 is one wave's and 15 find nothing to do.  Measured at hd 128, us, windows of 1 / 8 / 16:
+// 2000 pairs in runs 6.3 / 5.4 / 7.9, in single tokens 5.8 / 6.0 / 7.9; 4096 in single tokens 7.4 / 6.5 / 8.3; 16000 in runs
+// 22 / 6.9 / 8.4; 24000 32 / 8.3 / 8.8; 32000 40 / 10.3 / 9.1; 96000 107 / 21 / 15.
+constexpr int KV8_FEW = 2048;
+constexpr int KV8_SOME = 24576;
 
 typedef float f32x2_q8 __attribute__((ext_vector_type(2)));
 typedef uint16_t u16x2_q8 __attribute__((ext_vector_type(2)));
@@ -246,11 +250,10 @@ __device__ __forceinline__ void append_singles(const Kv8& c, int t, int sl, int 
 // One wave per (window of W tokens, KV head): it does the runs that begin in its window, so one wave alone
 // writes a page of a head; with windows of several tokens four runs of one token at a time, the others one
 // after the other.
-template <int HD, bool MANY>
+template <int HD, int W>
 __global__ __launch_bounds__(256) void kv8_append_kernel(Kv8 c, int n, const uint16_t* __restrict__ k, int64_t ks,
                                                          const uint16_t* __restrict__ v, int64_t vs,
                                                          const int32_t* __restrict__ slots) {
-    constexpr int W = MANY ? KV8_WINDOW : 1;
     const int lane = threadIdx.x & 63;
     const int64_t w = (int64_t)blockIdx.x * 4 + __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
     const int64_t base = w / c.Hkv * W;
@@ -262,7 +265,7 @@ __global__ __launch_bounds__(256) void kv8_append_kernel(Kv8 c, int n, const uin
     const bool in = sl >= 0 && sl < (int64_t)c.n_pages * KV8_PAGE;
     const int before = __shfl_up(sl, 1, 64), after = __shfl_down(sl, 1, 64);
     const bool begins = lane >= 1 && lane <= W && in && (sl % KV8_PAGE == 0 || before != sl - 1);
-    const bool single = MANY && begins && (sl % KV8_PAGE == KV8_PAGE - 1 || after != sl + 1);
+    const bool single = W > 1 && begins && (sl % KV8_PAGE == KV8_PAGE - 1 || after != sl + 1);
     unsigned long long ones = __ballot(single), first = __ballot(begins && !single);
     while (ones) {
         int l0 = 0;
@@ -289,11 +292,11 @@ __global__ __launch_bounds__(256) void kv8_append_kernel(Kv8 c, int n, const uin
 
 hipError_t launch_kv8_append(const Kv8& c, int n, const uint16_t* k, int64_t ks, const uint16_t* v, int64_t vs,
                              const int32_t* slots, hipStream_t s) {
-    const bool many = (int64_t)n * c.Hkv > KV8_MANY;
-    const int W = many ? KV8_WINDOW : 1;
+    const int64_t pairs = (int64_t)n * c.Hkv;
+    const int W = pairs <= KV8_FEW ? 1 : pairs <= KV8_SOME ? 8 : 16;
     const dim3 grid((unsigned)((((int64_t)n + W - 1) / W * c.Hkv + 3) / 4));
-    auto f = c.hd == 128 ? (many ? kv8_append_kernel<128, true> : kv8_append_kernel<128, false>)
-                         : (many ? kv8_append_kernel<64, true> : kv8_append_kernel<64, false>);
+    auto f = c.hd == 128 ? (W == 1 ? kv8_append_kernel<128, 1> : W == 8 ? kv8_append_kernel<128, 8> : kv8_append_kernel<128, 16>)
+                         : (W == 1 ? kv8_append_kernel<64, 1> : W == 8 ? kv8_append_kernel<64, 8> : kv8_append_kernel<64, 16>);
     hipLaunchKernelGGL(f, grid, dim3(256), 0, s, c, n, k, ks, v, vs, slots);
     return hipGetLastError();
 }

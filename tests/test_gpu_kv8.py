@@ -139,7 +139,7 @@ def test_append_token_by_token_and_in_runs(hkv, hd, piece):
         check_append(codes, scales, k, v, slots, want)
 
 
-@pytest.mark.parametrize("hkv,hd", [(8, 128), (9, 64)])
+@pytest.mark.parametrize("hkv,hd", [(8, 128), (9, 64), (32, 64), (28, 128)])
 def test_append_of_many_requests_at_once(hkv, hd):
     """Calls of some hundred requests, most with one token, some with a few or with more than a page."""
     rng = np.random.RandomState(hkv)
