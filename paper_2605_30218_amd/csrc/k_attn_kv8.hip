@@ -1,5 +1,15 @@
-// k_attn_kv8.hip -- attention of a batch's new tokens over the 8-bit paged K/V cache: one kernel (and
-// the joining of its splits) for rows of few query rows, one for longer chunks of tokens.
+// k_attn_kv8.hip -- attention of a batch's new tokens over the 8-bit paged K/V cache.
+//
+// out = sum_j exp(s_j - m) v_j / sum_j exp(s_j - m) in one pass over the positions, with a running reference m.  Two
+// kinds of blocks, both S^T = K Q^T and O^T = V^T P^T on the matrix cores with K and V as A operands straight in the
+// order in which the cache stores a page: "few" blocks for rows of at most 16 or 32 query rows (single tokens,
+// drafts), bound by the K/V stream, split over positions and joined where rows are few; "chunk" blocks for longer rows,
+// bound by the matrix cores and the vector units together.  A call without longer rows launches few blocks, one
+// with them both kinds in one grid.
+// Measured, hd 128 (us of a call in a captured graph): 64 rows of 512..768, 32 heads over 8: 18.7 (85 MB, 4.5 TB/s);
+// 128 rows of 127..2047, 40 over 8: 60.4 (4.8 TB/s); 32 rows of 4095..16383: 122 (5.5 TB/s; a plain read of 2 GiB
+// 5.3); 23 rows of four tokens, 28 over 4: 27.5; one prompt of 2001, 28 over 4: 50 (580 TFLOP/s); 4 chunks of 2048 behind
+// up to 6144: 579 (950 TFLOP/s; a library's product of 8192^3: 1390).
 #include <algorithm>
 
 #include "mg_device.h"
@@ -303,7 +313,10 @@ __device__ __forceinline__ void k8_query(const Kv8AttnArgs& a, const K8Row& row,
 
 // Rows of few query rows (tokens times query heads of a KV head <= 16 NT): one block per (row, KV head,
 // split of the row's pages), a wave taking every WAVES-th step of its pages.  The K/V stream
-// bounds it, so the matrix cores have the time for two terms of a probability.
+// bounds it, so the matrix cores have the time for two terms of a probability.  K's registers are loaded again as
+// soon as the scores are there, V's after its product, so that a wave has a step in flight at any time.  Pages are read once:
+// loads that leave no trace in the caches (32 rows of 4096..16384: 138 -> 122 us, 128 ragged rows 67.7 -> 60.4; only
+// what the memory-side cache still holds from the call before is slower, 64 MB of 23 rows 26.0 -> 27.5).
 template <int HD, int NT, int WAVES>
 struct K8FewShared {
     float o[WAVES][16 * NT][HD + 4];  // (padded rows)
@@ -556,7 +569,9 @@ __device__ __forceinline__ K8Span k8_span(const Kv8AttnArgs& a, const K8Row& row
 }
 
 // Rows of more query rows: one block of 8 waves per (row, KV head, 64 NT query rows, split of the positions that these see),
-// the tokens of a row's end first (they see the most).  The waves form two groups of four; a wave holds NT
+// the tokens of a row's end first (they see the most).  Bound by the matrix cores (37 % busy) and the vector units (47 %),
+// which hardly work at once: a product of 16x16x32 alone takes 20.6 cycles, with four vector instructions beside it most of
+// their sum, from two waves as from one.  The waves form two groups of four; a wave holds NT
 // tiles of query rows, the same in both groups, and each group takes half of the block's positions in stages of 4
 // pages, which go through a double buffer of the group's in LDS as bf16 matrix operands: a wave fetches and
 // converts one page, so that a code is converted once a group and an operand is one read for NT products.  The
@@ -900,15 +915,23 @@ __global__ __launch_bounds__(K8_THREADS) void attn_kv8_mixed_join_kernel(Kv8Attn
     k8_join<HD>(cpart + first * HD, (size_t)ROWS * HD, ml + 2 * first, 2 * ROWS, act, k8_out(a, row, kh, rr));
 }
 
-// The launch of rows of few query rows: tiles and waves of a block, pages of a split, splits of a row.
-// Measured on graphs of calls, 32 query heads over 8 KV heads of 128, us:
-//   - rows are split until two blocks a CU are there (three: 64 rows of 512..768, 512 blocks without a split,
-//     18 -> 24, as the join is a launch of its own; 23 rows of four tokens 25 -> 31);
+// The launch.  Measured on graphs of calls, 32 query heads over 8 KV heads of 128 where nothing else is said, us.
+// Calls of rows of few query rows:
+//   - rows are split until two blocks a CU are there (one: 23 rows of four tokens, 28 heads over 4, 27.9 -> 34.8; three: 64
+//     rows of 512..768, 512 blocks without a split, 18.9 -> 24.1, as the join is a launch of its own; four: 23 rows
+//     of four tokens 34.3, 40 rows of three 44.9 -> 40.7);
 //   - a split takes at most 128 pages (64: 32 rows of 4096..16384 122 -> 125, 128 ragged rows 60.4 -> 59.2;
 //     256: 122 -> 134);
 //   - where the blocks of unsplit rows fit the device at once and a row has few pages, one block of 8
 //     waves takes a row whole: one row of 512 7.1 -> 6.3, 32 rows of 512 12.1 -> 9.8; at 64 pages one row
 //     7.9 -> 9.7, but 32 rows 17.0 -> 14.7, so up to 32 pages, or 64 where the blocks are half of the CUs.
+// Calls with longer rows:
+//   - a row of few query rows is split at 256 pages, beside the chunks' blocks, which take as long (64: 8 rows of
+//     16000 beside a chunk of 512 57.8 -> 63.5, 30 of 4000 55.4 -> 63.2; no split: 103, 55.2), at 128 where
+//     these rows' blocks are an eighth of the CUs (a row of 16000 beside two chunks of 64 tokens 35.7 -> 26.2);
+//   - a tile of a chunk is split over its positions until there is a block a CU (two: one chunk of 64 behind 16000
+//     tokens 45.9 -> 55.1, one of 512 behind 512 27.0 -> 45.1, no call faster: a CU holds one block, and the splits'
+//     outputs are written and read), down to 4 stages a split (2: no difference; 8: 4 chunks of 2048 579 -> 600).
 struct K8Plan {
     int nt, waves, sp, nsplit;  // rows of few query rows: tiles and waves of a block, pages of a split, splits of a row
     int64_t tiles;              // of 128 query rows, of the longer rows: at most (a row's last may be partly empty); 0: none
@@ -936,7 +959,7 @@ static K8Plan k8_plan(const Kv8AttnArgs& a) {
     const int64_t blocks = (int64_t)a.B * a.c.Hkv;
     const int64_t want = std::max<int64_t>(1, (K8_BLOCKS_PER_CU * a.n_cu + blocks / 2) / blocks);
     int64_t sp = std::min<int64_t>(K8_MAX_PAGES, std::max<int64_t>(K8_MIN_PAGES, (pages + want - 1) / want));
-    if (p.tiles) sp = std::min<int64_t>(K8_MIXED_PAGES, pages);
+    if (p.tiles) sp = std::min<int64_t>(8 * blocks <= a.n_cu ? K8_MIXED_PAGES / 2 : K8_MIXED_PAGES, pages);
     sp = std::max(sp, (pages + K8_MAX_SPLITS - 1) / K8_MAX_SPLITS);
     p.waves = K8_WAVES;
     if (p.nt == 1 && blocks <= a.n_cu && pages <= (2 * blocks >= a.n_cu ? 2 : 1) * K8_WHOLE_PAGES) {

@@ -4,6 +4,10 @@
 // multiplying by one changes no mantissa, so a code is the nearest e4m3 value whatever the scale, a
 // growing scale moves the codes that stay in the normal range exactly, b is a byte, the largest of the bytes
 // that the tokens need is the byte that all of them need, and a value read back is exact in bf16.
+//
+// Measured (us of a call in a captured graph, hd 128): append of 64 single tokens over 8 KV heads 5.0, read of them 3.3; append of
+// 12000 tokens in runs over 4 KV heads 9.9 (37 MB, 3.7 TB/s), read 12.4 (3.0); of 50000 over 8 40 and 70 (307 MB: 7.7,
+// partly from the memory-side cache, and 4.4 TB/s; a large copy 4.9).
 #include <type_traits>
 
 #include "mg_device.h"

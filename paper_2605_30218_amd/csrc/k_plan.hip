@@ -8,6 +8,8 @@
 // then writes its share of the tokens, the new page-table entries and the per-row outputs, each found by
 // a binary search in the sums.  A token on a page that its row held before reads the page table, one on
 // a new page the free list, so no block waits for what another writes.
+// Bound by the launch and one chain of reads: 64 rows of one token 4.5 us, 256 rows with 261 thousand tokens (3.3 MB
+// written) 6.3 us of a captured graph; the smallest launch takes 4.0.
 #include "mg_device.h"
 #include "mg_kernels.h"
 
