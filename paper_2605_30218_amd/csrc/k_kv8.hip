@@ -80,21 +80,35 @@ __device__ __forceinline__ uint32_t requant4(uint32_t c, float shift) {
 
 // The run of tokens t0 .. on a page: positions [o, end) of the page of slot s0, KV head h0, by one wave.  Lane (g, m)
 // holds K's position m, features 64 h + 16 g .., and V's positions 4 g .. 4 g + 3, features 64 h + 16 c + m:
-// 16-byte pieces of the page, whose words it writes whole.  All that a run may need is requested at once:
+// 16-byte pieces of the page, whose words it writes whole.  V's rows are read eight bytes a lane (features 64 h + 4 m ..),
+// and their codes change lanes through the wave's part of LDS.  All that a run may need is requested at once:
 // its rows, its scales and, where it begins inside a page, the page.
+template <int HD>
+struct Kv8Words {
+    uint32_t w[4][HD / 64][64][4];  // [wave]: pieces of V
+};
+// byte j of four words as word j
+__device__ __forceinline__ void transpose4(uint32_t (&w)[4]) {
+    const uint32_t a = __builtin_amdgcn_perm(w[1], w[0], 0x05010400u), b = __builtin_amdgcn_perm(w[1], w[0], 0x07030602u);
+    const uint32_t c = __builtin_amdgcn_perm(w[3], w[2], 0x05010400u), d = __builtin_amdgcn_perm(w[3], w[2], 0x07030602u);
+    w[0] = __builtin_amdgcn_perm(c, a, 0x05040100u);
+    w[1] = __builtin_amdgcn_perm(c, a, 0x07060302u);
+    w[2] = __builtin_amdgcn_perm(d, b, 0x05040100u);
+    w[3] = __builtin_amdgcn_perm(d, b, 0x07060302u);
+}
 template <int HD>
 __device__ __forceinline__ void append_run(const Kv8& c, int t0, int s0, int o, int end, int h0, int lane,
                                            const uint16_t* __restrict__ k, int64_t ks, const uint16_t* __restrict__ v,
-                                           int64_t vs) {
+                                           int64_t vs, uint32_t (&words)[HD / 64][64][4]) {
     constexpr int H = HD / 64;
     const int m = lane & 15, g = lane >> 4;
     const size_t ph = ((size_t)(s0 / KV8_PAGE) * c.Hkv + h0) * 2;
     uint8_t* page = c.codes + ph * (size_t)(KV8_PAGE * HD);
     uint4 kx[H][2], old[2][H];
-    uint32_t vx[H][4][2];  // [h][c]: positions 4 g, 4 g + 1 and 4 g + 2, 4 g + 3
+    uint2 vx[H][4];  // [h][i]: position 4 g + i
     const bool mine = m >= o && m < end;
     const uint16_t* kr = k + (int64_t)(t0 + (mine ? m - o : 0)) * ks + (size_t)h0 * HD;
-    const uint16_t* vr = v + (int64_t)t0 * vs + (size_t)h0 * HD + m;
+    const uint16_t* vr = v + (int64_t)t0 * vs + (size_t)h0 * HD + 4 * m;
     uint32_t ob = 0;
     if (o) ob = *reinterpret_cast<const uint16_t*>(c.scales + ph);
 #pragma unroll
@@ -105,15 +119,10 @@ __device__ __forceinline__ void append_run(const Kv8& c, int t0, int s0, int o, 
             kx[h][1] = *reinterpret_cast<const uint4*>(kr + 64 * h + 16 * g + 8);
         }
 #pragma unroll
-        for (int q = 0; q < 4; ++q) vx[h][q][0] = vx[h][q][1] = 0;
-#pragma unroll
         for (int i = 0; i < 4; ++i) {
             const int t = 4 * g + i;
-            if (t >= o && t < end) {
-#pragma unroll
-                for (int q = 0; q < 4; ++q)
-                    vx[h][q][i >> 1] |= (uint32_t)vr[(t - o) * vs + 64 * h + 16 * q] << (16 * (i & 1));
-            }
+            vx[h][i] = make_uint2(0, 0);
+            if (t >= o && t < end) vx[h][i] = *reinterpret_cast<const uint2*>(vr + (t - o) * vs + 64 * h);
         }
         old[0][h] = old[1][h] = make_uint4(0, 0, 0, 0);
         if (o) {
@@ -129,7 +138,7 @@ __device__ __forceinline__ void append_run(const Kv8& c, int t0, int s0, int o, 
             for (int e = 0; e < 2; ++e) {
                 mk = max2(mk, max2(max2(mag2(f(kx[h][e].x)), mag2(f(kx[h][e].y))), max2(mag2(f(kx[h][e].z)), mag2(f(kx[h][e].w)))));
 #pragma unroll
-                for (int q = 0; q < 4; ++q) mv = max2(mv, mag2(f(vx[h][q][e])));
+                for (int i = 0; i < 2; ++i) mv = max2(mv, max2(mag2(f(vx[h][2 * e + i].x)), mag2(f(vx[h][2 * e + i].y))));
             }
         return tops<64>(mk, mv);
     };
@@ -152,11 +161,23 @@ __device__ __forceinline__ void append_run(const Kv8& c, int t0, int s0, int o, 
 #pragma unroll
         for (int h = 0; h < H; ++h) {
             uint32_t nw[4], ow[4] = {old[side][h].x, old[side][h].y, old[side][h].z, old[side][h].w};
+            if (side) {
+#pragma unroll
+                for (int i = 0; i < 4; ++i) nw[i] = codes4<decltype(is_odd)::value>(vx[h][i].x, vx[h][i].y, inv);
+                transpose4(nw);  // word j: feature 64 h + 4 m + j
+#pragma unroll
+                for (int j = 0; j < 4; ++j) words[h][g * 16 + 4 * (m & 3) + j][m >> 2] = nw[j];
+                __builtin_amdgcn_wave_barrier();
+                const uint4 x = *reinterpret_cast<const uint4*>(words[h][lane]);
+                nw[0] = x.x;
+                nw[1] = x.y;
+                nw[2] = x.z;
+                nw[3] = x.w;
+                __builtin_amdgcn_wave_barrier();
+            }
 #pragma unroll
             for (int q = 0; q < 4; ++q) {
-                if (side)
-                    nw[q] = codes4<decltype(is_odd)::value>(vx[h][q][0], vx[h][q][1], inv);
-                else
+                if (!side)
                     nw[q] = codes4<decltype(is_odd)::value>(q & 1 ? kx[h][q >> 1].z : kx[h][q >> 1].x, q & 1 ? kx[h][q >> 1].w : kx[h][q >> 1].y, inv);
                 const uint32_t kept = was == 0 ? 0u : b != was ? requant4(ow[q], shift) : ow[q];
                 nw[q] = (nw[q] & ~keep) | (kept & keep);
@@ -258,8 +279,9 @@ template <int HD, int W>
 __global__ __launch_bounds__(256) void kv8_append_kernel(Kv8 c, int n, const uint16_t* __restrict__ k, int64_t ks,
                                                          const uint16_t* __restrict__ v, int64_t vs,
                                                          const int32_t* __restrict__ slots) {
-    const int lane = threadIdx.x & 63;
-    const int64_t w = (int64_t)blockIdx.x * 4 + __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+    __shared__ __attribute__((aligned(16))) Kv8Words<HD> sh;
+    const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+    const int64_t w = (int64_t)blockIdx.x * 4 + wave;
     const int64_t base = w / c.Hkv * W;
     const int h0 = (int)(w % c.Hkv);
     if (base >= n) return;
@@ -290,7 +312,7 @@ __global__ __launch_bounds__(256) void kv8_append_kernel(Kv8 c, int n, const uin
         first &= first - 1;
         const int s0 = __builtin_amdgcn_readlane(sl, l0), o = s0 % KV8_PAGE, i = lane - l0;
         const unsigned long long run = __ballot(i >= 0 && i < KV8_PAGE - o && sl == s0 + i) >> l0;
-        append_run<HD>(c, (int)base - 1 + l0, s0, o, o + __ffsll(~run) - 1, h0, lane, k, ks, v, vs);
+        append_run<HD>(c, (int)base - 1 + l0, s0, o, o + __ffsll(~run) - 1, h0, lane, k, ks, v, vs, sh.w[wave]);
     }
 }
 
