@@ -334,12 +334,13 @@ __device__ __forceinline__ uint32_t value2(uint32_t w, float f) {
 }
 // One wave per (four slots of the list, KV head), 16 lanes a slot.  K: lane m has the 16-byte piece of features
 // 16 m ..; V: lane m the pieces of features 16 c + m, whose words hold four positions (the four slots of a
-// wave mostly), of which it takes its own.
+// wave mostly), of which it takes its own; the row goes through LDS to be written 16 bytes a lane.
 template <int HD>
 __global__ __launch_bounds__(256) void kv8_read_kernel(Kv8 c, int n, const int32_t* __restrict__ slots,
                                                        uint16_t* __restrict__ k, int64_t ks, uint16_t* __restrict__ v,
                                                        int64_t vs) {
     constexpr int H = HD / 64;
+    __shared__ __attribute__((aligned(16))) uint16_t sh[16][HD + 8];  // a slot's row of V
     const int lane = threadIdx.x & 63, m = lane & 15;
     const int64_t w = (int64_t)blockIdx.x * 4 + (threadIdx.x >> 6);
     const int64_t i = w / c.Hkv * 4 + (lane >> 4);
@@ -368,17 +369,20 @@ __global__ __launch_bounds__(256) void kv8_read_kernel(Kv8 c, int n, const int32
     }
     if (v) {
         const float f = __uint_as_float((sc >> 8) << 23);
-        uint16_t* out = v + i * vs + (size_t)h0 * HD + m;
+        uint16_t* row = sh[threadIdx.x >> 4];
         const uint32_t pick = (t & 3) * 0x0101u + 0x0400u;  // byte t % 4 of two words
 #pragma unroll
         for (int h = 0; h < H; ++h) {
             const uint32_t w = __builtin_amdgcn_perm(vp[h].y, vp[h].x, pick) & 0xffffu | __builtin_amdgcn_perm(vp[h].w, vp[h].z, pick) << 16;
             const uint32_t lo = value2<false>(w, f), hi = value2<true>(w, f);
-            out[64 * h] = (uint16_t)lo;
-            out[64 * h + 16] = (uint16_t)(lo >> 16);
-            out[64 * h + 32] = (uint16_t)hi;
-            out[64 * h + 48] = (uint16_t)(hi >> 16);
+            row[64 * h + m] = (uint16_t)lo;
+            row[64 * h + 16 + m] = (uint16_t)(lo >> 16);
+            row[64 * h + 32 + m] = (uint16_t)hi;
+            row[64 * h + 48 + m] = (uint16_t)(hi >> 16);
         }
+        __builtin_amdgcn_wave_barrier();
+        using piece = uint32_t __attribute__((ext_vector_type(HD / 32)));  // the row in 16 pieces
+        *reinterpret_cast<piece*>(v + i * vs + (size_t)h0 * HD + HD / 16 * m) = *reinterpret_cast<const piece*>(row + HD / 16 * m);
     }
 }
 
