@@ -5,8 +5,8 @@
 // growing scale moves the codes that stay in the normal range exactly, b is a byte, the largest of the bytes
 // that the tokens need is the byte that all of them need, and a value read back is exact in bf16.
 //
-// Measured (us of a call in a captured graph, hd 128): append of 64 single tokens over 8 KV heads 5.0, read of them 3.3; append of
-// 12000 tokens in runs over 4 KV heads 9.9 (37 MB, 3.7 TB/s), read 12.4 (3.0); of 50000 over 8 40 and 70 (307 MB: 7.7,
+// Measured (us of a call in a captured graph, hd 128): append of 64 single tokens over 8 KV heads 4.9, read of them 3.3; append of
+// 12000 tokens in runs over 4 KV heads 9.1 (37 MB, 4.1 TB/s), read 12.0 (3.1); of 50000 over 8 35 and 70 (307 MB: 8.8,
 // partly from the memory-side cache, and 4.4 TB/s; a large copy 4.9).
 #include <type_traits>
 
@@ -21,9 +21,9 @@ constexpr int KV8_MIN_BYTE = 16;  // 2^(16 - 127) times the least code, 2^-9, is
 // Tokens of a wave's window: 1 up to KV8_FEW (token, KV head) pairs, 8 up to KV8_SOME, 16 above.  A window of several tokens
 // does its runs one after the other (single tokens four at a time), but its waves have work where a run is long: with
 // windows of one a run of 16 is one wave's and 15 find nothing to do.  Measured at hd 128, us, windows of 1 / 8 / 16:
-// 2000 pairs in runs 6.3 / 5.4 / 7.9, in single tokens 5.8 / 6.0 / 7.9; 4096 in single tokens 7.4 / 6.5 / 8.3; 16000 in runs
-// 22 / 6.9 / 8.4; 24000 32 / 8.3 / 8.8; 32000 40 / 10.3 / 9.1; 96000 107 / 21 / 15.
-constexpr int KV8_FEW = 2048;
+// 512 pairs in single tokens 4.9 / 5.3 / 7.7, 1024 5.0 / 5.5 / 7.8, 2048 5.7 / 5.7 / 8.0, 8192 12.5 / 7.4 / 9.3; in runs 2000 pairs
+// 6.2 / 5.1 / 7.2, 16000 20 / 6.8 / 7.7, 24000 27 / 8.0 / 8.2, 32000 35 / 9.7 / 8.5, 96000 90 / 18 / 13.
+constexpr int KV8_FEW = 1024;
 constexpr int KV8_SOME = 24576;
 
 typedef float f32x2_q8 __attribute__((ext_vector_type(2)));
