@@ -309,7 +309,7 @@ typedef struct {
     float softcap;             /* 0: none; else 1e-15 .. 1e15 */
     const uint16_t* q;         /* [device] bf16 [n_tokens][Hq][hd], token stride q_stride values */
     int64_t q_stride;
-    uint16_t* out;             /* [device] as q, token stride out_stride; must not overlap q */
+    uint16_t* out;             /* [device] as q, token stride out_stride; must not overlap q (equal: MG_ERR_ARG) */
     int64_t out_stride;
     const int32_t* page_table; /* [device] [n_rows][max_pages_per_row] */
     const int32_t* lens;       /* [device] [n_rows] */

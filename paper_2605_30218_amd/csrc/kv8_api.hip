@@ -145,6 +145,7 @@ mg_status mg_kv8_attention(const mg_kv8_cache* cache, const mg_kv8_attn_args* ar
     const mg_status st = attn_args(cache, args, &a);
     if (st != MG_OK) return st;
     if (a.T == 0 || a.B == 0) return MG_OK;
+    if (a.out == a.q) return MG_ERR_ARG;
     const size_t need = kv8_attention_ws_bytes(a);
     if (need && (!workspace || workspace_bytes < need)) return MG_ERR_WORKSPACE;
     if (need && !aligned(workspace, 16)) return MG_ERR_ARG;

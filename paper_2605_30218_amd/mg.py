@@ -17,6 +17,7 @@ HERE = os.path.dirname(os.path.abspath(__file__))
 LIB_PATH = os.path.join(HERE, "libmg.so")
 
 MG_OK = 0
+MG_ERR_WORKSPACE = -3
 # repair actions (include/mg.h)
 REPAIR_ON_MISMATCH, REPAIR_TOKEN_ONLY, REPAIR_COPY_ALWAYS = 0, 1, 2
 KIND_FAST_GEMM, KIND_FAST_ATTN, KIND_CANON_GEMV, KIND_CANON_ATTN, KIND_GATE = range(5)
@@ -330,7 +331,7 @@ def batch_plan(ctx_len, n_new, free_pages, n_free, page_table, max_tokens, out=N
             _ints("n_free", n_free, dev, 1), M, _ints("page_table", page_table, dev))
     if out is None:
         buf = _new(3 * M + 3 * B + 2, torch.int32, dev, stream)
-        cu, lens, adm, pos, row, slot, left = buf.split_with_sizes((B + 1, B, B, M, M, M, 1))
+        cu, lens, adm, pos, row, slot, left = torch.unsafe_split_with_sizes(buf, (B + 1, B, B, M, M, M, 1))
         out = BatchPlan(cu, lens, adm, pos, row, slot, left)
         at = buf.data_ptr()
         lists = 3 * B + 1
@@ -428,14 +429,21 @@ def kv8_attention(codes, scales, q, page_table, lens, cu_new=None, max_new=1, ma
     if out is None:
         out = _new(q.shape, q.dtype, dev, stream)
     a = _attn_args(c, q, page_table, lens, cu_new, max_new, max_len, scale, window, softcap, out, dev)
-    cp, ap, lib = C.byref(c), C.byref(a), load()
-    if workspace is None:
-        need = lib.mg_kv8_attention_workspace_bytes(cp, ap)
-        workspace = _new(need, torch.uint8, dev, stream) if need else None
-    elif workspace.dtype is not torch.uint8 or workspace.device != dev or not workspace.is_contiguous():
-        _refuse("workspace", workspace, f"contiguous uint8 on {dev}")
-    ws, n = (None, 0) if workspace is None else (workspace.data_ptr(), workspace.numel())
-    _call("mg_kv8_attention", dev, stream, lib.mg_kv8_attention, cp, ap, ws, n)
+    args = "mg_kv8_attention", dev, stream, load().mg_kv8_attention, C.byref(c), C.byref(a)
+    if workspace is not None:
+        if workspace.dtype is not torch.uint8 or workspace.device != dev or not workspace.is_contiguous():
+            _refuse("workspace", workspace, f"contiguous uint8 on {dev}")
+        _call(*args, workspace.data_ptr(), workspace.numel())
+        return out
+    try:  # short calls need none, and asking first would take a tenth of their time
+        _call(*args, None, 0)
+    except MgError as e:
+        if e.status != MG_ERR_WORKSPACE:
+            raise
+        with torch.cuda.device(dev):
+            n = load().mg_kv8_attention_workspace_bytes(*args[4:])
+        workspace = _new(n, torch.uint8, dev, stream)
+        _call(*args, workspace.data_ptr(), n)
     return out
 
 

@@ -18,7 +18,7 @@ def cache(codes=P, scales=P, n_pages=8, hkv=2, hd=64):
 
 def attn(**kw):
     d = dict(n_rows=3, n_tokens=5, n_q_heads=4, max_new=2, max_len=0, max_pages_per_row=4, window=0, scale=0.0,
-             softcap=0.0, q=P, q_stride=256, out=P, out_stride=256, page_table=P, lens=P, cu_new=P) | kw
+             softcap=0.0, q=P, q_stride=256, out=4 * P, out_stride=256, page_table=P, lens=P, cu_new=P) | kw
     a = mg.MgKv8AttnArgs()
     for k, v in d.items():
         setattr(a, k, v)
@@ -93,6 +93,18 @@ def test_workspace_follows_the_host_bounds():
     assert need(n_rows=256, n_tokens=256, max_len=1024) == 0
     assert 0 < need(n_tokens=64, max_new=64) < 256 << 20
     assert need(n_tokens=8192, max_new=8192, max_len=2048) == 0
+
+
+def test_attention_refuses_a_short_workspace_and_work_in_place():
+    lib, c = mg.load(), cache(n_pages=1 << 20, hkv=8, hd=128)
+    a = attn(n_rows=1, n_tokens=1, n_q_heads=32, max_new=1, max_pages_per_row=1024, q_stride=4096, out_stride=4096)
+    need = lib.mg_kv8_attention_workspace_bytes(C.byref(c), C.byref(a))
+    assert need > 0
+    for ws, n in ((None, need), (P, need - 1), (P, 0)):
+        assert lib.mg_kv8_attention(C.byref(c), C.byref(a), ws, n, None) == WORKSPACE
+    assert lib.mg_kv8_attention(C.byref(c), C.byref(a), P + 4, need, None) == ARG
+    a.out = a.q
+    assert lib.mg_kv8_attention(C.byref(c), C.byref(a), P, need, None) == ARG
 
 
 def test_attention_of_nothing():
