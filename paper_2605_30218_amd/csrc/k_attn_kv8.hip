@@ -111,37 +111,44 @@ struct K8Acc {
         }
     }
 };
-// what the kernels derive from the scale and the cap: the exponent is x * f with x a score as k8_score
-// leaves it
+// what the kernels derive from the scale and the cap: the exponent is x * f with x a product q . k or what k8_cap makes of it
 struct K8Soft {
-    float f, zin, cap2;
+    float f, zin, most;  // most: of |q . k| up to which z is at most 1/2
 };
 __device__ __forceinline__ K8Soft k8_soft(const Kv8AttnArgs& a) {
-    return K8Soft{a.cap > 0.0f ? 1.0f : a.scale * 1.4426950408889634f, a.scale * a.inv_cap * 2.8853900817779268f,
-                  a.cap * 1.4426950408889634f};
+    constexpr float log2e = 1.4426950408889634f;
+    const float zin = a.scale * a.inv_cap;
+    return K8Soft{(a.cap > 0.0f ? a.cap : a.scale) * log2e, zin, 0.5f * ieee_div(1.0f, zin)};
 }
 
-// A product q . k as a score: itself, or capped, in log2 units.  tanh(z) = 1 - 2 / (1 + e^2z) is off by some 2^-23 whatever z, a
-// capped score by as much of the cap: up to K8_CAP_LARGE that is 2^-16, the accuracy of a two-term probability.  Larger caps
-// take z's series to z^7 below 1/8 (2^-29 of itself off), so that one far above the scores leaves them as they are; with
-// it for every cap, 24 rows of a mixed batch with a cap took 43 us instead of 36.
-enum { K8_UNCAPPED, K8_CAPPED, K8_CAPPED_LARGE };
-constexpr float K8_CAP_LARGE = 64.0f;
-template <int CAP>
-__device__ __forceinline__ float k8_score(float s, const K8Soft& so) {
-    if (CAP == K8_UNCAPPED) return s;
-    const float z2 = s * so.zin;  // 2 log2(e) z
-    float t = 1.0f - 2.0f * __builtin_amdgcn_rcpf(1.0f + __builtin_amdgcn_exp2f(z2));
-    if (CAP == K8_CAPPED_LARGE) {
-        const float z = z2 * 0.34657359027997264f, zz = z * z;
-        const float small = z * __builtin_fmaf(zz, __builtin_fmaf(zz, __builtin_fmaf(zz, -17.0f / 315.0f, 2.0f / 15.0f), -1.0f / 3.0f), 1.0f);
-        t = zz < 1.0f / 64.0f ? small : t;
-    }
-    return so.cap2 * t;
+// Capped scores: a step's products q . k become tanh(z), z = scale * q . k / cap.  Up to 1/2 by a polynomial that is off by 2^-25 of
+// tanh (fitted to tanh(z) / z - 1 over z^2, relative errors least), without a transcendental instruction; a step that
+// has larger ones takes 1 - 2 / (1 + e^2z) for those, off by some 2^-23.  So a score keeps its relative accuracy whatever
+// the cap.
+template <int NT>
+__device__ __forceinline__ void k8_cap(float (&x)[NT][8], const K8Soft& so) {
+    float top = 0.0f;
+#pragma unroll
+    for (int u = 0; u < NT; ++u)
+#pragma unroll
+        for (int i = 0; i < 8; ++i) top = fmaxf(top, __builtin_fabsf(x[u][i]));
+    const bool large = __any(!(top <= so.most));
+#pragma unroll
+    for (int u = 0; u < NT; ++u)
+#pragma unroll
+        for (int i = 0; i < 8; ++i) {
+            const float z = x[u][i] * so.zin, zz = z * z;
+            float t = __builtin_fmaf(z * zz, __builtin_fmaf(zz, __builtin_fmaf(zz, __builtin_fmaf(zz, 0.01724149f, -0.05304549f), 0.13325879f), -0.33333144f), z);
+            if (large) {
+                const float e = 1.0f - 2.0f * __builtin_amdgcn_rcpf(1.0f + __builtin_amdgcn_exp2f(2.8853900817779268f * z));
+                t = __builtin_fabsf(z) <= 0.5f ? t : e;
+            }
+            x[u][i] = t;
+        }
 }
 
 // scores: x[u][4 e + i] of position 16 e + 4 g + i of the step and column c of tile u
-template <int HD, int NT, int CAP>
+template <int HD, int NT, bool CAP>
 __device__ __forceinline__ void k8_scores(const uint4 (&kb)[2][HD / 64], const float (&ksc)[2],
                                           const uint4 (&qa)[NT][HD / 32], const K8Soft& so, float (&x)[NT][8]) {
 #pragma unroll
@@ -163,8 +170,9 @@ __device__ __forceinline__ void k8_scores(const uint4 (&kb)[2][HD / 64], const f
 #pragma unroll
         for (int u = 0; u < NT; ++u)
 #pragma unroll
-            for (int i = 0; i < 4; ++i) x[u][4 * e + i] = k8_score<CAP>(acc[u][i], so);
+            for (int i = 0; i < 4; ++i) x[u][4 * e + i] = acc[u][i];
     }
+    if (CAP) k8_cap<NT>(x, so);
 }
 
 // Whether the token at position p sees the step's position i of this lane: j0 the step's first position,
@@ -322,7 +330,7 @@ struct K8FewShared {
     float o[WAVES][16 * NT][HD + 4];  // (padded rows)
     float m[WAVES][16 * NT], l[WAVES][16 * NT];
 };
-template <int HD, int NT, int WAVES, int CAP>
+template <int HD, int NT, int WAVES, bool CAP>
 __device__ __forceinline__ void k8_few_block(const Kv8AttnArgs& a, int sp, int nsplit, int block, K8FewShared<HD, NT, WAVES>& sh) {
     constexpr int H = HD / 64;        // 1 KiB runs of a page of K or V
     constexpr int DT = HD / 16;       // output tiles
@@ -450,7 +458,7 @@ __device__ __forceinline__ void k8_few_block(const Kv8AttnArgs& a, int sp, int n
     }
 }
 
-template <int HD, int NT, int WAVES, int CAP>
+template <int HD, int NT, int WAVES, bool CAP>
 __global__ __launch_bounds__(64 * WAVES) __attribute__((amdgpu_waves_per_eu(NT == 2 || WAVES > 4 ? 2 : 3))) void attn_kv8_few_kernel(
     Kv8AttnArgs a, int sp, int nsplit) {
     __shared__ __attribute__((aligned(16))) K8FewShared<HD, NT, WAVES> sh;
@@ -587,7 +595,7 @@ struct K8ChunkShared {
     uint32_t nan_at[K8_GROUPS][2][K8_STAGE][64];  // NaN codes of V: bits 4 d .. of a lane: output tile d's four positions of a page
     int nan_any[K8_GROUPS][2][K8_STAGE];
 };
-template <int HD, int NT, int CAP>
+template <int HD, int NT, bool CAP>
 __device__ __forceinline__ void k8_chunk_block(const Kv8AttnArgs& a, int few, int tiles, int nsplit, float* part, int block,
                                                K8ChunkShared<HD>& sh) {
     constexpr int H = HD / 64, DT = HD / 16;
@@ -754,8 +762,9 @@ __device__ __forceinline__ void k8_chunk_block(const Kv8AttnArgs& a, int few, in
 #pragma unroll
                 for (int u = 0; u < NT; ++u)
 #pragma unroll
-                    for (int i = 0; i < 4; ++i) x[u][4 * e + i] = k8_score<CAP>(s[u][i], so);
+                    for (int i = 0; i < 4; ++i) x[u][4 * e + i] = s[u][i];
             }
+            if (CAP && any) k8_cap<NT>(x, so);
             __builtin_amdgcn_sched_barrier(0);
 #pragma unroll
             for (int d = 0; d < DT; ++d) vf[d] = *reinterpret_cast<const bf16x8_k8*>(tile[buf][hf][1][d][lane]);
@@ -876,7 +885,7 @@ __device__ __forceinline__ void k8_chunk_block(const Kv8AttnArgs& a, int few, in
 }
 
 // A call with longer rows: their blocks, then those of its rows of few query rows, in one launch.
-template <int HD, int CAP>
+template <int HD, bool CAP>
 __global__ __launch_bounds__(K8_CHUNK_THREADS) __attribute__((amdgpu_waves_per_eu(2))) void attn_kv8_mixed_kernel(
     Kv8AttnArgs a, int sp, int nsplit, int tiles, int csplit, float* cpart) {
     union Shared {
@@ -989,9 +998,7 @@ size_t kv8_attention_ws_bytes(const Kv8AttnArgs& a) {
 template <int HD, int NT, int WAVES>
 static void k8_launch_few(const Kv8AttnArgs& a, const K8Plan& p, hipStream_t s) {
     const dim3 grid((unsigned)((int64_t)a.B * a.c.Hkv * p.nsplit));
-    auto f = a.cap == 0.0f             ? attn_kv8_few_kernel<HD, NT, WAVES, K8_UNCAPPED>
-             : a.cap <= K8_CAP_LARGE ? attn_kv8_few_kernel<HD, NT, WAVES, K8_CAPPED>
-                                     : attn_kv8_few_kernel<HD, NT, WAVES, K8_CAPPED_LARGE>;
+    auto f = a.cap > 0.0f ? attn_kv8_few_kernel<HD, NT, WAVES, true> : attn_kv8_few_kernel<HD, NT, WAVES, false>;
     hipLaunchKernelGGL(f, grid, dim3(64 * WAVES), 0, s, a, p.sp, p.nsplit);
 }
 template <int HD>
@@ -1013,9 +1020,7 @@ static void k8_launch(const Kv8AttnArgs& a, const K8Plan& p, hipStream_t s) {
     }
     float* cpart = a.part + k8_few_floats(a, p);
     const dim3 grid((unsigned)(p.tiles * a.c.Hkv * p.csplit + (int64_t)a.B * a.c.Hkv * p.nsplit));
-    auto f = a.cap == 0.0f             ? attn_kv8_mixed_kernel<HD, K8_UNCAPPED>
-             : a.cap <= K8_CAP_LARGE ? attn_kv8_mixed_kernel<HD, K8_CAPPED>
-                                     : attn_kv8_mixed_kernel<HD, K8_CAPPED_LARGE>;
+    auto f = a.cap > 0.0f ? attn_kv8_mixed_kernel<HD, true> : attn_kv8_mixed_kernel<HD, false>;
     hipLaunchKernelGGL(f, grid, dim3(K8_CHUNK_THREADS), 0, s, a, p.sp, p.nsplit, (int)p.tiles, p.csplit, cpart);
     const int64_t joins = few_joins + (p.csplit > 1 ? p.tiles * a.c.Hkv * (K8_CHUNK_ROWS / K8_WAVES) : 0);
     if (joins)

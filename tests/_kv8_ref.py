@@ -104,8 +104,8 @@ def attention(cache, q, table, lens, cu, scale, window=0, softcap=0.0, p_bits=8)
       the output's rounding, half a step of bf16: 2^-8 |out|;
       a probability's rounding to p_bits bits: 2^-p_bits A;
       fp32 scores: hd + 16 roundings (the products' sum, scale, cap) of 2^-24 relative to scale * sum |q k|, E
-        at most (a capped score: 2^-21 of the cap more, or 2^-18 of the largest score where that is less and
-        the cap above 64, as its series keeps tanh's relative accuracy), and exp's argument, rounded once relative to the largest score: each weight moves by at most
+        at most (a capped score: 2^-20 of the largest score more, for tanh with an error of 2^-22
+        of itself below 1/2 and 2^-23 above), and exp's argument, rounded once relative to the largest score: each weight moves by at most
         2 (E + 2^-23 max|s|) of itself, twice for the quotient;
       fp32 sums over n positions and exp itself: (n + 32) 2^-23 A."""
     T, Hq, hd = q.shape
@@ -137,7 +137,7 @@ def attention(cache, q, table, lens, cu, scale, window=0, softcap=0.0, p_bits=8)
             if softcap:
                 s = softcap * np.tanh(s / softcap)
                 top = np.where(see, np.abs(s), 0.0).max(1)
-                E = E + (2.0 ** -21 * softcap if softcap <= 64 else np.minimum(2.0 ** -21 * softcap, 2.0 ** -18 * top))
+                E = E + 2.0 ** -20 * top
             s = np.where(see, s, -np.inf)
             with np.errstate(invalid="ignore"):
                 w = np.exp(s - s.max(1, keepdims=True))
