@@ -83,9 +83,54 @@ __device__ __forceinline__ K8Row k8_row(const Kv8AttnArgs& a, int r) {
     x.pgb = (x.len + 15) / 16;
     return x;
 }
+constexpr int K8_MIN_PAGES = 8;  // pages a split takes at least: a step of every wave
+// How rows of few query rows are split: pages of a split, splits of a row at most.  units > 0 (at most 64 rows): a split takes
+// fewer pages, down to sp / 2, as long as the splits of all rows together are at most `units`; most: the splits of a row then.
+struct K8Few {
+    int sp, nsplit, most, units;
+};
 // splits of npg pages among at most nsplit blocks of about sp pages (an even number each)
 __device__ __forceinline__ int k8_active(int npg, int sp, int nsplit) {
     return min(nsplit, max(1, (npg + sp - 1) / sp));
+}
+// Lane r: row r, its splits (0 where it has no tokens or more than LIMIT query rows), and those of the rows up to it.  All
+// lanes find the same pages of a split.
+struct K8Lanes {
+    K8Row row;
+    int act, sum;
+};
+template <int LIMIT>
+__device__ __forceinline__ K8Lanes k8_lanes(const Kv8AttnArgs& a, const K8Few& p) {
+    const int lane = threadIdx.x & 63;
+    K8Lanes x;
+    x.row = k8_row(a, min(lane, a.B - 1));
+    const bool live = lane < a.B && x.row.n > 0 && x.row.n * a.G <= LIMIT;
+    const int npg = live ? max(x.row.pgb - x.row.pga, 0) : 0;
+    int total = npg;
+#pragma unroll
+    for (int o = 32; o >= 1; o >>= 1) total += __shfl_xor(total, o, 64);
+    const int rows = __popcll(__ballot(live));
+    auto split = [&](int sp) {
+        x.act = live ? k8_active(npg, sp, sp == p.sp ? p.nsplit : p.most) : 0;
+        x.sum = x.act;
+#pragma unroll
+        for (int o = 1; o < 64; o <<= 1) {
+            const int v = __shfl_up(x.sum, o, 64);
+            if (lane >= o) x.sum += v;
+        }
+        return __builtin_amdgcn_readlane(x.sum, 63);
+    };
+    // a row's last split is half empty on average, wholly at worst: rows / 2 splits more than total / sp, or rows
+    auto pages = [&](int splits) {
+        return min(p.sp, max(max(p.sp / 2, K8_MIN_PAGES), (total + splits - 1) / max(splits, 1)));
+    };
+    const int sp = pages(p.units - rows / 2);
+    if (split(sp) > p.units && sp < p.sp) split(pages(p.units - rows));
+    return x;
+}
+__device__ __forceinline__ K8Row k8_of_lane(const K8Row& x, int at) {
+    return K8Row{__builtin_amdgcn_readlane(x.t0, at), __builtin_amdgcn_readlane(x.n, at), __builtin_amdgcn_readlane(x.len, at),
+                 __builtin_amdgcn_readlane(x.p0, at), __builtin_amdgcn_readlane(x.pga, at), __builtin_amdgcn_readlane(x.pgb, at)};
 }
 
 // ---- one step: 32 positions (two pages) against NT tiles of 16 query rows
@@ -330,19 +375,31 @@ struct K8FewShared {
     float o[WAVES][16 * NT][HD + 4];  // (padded rows)
     float m[WAVES][16 * NT], l[WAVES][16 * NT];
 };
-template <int HD, int NT, int WAVES, bool CAP>
-__device__ __forceinline__ void k8_few_block(const Kv8AttnArgs& a, int sp, int nsplit, int block, K8FewShared<HD, NT, WAVES>& sh) {
+template <int HD, int NT, int WAVES, bool CAP, bool EVEN>
+__device__ __forceinline__ void k8_few_block(const Kv8AttnArgs& a, const K8Few& few, int block, K8FewShared<HD, NT, WAVES>& sh) {
     constexpr int H = HD / 64;        // 1 KiB runs of a page of K or V
     constexpr int DT = HD / 16;       // output tiles
     const int lane = threadIdx.x & 63, c = lane & 15, g = lane >> 4;
     const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
     const int kh = block % a.c.Hkv;
-    const int r = block / a.c.Hkv % a.B, split = block / a.c.Hkv / a.B;
-    const K8Row row = k8_row(a, r);
-    if (row.n <= 0 || row.n * a.G > 16 * NT) return;
-    const int npg = max(row.pgb - row.pga, 0);
-    const int act = k8_active(npg, sp, nsplit);
-    if (split >= act) return;
+    int r = block / a.c.Hkv % a.B, split = block / a.c.Hkv / a.B, act;
+    K8Row row;
+    if (EVEN) {
+        const K8Lanes x = k8_lanes<16 * NT>(a, few);
+        const int index = block / a.c.Hkv;
+        const unsigned long long past = __ballot(x.sum > index);
+        if (!past) return;
+        r = __builtin_amdgcn_readfirstlane(__ffsll(past) - 1);
+        row = k8_of_lane(x.row, r);
+        act = __builtin_amdgcn_readlane(x.act, r);
+        split = index - (__builtin_amdgcn_readlane(x.sum, r) - act);
+    } else {
+        row = k8_row(a, r);
+        if (row.n <= 0 || row.n * a.G > 16 * NT) return;
+        act = k8_active(max(row.pgb - row.pga, 0), few.sp, few.nsplit);
+        if (split >= act) return;
+    }
+    const int npg = max(row.pgb - row.pga, 0), nsplit = few.most;
     const int per = ((npg + act - 1) / act + 1) & ~1;
     const int pg0 = row.pga + split * per, pg1 = split == act - 1 ? row.pgb : min(row.pgb, pg0 + per);
 
@@ -458,11 +515,11 @@ __device__ __forceinline__ void k8_few_block(const Kv8AttnArgs& a, int sp, int n
     }
 }
 
-template <int HD, int NT, int WAVES, bool CAP>
+template <int HD, int NT, int WAVES, bool CAP, bool EVEN>
 __global__ __launch_bounds__(64 * WAVES) __attribute__((amdgpu_waves_per_eu(NT == 2 || WAVES > 4 ? 2 : 3))) void attn_kv8_few_kernel(
-    Kv8AttnArgs a, int sp, int nsplit) {
+    Kv8AttnArgs a, K8Few few) {
     __shared__ __attribute__((aligned(16))) K8FewShared<HD, NT, WAVES> sh;
-    k8_few_block<HD, NT, WAVES, CAP>(a, sp, nsplit, blockIdx.x, sh);
+    k8_few_block<HD, NT, WAVES, CAP, EVEN>(a, few, blockIdx.x, sh);
 }
 
 // One query row's splits joined in their order by a wave: outputs at po + s * so, reference and sum of split s in lane s's
@@ -510,21 +567,29 @@ __device__ __forceinline__ uint16_t* k8_out(const Kv8AttnArgs& a, const K8Row& r
 
 // Joins the splits of rows of few query rows: a wave per query row of a (row, KV head); block: its index, of ROWB blocks a
 // (row, KV head).
-template <int HD, int NT>
-__device__ __forceinline__ void k8_few_join(const Kv8AttnArgs& a, int sp, int nsplit, int block, int rowb) {
+template <int HD, int NT, bool EVEN>
+__device__ __forceinline__ void k8_few_join(const Kv8AttnArgs& a, const K8Few& few, int block, int rowb) {
     const int rr = block % rowb * K8_WAVES + (threadIdx.x >> 6);
     const int kh = block / rowb % a.c.Hkv, r = block / rowb / a.c.Hkv;
-    const K8Row row = k8_row(a, r);
-    if (row.n <= 0 || row.n * a.G > 16 * NT || rr >= row.n * a.G) return;
-    const int act = k8_active(max(row.pgb - row.pga, 0), sp, nsplit);
-    if (act == 1) return;
+    K8Row row;
+    int act;
+    if (EVEN) {
+        const K8Lanes x = k8_lanes<16 * NT>(a, few);
+        row = k8_of_lane(x.row, r);
+        act = __builtin_amdgcn_readlane(x.act, r);
+    } else {
+        row = k8_row(a, r);
+        act = row.n <= 0 || row.n * a.G > 16 * NT ? 0 : k8_active(max(row.pgb - row.pga, 0), few.sp, few.nsplit);
+    }
+    if (act <= 1 || rr >= row.n * a.G) return;
+    const int nsplit = few.most;
     const size_t first = ((size_t)r * a.c.Hkv + kh) * nsplit * (16 * NT) + rr;
     const float* ml = a.part + (size_t)a.B * a.c.Hkv * nsplit * (16 * NT) * HD;
     k8_join<HD>(a.part + first * HD, (size_t)(16 * NT) * HD, ml + 2 * first, 2 * 16 * NT, act, k8_out(a, row, kh, rr));
 }
-template <int HD, int NT>
-__global__ __launch_bounds__(K8_THREADS) void attn_kv8_join_kernel(Kv8AttnArgs a, int sp, int nsplit, int rowb) {
-    k8_few_join<HD, NT>(a, sp, nsplit, blockIdx.x, rowb);
+template <int HD, int NT, bool EVEN>
+__global__ __launch_bounds__(K8_THREADS) void attn_kv8_join_kernel(Kv8AttnArgs a, K8Few few, int rowb) {
+    k8_few_join<HD, NT, EVEN>(a, few, blockIdx.x, rowb);
 }
 
 // Tile `index` of the rows of more than `few` query rows, their tiles of ROWS query rows counted row by row: the row, and the
@@ -887,7 +952,7 @@ __device__ __forceinline__ void k8_chunk_block(const Kv8AttnArgs& a, int few, in
 // A call with longer rows: their blocks, then those of its rows of few query rows, in one launch.
 template <int HD, bool CAP>
 __global__ __launch_bounds__(K8_CHUNK_THREADS) __attribute__((amdgpu_waves_per_eu(2))) void attn_kv8_mixed_kernel(
-    Kv8AttnArgs a, int sp, int nsplit, int tiles, int csplit, float* cpart) {
+    Kv8AttnArgs a, K8Few few, int tiles, int csplit, float* cpart) {
     union Shared {
         K8ChunkShared<HD> chunk;
         K8FewShared<HD, 1, K8_GROUPS * K8_WAVES> few;
@@ -897,18 +962,18 @@ __global__ __launch_bounds__(K8_CHUNK_THREADS) __attribute__((amdgpu_waves_per_e
     if ((int)blockIdx.x < chunks)
         k8_chunk_block<HD, K8_CHUNK_TILES, CAP>(a, 16, tiles, csplit, cpart, blockIdx.x, sh.chunk);
     else
-        k8_few_block<HD, 1, K8_GROUPS * K8_WAVES, CAP>(a, sp, nsplit, blockIdx.x - chunks, sh.few);
+        k8_few_block<HD, 1, K8_GROUPS * K8_WAVES, CAP, false>(a, few, blockIdx.x - chunks, sh.few);
 }
 
 // Joins the splits of attn_kv8_mixed_kernel: blocks of its longer rows' tiles (csplit > 1), a wave per query row, then of the
 // others.
 template <int HD>
-__global__ __launch_bounds__(K8_THREADS) void attn_kv8_mixed_join_kernel(Kv8AttnArgs a, int sp, int nsplit, int rowb, int tiles,
-                                                                        int csplit, const float* cpart) {
+__global__ __launch_bounds__(K8_THREADS) void attn_kv8_mixed_join_kernel(Kv8AttnArgs a, K8Few few, int rowb, int tiles, int csplit,
+                                                                        const float* cpart) {
     constexpr int ROWS = K8_CHUNK_ROWS, RB = ROWS / K8_WAVES;
     const int chunks = csplit > 1 ? tiles * a.c.Hkv * RB : 0;
     if ((int)blockIdx.x >= chunks) {
-        k8_few_join<HD, 1>(a, sp, nsplit, blockIdx.x - chunks, rowb);
+        k8_few_join<HD, 1, false>(a, few, blockIdx.x - chunks, rowb);
         return;
     }
     const int at = blockIdx.x / RB, kh = at % a.c.Hkv;
@@ -934,6 +999,10 @@ __global__ __launch_bounds__(K8_THREADS) void attn_kv8_mixed_join_kernel(Kv8Attn
 //   - where the blocks of unsplit rows fit the device at once and a row has few pages, one block of 8
 //     waves takes a row whole: one row of 512 7.1 -> 6.3, 32 rows of 512 12.1 -> 9.8; at 64 pages one row
 //     7.9 -> 9.7, but 32 rows 17.0 -> 14.7, so up to 32 pages, or 64 where the blocks are half of the CUs.
+//   - the host knows only the longest row; where a split takes 64 pages or more and a wave's lanes hold the rows (2 to 64), the
+//     blocks find from all lengths how few pages fill the same number of blocks (16 rows of 16..16000, 28 heads
+//     over 4: 37.1 -> 34.5, 40 of 16..7000 62.4 -> 57.6, 8 of four tokens behind 500..16000 37.6 -> 35.7; it takes a microsecond, so
+//     with small splits it loses: 8 rows of 1000 10.1 -> 11.6).
 // Calls with longer rows:
 //   - a row of few query rows is split at 256 pages, beside the chunks' blocks, which take as long (64: 8 rows of
 //     16000 beside a chunk of 512 57.8 -> 63.5, 30 of 4000 55.4 -> 63.2; no split: 103, 55.2), at 128 where
@@ -942,15 +1011,17 @@ __global__ __launch_bounds__(K8_THREADS) void attn_kv8_mixed_join_kernel(Kv8Attn
 //     tokens 45.9 -> 55.1, one of 512 behind 512 27.0 -> 45.1, no call faster: a CU holds one block, and the splits'
 //     outputs are written and read), down to 4 stages a split (2: no difference; 8: 4 chunks of 2048 579 -> 600).
 struct K8Plan {
-    int nt, waves, sp, nsplit;  // rows of few query rows: tiles and waves of a block, pages of a split, splits of a row
+    int nt, waves;              // rows of few query rows: tiles and waves of a block
+    K8Few few;                  // and how they are split
+    int64_t few_blocks;
     int64_t tiles;              // of 128 query rows, of the longer rows: at most (a row's last may be partly empty); 0: none
     int csplit;                 // splits of such a tile
 };
-constexpr int K8_MIN_PAGES = 8;  // pages a split takes at least: a step of every wave
 constexpr int K8_MAX_PAGES = 128;
 constexpr int K8_MAX_SPLITS = 64;
 constexpr int K8_BLOCKS_PER_CU = 2;
 constexpr int K8_WHOLE_PAGES = 32;
+constexpr int K8_EVEN_PAGES = 64;
 constexpr int K8_MIXED_PAGES = 256;
 constexpr int K8_CHUNK_BLOCKS_PER_CU = 1;
 // pages that a group of `tokens` neighbouring tokens of a row sees at most, by the host's bounds
@@ -975,8 +1046,15 @@ static K8Plan k8_plan(const Kv8AttnArgs& a) {
         p.waves = 2 * K8_WAVES;
         sp = pages;
     }
-    p.sp = (int)sp;
-    p.nsplit = (int)((pages + sp - 1) / sp);
+    const int nsplit = (int)((pages + sp - 1) / sp);
+    const int units = K8_BLOCKS_PER_CU * a.n_cu / a.c.Hkv;
+    p.few = K8Few{(int)sp, nsplit, nsplit, 0};
+    p.few_blocks = blocks * nsplit;
+    if (!p.tiles && nsplit > 1 && sp >= K8_EVEN_PAGES && a.B > 1 && a.B <= 64 && a.B < units && (int64_t)a.B * a.maxp <= 1 << 30) {
+        p.few.most = std::min(2 * nsplit, K8_MAX_SPLITS);
+        p.few.units = units;
+        p.few_blocks = std::max<int64_t>(p.few_blocks, (int64_t)units * a.c.Hkv);
+    }
     p.csplit = 1;
     if (p.tiles) {
         const int64_t stages = (k8_pages(a, std::min(a.max_new, K8_CHUNK_ROWS / a.G + 1)) + K8_STAGE - 1) / K8_STAGE;
@@ -987,7 +1065,7 @@ static K8Plan k8_plan(const Kv8AttnArgs& a) {
 }
 
 static size_t k8_few_floats(const Kv8AttnArgs& a, const K8Plan& p) {
-    return p.nsplit == 1 ? 0 : (size_t)a.B * a.c.Hkv * p.nsplit * (16 * p.nt) * (a.c.hd + 2);
+    return p.few.nsplit == 1 ? 0 : (size_t)a.B * a.c.Hkv * p.few.most * (16 * p.nt) * (a.c.hd + 2);
 }
 size_t kv8_attention_ws_bytes(const Kv8AttnArgs& a) {
     const K8Plan p = k8_plan(a);
@@ -995,43 +1073,38 @@ size_t kv8_attention_ws_bytes(const Kv8AttnArgs& a) {
     return (k8_few_floats(a, p) + chunk) * sizeof(float);
 }
 
-template <int HD, int NT, int WAVES>
-static void k8_launch_few(const Kv8AttnArgs& a, const K8Plan& p, hipStream_t s) {
-    const dim3 grid((unsigned)((int64_t)a.B * a.c.Hkv * p.nsplit));
-    auto f = a.cap > 0.0f ? attn_kv8_few_kernel<HD, NT, WAVES, true> : attn_kv8_few_kernel<HD, NT, WAVES, false>;
-    hipLaunchKernelGGL(f, grid, dim3(64 * WAVES), 0, s, a, p.sp, p.nsplit);
+template <int HD, int NT, int WAVES, bool EVEN>
+static void k8_launch_few(const Kv8AttnArgs& a, const K8Plan& p, int rowb, int64_t joins, hipStream_t s) {
+    auto f = a.cap > 0.0f ? attn_kv8_few_kernel<HD, NT, WAVES, true, EVEN> : attn_kv8_few_kernel<HD, NT, WAVES, false, EVEN>;
+    hipLaunchKernelGGL(f, dim3((unsigned)p.few_blocks), dim3(64 * WAVES), 0, s, a, p.few);
+    if (joins)
+        hipLaunchKernelGGL((attn_kv8_join_kernel<HD, NT, EVEN>), dim3((unsigned)joins), dim3(K8_THREADS), 0, s, a, p.few, rowb);
 }
 template <int HD>
 static void k8_launch(const Kv8AttnArgs& a, const K8Plan& p, hipStream_t s) {
     const int rowb = (int)(std::min<int64_t>((int64_t)a.max_new * a.G, 16 * p.nt) + K8_WAVES - 1) / K8_WAVES;
-    const int64_t few_joins = p.nsplit > 1 ? (int64_t)a.B * a.c.Hkv * rowb : 0;
+    const int64_t few_joins = p.few.nsplit > 1 ? (int64_t)a.B * a.c.Hkv * rowb : 0;
     if (p.tiles == 0) {
-        if (p.nt == 2)
-            k8_launch_few<HD, 2, K8_WAVES>(a, p, s);
-        else if (p.waves == K8_WAVES)
-            k8_launch_few<HD, 1, K8_WAVES>(a, p, s);
-        else
-            k8_launch_few<HD, 1, 2 * K8_WAVES>(a, p, s);
-        if (few_joins) {
-            auto f = p.nt == 2 ? attn_kv8_join_kernel<HD, 2> : attn_kv8_join_kernel<HD, 1>;
-            hipLaunchKernelGGL(f, dim3((unsigned)few_joins), dim3(K8_THREADS), 0, s, a, p.sp, p.nsplit, rowb);
-        }
+        auto f = p.nt == 2 ? (p.few.units ? k8_launch_few<HD, 2, K8_WAVES, true> : k8_launch_few<HD, 2, K8_WAVES, false>)
+                 : p.waves == K8_WAVES ? (p.few.units ? k8_launch_few<HD, 1, K8_WAVES, true> : k8_launch_few<HD, 1, K8_WAVES, false>)
+                                       : k8_launch_few<HD, 1, 2 * K8_WAVES, false>;
+        f(a, p, rowb, few_joins, s);
         return;
     }
     float* cpart = a.part + k8_few_floats(a, p);
-    const dim3 grid((unsigned)(p.tiles * a.c.Hkv * p.csplit + (int64_t)a.B * a.c.Hkv * p.nsplit));
+    const dim3 grid((unsigned)(p.tiles * a.c.Hkv * p.csplit + p.few_blocks));
     auto f = a.cap > 0.0f ? attn_kv8_mixed_kernel<HD, true> : attn_kv8_mixed_kernel<HD, false>;
-    hipLaunchKernelGGL(f, grid, dim3(K8_CHUNK_THREADS), 0, s, a, p.sp, p.nsplit, (int)p.tiles, p.csplit, cpart);
+    hipLaunchKernelGGL(f, grid, dim3(K8_CHUNK_THREADS), 0, s, a, p.few, (int)p.tiles, p.csplit, cpart);
     const int64_t joins = few_joins + (p.csplit > 1 ? p.tiles * a.c.Hkv * (K8_CHUNK_ROWS / K8_WAVES) : 0);
     if (joins)
-        hipLaunchKernelGGL(attn_kv8_mixed_join_kernel<HD>, dim3((unsigned)joins), dim3(K8_THREADS), 0, s, a, p.sp, p.nsplit,
-                           rowb, (int)p.tiles, p.csplit, cpart);
+        hipLaunchKernelGGL(attn_kv8_mixed_join_kernel<HD>, dim3((unsigned)joins), dim3(K8_THREADS), 0, s, a, p.few, rowb,
+                           (int)p.tiles, p.csplit, cpart);
 }
 
 bool kv8_attention_fits(const Kv8AttnArgs& a) {
     const K8Plan p = k8_plan(a);
     constexpr int64_t most = 1 << 22;  // blocks of a launch
-    return (int64_t)a.T * a.G <= (1 << 29) && p.tiles * a.c.Hkv * p.csplit + (int64_t)a.B * a.c.Hkv * p.nsplit <= most &&
+    return (int64_t)a.T * a.G <= (1 << 29) && p.tiles * a.c.Hkv * p.csplit + p.few_blocks <= most &&
            (int64_t)a.B * a.c.Hkv * 8 + p.tiles * a.c.Hkv * (p.csplit > 1 ? K8_CHUNK_ROWS / K8_WAVES : 0) <= 2 * most;
 }
 

@@ -405,6 +405,16 @@ def test_max_len_shapes_the_launch_only(max_len):
         Batch(np.add([700, 130], new), new, 8, 2, 128, seed=11).check(max_len=max_len)
 
 
+@pytest.mark.parametrize("max_len", [0, 700, 4000])
+@pytest.mark.parametrize("hq,hkv,hd,new", [(8, 2, 128, 1), (28, 4, 64, 4), (4, 1, 128, 1), (32, 8, 64, 3)])
+def test_rows_of_very_unequal_length_are_split_evenly(hq, hkv, hd, new, max_len):
+    """One long row among short, empty and absent ones, within the host's bound and past it."""
+    rng = np.random.RandomState(hq + new)
+    for lens in ([6000, 0, 40, 17, 3000, 5], [2000] * 9 + [4, 8000], list(rng.randint(0, 5000, 24)), [7000] + [90] * 63):
+        n = [0 if i % 5 == 4 else min(new, l) if l else 1 for i, l in enumerate(lens)]
+        Batch(lens, n, hq, hkv, hd, seed=len(lens)).check(max_len=max_len)
+
+
 @pytest.mark.parametrize("new", [1, 40])
 def test_offsets_past_32_bits(new):
     """Pages behind 4 GiB of codes."""
