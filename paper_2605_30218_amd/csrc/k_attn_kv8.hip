@@ -6,10 +6,10 @@
 // drafts), bound by the K/V stream, split over positions and joined where rows are few; "chunk" blocks for longer rows,
 // bound by the matrix cores and the vector units together.  A call without longer rows launches few blocks, one
 // with them both kinds in one grid.
-// Measured, hd 128 (us of a call in a captured graph): 64 rows of 512..768, 32 heads over 8: 18.7 (85 MB, 4.5 TB/s);
-// 128 rows of 127..2047, 40 over 8: 60.4 (4.8 TB/s); 32 rows of 4095..16383: 122 (5.5 TB/s; a streaming read
-// 6.2); 23 rows of four tokens, 28 over 4: 27.5; one prompt of 2001, 28 over 4: 50 (580 TFLOP/s); 4 chunks of 2048 behind
-// up to 6144: 579 (950 TFLOP/s; a library's product of 8192^3: 1390).
+// Measured, hd 128 (us of a call in a captured graph): 64 rows of 512..768, 32 heads over 8: 19.0 (85 MB, 4.5 TB/s);
+// 128 rows of 127..2047, 40 over 8: 60.4 (4.8 TB/s); 32 rows of 4095..16383: 121 (5.5 TB/s; a streaming read
+// 6.2); 23 rows of four tokens, 28 over 4: 27.0; one prompt of 2001, 28 over 4: 50 (580 TFLOP/s); 4 chunks of 2048 behind
+// up to 6144: 576 (955 TFLOP/s; a library's product of 8192^3: 1390).
 #include <algorithm>
 
 #include "mg_device.h"

@@ -275,6 +275,8 @@ BatchPlan = collections.namedtuple("BatchPlan", "cu_new lens admitted positions 
 _BF16 = (torch.bfloat16, torch.int16)
 _raw_stream = torch._C._cuda_getCurrentRawStream if hasattr(torch._C, "_cuda_getCurrentRawStream") else None
 
+_current_device = getattr(torch._C, "_cuda_getDevice", torch.cuda.current_device)
+
 
 def _refuse(name, t, want):
     what = f"{t.dtype} {tuple(t.shape)} strides {t.stride()} on {t.device}" if isinstance(t, torch.Tensor) else repr(t)
@@ -293,7 +295,7 @@ def _call(name, device, stream, fn, *args):
     """fn(*args, stream) on the tensors' device, on the given stream or the device's current one."""
     if device.type != "cuda":
         raise ValueError(f"{name}: tensors on the GPU are needed, got {device}")
-    if device.index != torch.cuda.current_device():
+    if device.index != _current_device():
         with torch.cuda.device(device):
             return _call(name, device, stream, fn, *args)
     if stream is not None:
@@ -384,18 +386,24 @@ def kv8_read(codes, scales, slots, k_out=None, v_out=None, stream=None):
     """mg_kv8_read: the values of slots [n] as bf16 rows (k, v), each [n, Hkv, hd].  Rows of slots
     outside the cache are not written: in a new tensor they hold anything."""
     c = _kv8(codes, scales)
-    dev, n = codes.device, slots.numel()
+    dev, shape = codes.device, (slots.numel(), c.n_kv_heads, c.head_dim)
+    n, heads, hd = shape
     if k_out is None:
-        k_out = _new((n, c.n_kv_heads, c.head_dim), torch.bfloat16, dev, stream)
+        k_out = _new(shape, torch.bfloat16, dev, stream)
+        kp, ks = k_out.data_ptr(), heads * hd
+    else:
+        kp, ks = _rows16("k_out", k_out, n, heads, hd, dev)
     if v_out is None:
-        v_out = _new((n, c.n_kv_heads, c.head_dim), torch.bfloat16, dev, stream)
-    kp, ks = _rows16("k_out", k_out, n, c.n_kv_heads, c.head_dim, dev)
-    vp, vs = _rows16("v_out", v_out, n, c.n_kv_heads, c.head_dim, dev)
+        v_out = _new(shape, torch.bfloat16, dev, stream)
+        vp, vs = v_out.data_ptr(), heads * hd
+    else:
+        vp, vs = _rows16("v_out", v_out, n, heads, hd, dev)
     _call("mg_kv8_read", dev, stream, load().mg_kv8_read, C.byref(c), n, _ints("slots", slots, dev), kp, ks, vp, vs)
     return k_out, v_out
 
 
 def _attn_args(c, q, page_table, lens, cu_new, max_new, max_len, scale, window, softcap, out, dev):
+    """The MgKv8AttnArgs of a call; out None: not known yet."""
     if q.dim() != 3 or q.shape[2] != c.head_dim:
         _refuse("q", q, f"[T, Hq, {c.head_dim}]")
     if page_table.dim() != 2:
@@ -403,7 +411,7 @@ def _attn_args(c, q, page_table, lens, cu_new, max_new, max_len, scale, window, 
     T, Hq, hd = q.shape
     B, maxp = page_table.shape
     qp, qs = _rows16("q", q, T, Hq, hd, dev)
-    op, os_ = _rows16("out", out, T, Hq, hd, dev)
+    op, os_ = (None, Hq * hd) if out is None else _rows16("out", out, T, Hq, hd, dev)
     return MgKv8AttnArgs(B, T, Hq, max_new, max_len, maxp, window, 0.0 if scale is None else scale, softcap, qp, qs, op,
                          os_, _ints("page_table", page_table, dev), _ints("lens", lens, dev, B),
                          None if cu_new is None else _ints("cu_new", cu_new, dev, B + 1))
@@ -426,9 +434,10 @@ def kv8_attention(codes, scales, q, page_table, lens, cu_new=None, max_new=1, ma
     uses, or None to take one per call."""
     c = _kv8(codes, scales)
     dev = codes.device
+    a = _attn_args(c, q, page_table, lens, cu_new, max_new, max_len, scale, window, softcap, out, dev)
     if out is None:
         out = _new(q.shape, q.dtype, dev, stream)
-    a = _attn_args(c, q, page_table, lens, cu_new, max_new, max_len, scale, window, softcap, out, dev)
+        a.out = out.data_ptr()
     args = "mg_kv8_attention", dev, stream, load().mg_kv8_attention, C.byref(c), C.byref(a)
     if workspace is not None:
         if workspace.dtype is not torch.uint8 or workspace.device != dev or not workspace.is_contiguous():
