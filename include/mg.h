@@ -288,7 +288,7 @@ mg_status mg_kv8_read(const mg_kv8_cache* cache, int n, const int32_t* slots, ui
  * cu_new[b + 1] - 1 of q (cu_new NULL: token b alone), the last of them at position lens[b] - 1, so
  * its token i of n stands at p = lens[b] - n + i; their own K/V are in the cache already.  A token sees
  * the positions j <= p, j > p - window (window > 0), whose page-table entry is a page of the cache
- * (entries outside 0 .. n_pages - 1 are holes).  With s_j = scale * q . k_j, or softcap *
+ * (entries outside 0 .. n_pages - 1 are holes, and so is what a length past the table lacks).  With s_j = scale * q . k_j, or softcap *
  * tanh(scale * q . k_j / softcap) where softcap > 0: out = sum_j softmax(s)_j v_j, rounded once to bf16; a
  * token that sees nothing gets zeros.  A NaN in a position that a token does not see has no effect
  * on it.  Query head h reads KV head h / (Hq / Hkv).  Rows without tokens and rows of out behind

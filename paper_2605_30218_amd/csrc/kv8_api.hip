@@ -67,7 +67,7 @@ mg_status attn_args(const mg_kv8_cache* c, const mg_kv8_attn_args* g, Kv8AttnArg
     a->max_new = g->max_new < g->n_tokens ? g->max_new : g->n_tokens;
     a->max_len = g->max_len && g->max_len < cap ? g->max_len : (int)cap;
     a->maxp = g->max_pages_per_row;
-    a->window = g->window < cap ? g->window : 0;  // (one of the whole row's length hides nothing)
+    a->window = g->window;
     a->scale = g->scale > 0.0f ? g->scale : (float)(1.0 / sqrt((double)c->head_dim));
     a->cap = g->softcap;
     a->inv_cap = g->softcap > 0.0f ? 1.0f / g->softcap : 0.0f;
