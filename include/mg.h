@@ -290,10 +290,12 @@ mg_status mg_kv8_read(const mg_kv8_cache* cache, int n, const int32_t* slots, ui
  * the positions j <= p, j > p - window (window > 0), whose page-table entry is a page of the cache
  * (entries outside 0 .. n_pages - 1 are holes, and so is what a length past the table lacks).  With s_j = scale * q . k_j, or softcap *
  * tanh(scale * q . k_j / softcap) where softcap > 0: out = sum_j softmax(s)_j v_j, rounded once to bf16; a
- * token that sees nothing gets zeros.  A NaN in a position that a token does not see has no effect
- * on it.  Query head h reads KV head h / (Hq / Hkv).  Rows without tokens and rows of out behind
+ * token that sees nothing gets zeros.  What stands at a position that a token does not see has no effect on
+ * it, NaN and infinity among it; a value of V that reads as NaN or infinity makes its feature NaN or infinity
+ * in the tokens that see it.  Query head h reads KV head h / (Hq / Hkv).  Rows without tokens and rows of out behind
  * the last token are left as they were.
- * Sums are fp32; a probability enters the product with V as two bf16 terms (16 bits) where a row has
+ * Sums are fp32 of terms up to 2^9 above their weights on average, so features overflow where |v| passes some
+ * 2^116 / (positions seen); a probability enters the product with V as two bf16 terms (16 bits) where a row has
  * few query rows (tokens times query heads of a KV head: up to 16, or 32 where no row of the call has
  * more), and as one (8 bits, as an output's) in longer chunks.  The order of a row's sums follows the
  * call's shape (rows, tokens, bounds) and the lengths, so the same call gives the same bits.  Calls whose

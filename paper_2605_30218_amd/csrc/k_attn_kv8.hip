@@ -51,8 +51,14 @@ __device__ __forceinline__ u32x4_k8 k8_load(uint64_t p, uint32_t off) {
     typedef const __attribute__((address_space(1))) char* gptr;
     return *reinterpret_cast<const __attribute__((address_space(1))) u32x4_k8*>(reinterpret_cast<gptr>(p) + off);
 }
-// high bit of every byte that is a NaN code
-__device__ __forceinline__ uint32_t k8_nan_bytes(uint32_t w) { return ((w & 0x7f7f7f7fu) + 0x01010101u) & 0x80808080u; }
+// Codes that are not finite in bf16: NaN, and those that stand for 2^128 or more, which only pages of scale bytes above 246
+// have (a code of exponent e stands for 2^(e - 7 + b - 127) and up, so e >= 262 - b).  k8_odd_add: what takes the
+// least such code under scale 2^(b - 127) (the float `scale`) to 0x80, in every byte; k8_odd_bytes: the high bit of each.
+__device__ __forceinline__ uint32_t k8_odd_add(float scale) {
+    const uint32_t b = __float_as_uint(scale) >> 23;
+    return 0x01010101u * (b < 247u ? 1u : 8u * (b - 246u));
+}
+__device__ __forceinline__ uint32_t k8_odd_bytes(uint32_t w, uint32_t add) { return ((w & 0x7f7f7f7fu) + add) & 0x80808080u; }
 
 // a lane's row c, all four lanes c, c + 16, c + 32, c + 48
 __device__ __forceinline__ float k8_col_max(float v) {
@@ -281,18 +287,20 @@ __device__ __forceinline__ void k8_softmax(const float (&x)[NT][8], float f, K8A
     }
 }
 
-// A NaN code of V under a probability of zero: in a step whose columns do not all see all positions it
-// must reach the columns that see it and no other.  Takes the NaN codes out of vb and puts a NaN into the outputs
+// A value of V that is not finite, under a probability of zero: in a step whose columns do not all see all positions it
+// must reach the columns that see it and no other.  Takes these codes out of vb and puts a NaN into the outputs
 // that see one, found by a product of the codes' and the columns' indicators.
 template <int HD, int NT>
-__device__ __forceinline__ void k8_mend_nan(uint4 (&vb)[2][HD / 64], K8Acc<HD, NT>& acc, const K8Row& row, int window,
-                                            int j0, int mapped, int g, const int (&pc)[NT]) {
+__device__ __forceinline__ void k8_mend_odd(uint4 (&vb)[2][HD / 64], const float (&vsc)[2], K8Acc<HD, NT>& acc, const K8Row& row,
+                                            int window, int j0, int mapped, int g, const int (&pc)[NT]) {
+    const uint32_t add[2] = {k8_odd_add(vsc[0]), k8_odd_add(vsc[1])};
     uint32_t any = 0;
 #pragma unroll
     for (int e = 0; e < 2; ++e)
 #pragma unroll
         for (int h = 0; h < HD / 64; ++h)
-            any |= k8_nan_bytes(vb[e][h].x) | k8_nan_bytes(vb[e][h].y) | k8_nan_bytes(vb[e][h].z) | k8_nan_bytes(vb[e][h].w);
+            any |= k8_odd_bytes(vb[e][h].x, add[e]) | k8_odd_bytes(vb[e][h].y, add[e]) | k8_odd_bytes(vb[e][h].z, add[e]) |
+                   k8_odd_bytes(vb[e][h].w, add[e]);
     if (!__any(any != 0)) return;
 #pragma unroll
     for (int u = 0; u < NT; ++u) {
@@ -309,7 +317,7 @@ __device__ __forceinline__ void k8_mend_nan(uint4 (&vb)[2][HD / 64], K8Acc<HD, N
                 uint32_t f[4];
 #pragma unroll
                 for (int e = 0; e < 2; ++e) {
-                    const uint32_t nb = k8_nan_bytes(q == 0 ? vb[e][h].x : q == 1 ? vb[e][h].y : q == 2 ? vb[e][h].z : vb[e][h].w);
+                    const uint32_t nb = k8_odd_bytes(q == 0 ? vb[e][h].x : q == 1 ? vb[e][h].y : q == 2 ? vb[e][h].z : vb[e][h].w, add[e]);
                     f[2 * e] = ((nb >> 7) & 1u) * 0x3f80u | ((nb >> 15) & 1u) * 0x3f800000u;
                     f[2 * e + 1] = ((nb >> 23) & 1u) * 0x3f80u | (nb >> 31) * 0x3f800000u;
                 }
@@ -323,10 +331,10 @@ __device__ __forceinline__ void k8_mend_nan(uint4 (&vb)[2][HD / 64], K8Acc<HD, N
     for (int e = 0; e < 2; ++e)
 #pragma unroll
         for (int h = 0; h < HD / 64; ++h) {
-            vb[e][h].x &= ~((k8_nan_bytes(vb[e][h].x) >> 7) * 0xffu);
-            vb[e][h].y &= ~((k8_nan_bytes(vb[e][h].y) >> 7) * 0xffu);
-            vb[e][h].z &= ~((k8_nan_bytes(vb[e][h].z) >> 7) * 0xffu);
-            vb[e][h].w &= ~((k8_nan_bytes(vb[e][h].w) >> 7) * 0xffu);
+            vb[e][h].x &= ~((k8_odd_bytes(vb[e][h].x, add[e]) >> 7) * 0xffu);
+            vb[e][h].y &= ~((k8_odd_bytes(vb[e][h].y, add[e]) >> 7) * 0xffu);
+            vb[e][h].z &= ~((k8_odd_bytes(vb[e][h].z, add[e]) >> 7) * 0xffu);
+            vb[e][h].w &= ~((k8_odd_bytes(vb[e][h].w, add[e]) >> 7) * 0xffu);
         }
 }
 
@@ -468,7 +476,7 @@ __device__ __forceinline__ void k8_few_block(const Kv8AttnArgs& a, const K8Few& 
             }
             bf16x8_k8 p[NT][2];
             k8_softmax<HD, NT, 2>(x, so.f, acc, p);
-            if (edge) k8_mend_nan<HD, NT>(vb, acc, row, a.window, j0, mapped, g, pc);
+            if (edge) k8_mend_odd<HD, NT>(vb, vsc, acc, row, a.window, j0, mapped, g, pc);
             k8_pv<HD, NT, 2>(vb, vsc, p, acc);
             __builtin_amdgcn_sched_barrier(0);
             if (more) fetch(s + WAVES, 1, vb);
@@ -662,8 +670,8 @@ template <int HD>
 struct K8ChunkShared {
     // operands of two stages, 16 bytes a lane: [stage][pair of pages][K: (page, h, half); V: output tile]
     uint32_t tile[K8_GROUPS][2][2][2][HD / 16][64][4];
-    uint32_t nan_at[K8_GROUPS][2][K8_STAGE][64];  // NaN codes of V: bits 4 d .. of a lane: output tile d's four positions of a page
-    int nan_any[K8_GROUPS][2][K8_STAGE];
+    uint32_t odd_at[K8_GROUPS][2][K8_STAGE][64];  // codes of V that are not finite: bits 4 d .. of a lane: output tile d's four positions of a page
+    int odd_any[K8_GROUPS][2][K8_STAGE];
 };
 template <int HD, int NT, bool CAP>
 __device__ __forceinline__ void k8_chunk_block(const Kv8AttnArgs& a, int few, int tiles, int nsplit, float* part, int block,
@@ -676,8 +684,8 @@ __device__ __forceinline__ void k8_chunk_block(const Kv8AttnArgs& a, int few, in
     const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6) % K8_WAVES;
     const int kh = block % a.c.Hkv;
     uint32_t(*tile)[2][2][DT][64][4] = sh.tile[group];
-    uint32_t(*nan_at)[K8_STAGE][64] = sh.nan_at[group];
-    int(*nan_any)[K8_STAGE] = sh.nan_any[group];
+    uint32_t(*odd_at)[K8_STAGE][64] = sh.odd_at[group];
+    int(*odd_any)[K8_STAGE] = sh.odd_any[group];
     const int split = block / a.c.Hkv % nsplit, index = block / a.c.Hkv / nsplit;
     const K8Tile at = k8_tile<ROWS>(a, few, index);
     if (at.r < 0) return;
@@ -701,9 +709,9 @@ __device__ __forceinline__ void k8_chunk_block(const Kv8AttnArgs& a, int few, in
     const K8Soft so = k8_soft(a);
     K8Acc<HD, NT> acc;
     acc.clear();
-    uint32_t nan_out[NT];  // bit 4 d + i: output i of tile d saw a NaN of V
+    uint32_t odd_out[NT];  // bit 4 d + i: output i of tile d saw a value of V that is not finite
 #pragma unroll
-    for (int u = 0; u < NT; ++u) nan_out[u] = 0;
+    for (int u = 0; u < NT; ++u) odd_out[u] = 0;
     const int32_t* ptab = a.page_table + (size_t)r * a.maxp;
     const size_t head_bytes = (size_t)2 * 16 * HD;
     const uint8_t* base = a.c.codes + (size_t)kh * head_bytes;
@@ -746,13 +754,14 @@ __device__ __forceinline__ void k8_chunk_block(const Kv8AttnArgs& a, int few, in
     };
     auto put = [&](int buf, const u32x4_k8 (&x)[2][H], const float (&xs)[2]) {
         const int pair = wave >> 1, e = wave & 1;
+        const uint32_t add = k8_odd_add(xs[1]);
         uint32_t any = 0;
 #pragma unroll
         for (int h = 0; h < H; ++h)
 #pragma unroll
-            for (int q = 0; q < 4; ++q) any |= (x[1][h][q] & 0x7f7f7f7fu) + 0x01010101u;
+            for (int q = 0; q < 4; ++q) any |= (x[1][h][q] & 0x7f7f7f7fu) + add;
         const bool some = __any((any & 0x80808080u) != 0);
-        if (lane == 0) nan_any[buf][wave] = some;
+        if (lane == 0) odd_any[buf][wave] = some;
         uint32_t at = 0;
 #pragma unroll
         for (int h = 0; h < H; ++h)
@@ -768,18 +777,18 @@ __device__ __forceinline__ void k8_chunk_block(const Kv8AttnArgs& a, int few, in
                 const uint2 w = k8_bf16x4(x[1][h][q], xs[1]);
                 *reinterpret_cast<u32x2_k8*>(&tile[buf][pair][1][4 * h + q][lane][2 * e]) = u32x2_k8{w.x, w.y};
             }
-        if (some) {  // NaN codes are noted, and their operands become 0
+        if (some) {  // codes that are not finite are noted, and their operands become 0
 #pragma unroll
             for (int h = 0; h < H; ++h)
 #pragma unroll
                 for (int q = 0; q < 4; ++q) {
-                    const uint32_t b = k8_nan_bytes(x[1][h][q]) >> 7;  // bits 0, 8, 16, 24
+                    const uint32_t b = k8_odd_bytes(x[1][h][q], add) >> 7;  // bits 0, 8, 16, 24
                     at |= ((b | b >> 7 | b >> 14 | b >> 21) & 15u) << (4 * (4 * h + q));
                     uint32_t* w = &tile[buf][pair][1][4 * h + q][lane][2 * e];
                     w[0] &= ~((b & 1u) * 0xffffu | (b >> 8 & 1u) * 0xffff0000u);
                     w[1] &= ~((b >> 16 & 1u) * 0xffffu | (b >> 24) * 0xffff0000u);
                 }
-            nan_at[buf][wave][lane] = at;
+            odd_at[buf][wave][lane] = at;
         }
     };
     // The second group's waves go first where both could issue: the groups meet at every barrier, and would
@@ -804,7 +813,7 @@ __device__ __forceinline__ void k8_chunk_block(const Kv8AttnArgs& a, int few, in
         };
         read_k(0, 0, kf);
         read_k(0, 1, kf);
-        const int bad[2] = {nan_any[buf][0] | nan_any[buf][1], nan_any[buf][2] | nan_any[buf][3]};
+        const int bad[2] = {odd_any[buf][0] | odd_any[buf][1], odd_any[buf][2] | odd_any[buf][3]};
         __builtin_amdgcn_sched_barrier(0);
         if (st + 1 < stages) fetch(st + 1, nx, nsc, map, id, sc, idn, scn);
 #pragma unroll
@@ -851,7 +860,7 @@ __device__ __forceinline__ void k8_chunk_block(const Kv8AttnArgs& a, int few, in
                 k8_softmax<HD, NT, 1>(x, so.f, acc, p);
             }
             if (any && bad[hf]) {
-                // NaN codes of V went into the tile as 0: a product of the codes' and the columns' indicators finds the
+                // V's codes that are not finite went into the tile as 0: a product of the codes' and the columns' indicators finds the
                 // outputs that see one, which become NaN at the end
                 // (tile by tile of query rows, the codes' indicators made anew for each: 32 registers less)
 #pragma unroll
@@ -859,7 +868,7 @@ __device__ __forceinline__ void k8_chunk_block(const Kv8AttnArgs& a, int few, in
                     uint32_t n[2];
 #pragma unroll
                     for (int e = 0; e < 2; ++e) {
-                        n[e] = nan_any[buf][2 * hf + e] ? nan_at[buf][2 * hf + e][lane] : 0u;
+                        n[e] = odd_any[buf][2 * hf + e] ? odd_at[buf][2 * hf + e][lane] : 0u;
                         asm("" : "+v"(n[e]));
                     }
                     u32x4_k8 sw;
@@ -882,7 +891,7 @@ __device__ __forceinline__ void k8_chunk_block(const Kv8AttnArgs& a, int few, in
                         for (int i = 0; i < 4; ++i) {
                             uint32_t one = hit[i] > 0.0f ? 1u : 0u;
                             asm("" : "+v"(one));  // (shifted, not chosen from 32 constants that would take registers)
-                            nan_out[u] |= one << (4 * d + i);
+                            odd_out[u] |= one << (4 * d + i);
                         }
                     }
                 }
@@ -907,7 +916,7 @@ __device__ __forceinline__ void k8_chunk_block(const Kv8AttnArgs& a, int few, in
         for (int d = 0; d < DT; ++d)
 #pragma unroll
             for (int i = 0; i < 4; ++i)
-                if (nan_out[u] >> (4 * d + i) & 1u) acc.o[u][d][i] = __builtin_nanf("");
+                if (odd_out[u] >> (4 * d + i) & 1u) acc.o[u][d][i] = __builtin_nanf("");
     }
     __syncthreads();
     f32x4_k8* other = reinterpret_cast<f32x4_k8*>(sh.tile[1]) + wave * (NT * DT * 64) + lane;

@@ -3,8 +3,11 @@ definitions in float64 and Python integers (_kv8_ref.py), each row of an attenti
 its own probabilities."""
 import numpy as np
 import pytest
+import torch
 
 import _kv8_ref as ref
+from _gpu_common import dev_i32
+from paper_2605_30218_amd import mg
 from test_gpu_kv8 import Batch
 
 pytestmark = pytest.mark.gpu
@@ -50,3 +53,63 @@ def test_window_of_rows_longer_than_their_page_table(window, new):
     b = Batch([64, 64, 64, 64], new, 8, 2, 64, seed=1, spare=0)
     b.lens = np.array([1000, 1000, PAST, min(3, new[3] - 1)])
     run_and_compare(b, window=window)
+
+
+# ---------------------------------------------------------------- values that are not finite in bf16
+
+
+def store_one(b, row, pos, head, side, d, x, others=0.0):
+    """The page of the row's position anew: x at (pos, head, side, d), `others` elsewhere in that head and side."""
+    hkv = b.codes.shape[1]
+    page = int(b.table[row, pos // 16])
+    old_k, old_v = mg.kv8_read(b.codes, b.scales, dev_i32(16 * page + np.arange(16)))
+    kv = [old_k, old_v]
+    kv[side][:, head] = others
+    kv[side][pos % 16, head, d] = x
+    mg.kv8_append(b.codes, b.scales, *kv, dev_i32(16 * page + np.arange(16)))
+
+
+def not_finite_as_nan(b):
+    """The cache with NaN for the values of V that bf16 does not hold."""
+    c = ref.RefCache.of(b.codes, b.scales)
+    v = c.val[:, :, 1]
+    v[np.abs(v) >= 2.0 ** 128] = np.nan
+    return c
+
+
+@pytest.mark.parametrize("hd", [64, 128])
+@pytest.mark.parametrize("new", [[1, 1, 1], [4, 2, 3], [12, 16, 9], [100, 1, 65]])
+@pytest.mark.parametrize("window", [0, 40])
+@pytest.mark.parametrize("x", [3.38e38, -3.38e38])
+def test_a_value_that_reads_as_infinity_reaches_only_who_sees_it(hd, new, window, x):
+    """V above 1.9375 * 2^127 at the last position, behind the length and before the window."""
+    b = Batch(np.add([50, 77, 200], new), new, 4, 2, hd, seed=7)
+    L = b.lens
+    store_one(b, 0, int(L[0]) - 1, 0, 1, 3, x)
+    store_one(b, 0, 2, 1, 1, 5, x)
+    if L[1] % 16:
+        store_one(b, 1, int(L[1]), 1, 1, 9, x)
+    store_one(b, 2, int(L[2]) - new[2] // 2 - 1, 1, 1, 40, x)
+    cache = not_finite_as_nan(b)
+    assert np.isnan(cache.val).any()
+    got = b.run(window=window)
+    got = compare(b, torch.where(got.isinf(), torch.nan, got), cache=cache, window=window)  # (who sees it: infinity or NaN)
+    assert np.isnan(got).any() and not np.isnan(got).all()
+
+
+@pytest.mark.parametrize("byte", [246, 247, 248, 251, 254])
+@pytest.mark.parametrize("new", [[1, 1], [5, 8], [70, 40]])
+@pytest.mark.parametrize("hd", [64, 128])
+def test_every_code_under_a_large_scale_has_no_effect_where_it_is_not_seen(byte, new, hd):
+    """The last page of a row: zeros up to the row's end, V's other positions hold every code under a scale whose larger
+    codes stand for infinity."""
+    b = Batch(np.add([36, 104], new) // 16 * 16 + 4, new, 4, 2, hd, seed=8)
+    idx = ref.byte_index(hd, 1)
+    for r in range(2):
+        page = int(b.table[r, (b.lens[r] - 1) // 16])
+        codes = np.zeros((2, 16 * hd), np.uint8)
+        codes[:, idx[4:].ravel()] = np.resize(np.arange(256), 12 * hd)
+        b.codes[page, :, 1] = torch.as_tensor(codes).cuda()
+        b.scales[page, :, 1] = byte
+    got = run_and_compare(b)
+    assert np.isfinite(got).all()
