@@ -218,7 +218,8 @@ mg_status mg_advance(mg_ctx* ctx, int B, const int32_t* emitted, int32_t* tokens
  * A page holds 16 positions.  Slot = page * 16 + position % 16.  The cache of one layer:
  *   codes  [n_pages][Hkv][K|V][16 * hd]  e4m3 values (OCP: 4 exponent bits, 3 mantissa bits,
  *          largest 448, no infinity, 0x7f / 0xff NaN)
- *   scales [n_pages][Hkv][K|V]           b = 0..255; a code stands for its value * 2^(b - 127)
+ *   scales [n_pages][Hkv][K|V]           b; a code stands for its value * 2^(b - 127).  0: nothing stored, else
+ *          16..254 (mg_kv8_append needs no more than 247 of its own; a page that another program filled may have more)
  * so one scale serves 16 positions of one KV head.  Order inside a page of a head, chosen so
  * that a wave reads matrix operands as contiguous 1 KiB runs:
  *   K: position t, feature d = 64 h + 16 g + j at byte ((h * 4 + g) * 16 + t) * 16 + j

@@ -45,6 +45,8 @@ __device__ __forceinline__ int need_byte(uint32_t mag) {
     const int b = (int)(mag >> 7) - 8 + ((mag & 0x7fu) > 0x60u);
     return max(b, KV8_MIN_BYTE);
 }
+// 2^(127 - b), for b up to 254, whose 2^-127 is below the normal range
+__device__ __forceinline__ float inverse(int b) { return __uint_as_float((uint32_t)max((254 - b) << 23, 0x00400000)); }
 // four finite bf16 values (two pairs) as codes: inv = 2^(127 - b)
 __device__ __forceinline__ uint32_t quant4(uint32_t lo, uint32_t hi, float inv) {
     const int w = __builtin_amdgcn_cvt_pk_fp8_f32(bf_lo(lo) * inv, bf_hi(lo) * inv, 0, false);
@@ -150,7 +152,7 @@ __device__ __forceinline__ void append_run(const Kv8& c, int t0, int s0, int o, 
     for (int side = 0; side < 2; ++side) {
         const int was = (int)(side ? ob >> 8 : ob & 0xffu);  // 0: the page starts anew
         const int b = max(was, need_byte(side ? top >> 16 : top & 0xffffu));
-        const float inv = __uint_as_float((uint32_t)(254 - b) << 23);
+        const float inv = inverse(b);
         const float shift = __uint_as_float((uint32_t)max(127 + was - b, 0) << 23);
         // positions of this lane's pieces that the run writes, as a byte mask of a word of V or all of K's piece
         uint32_t keep = 0;
@@ -258,7 +260,7 @@ __device__ __forceinline__ void append_singles(const Kv8& c, int t, int sl, int 
         if (live && b[side] != was && m == 0) c.scales[ph + side] = (uint8_t)b[side];
     }
     if (!live) return;
-    const float ik = __uint_as_float((uint32_t)(254 - b[0]) << 23), iv = __uint_as_float((uint32_t)(254 - b[1]) << 23);
+    const float ik = inverse(b[0]), iv = inverse(b[1]);
     uint8_t* kd = page + ((m * F / 16) * 16 + o) * 16 + m * F % 16;
 #pragma unroll
     for (int i = 0; i < F / 4; ++i) {

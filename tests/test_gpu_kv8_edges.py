@@ -8,7 +8,7 @@ import torch
 import _kv8_ref as ref
 from _gpu_common import dev_i32
 from paper_2605_30218_amd import mg
-from test_gpu_kv8 import Batch
+from test_gpu_kv8 import Batch, check_append, noisy_cache, rows_bf16
 
 pytestmark = pytest.mark.gpu
 
@@ -113,3 +113,19 @@ def test_every_code_under_a_large_scale_has_no_effect_where_it_is_not_seen(byte,
         b.scales[page, :, 1] = byte
     got = run_and_compare(b)
     assert np.isfinite(got).all()
+
+
+# ---------------------------------------------------------------- scale bytes
+
+
+@pytest.mark.parametrize("byte", [16, 230, 247, 253, 254])
+@pytest.mark.parametrize("hkv,hd", [(1, 64), (4, 128)])
+@pytest.mark.parametrize("start,n", [(3, 1), (3, 7), (20, 12)])
+def test_append_to_a_page_of_any_scale(byte, hkv, hd, start, n):
+    """Pages of another program under scales up to the largest: codes stay where the scale does, the new values are rounded
+    to it."""
+    rng = np.random.RandomState(byte)
+    codes, scales = noisy_cache(rng, 2, hkv, hd)
+    scales.fill_(byte)
+    k, v = (rows_bf16(rng, (n, hkv, hd)) * torch.tensor(2.0 ** (byte - 127)).to(torch.bfloat16) for _ in range(2))
+    check_append(codes, scales, k, v, np.arange(start, start + n, dtype=np.int32), ref.RefCache.of(codes, scales))
