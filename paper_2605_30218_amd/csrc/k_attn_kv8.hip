@@ -72,16 +72,14 @@ __device__ __forceinline__ float k8_col_sum(float v) {
 
 // What a row's tokens see: token i stands at p0 + i and sees the mapped positions of [0, len) that are
 // <= p0 + i and, with a window, > p0 + i - window.  A token stands anywhere below 2^31 (past the page table too) and a
-// window is any, so the comparisons are of differences that stay within 32 bits.
+// window is any, so p - window is only taken where it is at least -1.
 struct K8Row {
     int t0, n;      // its tokens of q
     int len, p0;    // positions in reach of the page table; position of its first token
     int pga, pgb;   // pages that any of its tokens sees: [pga, pgb)
 };
-// the first position of [0, len] that a token at p may see
-__device__ __forceinline__ int k8_first(int window, int p, int len) {
-    return window && p >= window ? min(p - window + 1, len) : 0;
-}
+// the last position that the window hides from a token at p, or -1
+__device__ __forceinline__ int k8_hidden(int window, int p) { return max(p, window - 1) - window; }
 __device__ __forceinline__ int k8_token(const Kv8AttnArgs& a, int t) { return min(max(t, 0), a.T); }
 __device__ __forceinline__ K8Row k8_row(const Kv8AttnArgs& a, int r) {
     K8Row x;
@@ -90,7 +88,7 @@ __device__ __forceinline__ K8Row k8_row(const Kv8AttnArgs& a, int r) {
     const int len = max(a.lens[r], 0);
     x.len = min(len, 16 * a.maxp);
     x.p0 = len - x.n;
-    x.pga = k8_first(a.window, x.p0, x.len) / 16;
+    x.pga = a.window ? min(k8_hidden(a.window, x.p0) + 1, x.len) / 16 : 0;
     x.pgb = (x.len + 15) / 16;
     return x;
 }
@@ -235,7 +233,7 @@ __device__ __forceinline__ void k8_scores(const uint4 (&kb)[2][HD / 64], const f
 // mapped bit e whether page e is one of the cache's.
 __device__ __forceinline__ bool k8_sees(const K8Row& row, int window, int j0, int mapped, int g, int i, int p) {
     const int j = j0 + 16 * (i >> 2) + 4 * g + (i & 3);
-    return ((mapped >> (i >> 2)) & 1) && j <= p && j < row.len && (!window || p - j < window);
+    return ((mapped >> (i >> 2)) & 1) && j <= p && j < row.len && (!window || j > k8_hidden(window, p));
 }
 
 // The online softmax of a step.  The reference m moves only when a row's probabilities of the step would sum to more than
@@ -461,7 +459,7 @@ __device__ __forceinline__ void k8_few_block(const Kv8AttnArgs& a, const K8Few& 
             }
             const int j0 = 16 * (ch + 2 * s);
             const bool edge = mapped != 3 || j0 + 31 > row.p0 || j0 + 32 > row.len ||
-                              (a.window && row.p0 + row.n - 1 - j0 >= a.window);
+                              (a.window && j0 <= k8_hidden(a.window, row.p0 + row.n - 1));
             float x[NT][8];
             k8_scores<HD, NT, CAP>(kb, ksc, qa, so, x);
             __builtin_amdgcn_sched_barrier(0);
@@ -647,7 +645,7 @@ template <int ROWS>
 __device__ __forceinline__ K8Span k8_span(const Kv8AttnArgs& a, const K8Row& row, int t, int nsplit) {
     const int p0 = row.p0 + t * ROWS / a.G, p1 = row.p0 + (min((t + 1) * ROWS, row.n * a.G) - 1) / a.G;
     K8Span x;
-    x.pg0 = k8_first(a.window, p0, row.len) / 16;
+    x.pg0 = a.window ? min(k8_hidden(a.window, p0) + 1, row.len) / 16 : 0;
     x.pg1 = max(0, min(p1 + 1, row.len) + 15) / 16;
     x.stages = max(0, (x.pg1 - x.pg0 + K8_STAGE - 1) / K8_STAGE);
     x.act = max(1, min(nsplit, x.stages / K8_MIN_STAGES));
@@ -820,9 +818,9 @@ __device__ __forceinline__ void k8_chunk_block(const Kv8AttnArgs& a, int few, in
         for (int hf = 0; hf < K8_STAGE / 2; ++hf) {
             const int j0 = 16 * (pg0 + st * K8_STAGE) + 32 * hf;
             // whether there is anything for this wave's tokens in these 32 positions
-            const bool any = j0 <= wp1 && !(a.window && wp0 - j0 - 31 >= a.window);
+            const bool any = j0 <= wp1 && !(a.window && j0 + 31 <= k8_hidden(a.window, wp0));
             const int mapped = now >> (2 * hf) & 3;
-            const bool edge = mapped != 3 || j0 + 31 > wp0 || j0 + 32 > row.len || (a.window && wp1 - j0 >= a.window);
+            const bool edge = mapped != 3 || j0 + 31 > wp0 || j0 + 32 > row.len || (a.window && j0 <= k8_hidden(a.window, wp1));
             if (hf == 1) {
                 read_k(1, 1, kf);
                 __builtin_amdgcn_sched_barrier(0);
