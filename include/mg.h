@@ -250,7 +250,8 @@ size_t mg_kv8_scale_bytes(int n_pages, int n_kv_heads, int head_dim);
  *   cu_new [B + 1]: tokens of the admitted rows before row b;  lens [B]: positions after the call
  *   (ctx_len[b] where not admitted, 0 where that is negative);  admitted [B] 0 or 1;
  *   positions, rows, slots [max_tokens]: of every new token, row by row, positions ascending
- *   (the item lists of mg_prefill; the slots of mg_kv8_append), -1 behind the last;
+ *   (the item lists of mg_prefill; the slots of mg_kv8_append), -1 behind the last; also the slot of a
+ *   token whose page-table entry is no page (outside 0 .. 2^27 - 1);
  *   *n_left: free pages that remain, so that free_pages[0 .. *n_left) is the next call's list.
  * free_pages must be distinct pages that no row holds.  1 <= B <= 1024.  All pointers [device];
  * n_left must not be n_free, nor lens be ctx_len (blocks of the launch read one while others

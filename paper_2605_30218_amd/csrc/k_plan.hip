@@ -122,7 +122,8 @@ __global__ __launch_bounds__(PL_THREADS) void batch_plan_kernel(PlanArgs a) {
             row = row_of(tok0, a.B, i);
             pos = ctx_s[row] + i - tok0[row];
             const int have = (ctx_s[row] + 15) / 16, pg = pos / 16;
-            slot = (pg < have ? a.page_table[(size_t)row * a.maxp + pg] : a.free_pages[n_free - 1 - (pg0[row] + pg - have)]) * 16 + pos % 16;
+            const int page = pg < have ? a.page_table[(size_t)row * a.maxp + pg] : a.free_pages[n_free - 1 - (pg0[row] + pg - have)];
+            slot = (uint32_t)page < 1u << 27 ? page * 16 + pos % 16 : -1;  // (any other id's slot would be another page's)
         }
         a.positions[i] = pos;
         a.rows[i] = row;

@@ -129,3 +129,17 @@ def test_append_to_a_page_of_any_scale(byte, hkv, hd, start, n):
     scales.fill_(byte)
     k, v = (rows_bf16(rng, (n, hkv, hd)) * torch.tensor(2.0 ** (byte - 127)).to(torch.bfloat16) for _ in range(2))
     check_append(codes, scales, k, v, np.arange(start, start + n, dtype=np.int32), ref.RefCache.of(codes, scales))
+
+
+# ---------------------------------------------------------------- the plan
+
+
+def test_plan_gives_no_slot_on_a_page_that_is_not_there():
+    """A row whose table lacks the page of its next position: no slot of another page stands for it."""
+    missing = [-1, -2 ** 27, -2 ** 31, 2 ** 27, 2 ** 31 - 1, -2 ** 28 + 3]
+    table = np.full((len(missing), 3), -1, np.int32)
+    table[:, 0] = missing
+    p = mg.batch_plan(dev_i32([5] * 6), dev_i32([13] * 6), dev_i32(np.arange(40)), dev_i32([40]), dev_i32(table), 100)
+    slots, at = p.slots.cpu().numpy()[:78].reshape(6, 13), 39 - np.arange(6)
+    assert (slots[:, :11] == -1).all()
+    np.testing.assert_array_equal(slots[:, 11:], 16 * at[:, None] + [0, 1])
