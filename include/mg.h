@@ -254,8 +254,8 @@ size_t mg_kv8_scale_bytes(int n_pages, int n_kv_heads, int head_dim);
  *   token whose page-table entry is no page (outside 0 .. 2^27 - 1);
  *   *n_left: free pages that remain, so that free_pages[0 .. *n_left) is the next call's list.
  * free_pages must be distinct pages that no row holds.  1 <= B <= 1024.  All pointers [device];
- * n_left must not be n_free, nor lens be ctx_len (blocks of the launch read one while others
- * write): MG_ERR_ARG. */
+ * no output may overlap an input or the page table, nor that an input (blocks of the launch read
+ * one while others write): MG_ERR_ARG. */
 mg_status mg_batch_plan(int B, int max_pages_per_row, const int32_t* ctx_len, const int32_t* n_new,
                         const int32_t* free_pages, const int32_t* n_free, int max_tokens, int32_t* page_table,
                         int32_t* cu_new, int32_t* lens, int32_t* admitted, int32_t* positions, int32_t* rows,

@@ -25,6 +25,15 @@ Kv8 view(const mg_kv8_cache* c) { return Kv8{c->codes, c->scales, c->n_pages, c-
 bool rows_ok(const mg_kv8_cache* c, const void* p, int64_t stride) {
     return aligned(p, 16) && stride % 8 == 0 && stride >= (int64_t)c->n_kv_heads * c->head_dim;
 }
+// n int32 values at p
+struct Ints {
+    const int32_t* p;
+    size_t n;
+    bool overlaps(const Ints& o) const {
+        const uintptr_t a = reinterpret_cast<uintptr_t>(p), b = reinterpret_cast<uintptr_t>(o.p);
+        return n && o.n && a < b + 4 * o.n && b < a + 4 * n;
+    }
+};
 mg_status status_of(hipError_t e) { return e == hipSuccess ? MG_OK : MG_ERR_HIP; }
 
 // compute units of the current device, looked up once a device (256 where that fails)
@@ -105,7 +114,17 @@ mg_status mg_batch_plan(int B, int max_pages_per_row, const int32_t* ctx_len, co
     if (!ctx_len || !n_new || !free_pages || !n_free || !page_table || !cu_new || !lens || !admitted || !n_left)
         return MG_ERR_ARG;
     if (max_tokens && (!positions || !rows || !slots)) return MG_ERR_ARG;
-    if (n_left == n_free || lens == ctx_len) return MG_ERR_ARG;
+    // blocks of the launch read the inputs while others write (of the free pages the host knows the first alone)
+    const size_t rows_n = B, items = max_tokens;
+    const Ints table{page_table, rows_n * max_pages_per_row};
+    const Ints in[] = {{ctx_len, rows_n}, {n_new, rows_n}, {n_free, 1}, {free_pages, 1}, table};
+    const Ints out[] = {{cu_new, rows_n + 1}, {lens, rows_n}, {admitted, rows_n}, {positions, items},
+                        {rows, items},        {slots, items}, {n_left, 1}};
+    for (const Ints& i : in)
+        for (const Ints& o : out)
+            if (i.overlaps(o)) return MG_ERR_ARG;
+    for (int i = 0; i < 4; ++i)
+        if (in[i].overlaps(table)) return MG_ERR_ARG;
     PlanArgs a{B,          max_pages_per_row, max_tokens, ctx_len, n_new,     free_pages, n_free, page_table,
                cu_new,     lens,              admitted,   positions, rows,    slots,      n_left};
     return status_of(launch_batch_plan(a, static_cast<hipStream_t>(stream)));

@@ -1,0 +1,26 @@
+"""Calls of the batch plan and of the 8-bit K/V cache that are refused (CPU): buffers that overlap, shapes and numbers that
+the C structures would hold as others.  The pointers of the refused calls are never followed."""
+import pytest
+
+from paper_2605_30218_amd import mg
+
+ARG = -1
+NAMES = ("ctx_len", "n_new", "free_pages", "n_free", "page_table", "cu_new", "lens", "admitted", "positions", "rows", "slots",
+         "n_left")
+
+
+def plan_status(B=300, maxp=8, most=500, **at):
+    """The status of a plan whose buffers stand 1 MiB apart, but for those whose addresses are given."""
+    p = {n: (i + 1) << 20 for i, n in enumerate(NAMES)} | at
+    return mg.load().mg_batch_plan(B, maxp, p["ctx_len"], p["n_new"], p["free_pages"], p["n_free"], most, *[p[n] for n in NAMES[4:]],
+                                   None)
+
+
+@pytest.mark.parametrize("name,out", [(i, o) for i in NAMES[:5] for o in NAMES[4:] if i != o])
+def test_plan_outputs_on_its_inputs_are_refused(name, out):
+    """Blocks of the launch read the inputs while others write: the same buffer, its last value, the value before it."""
+    at = (NAMES.index(name) + 1) << 20
+    values = {"ctx_len": 300, "n_new": 300, "n_free": 1, "free_pages": 1, "page_table": 300 * 8}[name]
+    length = {"page_table": 300 * 8, "cu_new": 301, "lens": 300, "admitted": 300, "n_left": 1}.get(out, 500)
+    for shift in (0, 4 * (values - 1), -4 * (length - 1)):
+        assert plan_status(**{out: at + shift}) == ARG, shift
