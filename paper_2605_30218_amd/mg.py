@@ -347,7 +347,7 @@ def batch_plan(ctx_len, n_new, free_pages, n_free, page_table, max_tokens, out=N
 def _kv8(codes, scales):
     """The MgKv8Cache of a layer's codes [n_pages, Hkv, 2, 16 hd] and scales [n_pages, Hkv, 2]."""
     shape = codes.shape
-    if codes.dtype is not torch.uint8 or len(shape) != 4 or shape[2] != 2 or not codes.is_contiguous():
+    if codes.dtype is not torch.uint8 or len(shape) != 4 or shape[2] != 2 or shape[3] % 16 or not codes.is_contiguous():
         _refuse("codes", codes, "contiguous uint8 [n_pages, Hkv, 2, 16 hd]")
     if scales.dtype is not torch.uint8 or scales.shape != shape[:3] or not scales.is_contiguous() or \
             scales.device != codes.device:

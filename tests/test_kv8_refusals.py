@@ -1,6 +1,7 @@
 """Calls of the batch plan and of the 8-bit K/V cache that are refused (CPU): buffers that overlap, shapes and numbers that
 the C structures would hold as others.  The pointers of the refused calls are never followed."""
 import pytest
+import torch
 
 from paper_2605_30218_amd import mg
 
@@ -24,3 +25,16 @@ def test_plan_outputs_on_its_inputs_are_refused(name, out):
     length = {"page_table": 300 * 8, "cu_new": 301, "lens": 300, "admitted": 300, "n_left": 1}.get(out, 500)
     for shift in (0, 4 * (values - 1), -4 * (length - 1)):
         assert plan_status(**{out: at + shift}) == ARG, shift
+
+
+def cpu_call(hd=64, width=None, call=mg.kv8_attention, **kw):
+    """An attention call on CPU tensors, which the binding refuses at the latest for where they are."""
+    codes, scales = (torch.zeros(s, dtype=torch.uint8) for s in ((4, 2, 2, width or 16 * hd), (4, 2, 2)))
+    q = torch.zeros((3, 4, hd), dtype=torch.bfloat16)
+    return call(codes, scales, q, torch.zeros((3, 4), dtype=torch.int32), torch.zeros(3, dtype=torch.int32), **kw)
+
+
+@pytest.mark.parametrize("width", [1030, 1025, 1039, 2056])
+def test_codes_of_no_whole_head_are_refused(width):
+    with pytest.raises(ValueError, match="codes"):
+        cpu_call(width=width)
