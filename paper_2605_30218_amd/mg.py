@@ -273,6 +273,7 @@ def margin_gate_noalloc(B, V, logits, protected_mask, tau, top1, margin, gate, g
 
 BatchPlan = collections.namedtuple("BatchPlan", "cu_new lens admitted positions rows slots n_left")
 _BF16 = (torch.bfloat16, torch.int16)
+_I32 = 1 << 31
 _raw_stream = torch._C._cuda_getCurrentRawStream if hasattr(torch._C, "_cuda_getCurrentRawStream") else None
 
 _current_device = getattr(torch._C, "_cuda_getDevice", torch.cuda.current_device)
@@ -410,6 +411,13 @@ def _attn_args(c, q, page_table, lens, cu_new, max_new, max_len, scale, window, 
         _refuse("page_table", page_table, "[B, max_pages]")
     T, Hq, hd = q.shape
     B, maxp = page_table.shape
+    # (ctypes takes what passes 32 bits without a word)
+    if not (-_I32 <= max_new < _I32 and -_I32 <= max_len < _I32 and -_I32 <= window < _I32):
+        for name, n in (("max_new", max_new), ("max_len", max_len), ("window", window)):
+            if not -_I32 <= n < _I32:
+                _refuse(name, n, "an int32")
+    if scale and abs(scale) < 1e-30 or softcap and abs(softcap) < 1e-30:
+        _refuse("scale, softcap", (scale, softcap), "0 or 1e-15 .. 1e15")
     qp, qs = _rows16("q", q, T, Hq, hd, dev)
     op, os_ = (None, Hq * hd) if out is None else _rows16("out", out, T, Hq, hd, dev)
     return MgKv8AttnArgs(B, T, Hq, max_new, max_len, maxp, window, 0.0 if scale is None else scale, softcap, qp, qs, op,

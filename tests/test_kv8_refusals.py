@@ -38,3 +38,20 @@ def cpu_call(hd=64, width=None, call=mg.kv8_attention, **kw):
 def test_codes_of_no_whole_head_are_refused(width):
     with pytest.raises(ValueError, match="codes"):
         cpu_call(width=width)
+
+
+@pytest.mark.parametrize("name", ["max_new", "max_len", "window"])
+@pytest.mark.parametrize("value", [2 ** 31, 2 ** 32 + 5, 2 ** 40, -2 ** 31 - 1, -2 ** 32 + 7])
+@pytest.mark.parametrize("call", [mg.kv8_attention, mg.kv8_attention_workspace_bytes])
+def test_numbers_past_32_bits_are_refused(name, value, call):
+    """The call's structure holds 32 bits: a window of 2^32 + 5 would be one of 5."""
+    with pytest.raises(ValueError, match=name):
+        cpu_call(call=call, **{name: value})
+
+
+@pytest.mark.parametrize("name", ["scale", "softcap"])
+@pytest.mark.parametrize("value", [1e-50, -1e-50, 1e-300])
+def test_factors_that_are_zero_in_32_bits_are_refused(name, value):
+    """0 stands for the default scale, and for no cap."""
+    with pytest.raises(ValueError, match=name):
+        cpu_call(**{name: value})
