@@ -411,6 +411,8 @@ def _attn_args(c, q, page_table, lens, cu_new, max_new, max_len, scale, window, 
         _refuse("page_table", page_table, "[B, max_pages]")
     T, Hq, hd = q.shape
     B, maxp = page_table.shape
+    if max_new is None:  # without token offsets every row has one
+        max_new = 1 if cu_new is None else max(T, 1)
     # (ctypes takes what passes 32 bits without a word)
     if not (-_I32 <= max_new < _I32 and -_I32 <= max_len < _I32 and -_I32 <= window < _I32):
         for name, n in (("max_new", max_new), ("max_len", max_len), ("window", window)):
@@ -425,7 +427,7 @@ def _attn_args(c, q, page_table, lens, cu_new, max_new, max_len, scale, window, 
                          None if cu_new is None else _ints("cu_new", cu_new, dev, B + 1))
 
 
-def kv8_attention_workspace_bytes(codes, scales, q, page_table, lens, cu_new=None, max_new=1, max_len=0, window=0):
+def kv8_attention_workspace_bytes(codes, scales, q, page_table, lens, cu_new=None, max_new=None, max_len=0, window=0):
     """mg_kv8_attention_workspace_bytes of the call with these arguments (no device work): for a program
     that keeps a workspace, as one that captures its step does."""
     c = _kv8(codes, scales)
@@ -434,10 +436,12 @@ def kv8_attention_workspace_bytes(codes, scales, q, page_table, lens, cu_new=Non
         return load().mg_kv8_attention_workspace_bytes(C.byref(c), C.byref(a))
 
 
-def kv8_attention(codes, scales, q, page_table, lens, cu_new=None, max_new=1, max_len=0, scale=None, window=0,
+def kv8_attention(codes, scales, q, page_table, lens, cu_new=None, max_new=None, max_len=0, scale=None, window=0,
                   softcap=0.0, out=None, workspace=None, stream=None):
     """mg_kv8_attention: q [T, Hq, hd] attends over the cache's positions of its rows -> out [T, Hq, hd]
     bf16.  Tokens behind the last row's are not written: in a new tensor they hold anything.
+    max_new: at least the most tokens of any row; None: all of q's with cu_new, else one.  A program that knows
+    a lower bound gives it: the launch, and with it the time and a probability's bits, follow it.
     workspace: a contiguous uint8 tensor of kv8_attention_workspace_bytes that no other call in flight
     uses, or None to take one per call."""
     c = _kv8(codes, scales)

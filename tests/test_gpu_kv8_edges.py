@@ -18,11 +18,11 @@ def probability_bits(new, G):
     return [16 if max(new) * G <= 32 or n * G <= 16 else 8 for n in new]
 
 
-def compare(b, got, cache=None, **kw):
-    """got against the definition, row by row within the bound of the row's probabilities."""
+def compare(b, got, cache=None, bits=None, **kw):
+    """got against the definition, row by row within the bound of the row's probabilities (bits: the same for all)."""
     kw["scale"] = kw.get("scale") or 1 / np.sqrt(b.hd)
     cache = ref.RefCache.of(b.codes, b.scales) if cache is None else cache
-    got, bits = ref.bf16(got), probability_bits(b.new, b.G)
+    got, bits = ref.bf16(got), [bits] * len(b.new) if bits else probability_bits(b.new, b.G)
     for p_bits in sorted(set(bits)):
         out, bound = ref.attention(cache, ref.bf16(b.q), b.table, b.lens, b.cu, p_bits=p_bits, **kw)
         for r in range(len(b.new)):
@@ -38,6 +38,24 @@ def compare(b, got, cache=None, **kw):
 
 def run_and_compare(b, max_len=0, **kw):
     return compare(b, b.run(max_len=max_len, **kw), **kw)
+
+
+# ---------------------------------------------------------------- bounds that a caller need not give
+
+
+@pytest.mark.parametrize("new", [[1, 1, 1], [3, 1, 2], [4, 0, 9], [70, 1, 20], [0, 0, 0]])
+def test_rows_of_several_tokens_without_a_bound_on_them(new):
+    """Token offsets alone say how many tokens a row has: without max_new every one of them is answered."""
+    b = Batch(np.add([300, 5, 900], new), new, 8, 2, 64, seed=3)
+    args = b.codes, b.scales, b.q.cuda(), dev_i32(b.table), dev_i32(b.lens), dev_i32(b.cu)
+    n = mg.kv8_attention_workspace_bytes(*args)
+    ws = torch.empty(n, dtype=torch.uint8, device="cuda")
+    outs = []
+    for workspace in (None, ws):
+        out = torch.full(b.q.shape, 9.0, dtype=torch.bfloat16, device="cuda")
+        outs.append(mg.kv8_attention(*args, out=out, workspace=workspace))
+        compare(b, outs[-1], bits=8)
+    assert torch.equal(*outs)
 
 
 # ---------------------------------------------------------------- windows
