@@ -296,6 +296,8 @@ def _call(name, device, stream, fn, *args):
     """fn(*args, stream) on the tensors' device, on the given stream or the device's current one."""
     if device.type != "cuda":
         raise ValueError(f"{name}: tensors on the GPU are needed, got {device}")
+    if stream is not None and stream.device != device:
+        raise ValueError(f"{name}: a stream of {device} is needed, got one of {stream.device}")
     if device.index != _current_device():
         with torch.cuda.device(device):
             return _call(name, device, stream, fn, *args)

@@ -55,3 +55,15 @@ def test_factors_that_are_zero_in_32_bits_are_refused(name, value):
     """0 stands for the default scale, and for no cap."""
     with pytest.raises(ValueError, match=name):
         cpu_call(**{name: value})
+
+
+def test_a_stream_of_another_device_is_refused():
+    """Its kernels would run there, on memory that need not be mapped."""
+    class Stream:
+        device, cuda_stream = torch.device("cuda", 1), 0
+
+    def never(*_):
+        raise AssertionError("the call was made")
+
+    with pytest.raises(ValueError, match="stream"):
+        mg._call("mg_kv8_attention", torch.device("cuda", 0), Stream(), never)
