@@ -8,7 +8,7 @@ import torch
 import _kv8_ref as ref
 from _gpu_common import dev_i32
 from paper_2605_30218_amd import mg
-from test_gpu_kv8 import Batch, check_append, noisy_cache, rows_bf16
+from test_gpu_kv8 import Batch, check_append, check_plan, noisy_cache, rows_bf16, tables
 
 pytestmark = pytest.mark.gpu
 
@@ -149,7 +149,108 @@ def test_append_to_a_page_of_any_scale(byte, hkv, hd, start, n):
     check_append(codes, scales, k, v, np.arange(start, start + n, dtype=np.int32), ref.RefCache.of(codes, scales))
 
 
+# ---------------------------------------------------------------- every refill of the page ids, every variant
+
+
+def with_holes(b, seed):
+    rng = np.random.RandomState(seed)
+    for r in range(len(b.lens)):
+        n = -(-int(b.lens[r]) // 16)
+        if n < 24:
+            continue
+        at = np.concatenate([rng.randint(0, n, n // 12), [x for x in (31, 32, 33, 63, 64, 65, 127, 128, 180, 212) if x < n - 8]])
+        b.table[r, at.astype(np.int64)] = rng.choice([-1, -9, 10 ** 6], len(at))
+    return b
+
+
+@pytest.mark.parametrize("hd", [64, 128])
+@pytest.mark.parametrize("holes,window", [(False, 0), (True, 0), (True, 3100)])
+def test_chunks_whose_groups_pass_many_pages(hd, holes, window):
+    """Tiles that one block takes whole: up to 150 pages a group of waves, so their ids are fetched three times."""
+    b = Batch(np.add([4500, 10, 0, 2100], 130), [130] * 4, 32, 8, hd, seed=31)
+    run_and_compare(with_holes(b, 1) if holes else b, window=window)
+
+
+@pytest.mark.parametrize("holes", [False, True])
+@pytest.mark.parametrize("ctx,new", [([4000], [200]), ([9000, 3], [64, 33])])
+def test_split_chunks_of_long_contexts(holes, ctx, new):
+    b = Batch(np.add(ctx, new), new, 16, 4, 64, seed=32)
+    run_and_compare(with_holes(b, 2) if holes else b)
+
+
+@pytest.mark.parametrize("hq,hkv,rows", [(8, 2, 3), (32, 8, 7)])
+@pytest.mark.parametrize("hd", [64, 128])
+@pytest.mark.parametrize("holes,window,cap", [(False, 0, 0.0), (True, 0, 0.0), (True, 4700, 20.0)])
+def test_long_short_rows_beside_a_chunk(hq, hkv, rows, hd, holes, window, cap):
+    """Rows of few tokens that are split and joined in the launch of the chunks: at 128 pages a split where these rows'
+    blocks are few, at 256 where they are not."""
+    new = [1, 60, 4] + [1] * (rows - 3)
+    ctx = [6000, 90, 5200] + [20 + 700 * i for i in range(rows - 3)]
+    b = Batch(np.add(ctx, new), new, hq, hkv, hd, seed=33)
+    run_and_compare(with_holes(b, 3) if holes else b, window=window, softcap=cap)
+
+
+@pytest.mark.parametrize("hd", [64, 128])
+@pytest.mark.parametrize("new", [1, 3])
+def test_splits_of_many_pages(hd, new):
+    """65 rows, so that the blocks do not share the lengths: splits of up to 128 pages, whose ids are fetched twice."""
+    lens = [9, 3100, 40, 2900] + [20 + i for i in range(61)]
+    run_and_compare(with_holes(Batch(lens, [new] * 65, 16, 8, hd, seed=34), 4))
+
+
+@pytest.mark.parametrize("hd", [64, 128])
+@pytest.mark.parametrize("holes,window,cap", [(True, 0, 0.0), (False, 900, 0.0), (False, 0, 20.0), (True, 2500, 50.0)])
+@pytest.mark.parametrize("hq,new", [(8, 1), (32, 1), (28, 4), (32, 5)])
+def test_even_splits_with_holes_windows_and_caps(hq, new, hd, holes, window, cap):
+    """One long row among many: splits that follow all rows' lengths, of one tile of query rows and of two."""
+    hkv = 4 if hq == 28 else 8
+    lens = [7000, 0, 40, 3000] + [5 * i + 6 for i in range(44)]
+    b = Batch(lens, [min(new, n) if i % 7 else 1 for i, n in enumerate(lens)], hq, hkv, hd, seed=35)
+    run_and_compare(with_holes(b, 5) if holes else b, window=window, softcap=cap)
+
+
+@pytest.mark.parametrize("hq,hkv,hd", [(32, 8, 128), (28, 4, 128), (4, 2, 64)])
+@pytest.mark.parametrize("new", [[1, 1, 1], [4, 2, 4], [10, 16, 12], [80, 1, 3]])
+@pytest.mark.parametrize("cap,window", [(0.5, 0), (30.0, 0), (30.0, 90), (1e5, 0)])
+def test_caps_on_every_kind_of_block(hq, hkv, hd, new, cap, window):
+    run_and_compare(Batch(np.add([300, 5, 1300], new), new, hq, hkv, hd, seed=36), softcap=cap, window=window)
+
+
+@pytest.mark.parametrize("hq,hkv,hd", [(28, 4, 128), (32, 8, 128), (4, 2, 64)])
+@pytest.mark.parametrize("new", [[4, 3, 4], [8, 1, 5], [60, 2, 1, 4]])
+def test_probabilities_keep_their_bits(hq, hkv, hd, new):
+    """16 bits for rows of up to 32 query rows among their kind, and for rows of up to 16 beside longer ones."""
+    b = Batch(np.add([400, 90, 1500, 33][:len(new)], new), new, hq, hkv, hd, seed=37)
+    run_and_compare(b)
+
+
+@pytest.mark.parametrize("x", [np.inf, -np.inf])
+@pytest.mark.parametrize("new", [[1, 1, 1], [6, 2, 4], [40, 1, 30]])
+def test_an_infinite_query_stays_in_its_row(x, new):
+    b = Batch(np.add([50, 77, 200], new), new, 4, 2, 64, seed=8)
+    b.q[b.cu[1] - 1, 2, 7] = float(x)
+    got = ref.bf16(b.run())
+    clean = b.q.clone()
+    clean[b.cu[1] - 1, 2, 7] = 0.0
+    out, bound = ref.attention(ref.RefCache.of(b.codes, b.scales), ref.bf16(clean), b.table, b.lens, b.cu, 1 / 8,
+                               p_bits=8 if max(new) > 16 else 16)
+    ok = np.abs(got - out) <= bound
+    ok[b.cu[1] - 1, 2] = True
+    assert ok.all()
+
+
 # ---------------------------------------------------------------- the plan
+
+
+@pytest.mark.parametrize("n_free,most,admitted", [(100, 100, [1, 1, 1, 1, 1]), (4, 100, [1, 1, 1, 0, 0]), (3, 100, [1, 1, 0, 0, 0]),
+                                                  (100, 39, [1, 1, 0, 0, 0]), (100, 20, [1, 1, 0, 0, 0]), (0, 100, [0, 0, 0, 0, 0]),
+                                                  (100, 0, [0, 0, 0, 0, 0])])
+def test_plan_admits_these_rows(n_free, most, admitted):
+    """Rows of 20, 0, 20, 1 and 0 new tokens, of 2, 0, 2, 1 and 0 new pages."""
+    ctx, new = np.array([0, 7, 16, 32, 5]), np.array([20, 0, 20, 1, 0])
+    table, free = tables(np.random.RandomState(0), ctx, 4, 100)
+    got = check_plan(ctx, new, free, n_free, table, most)
+    assert got["admitted"].tolist() == admitted
 
 
 def test_plan_gives_no_slot_on_a_page_that_is_not_there():
