@@ -323,8 +323,8 @@ def _new(shape, dtype, device, stream):
 
 def batch_plan(ctx_len, n_new, free_pages, n_free, page_table, max_tokens, out=None, stream=None):
     """mg_batch_plan: pages, slots and per-token lists of a batch from its requests' lengths.  All
-    tensors int32 on one GPU: ctx_len, n_new [B], free_pages [any], n_free [1] (the count in use),
-    page_table [B, max_pages] (updated in place).  out: a BatchPlan to write into, whose tensors the
+    tensors int32 on one GPU: ctx_len, n_new [B], free_pages [any], n_free [1] (the count in use, at
+    most free_pages' length), page_table [B, max_pages] (updated in place).  out: a BatchPlan to write into, whose tensors the
     caller keeps (a captured step), or None for new ones."""
     dev, M = ctx_len.device, int(max_tokens)
     if page_table.dim() != 2:
@@ -332,8 +332,10 @@ def batch_plan(ctx_len, n_new, free_pages, n_free, page_table, max_tokens, out=N
     if not 0 <= M <= 1 << 30:
         _refuse("max_tokens", M, "0 .. 2^30")
     B, maxp = page_table.shape
-    args = (_ints("ctx_len", ctx_len, dev, B), _ints("n_new", n_new, dev, B), _ints("free_pages", free_pages, dev),
-            _ints("n_free", n_free, dev, 1), M, _ints("page_table", page_table, dev))
+    count = _ints("n_free", n_free, dev, 1)
+    args = (_ints("ctx_len", ctx_len, dev, B), _ints("n_new", n_new, dev, B),
+            _ints("free_pages", free_pages, dev) or count,  # (an empty list has no address, and none is read)
+            count, M, _ints("page_table", page_table, dev))
     if out is None:
         buf = _new(3 * M + 3 * B + 2, torch.int32, dev, stream)
         cu, lens, adm, pos, row, slot, left = torch.unsafe_split_with_sizes(buf, (B + 1, B, B, M, M, M, 1))

@@ -262,3 +262,11 @@ def test_plan_gives_no_slot_on_a_page_that_is_not_there():
     slots, at = p.slots.cpu().numpy()[:78].reshape(6, 13), 39 - np.arange(6)
     assert (slots[:, :11] == -1).all()
     np.testing.assert_array_equal(slots[:, 11:], 16 * at[:, None] + [0, 1])
+
+
+@pytest.mark.parametrize("new,admitted", [([1, 3, 0], [1, 1, 1]), ([0, 0, 0], [1, 1, 1]), ([1, 9, 2], [1, 0, 0])])
+def test_plan_without_a_free_page(new, admitted):
+    """An empty list of free pages: what fits the rows' own pages is admitted."""
+    ctx, table = np.array([5, 8, 30]), np.array([[3, -1], [0, -1], [2, 1]], np.int32)
+    got = check_plan(ctx, np.array(new), np.array([], np.int32), 0, table, 20)
+    assert got["admitted"].tolist() == admitted
