@@ -224,8 +224,8 @@ mg_status mg_advance(mg_ctx* ctx, int B, const int32_t* emitted, int32_t* tokens
  * that a wave reads matrix operands as contiguous 1 KiB runs:
  *   K: position t, feature d = 64 h + 16 g + j at byte ((h * 4 + g) * 16 + t) * 16 + j
  *   V: position t = 4 g + i, feature d = 64 h + 16 c + m at byte ((h * 4 + g) * 16 + m) * 16 + 4 c + i
- * A value read back is exact in bf16 (but for codes that stand for 2^128, which finite values above
- * 1.9375 * 2^127 round to: infinity).  A zeroed pool is an empty cache. */
+ * A value read back is exact in bf16 (but for codes that stand for 2^128 or more, infinity: finite values
+ * above 1.9375 * 2^127 round to 2^128).  A zeroed pool is an empty cache. */
 typedef struct {
     uint8_t* codes;   /* [device], 16-byte aligned */
     uint8_t* scales;  /* [device], 2-byte aligned */
@@ -281,8 +281,8 @@ mg_status mg_kv8_append(const mg_kv8_cache* cache, int n_tokens, const uint16_t*
 
 /* The values of n slots as bf16 rows (exact): slot slots[i]'s K [Hkv][hd] at k + i * k_stride and V
  * likewise; either of k, v may be NULL.  Rows of slots outside the cache are left as they were.
- * For handing a request's cache to the bf16 pool or to another program.  Alignment and strides as
- * in mg_kv8_append. */
+ * For handing a request's cache to another program (a context's bf16 pool keeps a page's positions head by
+ * head, so the caller places these rows there itself).  Alignment and strides as in mg_kv8_append. */
 mg_status mg_kv8_read(const mg_kv8_cache* cache, int n, const int32_t* slots, uint16_t* k, int64_t k_stride,
                       uint16_t* v, int64_t v_stride, void* stream);
 

@@ -7,7 +7,9 @@
 //
 // Measured (us of a call in a captured graph, hd 128): append of 64 single tokens over 8 KV heads 4.9, read of them 3.3; append of
 // 12000 tokens in runs over 4 KV heads 9.1 (37 MB, 4.1 TB/s), read 12.0 (3.1); of 50000 over 8 35 and 70 (307 MB: 8.8,
-// partly from the memory-side cache, and 4.4 TB/s; a large copy 4.9).
+// partly from the memory-side cache, and 4.4 TB/s; a large copy 4.9).  The read fetches 2.2 times the codes: a wave of four slots takes
+// 64 bytes of each 128-byte line of K and touches the lines of V twice where its slots pass a multiple of four, and the
+// other part belongs to the next block, on another XCD's L2.
 #include <type_traits>
 
 #include "mg_device.h"
