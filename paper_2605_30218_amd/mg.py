@@ -445,7 +445,7 @@ def kv8_attention(codes, scales, q, page_table, lens, cu_new=None, max_new=None,
     """mg_kv8_attention: q [T, Hq, hd] attends over the cache's positions of its rows -> out [T, Hq, hd]
     bf16.  Tokens behind the last row's are not written: in a new tensor they hold anything.
     max_new: at least the most tokens of any row; None: all of q's with cu_new, else one.  A program that knows
-    a lower bound gives it: the launch, and with it the time and a probability's bits, follow it.
+    a smaller number gives it: the launch, and with it the time and a probability's bits, follow it.
     workspace: a contiguous uint8 tensor of kv8_attention_workspace_bytes that no other call in flight
     uses, or None to take one per call."""
     c = _kv8(codes, scales)
