@@ -325,6 +325,97 @@ size_t mg_kv8_attention_workspace_bytes(const mg_kv8_cache* cache, const mg_kv8_
 mg_status mg_kv8_attention(const mg_kv8_cache* cache, const mg_kv8_attn_args* args, void* workspace,
                            size_t workspace_bytes, void* stream);
 
+/* ---- (6) a 4-bit paged K/V cache, with the rotation of positions ------------------------------
+ *
+ * As (5), at half a byte a value: pages of 16 positions, slots and plans are the same, and so is what is said there of
+ * contexts, allocations, graphs and streams.  The cache of one layer, in the microscaling format of 4 bits:
+ *   codes  [n_pages][Hkv][K|V][8 * hd]  two e2m1 values a byte, the low nibble first (0, 0.5, 1, 1.5, 2, 3, 4, 6, bit 3 the sign)
+ *   scales [n_pages][Hkv][hd / 2 + 16]  b; a code stands for its value * 2^(b - 127).  255: the block holds a value that is not
+ *          finite, and all of it reads as NaN; else 16..253 where mg_kv4_append wrote it, 0 where nothing is stored
+ * A block is 32 features of a position's key, or a position's whole value of a KV head; its scale is the least power of two whose
+ * sevenfold holds its largest magnitude (what lies between 6 and 7 times it becomes 6).  Codes are the nearest, ties to even.
+ * So a position's codes depend on its own row alone, and nothing is rounded twice.  Order inside a page of a head:
+ *   K: position t, feature d = 32 g + j at byte (g * 16 + t) * 16 + j / 2, nibble j % 2; scale byte g * 16 + t
+ *   V: position t = 4 g + i, feature d = 16 c + m at byte (g * 16 + m) * hd / 8 + 2 c + i / 2, nibble i % 2; scale byte hd / 2 + t
+ * which is the order of the matrix instructions' 4-bit operands.  A value read back is exact in bf16 (but for codes that stand for
+ * 2^128 or more, infinity: finite values from 1.75 * 2^127 may become such a one).  A zeroed pool is an empty cache. */
+typedef struct {
+    uint8_t* codes;   /* [device], 16-byte aligned */
+    uint8_t* scales;  /* [device], 4-byte aligned */
+    int32_t n_pages;  /* 1..2^27 - 1, n_pages * n_kv_heads < 2^31 */
+    int32_t n_kv_heads;
+    int32_t head_dim; /* 64 or 128 */
+} mg_kv4_cache;
+
+/* Bytes of the two buffers of one layer (0 if the shape is unsupported). */
+size_t mg_kv4_code_bytes(int n_pages, int n_kv_heads, int head_dim);
+size_t mg_kv4_scale_bytes(int n_pages, int n_kv_heads, int head_dim);
+
+/* The new tokens' rows of a QKV projection into the cache, rotated on the way: for token i with position p = positions[i], every
+ * query head of q (n_q_heads of them; 0: none, q and q_out are not read) is rotated and written to q_out, every key of k is rotated
+ * and stored at slots[i], and v is stored there as it is.  Rotating a head x by p: with c, s = rope[p][2 j], rope[p][2 j + 1],
+ *   x'[j] = x[j] c - x[j + hd / 2] s,  x'[j + hd / 2] = x[j + hd / 2] c + x[j] s,   j < hd / 2,
+ * products and sums each rounded to fp32, x' to bf16 (the table and the arithmetic of mg_decode_step).  positions NULL: nothing is
+ * rotated (rope is not read; q is copied to q_out).
+ * Tokens with a negative position are left out: nothing is written for them.  A slot outside the cache stores nothing (its q is
+ * rotated).  A position of n_positions or more has no angle: its q_out and key become NaN.
+ * The tokens of four aligned positions of a page (4 g .. 4 g + 3) stand within four consecutive tokens of the call, as
+ * mg_batch_plan lists them: else the values (not the keys) of these four positions are undefined.  Two tokens with the same slot
+ * leave its key undefined, and its value is the later token's (if they stand so).
+ * q, k, v, q_out bf16 [n][heads][hd], 16-byte aligned, strides in values, multiples of 8 and >= heads * hd.  q_out may be q
+ * itself (with q's stride); else no written row may overlap a row of q, k or v: MG_ERR_ARG.  At most 2^26 (token, head) pairs of q and k a
+ * call.  slots, positions int32 [n]; rope fp32 [n_positions][hd], 16-byte aligned. */
+typedef struct {
+    int32_t n_tokens;
+    int32_t n_q_heads;         /* 0..4096 */
+    const uint16_t* q;
+    int64_t q_stride;
+    uint16_t* q_out;
+    int64_t q_out_stride;
+    const uint16_t* k;
+    int64_t k_stride;
+    const uint16_t* v;
+    int64_t v_stride;
+    const int32_t* slots;
+    const int32_t* positions;  /* or NULL */
+    const float* rope;         /* with positions */
+    int32_t n_positions;       /* rows of rope */
+} mg_kv4_append_args;
+mg_status mg_kv4_append(const mg_kv4_cache* cache, const mg_kv4_append_args* args, void* stream);
+
+/* As mg_kv8_read: the values of n slots as bf16 rows. */
+mg_status mg_kv4_read(const mg_kv4_cache* cache, int n, const int32_t* slots, uint16_t* k, int64_t k_stride,
+                      uint16_t* v, int64_t v_stride, void* stream);
+
+/* As mg_kv8_attention, over this cache: the same arguments, visibility, order and refusals.
+ * A value of K or V that is NaN (a scale byte of 255) makes the outputs of the tokens that see it NaN, of V in all features; so do a
+ * query value that is not finite and sums past fp32, which are reached where |v| passes some 2^100.  Query values enter as three 6-bit terms
+ * under the scale of 32 features: exact but for those below 2^-7 of their block's largest, which are off by at most 2^-15 of that.
+ * A probability times its value's scale enters the product with V as three such terms (off by at most 2^-14 of the largest of 32
+ * positions) where a row has few query rows (as in mg_kv8_attention), and as two (2^-9) in longer chunks. */
+size_t mg_kv4_attention_workspace_bytes(const mg_kv4_cache* cache, const mg_kv8_attn_args* args);
+mg_status mg_kv4_attention(const mg_kv4_cache* cache, const mg_kv8_attn_args* args, void* workspace,
+                           size_t workspace_bytes, void* stream);
+
+/* ---- (7) log probabilities of tokens ---------------------------------------------------------
+ *
+ * For answers and scores with log probabilities, from the logits that the margin gate reads: for each row r of n, with
+ * lse = ln sum_j e^logits[r][j],
+ *   logprob[r] = logits[r][tokens[r]] - lse (NaN where tokens[r] is outside 0..vocab - 1),
+ *   entropy[r] = - sum_j p_j ln p_j,  p_j = e^(logits[r][j] - lse),
+ *   top_tokens[r][i], top_logprobs[r][i], i < top: the row's largest logits in falling order, the lower index first among equal
+ *   ones, and their log probabilities; -1 and -inf where fewer than `top` logits are above -inf.
+ * Logits of -inf are masked: they have no part in the sums.  A row that is masked whole has log probabilities of -inf and an
+ * entropy of 0.  A NaN or +inf in a row makes its log probabilities and entropy NaN; NaN is never among the top tokens.
+ * logits fp32 (logits_bf16 = 0) or bf16, row stride `stride` values (>= vocab, any alignment of a value); 1 <= vocab <= 2^30,
+ * 0 <= top <= 32, top <= vocab, n <= 2^24.  logprob, entropy [n], top_tokens, top_logprobs [n][top]: any may be NULL (with
+ * logprob NULL tokens are not read).  No output may overlap the logits or tokens.  The workspace holds nothing between calls; the
+ * same call gives the same bits. */
+size_t mg_token_logprobs_workspace_bytes(int n, int vocab, int top);
+mg_status mg_token_logprobs(int n, int vocab, const void* logits, int logits_bf16, int64_t stride, const int32_t* tokens,
+                            int top, float* logprob, float* entropy, int32_t* top_tokens, float* top_logprobs,
+                            void* workspace, size_t workspace_bytes, void* stream);
+
 /* ---- measurement hooks (used by the benchmark; not part of the method) ---- */
 
 enum {

@@ -1,0 +1,628 @@
+// k_attn_kv4.hip -- attention of a batch's new tokens over the 4-bit paged K/V cache.
+//
+// out = sum_j exp(s_j - m) v_j / sum_j exp(s_j - m) in one pass over the positions, with a running reference m.  Both
+// products, S^T = K Q^T and O^T = V^T P^T, run on v_mfma_scale_f32_16x16x128_f8f6f4 with the cache's codes as they are:
+// no code is converted.  K's scale of 32 features is the instruction's own block scale.  V's scale of a position is not
+// along the product's axis, so it goes into the probability; a probability and a query value enter as e2m3 terms (6 bits, at the
+// rate of the 4-bit operand, twice that of 8 bits) whose block scale the lane that holds the block takes from its own values.
+#include <algorithm>
+#include <type_traits>
+
+#include "mg_attn_rows.h"
+
+namespace mg {
+namespace {
+
+typedef int i32x8_k4 __attribute__((ext_vector_type(8)));
+typedef int i32x6_k4 __attribute__((ext_vector_type(6)));
+typedef float f32x16_k4 __attribute__((ext_vector_type(16)));
+typedef float f32x32_k4 __attribute__((ext_vector_type(32)));
+
+constexpr int K4_STEP = 8;          // pages of a step: 128 positions, the products' depth
+constexpr int K4_FOLD = 13;         // probabilities under V's scale are held 2^-13 of themselves: up to 2^12 * 2^126 they stay finite
+constexpr uint32_t K4_LEAST = 12u << 23;  // of a block's scale: its terms' scales stay normal numbers
+
+template <int HD>
+struct K4Lane {  // what a lane loads of a page: 16 features' worth of four positions of V
+    typedef u32x4_k8 v;
+};
+template <>
+struct K4Lane<64> {
+    typedef u32x2_k8 v;
+};
+
+__device__ __forceinline__ i32x8_k4 k4_wide(const i32x6_k4& x) { return __builtin_shufflevector(x, x, 0, 1, 2, 3, 4, 5, -1, -1); }
+__device__ __forceinline__ i32x8_k4 k4_wide(const u32x4_k8& x) {
+    return __builtin_shufflevector(__builtin_bit_cast(int __attribute__((ext_vector_type(4))), x), __builtin_bit_cast(int __attribute__((ext_vector_type(4))), x),
+                                   0, 1, 2, 3, -1, -1, -1, -1);
+}
+// C + A B: A 16 rows of 128 e2m1 values, B 16 columns of 128 e2m3 values; lane 16 g + c holds values 32 g .. 32 g + 31 of row or
+// column c and their scale byte, and rows 4 g .. 4 g + 3 of column c of C.
+// Byte SB of sb is B's scale.
+template <int SB>
+__device__ __forceinline__ f32x4_k8 k4_mfma(const u32x4_k8& a, uint32_t sa, const i32x6_k4& b, uint32_t sb, f32x4_k8 c) {
+    return __builtin_amdgcn_mfma_scale_f32_16x16x128_f8f6f4(k4_wide(a), k4_wide(b), c, 4, 2, 0, (int)sa, SB, (int)sb);
+}
+
+// The scale 2^e (as float bits) under which values of up to `top` (float bits, finite) are below 4 in an e2m3 block, whose largest
+// is 7.5: the first term is off by 1/8 there at most, and 32 times that is in range again.
+__device__ __forceinline__ uint32_t k4_block_scale(uint32_t top) { return max(top & 0x7f800000u, K4_LEAST + (1u << 23)) - (1u << 23); }
+// 32 values (of even and of odd index, as the conversion takes them) as TERMS e2m3 blocks under scale, scale / 32, scale / 1024: off
+// by scale / 8, / 256, / 8192 after one, two, three, so by 2^-9 or 2^-14 of the largest at most
+template <int TERMS>
+__device__ __forceinline__ void k4_terms(f32x16_k4& even, f32x16_k4& odd, uint32_t scale, i32x6_k4 (&t)[TERMS]) {
+#pragma unroll
+    for (int k = 0; k < TERMS; ++k) {
+        const float s = __uint_as_float(scale - k * (5u << 23));
+        auto q = __builtin_amdgcn_cvt_scalef32_2xpk16_fp6_f32(even, odd, s);
+        // (the conversion takes several passes over its 32 sources: its result must not be placed on one of them, as the compiler
+        // does where they end here; such results were off now and then)
+        asm volatile("" : "+v"(q) : "v"(even), "v"(odd), "v"(s));
+        t[k] = __builtin_bit_cast(i32x6_k4, q);
+        if (k + 1 < TERMS) {
+            const f32x32_k4 y = __builtin_amdgcn_cvt_scalef32_pk32_f32_fp6(q, s);
+#pragma unroll
+            for (int i = 0; i < 16; ++i) {
+                even[i] -= y[2 * i];
+                odd[i] -= y[2 * i + 1];
+            }
+        }
+    }
+}
+
+// Query rows rr0 + 16 u + c of a row's KV head (row rr: token rr / G, head rr % G of the group) as B operands in LDS (registers are
+// what bounds a wave's tiles), and the positions of their tokens; columns past the row's last repeat its first.  Three terms of a
+// value: exact but for what is below 2^-7 of the largest of its 32 features, which is off by 2^-15 of that at most.  HD 128: an
+// operand a term.  HD 64: the first two terms share one (lanes 0..31 and 32..63, against K's features twice), the third has
+// one with zeros.
+template <int HD>
+constexpr int K4_OPS = HD == 128 ? 3 : 2;
+template <int HD>
+struct K4Query {
+    uint32_t op[K4_OPS<HD>][64][8];  // a lane's six words; the seventh of operand 0: byte k is operand k's scale
+};
+template <int HD>
+__device__ __forceinline__ int k4_query(const Kv8AttnArgs& a, const K8Row& row, int kh, int rr0, K4Query<HD>& q) {
+    const int lane = threadIdx.x & 63, c = lane & 15, g = lane >> 4;
+    int rr = rr0 + c;
+    rr = rr < row.n * a.G ? rr : 0;
+    const uint16_t* p = a.q + (int64_t)(row.t0 + rr / a.G) * a.q_stride + (size_t)(kh * a.G + rr % a.G) * HD + 32 * (HD == 128 ? g : g & 1);
+    uint32_t w[16], top = 0;
+#pragma unroll
+    for (int i = 0; i < 16; i += 4) *reinterpret_cast<uint4*>(w + i) = *reinterpret_cast<const uint4*>(p + 2 * i);
+    f32x16_k4 even, odds;
+#pragma unroll
+    for (int i = 0; i < 16; ++i) {
+        top = max(top, max(w[i] & 0x7fffu, (w[i] >> 16) & 0x7fffu));
+        even[i] = bf_lo(w[i]);
+        odds[i] = bf_hi(w[i]);
+    }
+    const uint32_t s = k4_block_scale(top << 16);
+    i32x6_k4 t[3];
+    k4_terms<3>(even, odds, s, t);
+    // (a value that is not finite makes the scores NaN)
+    const bool odd = top >= 0x7f80u;
+    const uint32_t b0 = odd ? 255u : s >> 23, b1 = odd ? 255u : (s >> 23) - 5, b2 = odd ? 255u : (s >> 23) - 10;
+    if constexpr (HD == 64) {
+#pragma unroll
+        for (int i = 0; i < 6; ++i) {
+            t[0][i] = g < 2 ? t[0][i] : t[1][i];
+            t[1][i] = g < 2 ? t[2][i] : 0;
+        }
+    }
+    q.op[0][lane][6] = HD == 128 ? b0 | b1 << 8 | b2 << 16 : g < 2 ? b0 | b2 << 8 : b1 | 127u << 8;
+#pragma unroll
+    for (int k = 0; k < K4_OPS<HD>; ++k) {
+        *reinterpret_cast<u32x4_k8*>(q.op[k][lane]) = u32x4_k8{(uint32_t)t[k][0], (uint32_t)t[k][1], (uint32_t)t[k][2], (uint32_t)t[k][3]};
+        *reinterpret_cast<u32x2_k8*>(q.op[k][lane] + 4) = u32x2_k8{(uint32_t)t[k][4], (uint32_t)t[k][5]};
+    }
+    return row.p0 + rr / a.G;
+}
+template <int HD>
+__device__ __forceinline__ i32x6_k4 k4_operand(const K4Query<HD>& q, int k) {
+    const int lane = threadIdx.x & 63;
+    const u32x4_k8 lo = *reinterpret_cast<const u32x4_k8*>(q.op[k][lane]);
+    const u32x2_k8 hi = *reinterpret_cast<const u32x2_k8*>(q.op[k][lane] + 4);
+    return i32x6_k4{(int)lo[0], (int)lo[1], (int)lo[2], (int)lo[3], (int)hi[0], (int)hi[1]};
+}
+
+template <int HD>
+struct K4Acc {
+    float m, l;  // reference of the exponents (log2 units); sum over the lane's positions
+    f32x4_k8 o[HD / 16];
+    __device__ __forceinline__ void clear() {
+        // below every finite score, and finite: exp2(masked - m) is 0 where nothing was seen yet
+        m = -3.0e38f;
+        l = 0.0f;
+#pragma unroll
+        for (int d = 0; d < HD / 16; ++d) o[d] = f32x4_k8{0.f, 0.f, 0.f, 0.f};
+    }
+};
+
+// A step's scores x (position 16 i + 4 g + r at x[4 i + r]) become its probabilities.  The reference moves only when a
+// score of the step passes it by K4_MOVE: exchanges between lanes and rescaled outputs are rare.
+constexpr float K4_MOVE = 12.0f;
+template <int HD>
+__device__ __forceinline__ void k4_probs(float (&x)[32], float f, K4Acc<HD>& acc) {
+    float mx = x[0];
+#pragma unroll
+    for (int i = 1; i < 32; ++i) mx = fmaxf(mx, x[i]);
+    if (__any(__builtin_fmaf(mx, f, -acc.m) > K4_MOVE)) {
+        const float mn = fmaxf(acc.m, k8_col_max(mx) * f);
+        const float al = __builtin_amdgcn_exp2f(acc.m - mn);
+        acc.m = mn;
+        acc.l *= al;
+#pragma unroll
+        for (int d = 0; d < HD / 16; ++d) acc.o[d] *= al;
+    }
+    float s[4];
+#pragma unroll
+    for (int i = 0; i < 32; ++i) {
+        x[i] = __builtin_amdgcn_exp2f(__builtin_fmaf(x[i], f, -acc.m));
+        s[i & 3] = i < 4 ? x[i] : s[i & 3] + x[i];
+    }
+    acc.l += (s[0] + s[1]) + (s[2] + s[3]);
+}
+
+// a wave-uniform float in a scalar register
+__device__ __forceinline__ float k4_scalar(float x) { return __uint_as_float(__builtin_amdgcn_readfirstlane(__float_as_uint(x))); }
+
+// Pages [pg0, pg1) of a row's table against 16 query rows: steps first, first + stride, ... of K4_STEP pages.  K's
+// registers are loaded again as soon as the scores are there, V's after its product, so that a wave has a step in flight at any
+// time.  ONCE: pages that no other wave reads, by loads that leave no trace in the caches.
+template <int HD, int TERMS, bool CAP, bool ONCE>
+__device__ __forceinline__ void k4_walk(const Kv8AttnArgs& a, const K8Row& row, int r, int kh, int pg0, int pg1, int first, int stride,
+                                        const K4Query<HD>& q, int pos, int p_hi, K4Acc<HD>& acc) {
+    typedef typename K4Lane<HD>::v vlane;
+    constexpr int DT = HD / 16;
+    constexpr size_t head_bytes = 16 * HD, head_scales = HD / 2 + 16;
+    const int lane = threadIdx.x & 63, g = lane >> 4;
+    K8Soft so = k8_soft(a);
+    so = K8Soft{k4_scalar(so.f), k4_scalar(so.zin), k4_scalar(so.most)};
+    const int32_t* ptab = a.page_table + (size_t)r * a.maxp;
+    const int p_lo = __builtin_amdgcn_readfirstlane(pos);  // of the wave's earliest token; p_hi: of its latest
+    typedef const __attribute__((address_space(1))) char* gptr;
+
+    for (int ch = pg0; ch < pg1; ch += K8_IDS) {
+        const int cnt = min(K8_IDS, pg1 - ch), steps = (cnt + K4_STEP - 1) / K4_STEP;
+        // the chunk's first step that is this wave's
+        const int done = (ch - pg0) / K4_STEP;
+        int s = first - done;
+        if (s < 0) s = (stride - (-s) % stride) % stride;
+        if (s >= steps) continue;
+        // lane i: page ch + i of the table and its place in the cache (a hole, or one past the split: page 0, unseen)
+        const int id = lane < cnt ? ptab[ch + lane] : -1;
+        const unsigned long long live_pages = __ballot(id >= 0 && id < a.c.n_pages);
+        const uint32_t place = (id >= 0 && id < a.c.n_pages ? (uint32_t)id : 0u) * (uint32_t)a.c.Hkv + (uint32_t)kh;
+        u32x4_k8 kb[K4_STEP];
+        vlane vb[K4_STEP];
+        uint32_t ks[K4_STEP], vs[K4_STEP];
+        auto fetch_k = [&](int s) {
+            // (made anew: a load then takes its page's address from scalar registers, and nothing of it is held meanwhile)
+            uint32_t k_lane = HD == 128 ? lane : lane & 31, at = place;
+            asm volatile("" : "+v"(k_lane), "+v"(at));
+            const uint32_t k_at = k_lane * 16u;
+#pragma unroll
+            for (int e = 0; e < K4_STEP; ++e) {
+                if (e % 2 == 0) __builtin_amdgcn_sched_barrier(0);  // (fewer addresses at a time)
+                const size_t ph = (uint32_t)__builtin_amdgcn_readlane((int)at, K4_STEP * s + e);
+                const uint64_t p = k8_uniform(a.c.codes + ph * head_bytes), ps = k8_uniform(a.c.scales + ph * head_scales);
+                auto* kp = reinterpret_cast<const __attribute__((address_space(1))) u32x4_k8*>(reinterpret_cast<gptr>(p) + k_at);
+                kb[e] = ONCE ? __builtin_nontemporal_load(kp) : *kp;
+                ks[e] = *reinterpret_cast<const __attribute__((address_space(1))) uint8_t*>(reinterpret_cast<gptr>(ps) + k_lane);
+            }
+        };
+        auto fetch_v = [&](int s) {
+            uint32_t v_lane = lane, at = place;
+            asm volatile("" : "+v"(v_lane), "+v"(at));
+            const uint32_t v_at = v_lane * (uint32_t)sizeof(vlane), vs_at = v_lane >> 4 << 2;
+#pragma unroll
+            for (int e = 0; e < K4_STEP; ++e) {
+                if (e % 2 == 0) __builtin_amdgcn_sched_barrier(0);
+                const size_t ph = (uint32_t)__builtin_amdgcn_readlane((int)at, K4_STEP * s + e);
+                const uint64_t p = k8_uniform(a.c.codes + ph * head_bytes + 8 * HD), ps = k8_uniform(a.c.scales + ph * head_scales + HD / 2);
+                auto* vp = reinterpret_cast<const __attribute__((address_space(1))) vlane*>(reinterpret_cast<gptr>(p) + v_at);
+                vb[e] = ONCE ? __builtin_nontemporal_load(vp) : *vp;
+                vs[e] = *reinterpret_cast<const __attribute__((address_space(1))) uint32_t*>(reinterpret_cast<gptr>(ps) + vs_at);
+            }
+        };
+        fetch_k(s);
+        fetch_v(s);
+        for (; s < steps; s += stride) {
+            const bool more = s + stride < steps;
+            const int j0 = 16 * (ch + K4_STEP * s);
+            const uint32_t mapped = (uint32_t)(live_pages >> (K4_STEP * s)) & 0xffu;
+            const bool edge = mapped != 0xffu || j0 + 127 > p_lo || j0 + 128 > row.len || (a.window && j0 <= k8_hidden(a.window, p_hi));
+            // whether a scale of V says that its value is not finite
+            uint32_t odd = 0;
+#pragma unroll
+            for (int e = 0; e < K4_STEP; ++e) odd |= vs[e] & ((vs[e] & 0x7f7f7f7fu) + 0x01010101u) & 0x80808080u;
+            const bool any_odd = __any(odd != 0);
+            float x[32];
+            {
+                asm volatile("" ::: "memory");  // (the queries are read anew, not held in registers)
+                const uint32_t qs = q.op[0][lane][6];
+                f32x4_k8 c[K4_STEP];
+#pragma unroll
+                for (int e = 0; e < K4_STEP; ++e) c[e] = f32x4_k8{0.f, 0.f, 0.f, 0.f};
+                const auto term = [&](auto K) {
+                    const i32x6_k4 b = k4_operand(q, K.value);
+#pragma unroll
+                    for (int e = 0; e < K4_STEP; ++e) c[e] = k4_mfma<K.value>(kb[e], ks[e], b, qs, c[e]);
+                };
+                term(std::integral_constant<int, 0>{});
+                term(std::integral_constant<int, 1>{});
+                if constexpr (K4_OPS<HD> == 3) term(std::integral_constant<int, 2>{});
+#pragma unroll
+                for (int i = 0; i < 32; ++i) x[i] = c[i >> 2][i & 3];
+            }
+            if (CAP) {
+                k8_cap(reinterpret_cast<float(&)[1][32]>(x), so);
+            }
+            if (edge) {  // the token at p sees lo < position <= hi of the lane's
+                int p = pos;
+                asm("" : "+v"(p));  // (nothing of this is held between steps)
+                const int hi = min(p, row.len - 1) - j0 - 4 * g, lo = (a.window ? k8_hidden(a.window, p) : -1) - j0 - 4 * g;
+#pragma unroll
+                for (int i = 0; i < 32; ++i) {
+                    const int at = 16 * (i >> 2) + (i & 3);
+                    x[i] = (mapped >> (i >> 2) & 1u) && at <= hi && at > lo ? x[i] : -__builtin_inff();
+                }
+            }
+            if (any_odd) {  // such a value reaches the columns that see it, and no other: their probabilities become NaN
+#pragma unroll
+                for (int i = 0; i < 32; ++i)
+                    x[i] = (vs[i >> 2] >> (8 * (i & 3)) & 0xffu) == 255u && x[i] != -__builtin_inff() ? __builtin_nanf("") : x[i];
+            }
+            k4_probs<HD>(x, so.f, acc);
+            f32x16_k4 y[2];
+            float top = 0.0f;
+#pragma unroll
+            for (int i = 0; i < 32; ++i) {
+                y[i & 1][i >> 1] = x[i] * __uint_as_float(((vs[i >> 2] >> (8 * (i & 3)) & 0xffu) << 23) - ((uint32_t)K4_FOLD << 23));
+                top = fmaxf(top, y[i & 1][i >> 1]);
+            }
+            const uint32_t sc = k4_block_scale(__float_as_uint(top));
+            i32x6_k4 p[TERMS];
+            k4_terms<TERMS>(y[0], y[1], sc, p);
+            // byte k: term k's scale (past fp32: NaN)
+            uint32_t ps = (sc >> 23) + K4_FOLD;
+            ps = ps > 254u ? 0xffffffu : ps * 0x10101u - 0xa0500u;
+            __builtin_amdgcn_sched_barrier(0);
+            if (more) fetch_k(s + stride);  // K's registers are free, and the scores'
+            __builtin_amdgcn_sched_barrier(0);
+#pragma unroll
+            for (int d = 0; d < DT; ++d) {
+                u32x4_k8 A;
+#pragma unroll
+                for (int e = 0; e < 4; ++e)
+                    A[e] = __builtin_amdgcn_perm(vb[2 * e + 1][d / 2], vb[2 * e][d / 2], d & 1 ? 0x07060302u : 0x05040100u);
+                acc.o[d] = k4_mfma<0>(A, 127u, p[0], ps, acc.o[d]);
+                acc.o[d] = k4_mfma<1>(A, 127u, p[1], ps, acc.o[d]);
+                if constexpr (TERMS == 3) acc.o[d] = k4_mfma<2>(A, 127u, p[2], ps, acc.o[d]);
+            }
+            __builtin_amdgcn_sched_barrier(0);
+            if (more) fetch_v(s + stride);
+        }
+    }
+}
+
+// Rows of few query rows (tokens times query heads of a KV head <= 16 NT): one block per (row, KV head, split of the row's pages).
+// A wave has one of the NT tiles of 16 query rows, and the waves of a tile take its steps in turn.
+template <int HD, int WAVES>
+struct K4FewShared {
+    float o[WAVES][16][HD + 4];  // (padded rows)
+    float m[WAVES][16], l[WAVES][16];
+    K4Query<HD> q[WAVES];
+};
+template <int HD, int NT, int WAVES, bool CAP, bool EVEN>
+__device__ __forceinline__ void k4_few_block(const Kv8AttnArgs& a, const K8Few& few, int block, K4FewShared<HD, WAVES>& sh) {
+    constexpr int DT = HD / 16;
+    const int lane = threadIdx.x & 63, c = lane & 15, g = lane >> 4;
+    const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+    const int kh = block % a.c.Hkv;
+    int r = block / a.c.Hkv % a.B, split = block / a.c.Hkv / a.B, act;
+    K8Row row;
+    if (EVEN) {
+        const K8Lanes x = k8_lanes<16 * NT>(a, few);
+        const int index = block / a.c.Hkv;
+        const unsigned long long past = __ballot(x.sum > index);
+        if (!past) return;
+        r = __builtin_amdgcn_readfirstlane(__ffsll(past) - 1);
+        row = k8_of_lane(x.row, r);
+        act = __builtin_amdgcn_readlane(x.act, r);
+        split = index - (__builtin_amdgcn_readlane(x.sum, r) - act);
+    } else {
+        row = k8_row(a, r);
+        if (row.n <= 0 || row.n * a.G > 16 * NT) return;
+        act = k8_active(max(row.pgb - row.pga, 0), few.sp, few.nsplit);
+        if (split >= act) return;
+    }
+    const int npg = max(row.pgb - row.pga, 0), nsplit = few.most;
+    const int per = (npg + act - 1) / act;
+    const int pg0 = min(row.pgb, row.pga + split * per), pg1 = split == act - 1 ? row.pgb : min(row.pgb, pg0 + per);
+
+    // (waves of a tile have the same queries: each writes its own, and waits for nobody)
+    const int tile = wave % NT;
+    const int pos = k4_query<HD>(a, row, kh, 16 * tile, sh.q[wave]);
+    K4Acc<HD> acc;
+    acc.clear();
+    if (16 * tile < row.n * a.G)
+        k4_walk<HD, 3, CAP, NT == 1>(a, row, r, kh, pg0, pg1, wave / NT, WAVES / NT, sh.q[wave], pos, row.p0 + row.n - 1, acc);
+
+    // the waves' shares join in LDS
+    const float ls = k8_col_sum(acc.l);
+    if (g == 0) {
+        sh.m[wave][c] = acc.m;
+        sh.l[wave][c] = ls;
+    }
+#pragma unroll
+    for (int d = 0; d < DT; ++d) *reinterpret_cast<f32x4_k8*>(&sh.o[wave][c][16 * d + 4 * g]) = acc.o[d];
+    __syncthreads();
+    const int live = row.n * a.G;
+    for (int i = threadIdx.x; i < live * (HD / 4); i += 64 * WAVES) {
+        const int rr = i / (HD / 4), d = i % (HD / 4) * 4;
+        const int w0 = rr / 16, rc = rr % 16;
+        float M = sh.m[w0][rc];
+#pragma unroll
+        for (int w = 1; w < WAVES / NT; ++w) M = fmaxf(M, sh.m[w0 + w * NT][rc]);
+        float L = 0.0f;
+        f32x4_k8 O = f32x4_k8{0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+        for (int w = 0; w < WAVES / NT; ++w) {
+            const float f = __builtin_amdgcn_exp2f(sh.m[w0 + w * NT][rc] - M);
+            L += f * sh.l[w0 + w * NT][rc];
+            O += f * *reinterpret_cast<const f32x4_k8*>(&sh.o[w0 + w * NT][rc][d]);
+        }
+        const int64_t tok = row.t0 + rr / a.G;
+        const int head = kh * a.G + rr % a.G;
+        if (act == 1) {
+            const float inv = L == 0.0f ? 0.0f : ieee_div(1.0f, L);
+            *reinterpret_cast<uint2*>(a.out + tok * a.out_stride + head * HD + d) =
+                make_uint2(k8_pack(O[0] * inv, O[1] * inv), k8_pack(O[2] * inv, O[3] * inv));
+        } else {
+            const size_t at = (((size_t)r * a.c.Hkv + kh) * nsplit + split) * (16 * NT) + rr;
+            *reinterpret_cast<f32x4_k8*>(a.part + at * HD + d) = O;
+            if (d == 0) {
+                float* ml = a.part + (size_t)a.B * a.c.Hkv * nsplit * (16 * NT) * HD + 2 * at;
+                ml[0] = M;
+                ml[1] = L;
+            }
+        }
+    }
+}
+
+template <int HD, int NT, int WAVES, bool CAP, bool EVEN>
+__global__ __launch_bounds__(64 * WAVES) __attribute__((amdgpu_waves_per_eu(2))) void attn_kv4_few_kernel(Kv8AttnArgs a, K8Few few) {
+    __shared__ __attribute__((aligned(16))) K4FewShared<HD, WAVES> sh;
+    k4_few_block<HD, NT, WAVES, CAP, EVEN>(a, few, blockIdx.x, sh);
+}
+
+// Joins the splits of rows of few query rows: a wave per query row of a (row, KV head); block: its index, of ROWB blocks a
+// (row, KV head).
+template <int HD, int NT, bool EVEN>
+__device__ __forceinline__ void k4_few_join(const Kv8AttnArgs& a, const K8Few& few, int block, int rowb) {
+    const int rr = block % rowb * K8_WAVES + (threadIdx.x >> 6);
+    const int kh = block / rowb % a.c.Hkv, r = block / rowb / a.c.Hkv;
+    K8Row row;
+    int act;
+    if (EVEN) {
+        const K8Lanes x = k8_lanes<16 * NT>(a, few);
+        row = k8_of_lane(x.row, r);
+        act = __builtin_amdgcn_readlane(x.act, r);
+    } else {
+        row = k8_row(a, r);
+        act = row.n <= 0 || row.n * a.G > 16 * NT ? 0 : k8_active(max(row.pgb - row.pga, 0), few.sp, few.nsplit);
+    }
+    if (act <= 1 || rr >= row.n * a.G) return;
+    const int nsplit = few.most;
+    const size_t first = ((size_t)r * a.c.Hkv + kh) * nsplit * (16 * NT) + rr;
+    const float* ml = a.part + (size_t)a.B * a.c.Hkv * nsplit * (16 * NT) * HD;
+    k8_join<HD>(a.part + first * HD, (size_t)(16 * NT) * HD, ml + 2 * first, 2 * 16 * NT, act, k8_out(a, row, kh, rr));
+}
+template <int HD, int NT, bool EVEN>
+__global__ __launch_bounds__(K8_THREADS) void attn_kv4_join_kernel(Kv8AttnArgs a, K8Few few, int rowb) {
+    k4_few_join<HD, NT, EVEN>(a, few, blockIdx.x, rowb);
+}
+
+// Rows of more query rows: one block per (row, KV head, 64 query rows, split of the positions that these see), the tokens of a
+// row's end first (they see the most).  Each wave takes its own 16 query rows over all of the block's pages; the waves read the
+// same codes at about the same time.
+constexpr int K4_CHUNK_ROWS = K8_WAVES * 16;
+constexpr int K4_MIN_STAGES = 2;  // steps that a split of a tile takes at least
+template <int HD, bool CAP>
+__device__ __forceinline__ void k4_chunk_block(const Kv8AttnArgs& a, int few, int tiles, int nsplit, float* part, int block,
+                                               K4Query<HD> (&sh)[K8_WAVES]) {
+    constexpr int DT = HD / 16, ROWS = K4_CHUNK_ROWS;
+    const int lane = threadIdx.x & 63, c = lane & 15, g = lane >> 4;
+    const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+    const int kh = block % a.c.Hkv;
+    const int split = block / a.c.Hkv % nsplit, index = block / a.c.Hkv / nsplit;
+    const K8Tile at = k8_tile<ROWS>(a, few, index);
+    if (at.r < 0) return;
+    const int r = __builtin_amdgcn_readfirstlane(at.r), t = __builtin_amdgcn_readfirstlane(at.t);
+    const K8Row row = k8_row(a, r);
+    const int live = row.n * a.G;
+    if (t * ROWS >= live) return;
+    const K8Span span = k8_span<ROWS, K4_STEP, K4_MIN_STAGES>(a, row, t, nsplit);
+    if (split >= span.act) return;
+    const int rr0 = t * ROWS + wave * 16;
+    // the block's pages, and those of them that this wave's tokens see
+    int pg0 = span.pg0 + span.stages * split / span.act * K4_STEP, pg1 = min(span.pg1, span.pg0 + span.stages * (split + 1) / span.act * K4_STEP);
+    const int wp0 = row.p0 + min(rr0, live - 1) / a.G, wp1 = row.p0 + (min(rr0 + 16, live) - 1) / a.G;
+    pg1 = min(pg1, (max(0, min(wp1 + 1, row.len)) + 15) / 16);
+    if (a.window) pg0 = max(pg0, pg0 + (min((k8_hidden(a.window, wp0) + 1) / 16, pg1) - pg0) / K4_STEP * K4_STEP);
+
+    const int pos = k4_query<HD>(a, row, kh, rr0, sh[wave]);
+    K4Acc<HD> acc;
+    acc.clear();
+    if (rr0 < live) k4_walk<HD, 2, CAP, false>(a, row, r, kh, pg0, pg1, 0, 1, sh[wave], pos, wp1, acc);
+    const float L = k8_col_sum(acc.l);
+    const float inv = L == 0.0f ? 0.0f : ieee_div(1.0f, L);
+    const int rr = rr0 + c;
+    if (rr >= live) return;
+    if (span.act > 1) {
+        const size_t pr = ((size_t)(index * a.c.Hkv + kh) * nsplit + split) * ROWS + wave * 16 + c;
+#pragma unroll
+        for (int d = 0; d < DT; ++d) *reinterpret_cast<f32x4_k8*>(part + pr * HD + 16 * d + 4 * g) = acc.o[d];
+        if (g == 0) {
+            float* ml = part + (size_t)tiles * a.c.Hkv * nsplit * ROWS * HD + 2 * pr;
+            ml[0] = acc.m;
+            ml[1] = L;
+        }
+        return;
+    }
+    uint16_t* out = k8_out(a, row, kh, rr) + 4 * g;
+#pragma unroll
+    for (int d = 0; d < DT; ++d)
+        *reinterpret_cast<uint2*>(out + 16 * d) =
+            make_uint2(k8_pack(acc.o[d][0] * inv, acc.o[d][1] * inv), k8_pack(acc.o[d][2] * inv, acc.o[d][3] * inv));
+}
+
+// A call with longer rows: their blocks, then those of its rows of few query rows, in one launch.
+template <int HD, bool CAP>
+__global__ __launch_bounds__(K8_THREADS) __attribute__((amdgpu_waves_per_eu(2))) void attn_kv4_mixed_kernel(Kv8AttnArgs a, K8Few few, int tiles,
+                                                                                                      int csplit, float* cpart) {
+    union Shared {
+        K4Query<HD> chunk[K8_WAVES];
+        K4FewShared<HD, K8_WAVES> few;
+    };
+    __shared__ __attribute__((aligned(16))) Shared sh;
+    const int chunks = tiles * a.c.Hkv * csplit;
+    if ((int)blockIdx.x < chunks)
+        k4_chunk_block<HD, CAP>(a, 16, tiles, csplit, cpart, blockIdx.x, sh.chunk);
+    else
+        k4_few_block<HD, 1, K8_WAVES, CAP, false>(a, few, blockIdx.x - chunks, sh.few);
+}
+
+// Joins the splits of attn_kv4_mixed_kernel: blocks of its longer rows' tiles (csplit > 1), a wave per query row, then of the
+// others.
+template <int HD>
+__global__ __launch_bounds__(K8_THREADS) void attn_kv4_mixed_join_kernel(Kv8AttnArgs a, K8Few few, int rowb, int tiles, int csplit,
+                                                                        const float* cpart) {
+    constexpr int ROWS = K4_CHUNK_ROWS, RB = ROWS / K8_WAVES;
+    const int chunks = csplit > 1 ? tiles * a.c.Hkv * RB : 0;
+    if ((int)blockIdx.x >= chunks) {
+        k4_few_join<HD, 1, false>(a, few, blockIdx.x - chunks, rowb);
+        return;
+    }
+    const int at = blockIdx.x / RB, kh = at % a.c.Hkv;
+    const K8Tile tile = k8_tile<ROWS>(a, 16, at / a.c.Hkv);
+    if (tile.r < 0) return;
+    const K8Row row = k8_row(a, tile.r);
+    const int i = blockIdx.x % RB * K8_WAVES + (threadIdx.x >> 6), rr = tile.t * ROWS + i;
+    if (rr >= row.n * a.G) return;
+    const int act = k8_span<ROWS, K4_STEP, K4_MIN_STAGES>(a, row, tile.t, csplit).act;
+    if (act == 1) return;
+    const size_t first = (size_t)at * csplit * ROWS + i;
+    const float* ml = cpart + (size_t)tiles * a.c.Hkv * csplit * ROWS * HD;
+    k8_join<HD>(cpart + first * HD, (size_t)ROWS * HD, ml + 2 * first, 2 * ROWS, act, k8_out(a, row, kh, rr));
+}
+
+// The launch.
+struct K4Plan {
+    int nt;                     // rows of few query rows: tiles of a block
+    K8Few few;                  // and how they are split
+    int64_t few_blocks;
+    int64_t tiles;              // of K4_CHUNK_ROWS query rows, of the longer rows: at most (a row's last may be partly empty); 0: none
+    int csplit;                 // splits of such a tile
+};
+constexpr int K4_MIN_PAGES = K4_STEP * K8_WAVES;  // pages a split takes at least: a step of every wave
+constexpr int K4_MAX_PAGES = 256;
+constexpr int K4_MAX_SPLITS = 64;
+constexpr int K4_BLOCKS_PER_CU = 2;
+constexpr int K4_EVEN_PAGES = 64;
+constexpr int K4_MIXED_PAGES = 256;
+constexpr int K4_CHUNK_BLOCKS_PER_CU = 2;
+// pages that a group of `tokens` neighbouring tokens of a row sees at most, by the host's bounds
+int64_t pages_seen(const Kv8AttnArgs& a, int64_t tokens) {
+    int64_t len = a.max_len;
+    if (a.window) len = std::min<int64_t>(len, (int64_t)a.window + tokens + 15);
+    return std::max<int64_t>(1, (len + 15) / 16);
+}
+K4Plan plan_of(const Kv8AttnArgs& a) {
+    K4Plan p;
+    const int64_t rows = (int64_t)a.max_new * a.G;
+    p.tiles = rows <= 32 ? 0 : (int64_t)a.T * a.G / K4_CHUNK_ROWS + std::min(a.B, a.T);
+    p.nt = rows <= 16 || p.tiles ? 1 : 2;
+    const int64_t pages = pages_seen(a, std::min(a.max_new, 16 * p.nt / a.G));
+    const int64_t blocks = (int64_t)a.B * a.c.Hkv;
+    const int64_t want = std::max<int64_t>(1, (K4_BLOCKS_PER_CU * a.n_cu + blocks / 2) / blocks);
+    int64_t sp = std::min<int64_t>(K4_MAX_PAGES, std::max<int64_t>(K4_MIN_PAGES, (pages + want - 1) / want));
+    if (p.tiles) sp = std::min<int64_t>(8 * blocks <= a.n_cu ? K4_MIXED_PAGES / 2 : K4_MIXED_PAGES, pages);
+    sp = std::max(sp, (pages + K4_MAX_SPLITS - 1) / K4_MAX_SPLITS);
+    const int nsplit = (int)((pages + sp - 1) / sp);
+    const int units = K4_BLOCKS_PER_CU * a.n_cu / a.c.Hkv;
+    p.few = K8Few{(int)sp, nsplit, nsplit, 0};
+    p.few_blocks = blocks * nsplit;
+    if (!p.tiles && nsplit > 1 && sp >= K4_EVEN_PAGES && a.B > 1 && a.B <= 64 && a.B < units && (int64_t)a.B * a.maxp <= 1 << 30) {
+        p.few.most = std::min(2 * nsplit, K4_MAX_SPLITS);
+        p.few.units = units;
+        p.few_blocks = std::max<int64_t>(p.few_blocks, (int64_t)units * a.c.Hkv);
+    }
+    p.csplit = 1;
+    if (p.tiles) {
+        const int64_t stages = (pages_seen(a, std::min(a.max_new, K4_CHUNK_ROWS / a.G + 1)) + K4_STEP - 1) / K4_STEP;
+        const int64_t most = std::min<int64_t>(K4_MAX_SPLITS, std::max<int64_t>(1, stages / K4_MIN_STAGES));
+        p.csplit = (int)std::min<int64_t>(most, std::max<int64_t>(1, K4_CHUNK_BLOCKS_PER_CU * a.n_cu / (p.tiles * a.c.Hkv)));
+    }
+    return p;
+}
+
+size_t few_floats(const Kv8AttnArgs& a, const K4Plan& p) {
+    return p.few.nsplit == 1 ? 0 : (size_t)a.B * a.c.Hkv * p.few.most * (16 * p.nt) * (a.c.hd + 2);
+}
+
+template <int HD, int NT, bool EVEN>
+void launch_few(const Kv8AttnArgs& a, const K4Plan& p, int rowb, int64_t joins, hipStream_t s) {
+    constexpr int WAVES = NT * K8_WAVES;
+    auto f = a.cap > 0.0f ? attn_kv4_few_kernel<HD, NT, WAVES, true, EVEN> : attn_kv4_few_kernel<HD, NT, WAVES, false, EVEN>;
+    hipLaunchKernelGGL(f, dim3((unsigned)p.few_blocks), dim3(64 * WAVES), 0, s, a, p.few);
+    if (joins)
+        hipLaunchKernelGGL((attn_kv4_join_kernel<HD, NT, EVEN>), dim3((unsigned)joins), dim3(K8_THREADS), 0, s, a, p.few, rowb);
+}
+template <int HD>
+void launch(const Kv8AttnArgs& a, const K4Plan& p, hipStream_t s) {
+    const int rowb = (int)(std::min<int64_t>((int64_t)a.max_new * a.G, 16 * p.nt) + K8_WAVES - 1) / K8_WAVES;
+    const int64_t few_joins = p.few.nsplit > 1 ? (int64_t)a.B * a.c.Hkv * rowb : 0;
+    if (p.tiles == 0) {
+        auto f = p.nt == 2 ? (p.few.units ? launch_few<HD, 2, true> : launch_few<HD, 2, false>)
+                           : (p.few.units ? launch_few<HD, 1, true> : launch_few<HD, 1, false>);
+        f(a, p, rowb, few_joins, s);
+        return;
+    }
+    float* cpart = a.part + few_floats(a, p);
+    const dim3 grid((unsigned)(p.tiles * a.c.Hkv * p.csplit + p.few_blocks));
+    auto f = a.cap > 0.0f ? attn_kv4_mixed_kernel<HD, true> : attn_kv4_mixed_kernel<HD, false>;
+    hipLaunchKernelGGL(f, grid, dim3(K8_THREADS), 0, s, a, p.few, (int)p.tiles, p.csplit, cpart);
+    const int64_t joins = few_joins + (p.csplit > 1 ? p.tiles * a.c.Hkv * (K4_CHUNK_ROWS / K8_WAVES) : 0);
+    if (joins)
+        hipLaunchKernelGGL(attn_kv4_mixed_join_kernel<HD>, dim3((unsigned)joins), dim3(K8_THREADS), 0, s, a, p.few, rowb,
+                           (int)p.tiles, p.csplit, cpart);
+}
+
+}  // namespace
+
+size_t kv4_attention_ws_bytes(const Kv8AttnArgs& a) {
+    const K4Plan p = plan_of(a);
+    const size_t chunk = p.csplit == 1 ? 0 : (size_t)p.tiles * a.c.Hkv * p.csplit * K4_CHUNK_ROWS * (a.c.hd + 2);
+    return (few_floats(a, p) + chunk) * sizeof(float);
+}
+
+bool kv4_attention_fits(const Kv8AttnArgs& a) {
+    const K4Plan p = plan_of(a);
+    constexpr int64_t most = 1 << 22;  // blocks of a launch
+    return (int64_t)a.T * a.G <= (1 << 29) && p.tiles * a.c.Hkv * p.csplit + p.few_blocks <= most &&
+           (int64_t)a.B * a.c.Hkv * 8 + p.tiles * a.c.Hkv * (p.csplit > 1 ? K4_CHUNK_ROWS / K8_WAVES : 0) <= 2 * most;
+}
+
+hipError_t launch_kv4_attention(const Kv8AttnArgs& a, hipStream_t s) {
+    const K4Plan p = plan_of(a);
+    if (a.c.hd == 128)
+        launch<128>(a, p, s);
+    else
+        launch<64>(a, p, s);
+    return hipGetLastError();
+}
+
+}  // namespace mg

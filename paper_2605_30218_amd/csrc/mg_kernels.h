@@ -244,6 +244,43 @@ size_t kv8_attention_ws_bytes(const Kv8AttnArgs& a);
 bool kv8_attention_fits(const Kv8AttnArgs& a);  // whether its launches are within the grid limits
 hipError_t launch_kv8_attention(const Kv8AttnArgs& a, hipStream_t s);
 
+// ---------------------------------------------------------------- 4-bit paged K/V cache
+// The cache is a Kv8 whose codes and scales are those of mg_kv4_cache (include/mg.h has the layout), and its attention takes the
+// 8-bit cache's arguments.
+struct Kv4AppendArgs {
+    Kv8 c;
+    int n, Hq;                  // tokens; query heads (0: none)
+    const uint16_t* q;
+    uint16_t* q_out;
+    const uint16_t *k, *v;
+    int64_t q_stride, q_out_stride, k_stride, v_stride;  // in values
+    const int32_t *slots, *positions;  // positions NULL: nothing is rotated
+    const float* rope;          // [n_positions][hd]
+    int n_positions;
+};
+hipError_t launch_kv4_append(const Kv4AppendArgs& a, hipStream_t s);
+hipError_t launch_kv4_read(const Kv8& c, int n, const int32_t* slots, uint16_t* k, int64_t ks, uint16_t* v, int64_t vs,
+                           hipStream_t s);
+size_t kv4_attention_ws_bytes(const Kv8AttnArgs& a);
+bool kv4_attention_fits(const Kv8AttnArgs& a);
+hipError_t launch_kv4_attention(const Kv8AttnArgs& a, hipStream_t s);
+
+// ---------------------------------------------------------------- token log probabilities (k_logprobs.hip)
+constexpr int LOGP_MAX_TOP = 32;
+struct LogpArgs {
+    int n, V, top;
+    bool bf16;
+    const void* logits;
+    int64_t stride;             // in values
+    const int32_t* tokens;
+    float *logprob, *entropy, *top_logprobs;  // any NULL: not wanted
+    int32_t* top_tokens;
+    int n_cu;
+    void* part;                 // logprobs_ws_bytes
+};
+size_t logprobs_ws_bytes(const LogpArgs& a);
+hipError_t launch_logprobs(const LogpArgs& a, hipStream_t s);
+
 // element-wise numerics probes used by the tests
 hipError_t launch_copy16(int64_t n16, const void* src, void* dst, hipStream_t s);
 // streaming read of n16 16-byte words; sink receives read_stream_blocks() words

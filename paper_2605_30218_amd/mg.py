@@ -45,6 +45,16 @@ class MgKv8Cache(C.Structure):
                 ("head_dim", C.c_int32)]
 
 
+class MgKv4Cache(C.Structure):
+    _fields_ = MgKv8Cache._fields_
+
+
+class MgKv4AppendArgs(C.Structure):
+    _fields_ = [("n_tokens", C.c_int32), ("n_q_heads", C.c_int32)] + \
+               [f for n in ("q", "q_out", "k", "v") for f in ((n, C.c_void_p), (n + "_stride", C.c_int64))] + \
+               [("slots", C.c_void_p), ("positions", C.c_void_p), ("rope", C.c_void_p), ("n_positions", C.c_int32)]
+
+
 class MgKv8AttnArgs(C.Structure):
     _fields_ = [(n, C.c_int32) for n in ("n_rows", "n_tokens", "n_q_heads", "max_new", "max_len",
                                          "max_pages_per_row", "window")] + \
@@ -79,6 +89,14 @@ SIGNATURES = {
     "mg_kv8_read": (I, [P, I, P, P, I64, P, I64, P]),
     "mg_kv8_attention_workspace_bytes": (SZ, [P, P]),
     "mg_kv8_attention": (I, [P, P, P, SZ, P]),
+    "mg_kv4_code_bytes": (SZ, [I, I, I]),
+    "mg_kv4_scale_bytes": (SZ, [I, I, I]),
+    "mg_kv4_append": (I, [P, P, P]),
+    "mg_kv4_read": (I, [P, I, P, P, I64, P, I64, P]),
+    "mg_kv4_attention_workspace_bytes": (SZ, [P, P]),
+    "mg_kv4_attention": (I, [P, P, P, SZ, P]),
+    "mg_token_logprobs_workspace_bytes": (SZ, [I, I, I]),
+    "mg_token_logprobs": (I, [I, I, P, I, I64, P, I, P, P, P, P, P, SZ, P]),
     "mg_profile_begin": (I, [P, I, I]),
     "mg_profile_end": (I, [P, I, P, P, P, P]),
     "mg_op_copy": (I, [I64, P, P, P]),
@@ -390,8 +408,12 @@ def kv8_append(codes, scales, k, v, slots, stream=None):
 def kv8_read(codes, scales, slots, k_out=None, v_out=None, stream=None):
     """mg_kv8_read: the values of slots [n] as bf16 rows (k, v), each [n, Hkv, hd].  Rows of slots
     outside the cache are not written: in a new tensor they hold anything."""
-    c = _kv8(codes, scales)
-    dev, shape = codes.device, (slots.numel(), c.n_kv_heads, c.head_dim)
+    return _read("mg_kv8_read", _kv8(codes, scales), codes.device, slots, k_out, v_out, stream)
+
+
+def _read(name, c, dev, slots, k_out, v_out, stream):
+    """The read call `name` of the library."""
+    shape = (slots.numel(), c.n_kv_heads, c.head_dim)
     n, heads, hd = shape
     if k_out is None:
         k_out = _new(shape, torch.bfloat16, dev, stream)
@@ -403,12 +425,12 @@ def kv8_read(codes, scales, slots, k_out=None, v_out=None, stream=None):
         vp, vs = v_out.data_ptr(), heads * hd
     else:
         vp, vs = _rows16("v_out", v_out, n, heads, hd, dev)
-    _call("mg_kv8_read", dev, stream, load().mg_kv8_read, C.byref(c), n, _ints("slots", slots, dev), kp, ks, vp, vs)
+    _call(name, dev, stream, getattr(load(), name), C.byref(c), n, _ints("slots", slots, dev), kp, ks, vp, vs)
     return k_out, v_out
 
 
 def _attn_args(c, q, page_table, lens, cu_new, max_new, max_len, scale, window, softcap, out, dev):
-    """The MgKv8AttnArgs of a call; out None: not known yet."""
+    """The MgKv8AttnArgs of a call (either cache's); out None: not known yet."""
     if q.dim() != 3 or q.shape[2] != c.head_dim:
         _refuse("q", q, f"[T, Hq, {c.head_dim}]")
     if page_table.dim() != 2:
@@ -448,13 +470,17 @@ def kv8_attention(codes, scales, q, page_table, lens, cu_new=None, max_new=None,
     a smaller number gives it: the launch, and with it the time and a probability's bits, follow it.
     workspace: a contiguous uint8 tensor of kv8_attention_workspace_bytes that no other call in flight
     uses, or None to take one per call."""
-    c = _kv8(codes, scales)
-    dev = codes.device
+    return _attention("mg_kv8_attention", _kv8(codes, scales), codes.device, q, page_table, lens, cu_new, max_new, max_len, scale,
+                      window, softcap, out, workspace, stream)
+
+
+def _attention(name, c, dev, q, page_table, lens, cu_new, max_new, max_len, scale, window, softcap, out, workspace, stream):
+    """The attention call `name` of the library over the cache c."""
     a = _attn_args(c, q, page_table, lens, cu_new, max_new, max_len, scale, window, softcap, out, dev)
     if out is None:
         out = _new(q.shape, q.dtype, dev, stream)
         a.out = out.data_ptr()
-    args = "mg_kv8_attention", dev, stream, load().mg_kv8_attention, C.byref(c), C.byref(a)
+    args = name, dev, stream, getattr(load(), name), C.byref(c), C.byref(a)
     if workspace is not None:
         if workspace.dtype is not torch.uint8 or workspace.device != dev or not workspace.is_contiguous():
             _refuse("workspace", workspace, f"contiguous uint8 on {dev}")
@@ -466,9 +492,150 @@ def kv8_attention(codes, scales, q, page_table, lens, cu_new=None, max_new=None,
         if e.status != MG_ERR_WORKSPACE:
             raise
         with torch.cuda.device(dev):
-            n = load().mg_kv8_attention_workspace_bytes(*args[4:])
+            n = getattr(load(), name + "_workspace_bytes")(*args[4:])
         workspace = _new(n, torch.uint8, dev, stream)
         _call(*args, workspace.data_ptr(), n)
+    return out
+
+
+# ---------------------------------------------------------------- 4-bit K/V cache
+
+
+def _kv4(codes, scales):
+    """The MgKv4Cache of a layer's codes [n_pages, Hkv, 2, 8 hd] and scales [n_pages, Hkv, hd / 2 + 16]."""
+    shape = codes.shape
+    if codes.dtype is not torch.uint8 or len(shape) != 4 or shape[2] != 2 or shape[3] % 8 or not codes.is_contiguous():
+        _refuse("codes", codes, "contiguous uint8 [n_pages, Hkv, 2, 8 hd]")
+    if scales.dtype is not torch.uint8 or scales.shape != (shape[0], shape[1], shape[3] // 16 + 16) or \
+            not scales.is_contiguous() or scales.device != codes.device:
+        _refuse("scales", scales, f"contiguous uint8 [n_pages, Hkv, hd / 2 + 16] for codes {tuple(shape)} on {codes.device}")
+    return MgKv4Cache(codes.data_ptr(), scales.data_ptr(), shape[0], shape[1], shape[3] // 8)
+
+
+def kv4_empty(n_pages, n_kv_heads, head_dim, device="cuda"):
+    """An empty 4-bit cache of one layer: (codes, scales)."""
+    if load().mg_kv4_code_bytes(n_pages, n_kv_heads, head_dim) == 0:
+        raise MgError("mg_kv4_code_bytes", -2)
+    return (torch.zeros((n_pages, n_kv_heads, 2, 8 * head_dim), dtype=torch.uint8, device=device),
+            torch.zeros((n_pages, n_kv_heads, head_dim // 2 + 16), dtype=torch.uint8, device=device))
+
+
+def rope_table(n_positions, head_dim, theta, device="cuda"):
+    """The rotation's table [n_positions, head_dim] of fp32 cos, sin (interleaved), from angles in float64, as mg_create makes it."""
+    ang = np.arange(n_positions)[:, None] * float(theta) ** (-2.0 * np.arange(head_dim // 2) / head_dim)
+    return torch.as_tensor(np.stack([np.cos(ang), np.sin(ang)], -1).reshape(n_positions, head_dim).astype(np.float32)).to(device)
+
+
+def kv4_append(codes, scales, k, v, slots, positions=None, rope=None, q=None, q_out=None, stream=None):
+    """mg_kv4_append: K and V rows [n, Hkv, hd] quantised into the cache at slots [n]; with positions [n] and rope [n_positions, hd]
+    K is rotated on the way, and the queries q [n, Hq, hd] into q_out (a new tensor if None; q itself for in place), which
+    is returned (None without q).  Rows of tokens with a negative position are not written: in a new tensor they hold anything."""
+    c = _kv4(codes, scales)
+    dev, n, hd = codes.device, slots.numel(), c.head_dim
+    kp, ks = _rows16("k", k, n, c.n_kv_heads, hd, dev)
+    vp, vs = _rows16("v", v, n, c.n_kv_heads, hd, dev)
+    if (positions is None) != (rope is None):
+        raise ValueError("kv4_append: positions and rope come together")
+    pp = rp = None
+    n_pos = 0
+    if positions is not None:
+        pp = _ints("positions", positions, dev, n)
+        if rope.dtype is not torch.float32 or rope.dim() != 2 or rope.shape[1] != hd or not rope.is_contiguous() or \
+                rope.device != dev or not 0 < rope.shape[0] < _I32:
+            _refuse("rope", rope, f"contiguous float32 [n_positions, {hd}] on {dev}")
+        rp, n_pos = rope.data_ptr(), rope.shape[0]
+    qp = op = None
+    qs = os_ = hq = 0
+    if q is not None:
+        if q.dim() != 3:
+            _refuse("q", q, f"bf16 [{n}, Hq, {hd}]")
+        hq = q.shape[1]
+        qp, qs = _rows16("q", q, n, hq, hd, dev)
+        if q_out is None:
+            q_out = _new(q.shape, q.dtype, dev, stream)
+            op, os_ = q_out.data_ptr(), hq * hd
+        else:
+            op, os_ = _rows16("q_out", q_out, n, hq, hd, dev)
+    elif q_out is not None:
+        raise ValueError("kv4_append: q_out without q")
+    a = MgKv4AppendArgs(n, hq, qp, qs, op, os_, kp, ks, vp, vs, _ints("slots", slots, dev), pp, rp, n_pos)
+    _call("mg_kv4_append", dev, stream, load().mg_kv4_append, C.byref(c), C.byref(a))
+    return q_out
+
+
+def kv4_read(codes, scales, slots, k_out=None, v_out=None, stream=None):
+    """mg_kv4_read: as kv8_read, from a 4-bit cache."""
+    return _read("mg_kv4_read", _kv4(codes, scales), codes.device, slots, k_out, v_out, stream)
+
+
+def kv4_attention_workspace_bytes(codes, scales, q, page_table, lens, cu_new=None, max_new=None, max_len=0, window=0):
+    """mg_kv4_attention_workspace_bytes: as kv8_attention_workspace_bytes."""
+    c = _kv4(codes, scales)
+    a = _attn_args(c, q, page_table, lens, cu_new, max_new, max_len, None, window, 0.0, q, codes.device)
+    with torch.cuda.device(codes.device):
+        return load().mg_kv4_attention_workspace_bytes(C.byref(c), C.byref(a))
+
+
+def kv4_attention(codes, scales, q, page_table, lens, cu_new=None, max_new=None, max_len=0, scale=None, window=0,
+                  softcap=0.0, out=None, workspace=None, stream=None):
+    """mg_kv4_attention: as kv8_attention, over a 4-bit cache; q as kv4_append rotated it."""
+    return _attention("mg_kv4_attention", _kv4(codes, scales), codes.device, q, page_table, lens, cu_new, max_new, max_len, scale,
+                      window, softcap, out, workspace, stream)
+
+
+# ---------------------------------------------------------------- token log probabilities
+
+TokenLogprobs = collections.namedtuple("TokenLogprobs", "logprob entropy top_tokens top_logprobs")
+
+
+def token_logprobs_workspace_bytes(n, vocab, top=0, device="cuda"):
+    """mg_token_logprobs_workspace_bytes of n rows (no device work)."""
+    with torch.cuda.device(device):
+        return load().mg_token_logprobs_workspace_bytes(n, vocab, top)
+
+
+def token_logprobs(logits, tokens, top=0, out=None, workspace=None, stream=None):
+    """mg_token_logprobs: the log probabilities of tokens [n] under logits [n, vocab] (float32 or bfloat16, rows of any stride), the
+    rows' entropies [n] and their `top` first alternatives [n, top].  out: a TokenLogprobs to write into (None fields are not
+    computed), or None for new tensors.  workspace: a contiguous uint8 tensor of token_logprobs_workspace_bytes that no other call
+    in flight uses, or None to take one per call."""
+    if logits.dim() != 2 or logits.dtype not in (torch.float32, torch.bfloat16):
+        _refuse("logits", logits, "float32 or bfloat16 [n, vocab]")
+    dev, (n, V) = logits.device, logits.shape
+    st = logits.stride()
+    if n and V > 1 and st[1] != 1:
+        _refuse("logits", logits, "rows without gaps")
+    if not 0 <= top <= 32:
+        _refuse("top", top, "0 .. 32")
+    if out is None:
+        buf = _new(n * (2 + 2 * top), torch.int32, dev, stream)
+        a, b, ids, c = torch.unsafe_split_with_sizes(buf, (n, n, n * top, n * top))
+        f = torch.float32
+        out = TokenLogprobs(a.view(f), b.view(f), ids.view(n, top), c.view(f).view(n, top))
+        at = buf.data_ptr()
+        ptrs = [at + 4 * k for k in (0, n, 2 * n, 2 * n + n * top)] if n else [None] * 4
+    else:
+        ptrs = []
+        for name, t, dt, shape in zip(TokenLogprobs._fields, out, (torch.float32, torch.float32, torch.int32, torch.float32),
+                                      ((n,), (n,), (n, top), (n, top))):
+            if t is not None and (t.dtype is not dt or t.shape != shape or t.device != dev or not t.is_contiguous()):
+                _refuse(name, t, f"contiguous {dt} {shape} on {dev}")
+            ptrs.append(None if t is None else t.data_ptr())
+    tok = None if tokens is None else _ints("tokens", tokens, dev, n)
+    args = ("mg_token_logprobs", dev, stream, load().mg_token_logprobs, n, V, logits.data_ptr(), int(logits.dtype is torch.bfloat16),
+            st[0] if n > 1 else V, tok, top, *ptrs)
+    if workspace is not None:
+        if workspace.dtype is not torch.uint8 or workspace.device != dev or not workspace.is_contiguous():
+            _refuse("workspace", workspace, f"contiguous uint8 on {dev}")
+        _call(*args, workspace.data_ptr(), workspace.numel())
+        return out
+    try:
+        _call(*args, None, 0)
+    except MgError as e:
+        if e.status != MG_ERR_WORKSPACE:
+            raise
+        size = token_logprobs_workspace_bytes(n, V, top, dev)
+        _call(*args, _new(size, torch.uint8, dev, stream).data_ptr(), size)
     return out
 
 
