@@ -5,6 +5,8 @@
 // no code is converted.  K's scale of 32 features is the instruction's own block scale.  V's scale of a position is not
 // along the product's axis, so it goes into the probability; a probability and a query value enter as e2m3 terms (6 bits, at the
 // rate of the 4-bit operand, twice that of 8 bits) whose block scale the lane that holds the block takes from its own values.
+#include <stddef.h>
+
 #include <algorithm>
 #include <type_traits>
 
@@ -38,18 +40,20 @@ __device__ __forceinline__ i32x8_k4 k4_wide(const u32x4_k8& x) {
 }
 // C + A B: A 16 rows of 128 e2m1 values, B 16 columns of 128 e2m3 values; lane 16 g + c holds values 32 g .. 32 g + 31 of row or
 // column c and their scale byte, and rows 4 g .. 4 g + 3 of column c of C.
-// Byte SB of sb is B's scale.
-template <int SB>
+// Byte SA of sa is A's scale, SB of sb B's.
+template <int SA, int SB>
 __device__ __forceinline__ f32x4_k8 k4_mfma(const u32x4_k8& a, uint32_t sa, const i32x6_k4& b, uint32_t sb, f32x4_k8 c) {
-    return __builtin_amdgcn_mfma_scale_f32_16x16x128_f8f6f4(k4_wide(a), k4_wide(b), c, 4, 2, 0, (int)sa, SB, (int)sb);
+    return __builtin_amdgcn_mfma_scale_f32_16x16x128_f8f6f4(k4_wide(a), k4_wide(b), c, 4, 2, SA, (int)sa, SB, (int)sb);
 }
 
-// The scale 2^e (as float bits) under which values of up to `top` (float bits, finite) are below 4 in an e2m3 block, whose largest
-// is 7.5: the first term is off by 1/8 there at most, and 32 times that is in range again.
-__device__ __forceinline__ uint32_t k4_block_scale(uint32_t top) { return max(top & 0x7f800000u, K4_LEAST + (1u << 23)) - (1u << 23); }
+// The scale 2^e (as float bits) under which values of up to `top` (float bits, finite) are below 2: the e2m3 values up to 2 are
+// multiples of 1/8, so that a term is off by 1/16 at most, and 32 times that is at most 2 again.
+__device__ __forceinline__ uint32_t k4_block_scale(uint32_t top) { return max(top & 0x7f800000u, K4_LEAST); }
 // 32 values (of even and of odd index, as the conversion takes them) as TERMS e2m3 blocks under scale, scale / 32, scale / 1024: off
-// by scale / 8, / 256, / 8192 after one, two, three, so by 2^-9 or 2^-14 of the largest at most
-template <int TERMS>
+// by scale / 16, / 512, / 16384 after one, two, three, so by 2^-9 or 2^-14 of the largest at most.  What a term leaves is found by
+// converting it back (BACK: one instruction of some 70 cycles and a subtraction a value, but 32 registers more), or by adding and taking away
+// a number whose last bit is scale / 8, which rounds as the conversion does.
+template <int TERMS, bool BACK>
 __device__ __forceinline__ void k4_terms(f32x16_k4& even, f32x16_k4& odd, uint32_t scale, i32x6_k4 (&t)[TERMS]) {
 #pragma unroll
     for (int k = 0; k < TERMS; ++k) {
@@ -59,12 +63,21 @@ __device__ __forceinline__ void k4_terms(f32x16_k4& even, f32x16_k4& odd, uint32
         // does where they end here; such results were off now and then)
         asm volatile("" : "+v"(q) : "v"(even), "v"(odd), "v"(s));
         t[k] = __builtin_bit_cast(i32x6_k4, q);
-        if (k + 1 < TERMS) {
-            const f32x32_k4 y = __builtin_amdgcn_cvt_scalef32_pk32_f32_fp6(q, s);
+        if (k + 1 == TERMS) break;
+        if (BACK) {
+            f32x32_k4 y = __builtin_amdgcn_cvt_scalef32_pk32_f32_fp6(q, s);
+            asm volatile("" : "+v"(y) : "v"(q), "v"(s));
 #pragma unroll
             for (int i = 0; i < 16; ++i) {
                 even[i] -= y[2 * i];
                 odd[i] -= y[2 * i + 1];
+            }
+        } else {
+            const float M = s * 0x1.8p+20f;
+#pragma unroll
+            for (int i = 0; i < 16; ++i) {
+                even[i] -= (even[i] + M) - M;
+                odd[i] -= (odd[i] + M) - M;
             }
         }
     }
@@ -79,10 +92,15 @@ template <int HD>
 constexpr int K4_OPS = HD == 128 ? 3 : 2;
 template <int HD>
 struct K4Query {
-    uint32_t op[K4_OPS<HD>][64][8];  // a lane's six words; the seventh of operand 0: byte k is operand k's scale
+    uint32_t lo[K4_OPS<HD>][64][4], hi[K4_OPS<HD>][64][2];  // a lane's six words
+    uint32_t scale[64];                                      // byte k: operand k's
 };
+// the position of query row rr's token
+__device__ __forceinline__ int k4_position(const Kv8AttnArgs& a, const K8Row& row, int rr) {
+    return row.p0 + (rr < row.n * a.G ? rr / a.G : 0);
+}
 template <int HD>
-__device__ __forceinline__ int k4_query(const Kv8AttnArgs& a, const K8Row& row, int kh, int rr0, K4Query<HD>& q) {
+__device__ __forceinline__ void k4_query(const Kv8AttnArgs& a, const K8Row& row, int kh, int rr0, K4Query<HD>& q) {
     const int lane = threadIdx.x & 63, c = lane & 15, g = lane >> 4;
     int rr = rr0 + c;
     rr = rr < row.n * a.G ? rr : 0;
@@ -99,7 +117,7 @@ __device__ __forceinline__ int k4_query(const Kv8AttnArgs& a, const K8Row& row, 
     }
     const uint32_t s = k4_block_scale(top << 16);
     i32x6_k4 t[3];
-    k4_terms<3>(even, odds, s, t);
+    k4_terms<3, false>(even, odds, s, t);
     // (a value that is not finite makes the scores NaN)
     const bool odd = top >= 0x7f80u;
     const uint32_t b0 = odd ? 255u : s >> 23, b1 = odd ? 255u : (s >> 23) - 5, b2 = odd ? 255u : (s >> 23) - 10;
@@ -110,19 +128,18 @@ __device__ __forceinline__ int k4_query(const Kv8AttnArgs& a, const K8Row& row, 
             t[1][i] = g < 2 ? t[2][i] : 0;
         }
     }
-    q.op[0][lane][6] = HD == 128 ? b0 | b1 << 8 | b2 << 16 : g < 2 ? b0 | b2 << 8 : b1 | 127u << 8;
+    q.scale[lane] = HD == 128 ? b0 | b1 << 8 | b2 << 16 : g < 2 ? b0 | b2 << 8 : b1 | 127u << 8;
 #pragma unroll
     for (int k = 0; k < K4_OPS<HD>; ++k) {
-        *reinterpret_cast<u32x4_k8*>(q.op[k][lane]) = u32x4_k8{(uint32_t)t[k][0], (uint32_t)t[k][1], (uint32_t)t[k][2], (uint32_t)t[k][3]};
-        *reinterpret_cast<u32x2_k8*>(q.op[k][lane] + 4) = u32x2_k8{(uint32_t)t[k][4], (uint32_t)t[k][5]};
+        *reinterpret_cast<u32x4_k8*>(q.lo[k][lane]) = u32x4_k8{(uint32_t)t[k][0], (uint32_t)t[k][1], (uint32_t)t[k][2], (uint32_t)t[k][3]};
+        *reinterpret_cast<u32x2_k8*>(q.hi[k][lane]) = u32x2_k8{(uint32_t)t[k][4], (uint32_t)t[k][5]};
     }
-    return row.p0 + rr / a.G;
 }
 template <int HD>
 __device__ __forceinline__ i32x6_k4 k4_operand(const K4Query<HD>& q, int k) {
     const int lane = threadIdx.x & 63;
-    const u32x4_k8 lo = *reinterpret_cast<const u32x4_k8*>(q.op[k][lane]);
-    const u32x2_k8 hi = *reinterpret_cast<const u32x2_k8*>(q.op[k][lane] + 4);
+    const u32x4_k8 lo = *reinterpret_cast<const u32x4_k8*>(q.lo[k][lane]);
+    const u32x2_k8 hi = *reinterpret_cast<const u32x2_k8*>(q.hi[k][lane]);
     return i32x6_k4{(int)lo[0], (int)lo[1], (int)lo[2], (int)lo[3], (int)hi[0], (int)hi[1]};
 }
 
@@ -241,21 +258,26 @@ __device__ __forceinline__ void k4_walk(const Kv8AttnArgs& a, const K8Row& row, 
             float x[32];
             {
                 asm volatile("" ::: "memory");  // (the queries are read anew, not held in registers)
-                const uint32_t qs = q.op[0][lane][6];
+                const uint32_t qs = q.scale[lane];
                 f32x4_k8 c[K4_STEP];
 #pragma unroll
                 for (int e = 0; e < K4_STEP; ++e) c[e] = f32x4_k8{0.f, 0.f, 0.f, 0.f};
                 const auto term = [&](auto K) {
                     const i32x6_k4 b = k4_operand(q, K.value);
 #pragma unroll
-                    for (int e = 0; e < K4_STEP; ++e) c[e] = k4_mfma<K.value>(kb[e], ks[e], b, qs, c[e]);
+                    for (int e = 0; e < K4_STEP; ++e) c[e] = k4_mfma<0, K.value>(kb[e], ks[e], b, qs, c[e]);
                 };
                 term(std::integral_constant<int, 0>{});
                 term(std::integral_constant<int, 1>{});
                 if constexpr (K4_OPS<HD> == 3) term(std::integral_constant<int, 2>{});
 #pragma unroll
+                for (int e = 0; e < K4_STEP; ++e) asm volatile("" : "+v"(c[e]));  // (here, not behind the branch of the loads)
+#pragma unroll
                 for (int i = 0; i < 32; ++i) x[i] = c[i >> 2][i & 3];
             }
+            __builtin_amdgcn_sched_barrier(0);
+            if (more) fetch_k(s + stride);  // K's registers are free
+            __builtin_amdgcn_sched_barrier(0);
             if (CAP) {
                 k8_cap(reinterpret_cast<float(&)[1][32]>(x), so);
             }
@@ -284,22 +306,19 @@ __device__ __forceinline__ void k4_walk(const Kv8AttnArgs& a, const K8Row& row, 
             }
             const uint32_t sc = k4_block_scale(__float_as_uint(top));
             i32x6_k4 p[TERMS];
-            k4_terms<TERMS>(y[0], y[1], sc, p);
+            k4_terms<TERMS, false>(y[0], y[1], sc, p);
             // byte k: term k's scale (past fp32: NaN)
             uint32_t ps = (sc >> 23) + K4_FOLD;
             ps = ps > 254u ? 0xffffffu : ps * 0x10101u - 0xa0500u;
-            __builtin_amdgcn_sched_barrier(0);
-            if (more) fetch_k(s + stride);  // K's registers are free, and the scores'
-            __builtin_amdgcn_sched_barrier(0);
 #pragma unroll
             for (int d = 0; d < DT; ++d) {
                 u32x4_k8 A;
 #pragma unroll
                 for (int e = 0; e < 4; ++e)
                     A[e] = __builtin_amdgcn_perm(vb[2 * e + 1][d / 2], vb[2 * e][d / 2], d & 1 ? 0x07060302u : 0x05040100u);
-                acc.o[d] = k4_mfma<0>(A, 127u, p[0], ps, acc.o[d]);
-                acc.o[d] = k4_mfma<1>(A, 127u, p[1], ps, acc.o[d]);
-                if constexpr (TERMS == 3) acc.o[d] = k4_mfma<2>(A, 127u, p[2], ps, acc.o[d]);
+                acc.o[d] = k4_mfma<0, 0>(A, 127u, p[0], ps, acc.o[d]);
+                acc.o[d] = k4_mfma<0, 1>(A, 127u, p[1], ps, acc.o[d]);
+                if constexpr (TERMS == 3) acc.o[d] = k4_mfma<0, 2>(A, 127u, p[2], ps, acc.o[d]);
             }
             __builtin_amdgcn_sched_barrier(0);
             if (more) fetch_v(s + stride);
@@ -344,7 +363,8 @@ __device__ __forceinline__ void k4_few_block(const Kv8AttnArgs& a, const K8Few& 
 
     // (waves of a tile have the same queries: each writes its own, and waits for nobody)
     const int tile = wave % NT;
-    const int pos = k4_query<HD>(a, row, kh, 16 * tile, sh.q[wave]);
+    k4_query<HD>(a, row, kh, 16 * tile, sh.q[wave]);
+    const int pos = k4_position(a, row, 16 * tile + c);
     K4Acc<HD> acc;
     acc.clear();
     if (16 * tile < row.n * a.G)
@@ -425,17 +445,47 @@ __global__ __launch_bounds__(K8_THREADS) void attn_kv4_join_kernel(Kv8AttnArgs a
     k4_few_join<HD, NT, EVEN>(a, few, blockIdx.x, rowb);
 }
 
-// Rows of more query rows: one block per (row, KV head, 64 query rows, split of the positions that these see), the tokens of a
-// row's end first (they see the most).  Each wave takes its own 16 query rows over all of the block's pages; the waves read the
-// same codes at about the same time.
-constexpr int K4_CHUNK_ROWS = K8_WAVES * 16;
-constexpr int K4_MIN_STAGES = 2;  // steps that a split of a tile takes at least
-template <int HD, bool CAP>
+// Rows of more query rows: one block per (row, KV head, 64 NT query rows, split of the positions that these see), the tokens of a
+// row's end first (they see the most).  A wave holds NT tiles of query rows; four waves share a step's codes through a double buffer in LDS: a
+// wave fetches two pages of the next step, K as it is, V's two pages joined into the words of its operands, V's scales as
+// numbers; one barrier a step parts the buffers.  GROUPS 2: the block has four waves more for the same query rows, and each group takes half of
+// its steps; their outputs join at the end.
+constexpr int K4_TILES = 2;  // tiles of 16 query rows of a wave
+constexpr int K4_CHUNK_ROWS = K8_WAVES * 16 * K4_TILES;
+constexpr int K4_MIN_STAGES = 4;  // steps that a split of a tile takes at least
+static_assert(K4_STEP == 2 * K8_WAVES, "a wave stages two pages");
+// values at a byte address of LDS: a register and a constant each, so that neighbouring reads share the register
+template <class T>
+__device__ __forceinline__ T k4_lds(uint32_t at) {
+    return *reinterpret_cast<const __attribute__((address_space(3))) T*>(at);
+}
+template <class T>
+__device__ __forceinline__ uint32_t k4_lds_at(const T* p) {
+    return (uint32_t)reinterpret_cast<uintptr_t>((const __attribute__((address_space(3))) T*)p);
+}
+template <int HD>
+struct K4Stage {
+    uint32_t k[K4_STEP][HD / 2][4];  // (HD 64: 32 lanes' words)
+    uint32_t v[HD / 16][64][4];      // operand of an output tile; word e: pages 2 e and 2 e + 1
+    uint8_t ks[64][K4_STEP];         // a lane's scale bytes of K, page by page
+    float vs[K4_STEP][16];           // V's scales (0 where the value is not finite)
+    uint32_t odd[K8_WAVES];          // bit 16 e + t: position t of page 2 word + e of V is not finite
+};
+template <int HD, int GROUPS>
+struct K4ChunkShared {
+    K4Stage<HD> stage[GROUPS][2];
+    K4Query<HD> q[K8_WAVES][K4_TILES];
+};
+template <int HD, int GROUPS, bool CAP>
 __device__ __forceinline__ void k4_chunk_block(const Kv8AttnArgs& a, int few, int tiles, int nsplit, float* part, int block,
-                                               K4Query<HD> (&sh)[K8_WAVES]) {
-    constexpr int DT = HD / 16, ROWS = K4_CHUNK_ROWS;
+                                               K4ChunkShared<HD, GROUPS>& sh) {
+    typedef typename K4Lane<HD>::v vlane;
+    typedef const __attribute__((address_space(1))) char* gptr;
+    constexpr int DT = HD / 16, ROWS = K4_CHUNK_ROWS, NT = K4_TILES;
+    constexpr size_t head_bytes = 16 * HD, head_scales = HD / 2 + 16;
     const int lane = threadIdx.x & 63, c = lane & 15, g = lane >> 4;
-    const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+    const int group = GROUPS == 1 ? 0 : __builtin_amdgcn_readfirstlane(threadIdx.x / K8_THREADS);
+    const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6) % K8_WAVES;
     const int kh = block % a.c.Hkv;
     const int split = block / a.c.Hkv % nsplit, index = block / a.c.Hkv / nsplit;
     const K8Tile at = k8_tile<ROWS>(a, few, index);
@@ -446,53 +496,269 @@ __device__ __forceinline__ void k4_chunk_block(const Kv8AttnArgs& a, int few, in
     if (t * ROWS >= live) return;
     const K8Span span = k8_span<ROWS, K4_STEP, K4_MIN_STAGES>(a, row, t, nsplit);
     if (split >= span.act) return;
-    const int rr0 = t * ROWS + wave * 16;
-    // the block's pages, and those of them that this wave's tokens see
-    int pg0 = span.pg0 + span.stages * split / span.act * K4_STEP, pg1 = min(span.pg1, span.pg0 + span.stages * (split + 1) / span.act * K4_STEP);
-    const int wp0 = row.p0 + min(rr0, live - 1) / a.G, wp1 = row.p0 + (min(rr0 + 16, live) - 1) / a.G;
-    pg1 = min(pg1, (max(0, min(wp1 + 1, row.len)) + 15) / 16);
-    if (a.window) pg0 = max(pg0, pg0 + (min((k8_hidden(a.window, wp0) + 1) / 16, pg1) - pg0) / K4_STEP * K4_STEP);
+    // the block's steps, and the group's of them; most: those of the group that has more
+    const int b0 = span.stages * split / span.act, b1 = span.stages * (split + 1) / span.act, half = GROUPS == 1 ? b1 : (b0 + b1 + 1) / 2;
+    const int st0 = group ? half : b0, steps = (group ? b1 : half) - st0, most = half - b0;
+    const int pg0 = span.pg0 + st0 * K4_STEP, pg1 = min(span.pg1, pg0 + steps * K4_STEP);
+    const int rr0 = t * ROWS + wave * (16 * NT);
+    const int wp0 = row.p0 + min(rr0, live - 1) / a.G, wp1 = row.p0 + (min(rr0 + 16 * NT, live) - 1) / a.G;
 
-    const int pos = k4_query<HD>(a, row, kh, rr0, sh[wave]);
-    K4Acc<HD> acc;
-    acc.clear();
-    if (rr0 < live) k4_walk<HD, 2, CAP, false>(a, row, r, kh, pg0, pg1, 0, 1, sh[wave], pos, wp1, acc);
-    const float L = k8_col_sum(acc.l);
-    const float inv = L == 0.0f ? 0.0f : ieee_div(1.0f, L);
-    const int rr = rr0 + c;
-    if (rr >= live) return;
-    if (span.act > 1) {
-        const size_t pr = ((size_t)(index * a.c.Hkv + kh) * nsplit + split) * ROWS + wave * 16 + c;
+    int pos[NT];
+    K4Acc<HD> acc[NT];
 #pragma unroll
-        for (int d = 0; d < DT; ++d) *reinterpret_cast<f32x4_k8*>(part + pr * HD + 16 * d + 4 * g) = acc.o[d];
-        if (g == 0) {
-            float* ml = part + (size_t)tiles * a.c.Hkv * nsplit * ROWS * HD + 2 * pr;
-            ml[0] = acc.m;
-            ml[1] = L;
-        }
-        return;
+    for (int u = 0; u < NT; ++u)
+        if (u % GROUPS == group) k4_query<HD>(a, row, kh, rr0 + 16 * u, sh.q[wave][u]);
+#pragma unroll
+    for (int u = 0; u < NT; ++u) {
+        pos[u] = k4_position(a, row, rr0 + 16 * u + c);
+        acc[u].clear();
     }
-    uint16_t* out = k8_out(a, row, kh, rr) + 4 * g;
+    K8Soft so = k8_soft(a);
+    so = K8Soft{k4_scalar(so.f), k4_scalar(so.zin), k4_scalar(so.most)};
+    const int32_t* ptab = a.page_table + (size_t)r * a.maxp;
+
+    // lane i: page pg0 + 64 n + i of the 64 that hold the step fetched last (a hole, or one past the block's: page 0, unseen), and the next 64's
+    auto page_id = [&](int i) { return i < pg1 ? ptab[i] : -1; };
+    auto valid = [&](int v) { return v >= 0 && v < a.c.n_pages; };
+    int idn = page_id(pg0 + lane);
+    uint32_t place = 0;
+    unsigned long long live_pages = 0;
+    u32x4_k8 nk[2];
+    vlane nv[2];
+    uint32_t nks[2], nvs;
+    uint32_t map = 0;
+    auto fetch = [&](int st) {
+        const int at = st * K4_STEP % K8_IDS;
+        if (at == 0) {
+            live_pages = __ballot(valid(idn));
+            place = (valid(idn) ? (uint32_t)idn : 0u) * (uint32_t)a.c.Hkv + (uint32_t)kh;
+            idn = page_id(pg0 + st * K4_STEP + K8_IDS + lane);
+        }
+        map = (uint32_t)(live_pages >> at) & 0xffu;
+        uint32_t ln = lane, pl = place;
+        asm volatile("" : "+v"(ln), "+v"(pl));
+        const uint32_t kl = HD == 128 ? ln : ln & 31;
+        uint32_t ph[2];
 #pragma unroll
-    for (int d = 0; d < DT; ++d)
-        *reinterpret_cast<uint2*>(out + 16 * d) =
-            make_uint2(k8_pack(acc.o[d][0] * inv, acc.o[d][1] * inv), k8_pack(acc.o[d][2] * inv, acc.o[d][3] * inv));
+        for (int e = 0; e < 2; ++e) {
+            ph[e] = (uint32_t)__builtin_amdgcn_readlane((int)pl, at + 2 * wave + e);
+            const uint64_t p = k8_uniform(a.c.codes + (size_t)ph[e] * head_bytes), ps = k8_uniform(a.c.scales + (size_t)ph[e] * head_scales);
+            nk[e] = *reinterpret_cast<const __attribute__((address_space(1))) u32x4_k8*>(reinterpret_cast<gptr>(p) + kl * 16u);
+            nv[e] = *reinterpret_cast<const __attribute__((address_space(1))) vlane*>(reinterpret_cast<gptr>(p) + (8 * HD + ln * (uint32_t)sizeof(vlane)));
+            nks[e] = *reinterpret_cast<const __attribute__((address_space(1))) uint8_t*>(reinterpret_cast<gptr>(ps) + kl);
+        }
+        // lanes 0..15 and 16..31: the scales of V's sixteen positions of both pages
+        const uint8_t* ps = a.c.scales + (size_t)(ln & 16 ? ph[1] : ph[0]) * head_scales + HD / 2 + (ln & 15);
+        nvs = *ps;
+    };
+    auto put = [&](K4Stage<HD>& s) {
+#pragma unroll
+        for (int e = 0; e < 2; ++e)
+            if (HD == 128 || lane < 32) *reinterpret_cast<u32x4_k8*>(s.k[2 * wave + e][lane]) = nk[e];
+        *reinterpret_cast<uint16_t*>(&s.ks[lane][2 * wave]) = (uint16_t)(nks[0] | nks[1] << 8);
+#pragma unroll
+        for (int d = 0; d < DT; ++d) s.v[d][lane][wave] = __builtin_amdgcn_perm(nv[1][d / 2], nv[0][d / 2], d & 1 ? 0x07060302u : 0x05040100u);
+        const unsigned long long odd = __ballot(nvs == 255u);
+        if (lane < 32) s.vs[2 * wave + (lane >> 4)][lane & 15] = __uint_as_float(nvs == 255u ? 0u : nvs << 23);
+        if (lane == 0) s.odd[wave] = (uint32_t)odd;
+    };
+
+    // a lane's places in LDS
+    uint32_t q16 = k4_lds_at(&sh.q[wave][0]) + 16 * lane;
+    asm("" : "+v"(q16));
+    uint32_t now = 0;
+    if (steps) {
+        fetch(0);
+        put(sh.stage[group][0]);
+    }
+    if (group) __builtin_amdgcn_s_setprio(1);  // (the groups meet at every barrier, and would else want the same units at the same times)
+    for (int st = 0; st < most; ++st) {
+        const K4Stage<HD>& s = sh.stage[group][st & 1];
+        now = map;
+        __syncthreads();  // (also keeps the queries' reads in the loop: they are not held in registers)
+        if (st + 1 < steps) fetch(st + 1);
+        const int j0 = 16 * (pg0 + st * K4_STEP);
+        // whether there is anything for this wave's tokens in these positions
+        if (st < steps && j0 <= wp1 && !(a.window && j0 + 127 <= k8_hidden(a.window, wp0))) {
+            const bool edge = now != 0xffu || j0 + 127 > wp0 || j0 + 128 > row.len || (a.window && j0 <= k8_hidden(a.window, wp1));
+            constexpr uint32_t LO = offsetof(K4Query<HD>, lo), HI = offsetof(K4Query<HD>, hi), SC = offsetof(K4Query<HD>, scale);
+            constexpr uint32_t SV = offsetof(K4Stage<HD>, v), SKS = offsetof(K4Stage<HD>, ks), SVS = offsetof(K4Stage<HD>, vs);
+            uint32_t ln = lane;
+            asm("" : "+v"(ln));
+            const uint32_t base = k4_lds_at(&s), s16 = base + 16 * ln, sk = HD == 128 ? s16 : base + 16 * (ln & 31);
+            const uint32_t odd = s.odd[0] | s.odd[1] | s.odd[2] | s.odd[3];
+            float x[NT][32];
+            {
+                f32x4_k8 sc[NT][K4_STEP];
+                const u32x2_k8 ks = k4_lds<u32x2_k8>(base + SKS + 8 * ln);
+                uint32_t qs[NT];
+                const uint32_t q8 = q16 - 8 * ln, q4 = q8 - 4 * ln;
+#pragma unroll
+                for (int u = 0; u < NT; ++u) {
+                    qs[u] = k4_lds<uint32_t>(q4 + (uint32_t)(u * sizeof(K4Query<HD>)) + SC);
+#pragma unroll
+                    for (int e = 0; e < K4_STEP; ++e) sc[u][e] = f32x4_k8{0.f, 0.f, 0.f, 0.f};
+                }
+                u32x4_k8 kb[K4_STEP];
+#pragma unroll
+                for (int e = 0; e < K4_STEP; ++e) kb[e] = k4_lds<u32x4_k8>(sk + e * 8 * HD);
+                // (a term's operands are requested before the products of the one before it)
+                i32x6_k4 b[2][NT];
+                const auto read = [&](int k) {
+#pragma unroll
+                    for (int u = 0; u < NT; ++u) {
+                        const uint32_t at = (uint32_t)(u * sizeof(K4Query<HD>));
+                        const u32x4_k8 lo = k4_lds<u32x4_k8>(q16 + at + LO + k * 1024);
+                        const u32x2_k8 hi = k4_lds<u32x2_k8>(q8 + at + HI + k * 512);
+                        b[k & 1][u] = i32x6_k4{(int)lo[0], (int)lo[1], (int)lo[2], (int)lo[3], (int)hi[0], (int)hi[1]};
+                    }
+                    __builtin_amdgcn_sched_barrier(0);
+                };
+                const auto term = [&](auto K) {
+#pragma unroll
+                    for (int u = 0; u < NT; ++u) {
+                        const i32x6_k4& o = b[K.value & 1][u];
+                        sc[u][0] = k4_mfma<0, K.value>(kb[0], ks[0], o, qs[u], sc[u][0]);
+                        sc[u][1] = k4_mfma<1, K.value>(kb[1], ks[0], o, qs[u], sc[u][1]);
+                        sc[u][2] = k4_mfma<2, K.value>(kb[2], ks[0], o, qs[u], sc[u][2]);
+                        sc[u][3] = k4_mfma<3, K.value>(kb[3], ks[0], o, qs[u], sc[u][3]);
+                        sc[u][4] = k4_mfma<0, K.value>(kb[4], ks[1], o, qs[u], sc[u][4]);
+                        sc[u][5] = k4_mfma<1, K.value>(kb[5], ks[1], o, qs[u], sc[u][5]);
+                        sc[u][6] = k4_mfma<2, K.value>(kb[6], ks[1], o, qs[u], sc[u][6]);
+                        sc[u][7] = k4_mfma<3, K.value>(kb[7], ks[1], o, qs[u], sc[u][7]);
+                    }
+                    __builtin_amdgcn_sched_barrier(0);
+                };
+                read(0);
+                read(1);
+                term(std::integral_constant<int, 0>{});
+                if constexpr (K4_OPS<HD> == 3) read(2);
+                term(std::integral_constant<int, 1>{});
+                if constexpr (K4_OPS<HD> == 3) term(std::integral_constant<int, 2>{});
+#pragma unroll
+                for (int u = 0; u < NT; ++u) {
+#pragma unroll
+                    for (int e = 0; e < K4_STEP; ++e) asm volatile("" : "+v"(sc[u][e]));  // (here, not behind the branches that follow)
+#pragma unroll
+                    for (int i = 0; i < 32; ++i) x[u][i] = sc[u][i >> 2][i & 3];
+                }
+            }
+            i32x6_k4 p[NT][2];
+            uint32_t ps[NT];
+            __builtin_amdgcn_sched_barrier(0);
+#pragma unroll
+            for (int u = 0; u < NT; ++u) {
+                if (CAP) k8_cap(reinterpret_cast<float(&)[1][32]>(x[u]), so);
+                if (edge) {
+                    int pp = pos[u];
+                    asm("" : "+v"(pp));
+                    const int hi = min(pp, row.len - 1) - j0 - 4 * g, lo = (a.window ? k8_hidden(a.window, pp) : -1) - j0 - 4 * g;
+#pragma unroll
+                    for (int i = 0; i < 32; ++i) {
+                        const int at = 16 * (i >> 2) + (i & 3);
+                        x[u][i] = (now >> (i >> 2) & 1u) && at <= hi && at > lo ? x[u][i] : -__builtin_inff();
+                    }
+                }
+                if (__any(odd != 0)) {  // a value of V that is not finite: the columns that see it, and no other, become NaN
+#pragma unroll
+                    for (int i = 0; i < 32; ++i)
+                        x[u][i] = (s.odd[i >> 3] >> (4 * g) >> (16 * (i >> 2 & 1) + (i & 3)) & 1u) && x[u][i] != -__builtin_inff() ? __builtin_nanf("") : x[u][i];
+                }
+                k4_probs<HD>(x[u], so.f, acc[u]);
+                f32x16_k4 y[2];
+                float top = 0.0f;
+#pragma unroll
+                for (int e = 0; e < K4_STEP; ++e) {
+                    const f32x4_k8 v = k4_lds<f32x4_k8>(base + SVS + 64 * e + 16 * g);
+#pragma unroll
+                    for (int i = 0; i < 4; ++i) {
+                        y[i & 1][2 * e + (i >> 1)] = x[u][4 * e + i] * v[i];
+                        top = fmaxf(top, y[i & 1][2 * e + (i >> 1)]);
+                    }
+                }
+                const uint32_t bs = k4_block_scale(__float_as_uint(top));
+                k4_terms<2, !CAP>(y[0], y[1], bs, p[u]);
+                ps[u] = bs == 0x7f800000u ? 0xffffu : (bs >> 23) * 0x101u - 0x500u;  // (past fp32: NaN)
+            }
+#pragma unroll
+            for (int d = 0; d < DT; ++d) {
+                const u32x4_k8 A = k4_lds<u32x4_k8>(s16 + SV + d * 1024);
+#pragma unroll
+                for (int u = 0; u < NT; ++u) {
+                    acc[u].o[d] = k4_mfma<0, 0>(A, 127u, p[u][0], ps[u], acc[u].o[d]);
+                    acc[u].o[d] = k4_mfma<0, 1>(A, 127u, p[u][1], ps[u], acc[u].o[d]);
+                }
+            }
+        }
+        if (st + 1 < steps) put(sh.stage[group][(st + 1) & 1]);
+    }
+#pragma unroll
+    for (int u = 0; u < NT; ++u) acc[u].l = k8_col_sum(acc[u].l);
+    if constexpr (GROUPS == 2) {  // the second group's outputs join the first's, through the stages
+        static_assert(K8_WAVES * NT * 64 * (DT * 4 + 2) * sizeof(float) <= sizeof(sh.stage), "a group's outputs fit the stages");
+        f32x4_k8* other = reinterpret_cast<f32x4_k8*>(sh.stage) + wave * (NT * DT * 64) + lane;
+        float* other_ml = reinterpret_cast<float*>(reinterpret_cast<f32x4_k8*>(sh.stage) + K8_WAVES * NT * DT * 64) + wave * (2 * NT * 64) + lane;
+        __syncthreads();
+        if (group) {
+#pragma unroll
+            for (int u = 0; u < NT; ++u) {
+                other_ml[2 * u * 64] = acc[u].m;
+                other_ml[(2 * u + 1) * 64] = acc[u].l;
+#pragma unroll
+                for (int d = 0; d < DT; ++d) other[(u * DT + d) * 64] = acc[u].o[d];
+            }
+        }
+        __syncthreads();
+        if (group) return;
+#pragma unroll
+        for (int u = 0; u < NT; ++u) {
+            const float m1 = other_ml[2 * u * 64], M = fmaxf(acc[u].m, m1);
+            const float f0 = __builtin_amdgcn_exp2f(acc[u].m - M), f1 = __builtin_amdgcn_exp2f(m1 - M);
+            acc[u].m = M;
+            acc[u].l = acc[u].l * f0 + other_ml[(2 * u + 1) * 64] * f1;
+#pragma unroll
+            for (int d = 0; d < DT; ++d) acc[u].o[d] = acc[u].o[d] * f0 + other[(u * DT + d) * 64] * f1;
+        }
+    }
+#pragma unroll
+    for (int u = 0; u < NT; ++u) {
+        const float L = acc[u].l;
+        const float inv = L == 0.0f ? 0.0f : ieee_div(1.0f, L);
+        const int rr = rr0 + 16 * u + c;
+        if (rr >= live) continue;
+        if (span.act > 1) {
+            const size_t pr = ((size_t)(index * a.c.Hkv + kh) * nsplit + split) * ROWS + wave * (16 * NT) + 16 * u + c;
+#pragma unroll
+            for (int d = 0; d < DT; ++d) *reinterpret_cast<f32x4_k8*>(part + pr * HD + 16 * d + 4 * g) = acc[u].o[d];
+            if (g == 0) {
+                float* ml = part + (size_t)tiles * a.c.Hkv * nsplit * ROWS * HD + 2 * pr;
+                ml[0] = acc[u].m;
+                ml[1] = L;
+            }
+            continue;
+        }
+        uint16_t* out = k8_out(a, row, kh, rr) + 4 * g;
+#pragma unroll
+        for (int d = 0; d < DT; ++d)
+            *reinterpret_cast<uint2*>(out + 16 * d) =
+                make_uint2(k8_pack(acc[u].o[d][0] * inv, acc[u].o[d][1] * inv), k8_pack(acc[u].o[d][2] * inv, acc[u].o[d][3] * inv));
+    }
 }
 
 // A call with longer rows: their blocks, then those of its rows of few query rows, in one launch.
-template <int HD, bool CAP>
-__global__ __launch_bounds__(K8_THREADS) __attribute__((amdgpu_waves_per_eu(2))) void attn_kv4_mixed_kernel(Kv8AttnArgs a, K8Few few, int tiles,
-                                                                                                      int csplit, float* cpart) {
+template <int HD, int GROUPS, bool CAP>
+__global__ __launch_bounds__(GROUPS* K8_THREADS) __attribute__((amdgpu_waves_per_eu(2))) void attn_kv4_mixed_kernel(
+    Kv8AttnArgs a, K8Few few, int tiles, int csplit, float* cpart) {
     union Shared {
-        K4Query<HD> chunk[K8_WAVES];
-        K4FewShared<HD, K8_WAVES> few;
+        K4ChunkShared<HD, GROUPS> chunk;
+        K4FewShared<HD, GROUPS * K8_WAVES> few;
     };
     __shared__ __attribute__((aligned(16))) Shared sh;
     const int chunks = tiles * a.c.Hkv * csplit;
     if ((int)blockIdx.x < chunks)
-        k4_chunk_block<HD, CAP>(a, 16, tiles, csplit, cpart, blockIdx.x, sh.chunk);
+        k4_chunk_block<HD, GROUPS, CAP>(a, 16, tiles, csplit, cpart, blockIdx.x, sh.chunk);
     else
-        k4_few_block<HD, 1, K8_WAVES, CAP, false>(a, few, blockIdx.x - chunks, sh.few);
+        k4_few_block<HD, 1, GROUPS * K8_WAVES, CAP, false>(a, few, blockIdx.x - chunks, sh.few);
 }
 
 // Joins the splits of attn_kv4_mixed_kernel: blocks of its longer rows' tiles (csplit > 1), a wave per query row, then of the
@@ -526,14 +792,16 @@ struct K4Plan {
     int64_t few_blocks;
     int64_t tiles;              // of K4_CHUNK_ROWS query rows, of the longer rows: at most (a row's last may be partly empty); 0: none
     int csplit;                 // splits of such a tile
+    int groups;                 // of waves of a block in a call with longer rows
 };
+constexpr int K4_GROUP_BLOCKS_PER_CU = 2;
 constexpr int K4_MIN_PAGES = K4_STEP * K8_WAVES;  // pages a split takes at least: a step of every wave
 constexpr int K4_MAX_PAGES = 256;
 constexpr int K4_MAX_SPLITS = 64;
 constexpr int K4_BLOCKS_PER_CU = 2;
 constexpr int K4_EVEN_PAGES = 64;
 constexpr int K4_MIXED_PAGES = 256;
-constexpr int K4_CHUNK_BLOCKS_PER_CU = 2;
+constexpr int K4_CHUNK_BLOCKS_PER_CU = 1;
 // pages that a group of `tokens` neighbouring tokens of a row sees at most, by the host's bounds
 int64_t pages_seen(const Kv8AttnArgs& a, int64_t tokens) {
     int64_t len = a.max_len;
@@ -560,11 +828,12 @@ K4Plan plan_of(const Kv8AttnArgs& a) {
         p.few.units = units;
         p.few_blocks = std::max<int64_t>(p.few_blocks, (int64_t)units * a.c.Hkv);
     }
-    p.csplit = 1;
+    p.csplit = p.groups = 1;
     if (p.tiles) {
         const int64_t stages = (pages_seen(a, std::min(a.max_new, K4_CHUNK_ROWS / a.G + 1)) + K4_STEP - 1) / K4_STEP;
         const int64_t most = std::min<int64_t>(K4_MAX_SPLITS, std::max<int64_t>(1, stages / K4_MIN_STAGES));
         p.csplit = (int)std::min<int64_t>(most, std::max<int64_t>(1, K4_CHUNK_BLOCKS_PER_CU * a.n_cu / (p.tiles * a.c.Hkv)));
+        p.groups = p.tiles * a.c.Hkv * p.csplit <= K4_GROUP_BLOCKS_PER_CU * a.n_cu ? 2 : 1;
     }
     return p;
 }
@@ -593,8 +862,9 @@ void launch(const Kv8AttnArgs& a, const K4Plan& p, hipStream_t s) {
     }
     float* cpart = a.part + few_floats(a, p);
     const dim3 grid((unsigned)(p.tiles * a.c.Hkv * p.csplit + p.few_blocks));
-    auto f = a.cap > 0.0f ? attn_kv4_mixed_kernel<HD, true> : attn_kv4_mixed_kernel<HD, false>;
-    hipLaunchKernelGGL(f, grid, dim3(K8_THREADS), 0, s, a, p.few, (int)p.tiles, p.csplit, cpart);
+    auto f = p.groups == 2 ? (a.cap > 0.0f ? attn_kv4_mixed_kernel<HD, 2, true> : attn_kv4_mixed_kernel<HD, 2, false>)
+                           : (a.cap > 0.0f ? attn_kv4_mixed_kernel<HD, 1, true> : attn_kv4_mixed_kernel<HD, 1, false>);
+    hipLaunchKernelGGL(f, grid, dim3(p.groups * K8_THREADS), 0, s, a, p.few, (int)p.tiles, p.csplit, cpart);
     const int64_t joins = few_joins + (p.csplit > 1 ? p.tiles * a.c.Hkv * (K4_CHUNK_ROWS / K8_WAVES) : 0);
     if (joins)
         hipLaunchKernelGGL(attn_kv4_mixed_join_kernel<HD>, dim3((unsigned)joins), dim3(K8_THREADS), 0, s, a, p.few, rowb,
