@@ -4,7 +4,14 @@
 //   log p(t) = x_t - m - ln S,  entropy = ln S - T / S,
 // and the alternatives are the logits that come first by (value, then lower index).  One pass: a wave reads 2048 logits into
 // registers, takes their sums under a running reference and moves those that beat the last of its `top` best into a list
-// that it keeps sorted over its lanes; states and lists of a row's waves and segments join at the end.
+// that it keeps sorted over its lanes; states and lists of a row's waves and segments join at the end.  A list that starts empty
+// would take in some hundred logits one after the other before its last keeps most out, so the waves of a block first agree on a
+// value that `top` of their logits reach: the least of what enough lanes' largest reach in each wave.
+//
+// What bounds it: the logits' bytes where rows are many (2001 rows of 152064 bf16 with 8 alternatives 128 us, 4.75 TB/s, 2001 of
+// 32000 fp32 with 20 49.7 us, 5.2 TB/s; a large read reaches 6.1), and where they are few the chain of load, floor, list, join and the second
+// launch (one row of 128256 fp32 with 5 alternatives 10.6 us, the join alone 4; 64 rows with 20 16.8 us, 9.1 without alternatives).
+// Exponentials take the logits' differences from the reference in 32 bits; nothing is rounded to fewer.
 #include <algorithm>
 
 #include "mg_device.h"
@@ -18,6 +25,9 @@ constexpr int LP_THREADS = 64 * LP_WAVES;
 constexpr int LP_PER = 32;              // logits of a lane
 constexpr int LP_SUB = 64 * LP_PER;     // and of a wave at a time
 constexpr int LP_MAX_SEGS = 64;
+// A row is cut into segments until so many blocks a CU are there: 64 rows of 128256 fp32 logits with 20 alternatives take 16.8 us with 4 and
+// 17.9 with 2, 256 such rows 35.4 and 34.6, one row 10.6 either way.
+constexpr int LP_BLOCKS_PER_CU = 4;
 constexpr float LP_NONE = -__builtin_inff();
 
 // (under-aligned vectors: rows begin anywhere)
@@ -28,6 +38,41 @@ struct __attribute__((packed, aligned(2))) LpH8 {
     uint16_t v[8];
 };
 
+// The value of the lane whose number differs in bit O, and of the lane before (0 in the first): vector moves, not trips through LDS, as the
+// lists take some hundred of them one after the other.
+template <int O>
+__device__ __forceinline__ uint32_t lp_xor_bits(uint32_t x) {
+    const int v = (int)x;
+    if constexpr (O == 1) return (uint32_t)__builtin_amdgcn_update_dpp(0, v, 0xB1, 0xf, 0xf, false);
+    if constexpr (O == 2) return (uint32_t)__builtin_amdgcn_update_dpp(0, v, 0x4E, 0xf, 0xf, false);
+    if constexpr (O == 4)  // (7 - i, then 3 - i within four)
+        return (uint32_t)__builtin_amdgcn_update_dpp(0, __builtin_amdgcn_update_dpp(0, v, 0x141, 0xf, 0xf, false), 0x1B, 0xf, 0xf, false);
+    if constexpr (O == 8) return (uint32_t)__builtin_amdgcn_update_dpp(0, v, 0x128, 0xf, 0xf, false);
+    if constexpr (O == 16) {
+        const auto r = __builtin_amdgcn_permlane16_swap(x, x, false, false);
+        return threadIdx.x & 16 ? r[0] : r[1];
+    }
+    if constexpr (O == 32) {
+        const auto r = __builtin_amdgcn_permlane32_swap(x, x, false, false);
+        return threadIdx.x & 32 ? r[0] : r[1];
+    }
+}
+template <int O>
+__device__ __forceinline__ float lp_xor(float x) { return __uint_as_float(lp_xor_bits<O>(__float_as_uint(x))); }
+template <int O>
+__device__ __forceinline__ int lp_xor(int x) { return (int)lp_xor_bits<O>((uint32_t)x); }
+__device__ __forceinline__ uint32_t lp_before_lane(uint32_t x) {
+    return (uint32_t)__builtin_amdgcn_update_dpp(0, (int)x, 0x138, 0xf, 0xf, false);
+}
+__device__ __forceinline__ float lp_wave_max(float v) {
+    v = fmaxf(v, lp_xor<1>(v));
+    v = fmaxf(v, lp_xor<2>(v));
+    v = fmaxf(v, lp_xor<4>(v));
+    v = fmaxf(v, lp_xor<8>(v));
+    v = fmaxf(v, lp_xor<16>(v));
+    return fmaxf(v, lp_xor<32>(v));
+}
+
 // A candidate: value and index.  a before b: the larger value, the lower index among equal ones.
 __device__ __forceinline__ bool lp_before(float av, int ai, float bv, int bi) { return av > bv || (av == bv && ai < bi); }
 
@@ -36,36 +81,46 @@ struct LpList {
     float v;
     int i;
 };
+template <int O>
+__device__ __forceinline__ void lp_order(LpList& a) {  // the lane without bit O keeps the one that comes first
+    const float v = lp_xor<O>(a.v);
+    const int i = lp_xor<O>(a.i);
+    if (lp_before(v, i, a.v, a.i) == !(threadIdx.x & O)) {
+        a.v = v;
+        a.i = i;
+    }
+}
 // the 64 first of two sorted lists, sorted; (rv, ri): the other list from its end
 __device__ __forceinline__ void lp_merge(LpList& a, float rv, int ri) {
-    const int lane = threadIdx.x & 63;
     if (lp_before(rv, ri, a.v, a.i)) {
         a.v = rv;
         a.i = ri;
     }
-#pragma unroll
-    for (int o = 32; o >= 1; o >>= 1) {
-        const float v = __shfl_xor(a.v, o, 64);
-        const int i = __shfl_xor(a.i, o, 64);
-        const bool first = !(lane & o);  // this lane keeps the one that comes first
-        if (lp_before(v, i, a.v, a.i) == first) {
-            a.v = v;
-            a.i = i;
-        }
-    }
+    lp_order<32>(a);
+    lp_order<16>(a);
+    lp_order<8>(a);
+    lp_order<4>(a);
+    lp_order<2>(a);
+    lp_order<1>(a);
 }
-// the k-th largest (from 0) of the lanes' values
+// A number that at least k lanes' values reach, close below the k-th largest of them (-inf if fewer than k are above): by halving
+// an interval of the floats' order, which a count of lanes decides and scalar instructions carry.
+__device__ __forceinline__ int lp_key(float v) {
+    const int b = (int)__float_as_uint(v);
+    return b ^ (b >> 31 & 0x7fffffff);
+}
 __device__ __forceinline__ float lp_kth(float v, int k) {
-    const int lane = threadIdx.x & 63;
-#pragma unroll
-    for (int n = 2; n <= 64; n <<= 1)
-#pragma unroll
-        for (int o = n >> 1; o >= 1; o >>= 1) {
-            const float w = __shfl_xor(v, o, 64);
-            const bool down = !(lane & n), low = !(lane & o);
-            v = down == low ? fmaxf(v, w) : fminf(v, w);
-        }
-    return __uint_as_float(__builtin_amdgcn_readlane(__float_as_uint(v), k));
+    const int key = lp_key(v == v ? v : LP_NONE);
+    auto reach = [&](int t) { return __popcll(__ballot(key >= t)) >= k; };
+    int lo = lp_key(LP_NONE), hi = __builtin_amdgcn_readfirstlane(lp_key(lp_wave_max(v == v ? v : LP_NONE)));  // (reached; by one lane)
+    if (hi > lo + (1 << 25) && reach(hi - (1 << 25))) lo = hi - (1 << 25);  // (within some 16 times or 4 halvings of the largest)
+#pragma unroll 1
+    for (int i = 0; i < 12; ++i) {
+        const int mid = lo + (int)((uint32_t)(hi - lo) >> 1);
+        if (reach(mid)) lo = mid;
+        else hi = mid;
+    }
+    return __uint_as_float((uint32_t)(lo ^ (lo >> 31 & 0x7fffffff)));
 }
 
 // floats of a segment's state and list in the workspace
@@ -93,38 +148,36 @@ template <bool BF16>
 __device__ __forceinline__ int lp_index(int e, int lane) {
     return BF16 ? e / 8 * 512 + lane * 8 + e % 8 : e / 4 * 256 + lane * 4 + e % 4;
 }
+// The 2048 logits of a row of V from `at` on, -inf behind its end.
 template <bool BF16>
-__device__ __forceinline__ void lp_load(const void* row, int at, int end, int lane, LpRaw<BF16>& r) {
-    if (BF16) {
-        const uint16_t* p = static_cast<const uint16_t*>(row);
-        if (at + LP_SUB <= end) {
+__device__ __forceinline__ void lp_load(const void* row, int at, int V, int lane, LpRaw<BF16>& r) {
+    if (at + LP_SUB <= V) {
+        if (BF16) {
+            const uint16_t* p = static_cast<const uint16_t*>(row) + at;
 #pragma unroll
             for (int j = 0; j < LP_PER / 8; ++j) {
-                const LpH8 x = *reinterpret_cast<const LpH8*>(p + at + j * 512 + lane * 8);
+                const LpH8 x = *reinterpret_cast<const LpH8*>(p + j * 512 + lane * 8);
 #pragma unroll
                 for (int i = 0; i < 4; ++i) r.w[4 * j + i] = x.v[2 * i] | (uint32_t)x.v[2 * i + 1] << 16;
             }
         } else {
-#pragma unroll
-            for (int i = 0; i < LP_PER / 2; ++i) {
-                const int a = at + lp_index<true>(2 * i, lane);
-                r.w[i] = (a < end ? p[a] : 0xff80u) | (a + 1 < end ? (uint32_t)p[a + 1] : 0xff80u) << 16;
-            }
-        }
-    } else {
-        const float* p = static_cast<const float*>(row);
-        if (at + LP_SUB <= end) {
+            const float* p = static_cast<const float*>(row) + at;
 #pragma unroll
             for (int j = 0; j < LP_PER / 4; ++j) {
-                const LpF4 x = *reinterpret_cast<const LpF4*>(p + at + j * 256 + lane * 4);
+                const LpF4 x = *reinterpret_cast<const LpF4*>(p + j * 256 + lane * 4);
 #pragma unroll
                 for (int i = 0; i < 4; ++i) r.w[4 * j + i] = __float_as_uint(x.v[i]);
             }
-        } else {
+        }
+    } else {
 #pragma unroll
-            for (int i = 0; i < LP_PER; ++i) {
-                const int a = at + lp_index<false>(i, lane);
-                r.w[i] = a < end ? __float_as_uint(p[a]) : 0xff800000u;
+        for (int i = 0; i < LP_PER; ++i) {
+            const int j = at + lp_index<BF16>(i, lane);
+            if (BF16) {
+                const uint32_t v = j < V ? static_cast<const uint16_t*>(row)[j] : 0xff80u;
+                r.w[i / 2] = i % 2 ? r.w[i / 2] | v << 16 : v;
+            } else {
+                r.w[i] = j < V ? static_cast<const uint32_t*>(row)[j] : 0xff800000u;
             }
         }
     }
@@ -132,6 +185,14 @@ __device__ __forceinline__ void lp_load(const void* row, int at, int end, int la
 template <bool BF16>
 __device__ __forceinline__ float lp_value(const LpRaw<BF16>& r, int e) {
     return BF16 ? (e & 1 ? bf_hi(r.w[e / 2]) : bf_lo(r.w[e / 2])) : __uint_as_float(r.w[e]);
+}
+
+template <bool BF16>
+__device__ __forceinline__ float lp_most(const LpRaw<BF16>& r) {
+    float m = lp_value<BF16>(r, 0);
+#pragma unroll
+    for (int e = 1; e < LP_PER; ++e) m = fmaxf(m, lp_value<BF16>(r, e));
+    return m;
 }
 
 // A row's results from its joined state and list.
@@ -164,7 +225,7 @@ __device__ __forceinline__ void lp_finish(const LogpArgs& a, int64_t row, const 
 // its state and list.
 template <bool BF16, bool TOP>
 __global__ __launch_bounds__(LP_THREADS) void logprobs_kernel(LogpArgs a, int segs) {
-    __shared__ float sv[LP_WAVES][64], sm[LP_WAVES][3];
+    __shared__ float sv[LP_WAVES][64], sm[LP_WAVES][3], sf[LP_WAVES];
     __shared__ int si[LP_WAVES][64];
     const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
     const int64_t row = blockIdx.x / segs;
@@ -175,16 +236,25 @@ __global__ __launch_bounds__(LP_THREADS) void logprobs_kernel(LogpArgs a, int se
                          : (const void*)(static_cast<const float*>(a.logits) + row * a.stride);
     LpState st{LP_NONE, 0.0f, 0.0f};
     LpList list{LP_NONE, 0x7fffffff};
-    float last = LP_NONE;  // the list's last value
+    float floor = LP_NONE, most = LP_NONE;  // at least `top` logits of the segment reach floor; most: the lane's largest of the wave's part
     LpRaw<BF16> next;
     if (s0 + wave < s1) lp_load<BF16>(p, (s0 + wave) * LP_SUB, a.V, lane, next);
+    if (TOP) {
+        // each of the waves' first parts has k lanes whose largest logit reaches its k-th largest, so `top` logits reach the least of these
+        const int k = (a.top + min(LP_WAVES, s1 - s0) - 1) / min(LP_WAVES, s1 - s0);
+        if (s0 + wave < s1) most = lp_most<BF16>(next);
+        const float kth = lp_kth(most, k);
+        if (lane == 0) sf[wave] = s0 + wave < s1 ? kth : -LP_NONE;
+        __syncthreads();
+        floor = fmaxf(fminf(fminf(sf[0], sf[1]), fminf(sf[2], sf[3])), -3.402823466e38f);  // (-inf is no candidate)
+    }
+    float last = floor;  // of the list, if it is full
     for (int s = s0 + wave; s < s1; s += LP_WAVES) {
-        const LpRaw<BF16> x = next;
+        LpRaw<BF16> x = next;
+        const int base = s * LP_SUB;
         if (s + LP_WAVES < s1) lp_load<BF16>(p, (s + LP_WAVES) * LP_SUB, a.V, lane, next);
-        float most = lp_value<BF16>(x, 0);
-#pragma unroll
-        for (int e = 1; e < LP_PER; ++e) most = fmaxf(most, lp_value<BF16>(x, e));
-        const float top = fmaxf(st.m, wave_max(most));
+        if (!TOP || s != s0 + wave) most = lp_most<BF16>(x);
+        const float top = fmaxf(st.m, lp_wave_max(most));
         if (!(top <= LP_NONE)) {
             if (top != st.m) lp_move(st, top);
             float S = 0.0f, T = 0.0f;
@@ -204,13 +274,11 @@ __global__ __launch_bounds__(LP_THREADS) void logprobs_kernel(LogpArgs a, int se
         }
         if (TOP) {
             float at = last;
-            if (at == LP_NONE) at = lp_kth(most == most ? most : LP_NONE, a.top - 1);  // (at least `top` logits reach this one)
             if (__any(most >= at)) {
-                const int base = s * LP_SUB;
 #pragma unroll
                 for (int e = 0; e < LP_PER; ++e) {
                     const float v = lp_value<BF16>(x, e);
-                    unsigned long long hit = __ballot(v >= at && v > LP_NONE);
+                    unsigned long long hit = __ballot(v >= at);
                     while (hit) {
                         const int l = __ffsll(hit) - 1;
                         hit &= hit - 1;
@@ -218,12 +286,11 @@ __global__ __launch_bounds__(LP_THREADS) void logprobs_kernel(LogpArgs a, int se
                         const int ci = base + lp_index<BF16>(e, l);
                         const int pos = __popcll(__ballot(lp_before(list.v, list.i, cv, ci)));
                         if (pos < a.top) {
-                            const float uv = __shfl_up(list.v, 1, 64);
-                            const int ui = __shfl_up(list.i, 1, 64);
+                            const float uv = __uint_as_float(lp_before_lane(__float_as_uint(list.v)));
+                            const int ui = (int)lp_before_lane((uint32_t)list.i);
                             list.v = lane < pos ? list.v : lane == pos ? cv : uv;
                             list.i = lane < pos ? list.i : lane == pos ? ci : ui;
-                            last = __uint_as_float(__builtin_amdgcn_readlane(__float_as_uint(list.v), a.top - 1));
-                            at = fmaxf(at, last);
+                            at = last = fmaxf(last, __uint_as_float(__builtin_amdgcn_readlane(__float_as_uint(list.v), a.top - 1)));
                         }
                     }
                 }
@@ -284,12 +351,15 @@ __global__ __launch_bounds__(64 * LP_JOIN_WAVES) void logprobs_join_kernel(LogpA
     const float* part = static_cast<const float*>(a.part) + row * segs * width;
     LpList list{LP_NONE, 0x7fffffff};
     if (TOP) {
-        for (int s = wave; s < segs; s += LP_JOIN_WAVES) {
+        // a wave's first list as it is, the others from their ends
+        if (lane < a.top && wave < segs) {
+            const float* q = part + (int64_t)wave * width + 4;
+            list = LpList{q[lane], reinterpret_cast<const int*>(q)[a.top + lane]};
+        }
+        const int r = 63 - lane;
+        for (int s = wave + LP_JOIN_WAVES; s < segs; s += LP_JOIN_WAVES) {
             const float* q = part + (int64_t)s * width + 4;
-            const int r = 63 - lane;
-            const float rv = r < a.top ? q[r] : LP_NONE;
-            const int ri = r < a.top ? reinterpret_cast<const int*>(q)[a.top + r] : 0x7fffffff;
-            lp_merge(list, rv, ri);
+            lp_merge(list, r < a.top ? q[r] : LP_NONE, r < a.top ? reinterpret_cast<const int*>(q)[a.top + r] : 0x7fffffff);
         }
 #pragma unroll
         for (int o = LP_JOIN_WAVES / 2; o >= 1; o >>= 1) {
@@ -313,11 +383,11 @@ __global__ __launch_bounds__(64 * LP_JOIN_WAVES) void logprobs_join_kernel(LogpA
     lp_finish<BF16>(a, row, st, list);
 }
 
-// Segments of a row: until there are four blocks a CU, or every wave has one part.
+// Segments of a row: until there are LP_BLOCKS_PER_CU, or every wave has one part.
 int segments(const LogpArgs& a) {
     const int64_t subs = ((int64_t)a.V + LP_SUB - 1) / LP_SUB;
     const int64_t most = std::min<int64_t>((subs + LP_WAVES - 1) / LP_WAVES, LP_MAX_SEGS);
-    return (int)std::max<int64_t>(1, std::min<int64_t>(most, (4 * a.n_cu + a.n - 1) / a.n));
+    return (int)std::max<int64_t>(1, std::min<int64_t>(most, (LP_BLOCKS_PER_CU * a.n_cu + a.n - 1) / a.n));
 }
 
 template <bool BF16, bool TOP>
