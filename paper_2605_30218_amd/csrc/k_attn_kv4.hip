@@ -46,13 +46,22 @@ __device__ __forceinline__ f32x4_k8 k4_mfma(const u32x4_k8& a, uint32_t sa, cons
     return __builtin_amdgcn_mfma_scale_f32_16x16x128_f8f6f4(k4_wide(a), k4_wide(b), c, 4, 2, SA, (int)sa, SB, (int)sb);
 }
 
-// The scale 2^e (as float bits) under which values of up to `top` (float bits, finite) are below 2: the e2m3 values up to 2 are
-// multiples of 1/8, so that a term is off by 1/16 at most, and 32 times that is at most 2 again.
+// e2m3 values are multiples of 1/8 up to 2, of 1/4 up to 4, of 1/2 up to 7.5.
+// The scale 2^e (as float bits) under which values of up to `top` (float bits, finite) are below 2: a term is off by 1/16 at most, and
+// 32 times that is at most 2 again.  So after one, two, three terms under scale, scale / 32, scale / 1024 what is left is scale / 16, / 512, / 16384
+// at most: 2^-9 or 2^-14 of the largest.
 __device__ __forceinline__ uint32_t k4_block_scale(uint32_t top) { return max(top & 0x7f800000u, K4_LEAST); }
-// 32 values (of even and of odd index, as the conversion takes them) as TERMS e2m3 blocks under scale, scale / 32, scale / 1024: off
-// by scale / 16, / 512, / 16384 after one, two, three, so by 2^-9 or 2^-14 of the largest at most.  What a term leaves is found by
-// converting it back (BACK: one instruction of some 70 cycles and a subtraction a value, but 32 registers more), or by adding and taking away
-// a number whose last bit is scale / 8, which rounds as the conversion does.
+// For two terms, the scale under which `top` is from 3.75 to 7.5: a first term leaves 1/4 of a value from 4 up, 1/8 from 2 up, 1/16 below, and 32 times
+// that is within the format but for a sixteenth of the first, which become 7.5.  So two terms leave 1/64 of a value from 4 up, 1/256 from 2
+// up, 1/512 below: 2^-8 of a value, or 1/1920 of the largest, at most.  (Chunks of 2048 tokens over 2048 to 8192 positions were off
+// by 0.0039 of their outputs, the bf16 results' rounding, 0.0016, among it, with two terms under the scale above, by 0.0020 with these, in
+// the same time; three terms under the scale above took 585 us instead of 510.)
+__device__ __forceinline__ uint32_t k4_pair_scale(float top) {
+    return max(__float_as_uint(top * (16.0f / 15.0f)) & 0x7f800000u, K4_LEAST + (2u << 23)) - (2u << 23);
+}
+// 32 values (of even and of odd index, as the conversion takes them) as TERMS e2m3 blocks under scale, scale / 32, scale / 1024.  What a
+// term leaves is found by converting it back (BACK: one instruction of some 70 cycles and a subtraction a value, but 32 registers more), or,
+// where it is below 2, by adding and taking away a number whose last bit is scale / 8, which rounds as the conversion does.
 template <int TERMS, bool BACK>
 __device__ __forceinline__ void k4_terms(f32x16_k4& even, f32x16_k4& odd, uint32_t scale, i32x6_k4 (&t)[TERMS]) {
 #pragma unroll
@@ -475,6 +484,7 @@ template <int HD, int GROUPS>
 struct K4ChunkShared {
     K4Stage<HD> stage[GROUPS][2];
     K4Query<HD> q[K8_WAVES][K4_TILES];
+    int pos[K8_WAVES][K4_TILES][16];  // of the columns' tokens (few steps need them: they are not held in registers)
 };
 template <int HD, int GROUPS, bool CAP>
 __device__ __forceinline__ void k4_chunk_block(const Kv8AttnArgs& a, int few, int tiles, int nsplit, float* part, int block,
@@ -503,14 +513,13 @@ __device__ __forceinline__ void k4_chunk_block(const Kv8AttnArgs& a, int few, in
     const int rr0 = t * ROWS + wave * (16 * NT);
     const int wp0 = row.p0 + min(rr0, live - 1) / a.G, wp1 = row.p0 + (min(rr0 + 16 * NT, live) - 1) / a.G;
 
-    int pos[NT];
     K4Acc<HD> acc[NT];
 #pragma unroll
     for (int u = 0; u < NT; ++u)
         if (u % GROUPS == group) k4_query<HD>(a, row, kh, rr0 + 16 * u, sh.q[wave][u]);
 #pragma unroll
     for (int u = 0; u < NT; ++u) {
-        pos[u] = k4_position(a, row, rr0 + 16 * u + c);
+        if (group == 0 && lane < 16) sh.pos[wave][u][lane] = k4_position(a, row, rr0 + 16 * u + lane);
         acc[u].clear();
     }
     K8Soft so = k8_soft(a);
@@ -650,8 +659,7 @@ __device__ __forceinline__ void k4_chunk_block(const Kv8AttnArgs& a, int few, in
             for (int u = 0; u < NT; ++u) {
                 if (CAP) k8_cap(reinterpret_cast<float(&)[1][32]>(x[u]), so);
                 if (edge) {
-                    int pp = pos[u];
-                    asm("" : "+v"(pp));
+                    const int pp = sh.pos[wave][u][lane & 15];
                     const int hi = min(pp, row.len - 1) - j0 - 4 * g, lo = (a.window ? k8_hidden(a.window, pp) : -1) - j0 - 4 * g;
 #pragma unroll
                     for (int i = 0; i < 32; ++i) {
@@ -676,9 +684,9 @@ __device__ __forceinline__ void k4_chunk_block(const Kv8AttnArgs& a, int few, in
                         top = fmaxf(top, y[i & 1][2 * e + (i >> 1)]);
                     }
                 }
-                const uint32_t bs = k4_block_scale(__float_as_uint(top));
-                k4_terms<2, !CAP>(y[0], y[1], bs, p[u]);
-                ps[u] = bs == 0x7f800000u ? 0xffffu : (bs >> 23) * 0x101u - 0x500u;  // (past fp32: NaN)
+                const uint32_t bs = k4_pair_scale(top);
+                k4_terms<2, true>(y[0], y[1], bs, p[u]);
+                ps[u] = bs >= 0x7e800000u ? 0xffffu : (bs >> 23) * 0x101u - 0x500u;  // (past fp32: NaN)
             }
 #pragma unroll
             for (int d = 0; d < DT; ++d) {
