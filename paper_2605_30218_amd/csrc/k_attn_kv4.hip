@@ -17,12 +17,11 @@ namespace {
 
 typedef int i32x8_k4 __attribute__((ext_vector_type(8)));
 typedef int i32x6_k4 __attribute__((ext_vector_type(6)));
+typedef uint32_t u32x6_k4 __attribute__((ext_vector_type(6)));
 typedef float f32x16_k4 __attribute__((ext_vector_type(16)));
 typedef float f32x32_k4 __attribute__((ext_vector_type(32)));
 
 constexpr int K4_STEP = 8;          // pages of a step: 128 positions, the products' depth
-constexpr int K4_FOLD = 13;         // probabilities under V's scale are held 2^-13 of themselves: up to 2^12 * 2^126 they stay finite
-constexpr uint32_t K4_LEAST = 12u << 23;  // of a block's scale: its terms' scales stay normal numbers
 
 template <int HD>
 struct K4Lane {  // what a lane loads of a page: 16 features' worth of four positions of V
@@ -46,50 +45,54 @@ __device__ __forceinline__ f32x4_k8 k4_mfma(const u32x4_k8& a, uint32_t sa, cons
     return __builtin_amdgcn_mfma_scale_f32_16x16x128_f8f6f4(k4_wide(a), k4_wide(b), c, 4, 2, SA, (int)sa, SB, (int)sb);
 }
 
-// e2m3 values are multiples of 1/8 up to 2, of 1/4 up to 4, of 1/2 up to 7.5.
-// The scale 2^e (as float bits) under which values of up to `top` (float bits, finite) are below 2: a term is off by 1/16 at most, and
-// 32 times that is at most 2 again.  So after one, two, three terms under scale, scale / 32, scale / 1024 what is left is scale / 16, / 512, / 16384
-// at most: 2^-9 or 2^-14 of the largest.
-__device__ __forceinline__ uint32_t k4_block_scale(uint32_t top) { return max(top & 0x7f800000u, K4_LEAST); }
-// For two terms, the scale under which `top` is from 3.75 to 7.5: a first term leaves 1/4 of a value from 4 up, 1/8 from 2 up, 1/16 below, and 32 times
-// that is within the format but for a sixteenth of the first, which become 7.5.  So two terms leave 1/64 of a value from 4 up, 1/256 from 2
-// up, 1/512 below: 2^-8 of a value, or 1/1920 of the largest, at most.  (Chunks of 2048 tokens over 2048 to 8192 positions were off
-// by 0.0039 of their outputs, the bf16 results' rounding, 0.0016, among it, with two terms under the scale above, by 0.0020 with these, in
-// the same time; three terms under the scale above took 585 us instead of 510.)
-__device__ __forceinline__ uint32_t k4_pair_scale(float top) {
-    return max(__float_as_uint(top * (16.0f / 15.0f)) & 0x7f800000u, K4_LEAST + (2u << 23)) - (2u << 23);
+// 32 values (of even and of odd index, as the conversion takes them) as e2m3 values under a scale.
+__device__ __forceinline__ i32x6_k4 k4_block(const f32x16_k4& even, const f32x16_k4& odd, float scale) {
+    auto q = __builtin_amdgcn_cvt_scalef32_2xpk16_fp6_f32(even, odd, scale);
+    // (the conversion takes several passes over its 32 sources: its result must not be placed on one of them, as the compiler
+    // does where they end here; such results were off now and then)
+    asm volatile("" : "+v"(q) : "v"(even), "v"(odd), "v"(scale));
+    return __builtin_bit_cast(i32x6_k4, q);
 }
-// 32 values (of even and of odd index, as the conversion takes them) as TERMS e2m3 blocks under scale, scale / 32, scale / 1024.  What a
-// term leaves is found by converting it back (BACK: one instruction of some 70 cycles and a subtraction a value, but 32 registers more), or,
-// where it is below 2, by adding and taking away a number whose last bit is scale / 8, which rounds as the conversion does.
-template <int TERMS, bool BACK>
-__device__ __forceinline__ void k4_terms(f32x16_k4& even, f32x16_k4& odd, uint32_t scale, i32x6_k4 (&t)[TERMS]) {
+// e2m3 values are multiples of 1/8 up to 2, of 1/4 up to 4, of 1/2 up to 7.5.
+// Three terms of 32 query values under scales s, s / 32, s / 1024, with s the power of two under which the largest (`top`, float bits, finite) is
+// below 2: a term is off by 1/16 of its scale at most, and 32 times that is at most 2 again, so s / 16384 or 2^-14 of the largest is left in the end.
+// What a term leaves is found by adding and taking away a number whose last bit is an eighth of its scale, which rounds as the conversion does.
+__device__ __forceinline__ uint32_t k4_triple(f32x16_k4& even, f32x16_k4& odd, uint32_t top, i32x6_k4 (&t)[3]) {
+    const uint32_t scale = max(top & 0x7f800000u, 12u << 23);  // (the third's is a normal number)
 #pragma unroll
-    for (int k = 0; k < TERMS; ++k) {
-        const float s = __uint_as_float(scale - k * (5u << 23));
-        auto q = __builtin_amdgcn_cvt_scalef32_2xpk16_fp6_f32(even, odd, s);
-        // (the conversion takes several passes over its 32 sources: its result must not be placed on one of them, as the compiler
-        // does where they end here; such results were off now and then)
-        asm volatile("" : "+v"(q) : "v"(even), "v"(odd), "v"(s));
-        t[k] = __builtin_bit_cast(i32x6_k4, q);
-        if (k + 1 == TERMS) break;
-        if (BACK) {
-            f32x32_k4 y = __builtin_amdgcn_cvt_scalef32_pk32_f32_fp6(q, s);
-            asm volatile("" : "+v"(y) : "v"(q), "v"(s));
+    for (int k = 0; k < 3; ++k) {
+        const float s = __uint_as_float(scale - k * (5u << 23)), M = s * 0x1.8p+20f;
+        t[k] = k4_block(even, odd, s);
+        if (k == 2) break;
 #pragma unroll
-            for (int i = 0; i < 16; ++i) {
-                even[i] -= y[2 * i];
-                odd[i] -= y[2 * i + 1];
-            }
-        } else {
-            const float M = s * 0x1.8p+20f;
-#pragma unroll
-            for (int i = 0; i < 16; ++i) {
-                even[i] -= (even[i] + M) - M;
-                odd[i] -= (odd[i] + M) - M;
-            }
+        for (int i = 0; i < 16; ++i) {
+            even[i] -= (even[i] + M) - M;
+            odd[i] -= (odd[i] + M) - M;
         }
     }
+    return scale >> 23;
+}
+// Two terms of 32 weights of V of at most `top` under scales s and s / 32, with s the power of two under which top is from 3.75 to 7.5; returned: the scales'
+// bytes.  The first leaves s / 4 of a value from 4 s up, s / 8 from 2 s up, s / 16 below; under s / 32 a sixteenth of those from 4 s up are past the
+// format and become 7.5.  So s / 64, s / 256, s / 512 are left: 2^-8 of a value, as a bf16 weight would be off, or 1/1920 of the largest, at most.
+// What the first leaves is found by converting it back, one instruction of some 70 cycles.
+// Chunks of 2048 tokens over 2048 to 8192 positions were off by 0.0039 of their outputs, the bf16 results' rounding, 0.0016, among it, with two terms
+// of which the first is held below 2 s as above, by 0.0020 with these, in the same time; three terms took 585 us instead of 510 there, and a step of 64
+// rows 14.6 us instead of 13.7, off by 0.0017.
+__device__ __forceinline__ uint32_t k4_pair(f32x16_k4& even, f32x16_k4& odd, float top, i32x6_k4 (&t)[2]) {
+    constexpr uint32_t least = 7u << 23;  // (the second's is a normal number)
+    const uint32_t scale = max(__float_as_uint(top * (16.0f / 15.0f)) & 0x7f800000u, least + (2u << 23)) - (2u << 23);
+    const float s = __uint_as_float(scale);
+    t[0] = k4_block(even, odd, s);
+    f32x32_k4 y = __builtin_amdgcn_cvt_scalef32_pk32_f32_fp6(__builtin_bit_cast(u32x6_k4, t[0]), s);
+    asm volatile("" : "+v"(y) : "v"(t[0]), "v"(s));
+#pragma unroll
+    for (int i = 0; i < 16; ++i) {
+        even[i] -= y[2 * i];
+        odd[i] -= y[2 * i + 1];
+    }
+    t[1] = k4_block(even, odd, __uint_as_float(scale - (5u << 23)));
+    return (scale >> 23) * 0x101u - 0x500u;
 }
 
 // Query rows rr0 + 16 u + c of a row's KV head (row rr: token rr / G, head rr % G of the group) as B operands in LDS (registers are
@@ -124,12 +127,11 @@ __device__ __forceinline__ void k4_query(const Kv8AttnArgs& a, const K8Row& row,
         even[i] = bf_lo(w[i]);
         odds[i] = bf_hi(w[i]);
     }
-    const uint32_t s = k4_block_scale(top << 16);
     i32x6_k4 t[3];
-    k4_terms<3, false>(even, odds, s, t);
+    const uint32_t s = k4_triple(even, odds, top << 16, t);
     // (a value that is not finite makes the scores NaN)
     const bool odd = top >= 0x7f80u;
-    const uint32_t b0 = odd ? 255u : s >> 23, b1 = odd ? 255u : (s >> 23) - 5, b2 = odd ? 255u : (s >> 23) - 10;
+    const uint32_t b0 = odd ? 255u : s, b1 = odd ? 255u : s - 5, b2 = odd ? 255u : s - 10;
     if constexpr (HD == 64) {
 #pragma unroll
         for (int i = 0; i < 6; ++i) {
@@ -165,16 +167,17 @@ struct K4Acc {
     }
 };
 
-// A step's scores x (position 16 i + 4 g + r at x[4 i + r]) become its probabilities.  The reference moves only when a
-// score of the step passes it by K4_MOVE: exchanges between lanes and rescaled outputs are rare.
-constexpr float K4_MOVE = 12.0f;
+// A step's scores x (position 16 i + 4 g + r at x[4 i + r]) become its probabilities, of at most 1/2: the reference is K4_FOLD above the scores that
+// moved it last, so that a probability times a value's scale, up to 2^126, is finite.  It moves only when a score of the step passes it
+// by -1: exchanges between lanes and rescaled outputs are rare.
+constexpr float K4_FOLD = 13.0f;
 template <int HD>
 __device__ __forceinline__ void k4_probs(float (&x)[32], float f, K4Acc<HD>& acc) {
     float mx = x[0];
 #pragma unroll
     for (int i = 1; i < 32; ++i) mx = fmaxf(mx, x[i]);
-    if (__any(__builtin_fmaf(mx, f, -acc.m) > K4_MOVE)) {
-        const float mn = fmaxf(acc.m, k8_col_max(mx) * f);
+    if (__any(__builtin_fmaf(mx, f, -acc.m) > -1.0f)) {
+        const float mn = fmaxf(acc.m, __builtin_fmaf(k8_col_max(mx), f, K4_FOLD));
         const float al = __builtin_amdgcn_exp2f(acc.m - mn);
         acc.m = mn;
         acc.l *= al;
@@ -196,7 +199,7 @@ __device__ __forceinline__ float k4_scalar(float x) { return __uint_as_float(__b
 // Pages [pg0, pg1) of a row's table against 16 query rows: steps first, first + stride, ... of K4_STEP pages.  K's
 // registers are loaded again as soon as the scores are there, V's after its product, so that a wave has a step in flight at any
 // time.  ONCE: pages that no other wave reads, by loads that leave no trace in the caches.
-template <int HD, int TERMS, bool CAP, bool ONCE>
+template <int HD, bool CAP, bool ONCE>
 __device__ __forceinline__ void k4_walk(const Kv8AttnArgs& a, const K8Row& row, int r, int kh, int pg0, int pg1, int first, int stride,
                                         const K4Query<HD>& q, int pos, int p_hi, K4Acc<HD>& acc) {
     typedef typename K4Lane<HD>::v vlane;
@@ -304,21 +307,19 @@ __device__ __forceinline__ void k4_walk(const Kv8AttnArgs& a, const K8Row& row, 
 #pragma unroll
                 for (int i = 0; i < 32; ++i)
                     x[i] = (vs[i >> 2] >> (8 * (i & 3)) & 0xffu) == 255u && x[i] != -__builtin_inff() ? __builtin_nanf("") : x[i];
+#pragma unroll
+                for (int e = 0; e < K4_STEP; ++e) vs[e] &= ~(((vs[e] & ((vs[e] & 0x7f7f7f7fu) + 0x01010101u) & 0x80808080u) >> 7) * 255u);
             }
             k4_probs<HD>(x, so.f, acc);
             f32x16_k4 y[2];
             float top = 0.0f;
 #pragma unroll
             for (int i = 0; i < 32; ++i) {
-                y[i & 1][i >> 1] = x[i] * __uint_as_float(((vs[i >> 2] >> (8 * (i & 3)) & 0xffu) << 23) - ((uint32_t)K4_FOLD << 23));
+                y[i & 1][i >> 1] = x[i] * __uint_as_float((vs[i >> 2] >> (8 * (i & 3)) & 0xffu) << 23);
                 top = fmaxf(top, y[i & 1][i >> 1]);
             }
-            const uint32_t sc = k4_block_scale(__float_as_uint(top));
-            i32x6_k4 p[TERMS];
-            k4_terms<TERMS, false>(y[0], y[1], sc, p);
-            // byte k: term k's scale (past fp32: NaN)
-            uint32_t ps = (sc >> 23) + K4_FOLD;
-            ps = ps > 254u ? 0xffffffu : ps * 0x10101u - 0xa0500u;
+            i32x6_k4 p[2];
+            const uint32_t ps = k4_pair(y[0], y[1], top, p);
 #pragma unroll
             for (int d = 0; d < DT; ++d) {
                 u32x4_k8 A;
@@ -327,7 +328,6 @@ __device__ __forceinline__ void k4_walk(const Kv8AttnArgs& a, const K8Row& row, 
                     A[e] = __builtin_amdgcn_perm(vb[2 * e + 1][d / 2], vb[2 * e][d / 2], d & 1 ? 0x07060302u : 0x05040100u);
                 acc.o[d] = k4_mfma<0, 0>(A, 127u, p[0], ps, acc.o[d]);
                 acc.o[d] = k4_mfma<0, 1>(A, 127u, p[1], ps, acc.o[d]);
-                if constexpr (TERMS == 3) acc.o[d] = k4_mfma<0, 2>(A, 127u, p[2], ps, acc.o[d]);
             }
             __builtin_amdgcn_sched_barrier(0);
             if (more) fetch_v(s + stride);
@@ -377,7 +377,7 @@ __device__ __forceinline__ void k4_few_block(const Kv8AttnArgs& a, const K8Few& 
     K4Acc<HD> acc;
     acc.clear();
     if (16 * tile < row.n * a.G)
-        k4_walk<HD, 3, CAP, NT == 1>(a, row, r, kh, pg0, pg1, wave / NT, WAVES / NT, sh.q[wave], pos, row.p0 + row.n - 1, acc);
+        k4_walk<HD, CAP, NT == 1>(a, row, r, kh, pg0, pg1, wave / NT, WAVES / NT, sh.q[wave], pos, row.p0 + row.n - 1, acc);
 
     // the waves' shares join in LDS
     const float ls = k8_col_sum(acc.l);
@@ -684,9 +684,7 @@ __device__ __forceinline__ void k4_chunk_block(const Kv8AttnArgs& a, int few, in
                         top = fmaxf(top, y[i & 1][2 * e + (i >> 1)]);
                     }
                 }
-                const uint32_t bs = k4_pair_scale(top);
-                k4_terms<2, true>(y[0], y[1], bs, p[u]);
-                ps[u] = bs >= 0x7e800000u ? 0xffffu : (bs >> 23) * 0x101u - 0x500u;  // (past fp32: NaN)
+                ps[u] = k4_pair(y[0], y[1], top, p[u]);
             }
 #pragma unroll
             for (int d = 0; d < DT; ++d) {

@@ -108,7 +108,7 @@ class RefCache:
                         self.unit[s // PAGE, :, s % PAGE] = np.exp2(np.where(b[i, :, 0] == 255, 0, b[i, :, 0]) - 127.0)
 
 
-def attention(cache, q, table, lens, cu, scale, window=0, softcap=0.0, terms=2):
+def attention(cache, q, table, lens, cu, scale, window=0, softcap=0.0):
     """(out, bound) in float64: the definition's result for q [T][Hq][hd], and how far a bf16 result may be from it.  With w the
     softmax weights and A = sum_j w_j |v_j| the bound adds
       the output's rounding, half a step of bf16: 2^-8 |out|;
@@ -116,11 +116,10 @@ def attention(cache, q, table, lens, cu, scale, window=0, softcap=0.0, terms=2):
         score by 2^-15 * scale * sum (largest of the block) |k|;
       fp32 scores: hd + 16 roundings of 2^-24 relative to scale * sum |q k| (a capped score: 2^-20 of the largest score more), and exp's argument,
         rounded once relative to the largest score; each weight moves by at most 2 (E + 2^-23 max|s|) of itself, twice for the quotient;
-      a probability times its value's scale as 6-bit terms, for each code.  Three: the first under a scale S that is at most half of
-        the largest of its 32 positions leaves S / 8, the others S / 256 and S / 8192, so 2^-14 of that largest.  Two, under s with
-        the largest from 3.75 s to 7.5 s: the first leaves s / 4 of a number x from 4 s up, s / 8 from 2 s, s / 16 below; the
-        second's steps, under s / 32, are 1/2, 1/4, 1/8 of that with nothing above 7.5, so it leaves s (1/4 - 7.5/32) = s / 64, s / 256,
-        s / 512: 2^-8 x from 4 s up, 2^-9 x from 2 s, below them s / 512 <= largest / 1920;
+      a probability times its value's scale as two 6-bit terms, for each code, under s and s / 32 with the largest of its 32 positions from
+        3.75 s to 7.5 s: the first leaves s / 4 of a number x from 4 s up, s / 8 from 2 s, s / 16 below; the second's steps, under s / 32,
+        are 1/2, 1/4, 1/8 of that with nothing above 7.5, so it leaves s (1/4 - 7.5/32) = s / 64, s / 256, s / 512: 2^-8 x from 4 s up,
+        2^-9 x from 2 s, below them s / 512 <= largest / 1920;
         these 32 positions lie within 127 of each other;
       fp32 sums over n positions and exp itself: (n + 32) 2^-23 A."""
     T, Hq, hd = q.shape
@@ -167,7 +166,7 @@ def attention(cache, q, table, lens, cu, scale, window=0, softcap=0.0, terms=2):
             rel = 4 * (E + 2.0 ** -23 * top) + (L + 32) * 2.0 ** -23
             big = maximum_filter1d(w * u, 255, axis=1, mode="constant")
             code = np.abs(v) / np.where(u > 0, u, 1.0)[:, None]
-            P = (2.0 ** -14 * big if terms == 3 else np.maximum(2.0 ** -8 * w * u, big / 1920)) @ code
+            P = np.maximum(2.0 ** -8 * w * u, big / 1920) @ code
             o[(see & bad).any(1) | (odd & some)] = np.nan
             out[t0:t1, h * G:(h + 1) * G] = o.reshape(n, G, hd)
             b = 2.0 ** -8 * np.abs(o) + (1 + 2.0 ** -8) * (rel[:, None] * A + P) + 1e-38

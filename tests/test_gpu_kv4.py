@@ -200,7 +200,7 @@ class Batch:
         kw["scale"] = kw.get("scale") or 1 / np.sqrt(self.hd)
         most = int(self.new.max()) * self.G
         args = (ref.RefCache.of(self.codes, self.scales), bf16(self.q), self.table, self.lens, self.cu)
-        out, bound = ref.attention(*args, terms=3 if most <= 32 else 2, **kw)
+        out, bound = ref.attention(*args, **kw)
         got = bf16(got)
         np.testing.assert_array_equal(np.isnan(got), np.isnan(out))
         worst = np.nanmax(np.abs(got - out) / np.where(bound > 0, bound, 1e-38)) if out.size else 0.0
@@ -387,7 +387,7 @@ def test_offsets_past_32_bits(new):
     small.append(bf16(k), bf16(v), s2)
     for side, x in enumerate(back):
         np.testing.assert_array_equal(bf16(x), small.val[s2 // 16, :, side, s2 % 16])
-    out, bound = ref.attention(small, bf16(q), t2, [L], [0, new], 1 / np.sqrt(hd), terms=3 if new == 1 else 2)
+    out, bound = ref.attention(small, bf16(q), t2, [L], [0, new], 1 / np.sqrt(hd))
     assert (np.abs(bf16(got) - out) <= bound).all()
 
 
