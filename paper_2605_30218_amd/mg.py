@@ -330,6 +330,14 @@ def _call(name, device, stream, fn, *args):
         raise MgError(name, rc)
 
 
+def _sized(device, fn, *args):
+    """fn(*args), a question of the library's that depends on the device, on that device."""
+    if device.index == _current_device():
+        return fn(*args)
+    with torch.cuda.device(device):
+        return fn(*args)
+
+
 def _new(shape, dtype, device, stream):
     """A tensor of torch's allocator that the call's stream may write: of that stream's own memory, which
     neither earlier work of the current one still reads nor later work takes too soon."""
@@ -491,8 +499,7 @@ def _attention(name, c, dev, q, page_table, lens, cu_new, max_new, max_len, scal
     except MgError as e:
         if e.status != MG_ERR_WORKSPACE:
             raise
-        with torch.cuda.device(dev):
-            n = getattr(load(), name + "_workspace_bytes")(*args[4:])
+        n = _sized(dev, getattr(load(), name + "_workspace_bytes"), *args[4:])
         workspace = _new(n, torch.uint8, dev, stream)
         _call(*args, workspace.data_ptr(), n)
     return out
@@ -608,10 +615,9 @@ def token_logprobs(logits, tokens, top=0, out=None, workspace=None, stream=None)
     if not 0 <= top <= 32:
         _refuse("top", top, "0 .. 32")
     if out is None:
-        buf = _new(n * (2 + 2 * top), torch.int32, dev, stream)
+        buf = _new(n * (2 + 2 * top), torch.float32, dev, stream)
         a, b, ids, c = torch.unsafe_split_with_sizes(buf, (n, n, n * top, n * top))
-        f = torch.float32
-        out = TokenLogprobs(a.view(f), b.view(f), ids.view(n, top), c.view(f).view(n, top))
+        out = TokenLogprobs(a, b, ids.view(torch.int32).view(n, top), c.view(n, top))
         at = buf.data_ptr()
         ptrs = [at + 4 * k for k in (0, n, 2 * n, 2 * n + n * top)] if n else [None] * 4
     else:
@@ -624,18 +630,13 @@ def token_logprobs(logits, tokens, top=0, out=None, workspace=None, stream=None)
     tok = None if tokens is None else _ints("tokens", tokens, dev, n)
     args = ("mg_token_logprobs", dev, stream, load().mg_token_logprobs, n, V, logits.data_ptr(), int(logits.dtype is torch.bfloat16),
             st[0] if n > 1 else V, tok, top, *ptrs)
-    if workspace is not None:
-        if workspace.dtype is not torch.uint8 or workspace.device != dev or not workspace.is_contiguous():
-            _refuse("workspace", workspace, f"contiguous uint8 on {dev}")
-        _call(*args, workspace.data_ptr(), workspace.numel())
-        return out
-    try:
-        _call(*args, None, 0)
-    except MgError as e:
-        if e.status != MG_ERR_WORKSPACE:
-            raise
-        size = token_logprobs_workspace_bytes(n, V, top, dev)
-        _call(*args, _new(size, torch.uint8, dev, stream).data_ptr(), size)
+    if workspace is None:
+        size = _sized(dev, load().mg_token_logprobs_workspace_bytes, n, V, top) if dev.type == "cuda" else 0
+        if size:
+            workspace = _new(size, torch.uint8, dev, stream)
+    elif workspace.dtype is not torch.uint8 or workspace.device != dev or not workspace.is_contiguous():
+        _refuse("workspace", workspace, f"contiguous uint8 on {dev}")
+    _call(*args, *((None, 0) if workspace is None else (workspace.data_ptr(), workspace.numel())))
     return out
 
 
