@@ -64,10 +64,9 @@ __device__ __forceinline__ void k4_put_k(const uint32_t (&w)[4], uint8_t* codes,
 struct K4At {
     int page, t;
 };
-__device__ __forceinline__ K4At k4_at(const Kv4AppendArgs& a, int tok) {
-    const int s = a.slots[tok];
-    const bool ok = s >= 0 && (s >> 4) < a.c.n_pages && !(a.positions && a.positions[tok] < 0);
-    return K4At{ok ? s >> 4 : -1, s & 15};
+__device__ __forceinline__ K4At k4_at(const Kv4AppendArgs& a, int slot, int pos) {
+    const bool ok = slot >= 0 && (slot >> 4) < a.c.n_pages && pos >= 0;
+    return K4At{ok ? slot >> 4 : -1, slot & 15};
 }
 
 // Queries and keys: HD / 16 lanes a head, each with eight pairs (i, i + HD / 2) of it; a lane takes U heads of a token and reads
@@ -91,9 +90,9 @@ __device__ __forceinline__ void k4_rotate(const Kv4AppendArgs& a, int block) {
         }
     }
     float cs[16];
+    const int slot = a.slots[tok], pos = a.positions ? a.positions[tok] : 0;
+    if (pos < 0) return;
     if (a.positions) {
-        const int pos = a.positions[tok];
-        if (pos < 0) return;
         if (pos < a.n_positions) {
             const float* r = a.rope + (int64_t)pos * HD + 2 * at;
 #pragma unroll
@@ -103,7 +102,7 @@ __device__ __forceinline__ void k4_rotate(const Kv4AppendArgs& a, int block) {
             for (int i = 0; i < 16; ++i) cs[i] = __builtin_nanf("");
         }
     }
-    const K4At where = k4_at(a, tok);
+    const K4At where = k4_at(a, slot, pos);
 #pragma unroll
     for (int u = 0; u < U; ++u) {
         const int h = h0 + u * groups;
@@ -143,20 +142,24 @@ __device__ __forceinline__ void k4_values(const Kv4AppendArgs& a, int block) {
     const int groups = (a.c.Hkv + 3) / 4;  // (a wave's four heads are one token's)
     const int tok = (int)(task / 4 / groups), h = (int)(task / 4 % groups * 4 + task % 4);
     if (tok >= a.n || h >= a.c.Hkv) return;
-    const K4At at = k4_at(a, tok);
-    if (at.page < 0) return;
-    const auto here = [&](const K4At& o) { return o.page == at.page && (o.t >> 2) == (at.t >> 2); };
+    int slot[7], pos[7];  // of the tokens from tok - 3 to tok + 3, all requested at once
 #pragma unroll
-    for (int i = 1; i < 4; ++i)
-        if (tok >= i && here(k4_at(a, tok - i))) return;
+    for (int i = 0; i < 7; ++i) {
+        const int o = min(max(tok + i - 3, 0), a.n - 1);
+        slot[i] = a.slots[o];
+        pos[i] = a.positions ? a.positions[o] : 0;
+    }
+    const K4At at = k4_at(a, slot[3], pos[3]);
+    if (at.page < 0) return;
     int src[4] = {-1, -1, -1, -1};  // the token at each of the four positions
 #pragma unroll
-    for (int i = 0; i < 4; ++i) {
-        if (tok + i >= a.n) break;
-        const K4At o = k4_at(a, tok + i);
+    for (int i = 0; i < 7; ++i) {
+        const K4At o = k4_at(a, slot[i], pos[i]);
+        const bool here = tok + i - 3 >= 0 && tok + i - 3 < a.n && o.page == at.page && (o.t >> 2) == (at.t >> 2);
+        if (i < 3 && here) return;
 #pragma unroll
         for (int j = 0; j < 4; ++j)
-            if (here(o) && (o.t & 3) == j) src[j] = tok + i;
+            if (i >= 3 && here && (o.t & 3) == j) src[j] = tok + i - 3;
     }
     uint32_t keep = 0;  // the nibbles of the positions that have none
 #pragma unroll
