@@ -195,9 +195,17 @@ __device__ __forceinline__ float lp_most(const LpRaw<BF16>& r) {
     return m;
 }
 
-// A row's results from its joined state and list.
+// The logit of a row's token, or NaN for a token outside the vocabulary.
 template <bool BF16>
-__device__ __forceinline__ void lp_finish(const LogpArgs& a, int64_t row, const LpState& s, const LpList& list) {
+__device__ __forceinline__ float lp_token(const LogpArgs& a, int64_t row) {
+    const int t = a.logprob ? a.tokens[row] : -1;
+    if (t < 0 || t >= a.V) return __builtin_nanf("");
+    const int64_t at = row * a.stride + t;
+    return BF16 ? bf2f(static_cast<const uint16_t*>(a.logits)[at]) : static_cast<const float*>(a.logits)[at];
+}
+// A row's results from its joined state and list and its token's logit.
+template <bool BF16>
+__device__ __forceinline__ void lp_finish(const LogpArgs& a, int64_t row, const LpState& s, const LpList& list, float x) {
     const int lane = threadIdx.x & 63;
     const float ln = s.S == 0.0f ? 0.0f : logf(s.S);
     if (lane < a.top) {
@@ -207,17 +215,8 @@ __device__ __forceinline__ void lp_finish(const LogpArgs& a, int64_t row, const 
     }
     if (lane == 0) {
         if (a.entropy) a.entropy[row] = s.S == 0.0f ? 0.0f : ln - ieee_div(s.T, s.S);
-        if (a.logprob) {
-            const int t = a.tokens[row];
-            float x = __builtin_nanf("");
-            if (t >= 0 && t < a.V) {
-                const int64_t at = row * a.stride + t;
-                x = BF16 ? bf2f(static_cast<const uint16_t*>(a.logits)[at]) : static_cast<const float*>(a.logits)[at];
-                // (a row that is masked whole has no reference)
-                x = s.m == LP_NONE && s.S == 0.0f ? x : (x - s.m) - ln;
-            }
-            a.logprob[row] = x;
-        }
+        // (a row that is masked whole has no reference)
+        if (a.logprob) a.logprob[row] = s.m == LP_NONE && s.S == 0.0f ? x : (x - s.m) - ln;
     }
 }
 
@@ -238,6 +237,7 @@ __global__ __launch_bounds__(LP_THREADS) void logprobs_kernel(LogpArgs a, int se
     LpList list{LP_NONE, 0x7fffffff};
     float floor = LP_NONE, most = LP_NONE;  // at least `top` logits of the segment reach floor; most: the lane's largest of the wave's part
     LpRaw<BF16> next;
+    const float own = wave == 0 && segs == 1 ? lp_token<BF16>(a, row) : 0.0f;  // (requested before it is needed)
     if (s0 + wave < s1) lp_load<BF16>(p, (s0 + wave) * LP_SUB, a.V, lane, next);
     if (TOP) {
         // each of the waves' first parts has k lanes whose largest logit reaches its k-th largest, so `top` logits reach the least of these
@@ -328,7 +328,7 @@ __global__ __launch_bounds__(LP_THREADS) void logprobs_kernel(LogpArgs a, int se
         for (int w = 1; w < LP_WAVES; ++w) lp_merge(list, sv[w][63 - lane], si[w][63 - lane]);
     }
     if (segs == 1) {
-        lp_finish<BF16>(a, row, sum, list);
+        lp_finish<BF16>(a, row, sum, list, own);
         return;
     }
     float* part = static_cast<float*>(a.part) + (int64_t)blockIdx.x * lp_width(a.top);
@@ -349,6 +349,12 @@ __global__ __launch_bounds__(64 * LP_JOIN_WAVES) void logprobs_join_kernel(LogpA
     const int64_t row = blockIdx.x;
     const int width = lp_width(a.top);
     const float* part = static_cast<const float*>(a.part) + row * segs * width;
+    const float own = wave ? 0.0f : lp_token<BF16>(a, row);
+    LpState st{LP_NONE, 0.0f, 0.0f};
+    if (lane < segs) {
+        const float4 x = *reinterpret_cast<const float4*>(part + (int64_t)lane * width);
+        st = LpState{x.x, x.y, x.z};
+    }
     LpList list{LP_NONE, 0x7fffffff};
     if (TOP) {
         // a wave's first list as it is, the others from their ends
@@ -372,15 +378,10 @@ __global__ __launch_bounds__(64 * LP_JOIN_WAVES) void logprobs_join_kernel(LogpA
         }
     }
     if (wave) return;
-    LpState st{LP_NONE, 0.0f, 0.0f};
-    if (lane < segs) {
-        const float4 x = *reinterpret_cast<const float4*>(part + (int64_t)lane * width);
-        st = LpState{x.x, x.y, x.z};
-    }
     lp_move(st, wave_max(st.m));
     st.S = wave_sum_fast(st.S);
     st.T = wave_sum_fast(st.T);
-    lp_finish<BF16>(a, row, st, list);
+    lp_finish<BF16>(a, row, st, list, own);
 }
 
 // Segments of a row: until there are LP_BLOCKS_PER_CU, or every wave has one part.
