@@ -337,6 +337,9 @@ __device__ __forceinline__ void k4_walk(const Kv8AttnArgs& a, const K8Row& row, 
 
 // Rows of few query rows (tokens times query heads of a KV head <= 16 NT): one block per (row, KV head, split of the row's pages).
 // A wave has one of the NT tiles of 16 query rows, and the waves of a tile take its steps in turn.
+// Long rows are bound by the cache's bytes: 32 rows of 4096 to 16384 take 81 us, 4.3 TB/s, and 77 with the loads alone, as the scales' records of 80
+// bytes lie in lines of 128 that blocks on two XCDs fetch (without them 6.7 us less).  Shorter ones by what a step takes after its loads, some 2300 cycles
+// of matrix and vector instructions, which do not overlap, and by the chain of length, page ids, codes before: 64 rows of 640 13.7 us, one of 512 6.0.
 template <int HD, int WAVES>
 struct K4FewShared {
     float o[WAVES][16][HD + 4];  // (padded rows)
@@ -454,11 +457,15 @@ __global__ __launch_bounds__(K8_THREADS) void attn_kv4_join_kernel(Kv8AttnArgs a
     k4_few_join<HD, NT, EVEN>(a, few, blockIdx.x, rowb);
 }
 
-// Rows of more query rows: one block per (row, KV head, 64 NT query rows, split of the positions that these see), the tokens of a
-// row's end first (they see the most).  A wave holds NT tiles of query rows; four waves share a step's codes through a double buffer in LDS: a
+// Rows of more query rows: one block per (row, KV head, 128 query rows, split of the positions that these see), the tokens of a
+// row's end first (they see the most).  A wave holds two tiles of query rows; four waves share a step's codes through a double buffer in LDS: a
 // wave fetches two pages of the next step, K as it is, V's two pages joined into the words of its operands, V's scales as
 // numbers; one barrier a step parts the buffers.  GROUPS 2: the block has four waves more for the same query rows, and each group takes half of
 // its steps; their outputs join at the end.
+// Bound by issue: a tile's step is 40 matrix instructions (16 cycles each) and some 200 vector ones (32 exponentials among them), three conversions of
+// 70 cycles; counters show the two kinds' cycles add up to the time (matrix cores 29 % busy, vector units 74 %).  Four chunks of 2048 tokens behind
+// 0 to 6144 take 510 us, 1075 TFLOP/s of the definition's operations, where the 8-bit cache takes 581.  A barrier's wait is short; blocks in the order of
+// what they see over all rows instead of row by row: 505 us there, but 71 instead of 67 for two prompts of 1500.
 constexpr int K4_TILES = 2;  // tiles of 16 query rows of a wave
 constexpr int K4_CHUNK_ROWS = K8_WAVES * 16 * K4_TILES;
 constexpr int K4_MIN_STAGES = 4;  // steps that a split of a tile takes at least
@@ -800,14 +807,28 @@ struct K4Plan {
     int csplit;                 // splits of such a tile
     int groups;                 // of waves of a block in a call with longer rows
 };
-constexpr int K4_GROUP_BLOCKS_PER_CU = 2;
-constexpr int K4_MIN_PAGES = K4_STEP * K8_WAVES;  // pages a split takes at least: a step of every wave
-constexpr int K4_MAX_PAGES = 1024;  // and at most (with 256, 32 rows over 8000 to 16000 positions took 89.6 us instead of 83.7)
-constexpr int K4_MAX_SPLITS = 64;
+// Each choice with what was measured beside it (us; rows of one token with 32 query heads over 8 KV heads of 128, if not said otherwise):
+// Rows of few query rows are split until there are two blocks a CU, which is what the registers let reside (four: 64 rows of 640 positions 19.5
+// instead of 13.7, 32 rows of 50 to 9000 45 instead of 41, 8 rows of 2000 the same).
 constexpr int K4_BLOCKS_PER_CU = 2;
+// Pages that a split takes at least: a step of every wave (half of that: one row of 512 8.3 instead of 6.0, for the join's launch, one of 16384 17.4
+// instead of 12.1; twice: 8 rows of 2000 12.1 instead of 10.4),
+constexpr int K4_MIN_PAGES = K4_STEP * K8_WAVES;
+// and at most (256: 32 rows of 4096 to 16384 89.6 instead of 83.7),
+constexpr int K4_MAX_PAGES = 1024;
+// and beside longer rows, whose blocks take longer (64, 256, 1024: 10 rows of 2000 to 15000 beside two chunks 250, 241, 237 in all; 1024: three
+// of 16000 beside a chunk of 40 67 instead of 57).
+constexpr int K4_MIXED_PAGES = 512;
+constexpr int K4_MAX_SPLITS = 64;
+// From splits of so many pages on, the blocks find from all lengths how few pages a split may take (never: 32 rows of 4096 to 16384 87.5 instead of 80.3, of
+// 50 to 9000 47.8 instead of 41.3; from 16 pages on: 8 rows of 2000 14.3 instead of 10.4, for the lengths that every block then reads).
 constexpr int K4_EVEN_PAGES = 64;
-constexpr int K4_MIXED_PAGES = 256;
+// Longer rows: tiles are split while they leave CUs without a block (two blocks a CU: a prompt of 1000 45 instead of 26, as the splits' outputs are
+// written and joined). Splits of 2 and of 8 steps at least were as fast as of 4.
 constexpr int K4_CHUNK_BLOCKS_PER_CU = 1;
+// A block has two groups of waves up to so many blocks a CU (always: four chunks of 2048 588 instead of 505; never: a prompt of 2001 57 instead
+// of 50, the mixed batch of 20 tokens and 4 chunks 46 instead of 39).
+constexpr int K4_GROUP_BLOCKS_PER_CU = 2;
 // pages that a group of `tokens` neighbouring tokens of a row sees at most, by the host's bounds
 int64_t pages_seen(const Kv8AttnArgs& a, int64_t tokens) {
     int64_t len = a.max_len;
@@ -823,7 +844,7 @@ K4Plan plan_of(const Kv8AttnArgs& a) {
     const int64_t blocks = (int64_t)a.B * a.c.Hkv;
     const int64_t want = std::max<int64_t>(1, (K4_BLOCKS_PER_CU * a.n_cu + blocks / 2) / blocks);
     int64_t sp = std::min<int64_t>(K4_MAX_PAGES, std::max<int64_t>(K4_MIN_PAGES, (pages + want - 1) / want));
-    if (p.tiles) sp = std::min<int64_t>(8 * blocks <= a.n_cu ? K4_MIXED_PAGES / 2 : K4_MIXED_PAGES, pages);
+    if (p.tiles) sp = std::min<int64_t>(K4_MIXED_PAGES, pages);
     sp = std::max(sp, (pages + K4_MAX_SPLITS - 1) / K4_MAX_SPLITS);
     const int nsplit = (int)((pages + sp - 1) / sp);
     const int units = K4_BLOCKS_PER_CU * a.n_cu / a.c.Hkv;

@@ -116,7 +116,7 @@ __device__ __forceinline__ float lp_kth(float v, int k) {
     if (hi > lo + (1 << 25) && reach(hi - (1 << 25))) lo = hi - (1 << 25);  // (within some 16 times or 4 halvings of the largest)
 #pragma unroll 1
     for (int i = 0; i < 12; ++i) {
-        const int mid = lo + (int)((uint32_t)(hi - lo) >> 1);
+        const int mid = lo + (int)(((uint32_t)hi - (uint32_t)lo) >> 1);
         if (reach(mid)) lo = mid;
         else hi = mid;
     }

@@ -359,10 +359,10 @@ def test_rows_of_very_unequal_length(hq, hkv, hd, new, max_len):
 
 
 @pytest.mark.parametrize("hd", [64, 128])
-@pytest.mark.parametrize("holes,window,cap", [(False, 0, 0.0), (True, 4700, 20.0)])
-def test_long_short_rows_beside_a_chunk(hd, holes, window, cap):
+@pytest.mark.parametrize("holes,window,cap,long", [(False, 0, 0.0, 5000), (True, 4700, 20.0, 5000), (False, 0, 0.0, 9000), (True, 8700, 20.0, 12000)])
+def test_long_short_rows_beside_a_chunk(hd, holes, window, cap, long):
     new = [1, 1, 90, 1]
-    b = Batch(np.add([5000, 9, 4000, 2500], new), new, 32, 8, hd, seed=18)
+    b = Batch(np.add([long, 9, 4000, 2500], new), new, 32, 8, hd, seed=18)
     if holes:
         b.table[np.random.RandomState(1).rand(*b.table.shape) < 0.1] = -1
     b.check(window=window, softcap=cap)
