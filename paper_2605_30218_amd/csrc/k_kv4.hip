@@ -4,6 +4,9 @@
 // rounded to fp32 each, the result to bf16, as the decode path's own rotation.  A block of values (32 features of a key, a whole
 // value) becomes e2m1 codes under the least power of two whose sevenfold holds its largest magnitude: dividing by it is exact, so a
 // code is the nearest one whatever the scale, and nothing written before is rounded again.
+//
+// Many tokens are bound by bytes: 12000 of 28 query heads over 4 of 128 take 39.8 us, 203 MB at 5.1 TB/s (a copy of 200 MiB: 5.4), the read
+// of them 8.2 us; few by the chain of slot, row, maximum, code: 64 tokens of 32 heads over 8 4.8 us, their read 2.8, a launch that does nothing 1.6.
 #include "mg_device.h"
 #include "mg_kernels.h"
 
@@ -216,11 +219,12 @@ __global__ __launch_bounds__(K4_THREADS) void kv4_append_kernel(Kv4AppendArgs a,
         k4_values<HD>(a, blockIdx.x - rotate_blocks);
 }
 
-// Read: HD / 8 lanes a slot of a head, each with eight features.
+// Read: HD / 8 lanes a slot of a head, each with eight features.  (V by eight loads of a byte a lane: 12000 slots of 4 heads 9.4 us instead of 8.2.)
 template <int HD>
 __global__ __launch_bounds__(K4_THREADS) void kv4_read_kernel(Kv8 c, int n, const int32_t* __restrict__ slots, uint16_t* k,
                                                               int64_t ks, uint16_t* v, int64_t vs) {
     constexpr int L = HD / 8;
+    __shared__ uint32_t all[K4_THREADS];
     const int64_t task = (int64_t)blockIdx.x * K4_THREADS + threadIdx.x;
     const int lane = (int)(task % L), h = (int)(task / L % c.Hkv);
     const int64_t i = task / L / c.Hkv;
@@ -245,11 +249,26 @@ __global__ __launch_bounds__(K4_THREADS) void kv4_read_kernel(Kv8 c, int n, cons
         put(*reinterpret_cast<const uint32_t*>(codes + at * 16 + lane % 4 * 4), scales[at], k + i * ks + h * HD + 8 * lane);
     }
     if (v) {
-        // features 8 lane .. of tile lane / 2: m = 8 (lane % 2) ..
-        const uint8_t* p = codes + 8 * HD + ((t >> 2) * 16 + lane % 2 * 8) * (HD / 8) + lane / 2 * 2 + (t & 3) / 2;
+        // A position's codes lie at every second byte or so of its four positions': a lane loads what it has of 16 bytes (HD 128: its
+        // feature m of all tiles, HD 64: two), keeps the nibbles of its position, and takes the other lanes' by way of LDS.
+        const u32x4_k4 x = *reinterpret_cast<const u32x4_k4*>(codes + 8 * HD + (t >> 2) * (2 * HD) + lane * 16);
+        uint32_t own = 0;
+#pragma unroll
+        for (int j = 0; j < 4; ++j) {
+            const uint32_t y = x[j] >> (4 * (t & 3)) & 0x000f000fu;
+            own |= ((y | y >> 12) & 0xffu) << (8 * j);
+        }
+        all[threadIdx.x] = own;
+        // (the lanes of a slot are of one wave, whose LDS accesses keep their order)
+        __builtin_amdgcn_fence(__ATOMIC_RELEASE, "wavefront");
+        __builtin_amdgcn_wave_barrier();
+        __builtin_amdgcn_fence(__ATOMIC_ACQUIRE, "wavefront");
         uint32_t w = 0;
 #pragma unroll
-        for (int m = 0; m < 8; ++m) w |= ((uint32_t)p[m * (HD / 8)] >> (4 * (t & 1)) & 15u) << (4 * m);
+        for (int m = 0; m < 8; ++m) {  // features 8 lane .. of tile lane / 2
+            const uint32_t o = all[threadIdx.x - lane + (HD == 128 ? lane % 2 * 8 + m : lane % 2 * 4 + m / 2)];
+            w |= (o >> (lane / 2 * 4 + (HD == 128 ? 0 : m % 2 * 16)) & 15u) << (4 * m);
+        }
         put(w, scales[HD / 2 + t], v + i * vs + h * HD + 8 * lane);
     }
 }
@@ -257,11 +276,13 @@ __global__ __launch_bounds__(K4_THREADS) void kv4_read_kernel(Kv8 c, int n, cons
 template <int HD>
 void append(const Kv4AppendArgs& a, hipStream_t s) {
     const int heads = a.Hq + a.c.Hkv;
-    const int u = 4;
-    const int64_t lanes = (int64_t)a.n * ((heads + u - 1) / u) * (HD / 16);
+    // (heads of a lane: with 1, 2, 4, 8 of them 64 tokens of 40 heads take 4.8, 4.8, 5.8, 9.0 us, 12000 of 32 41.3, 39.7, 40.2, 42.1, 12000 of 40
+    // 62, 59, 58, 62)
+    constexpr int U = 2;
+    const int64_t lanes = (int64_t)a.n * ((heads + U - 1) / U) * (HD / 16);
     const int64_t rot = (lanes + K4_THREADS - 1) / K4_THREADS;
     const int64_t val = ((int64_t)a.n * ((a.c.Hkv + 3) / 4) * 64 + K4_THREADS - 1) / K4_THREADS;
-    hipLaunchKernelGGL((kv4_append_kernel<HD, 4>), dim3((unsigned)(rot + val)), dim3(K4_THREADS), 0, s, a, (int)rot);
+    hipLaunchKernelGGL((kv4_append_kernel<HD, U>), dim3((unsigned)(rot + val)), dim3(K4_THREADS), 0, s, a, (int)rot);
 }
 
 }  // namespace
