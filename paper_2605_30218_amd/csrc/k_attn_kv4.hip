@@ -808,8 +808,9 @@ struct K4Plan {
     int groups;                 // of waves of a block in a call with longer rows
 };
 // Each choice with what was measured beside it (us; rows of one token with 32 query heads over 8 KV heads of 128, if not said otherwise):
-// Rows of few query rows are split until there are two blocks a CU, which is what the registers let reside (four: 64 rows of 640 positions 19.5
-// instead of 13.7, 32 rows of 50 to 9000 45 instead of 41, 8 rows of 2000 the same).
+// Rows of few query rows are split until there are two blocks of four waves a CU, or one of eight, which is what the registers let reside (four:
+// 64 rows of 640 positions 19.5 instead of 13.7, 32 rows of 50 to 9000 45 instead of 41, 8 rows of 2000 the same; two of eight: 23 rows of four tokens
+// behind 300 to 5000, 28 heads over 4, 27.2 instead of 20.3, 8 of six tokens behind 1000 to 4000 22.9 instead of 16.4).
 constexpr int K4_BLOCKS_PER_CU = 2;
 // Pages that a split takes at least: a step of every wave (half of that: one row of 512 8.3 instead of 6.0, for the join's launch, one of 16384 17.4
 // instead of 12.1; twice: 8 rows of 2000 12.1 instead of 10.4),
@@ -842,12 +843,13 @@ K4Plan plan_of(const Kv8AttnArgs& a) {
     p.nt = rows <= 16 || p.tiles ? 1 : 2;
     const int64_t pages = pages_seen(a, std::min(a.max_new, 16 * p.nt / a.G));
     const int64_t blocks = (int64_t)a.B * a.c.Hkv;
-    const int64_t want = std::max<int64_t>(1, (K4_BLOCKS_PER_CU * a.n_cu + blocks / 2) / blocks);
+    const int reside = K4_BLOCKS_PER_CU * a.n_cu / p.nt;
+    const int64_t want = std::max<int64_t>(1, (reside + blocks / 2) / blocks);
     int64_t sp = std::min<int64_t>(K4_MAX_PAGES, std::max<int64_t>(K4_MIN_PAGES, (pages + want - 1) / want));
     if (p.tiles) sp = std::min<int64_t>(K4_MIXED_PAGES, pages);
     sp = std::max(sp, (pages + K4_MAX_SPLITS - 1) / K4_MAX_SPLITS);
     const int nsplit = (int)((pages + sp - 1) / sp);
-    const int units = K4_BLOCKS_PER_CU * a.n_cu / a.c.Hkv;
+    const int units = reside / a.c.Hkv;
     p.few = K8Few{(int)sp, nsplit, nsplit, 0};
     p.few_blocks = blocks * nsplit;
     if (!p.tiles && nsplit > 1 && sp >= K4_EVEN_PAGES && a.B > 1 && a.B <= 64 && a.B < units && (int64_t)a.B * a.maxp <= 1 << 30) {
