@@ -172,25 +172,35 @@ struct K4Acc {
 // by -1: exchanges between lanes and rescaled outputs are rare.
 constexpr float K4_FOLD = 13.0f;
 template <int HD>
-__device__ __forceinline__ void k4_probs(float (&x)[32], float f, K4Acc<HD>& acc) {
+__device__ __forceinline__ void k4_move(float mx, float f, K4Acc<HD>& acc) {
+    const float mn = fmaxf(acc.m, __builtin_fmaf(k8_col_max(mx), f, K4_FOLD));
+    const float al = __builtin_amdgcn_exp2f(acc.m - mn);
+    acc.m = mn;
+    acc.l *= al;
+#pragma unroll
+    for (int d = 0; d < HD / 16; ++d) acc.o[d] *= al;
+}
+__device__ __forceinline__ float k4_most(const float (&x)[32]) {
     float mx = x[0];
 #pragma unroll
     for (int i = 1; i < 32; ++i) mx = fmaxf(mx, x[i]);
-    if (__any(__builtin_fmaf(mx, f, -acc.m) > -1.0f)) {
-        const float mn = fmaxf(acc.m, __builtin_fmaf(k8_col_max(mx), f, K4_FOLD));
-        const float al = __builtin_amdgcn_exp2f(acc.m - mn);
-        acc.m = mn;
-        acc.l *= al;
-#pragma unroll
-        for (int d = 0; d < HD / 16; ++d) acc.o[d] *= al;
-    }
+    return mx;
+}
+// the exponentials in place; returned: their sum
+__device__ __forceinline__ float k4_exp(float (&x)[32], float f, float m) {
     float s[4];
 #pragma unroll
     for (int i = 0; i < 32; ++i) {
-        x[i] = __builtin_amdgcn_exp2f(__builtin_fmaf(x[i], f, -acc.m));
+        x[i] = __builtin_amdgcn_exp2f(__builtin_fmaf(x[i], f, -m));
         s[i & 3] = i < 4 ? x[i] : s[i & 3] + x[i];
     }
-    acc.l += (s[0] + s[1]) + (s[2] + s[3]);
+    return (s[0] + s[1]) + (s[2] + s[3]);
+}
+template <int HD>
+__device__ __forceinline__ void k4_probs(float (&x)[32], float f, K4Acc<HD>& acc) {
+    const float mx = k4_most(x);
+    if (__any(__builtin_fmaf(mx, f, -acc.m) > -1.0f)) k4_move(mx, f, acc);
+    acc.l += k4_exp(x, f, acc.m);
 }
 
 // a wave-uniform float in a scalar register
@@ -462,9 +472,9 @@ __global__ __launch_bounds__(K8_THREADS) void attn_kv4_join_kernel(Kv8AttnArgs a
 // wave fetches two pages of the next step, K as it is, V's two pages joined into the words of its operands, V's scales as
 // numbers; one barrier a step parts the buffers.  GROUPS 2: the block has four waves more for the same query rows, and each group takes half of
 // its steps; their outputs join at the end.
-// Bound by issue: a tile's step is 40 matrix instructions (16 cycles each) and some 200 vector ones (32 exponentials among them), three conversions of
-// 70 cycles; counters show the two kinds' cycles add up to the time (matrix cores 29 % busy, vector units 74 %).  Four chunks of 2048 tokens behind
-// 0 to 6144 take 510 us, 1075 TFLOP/s of the definition's operations, where the 8-bit cache takes 581.  A barrier's wait is short; blocks in the order of
+// Bound by issue: a tile's step is 40 matrix instructions (16 cycles each) and some 185 vector ones (32 exponentials among them), three conversions of
+// 70 cycles; counters show the two kinds' cycles add up to the time (matrix cores 26 % busy, vector units 68 %).  Four chunks of 2048 tokens behind
+// 0 to 6144 take 495 us, 1110 TFLOP/s of the definition's operations, where the 8-bit cache takes 581.  A barrier's wait is short; blocks in the order of
 // what they see over all rows instead of row by row: 505 us there, but 71 instead of 67 for two prompts of 1500.
 constexpr int K4_TILES = 2;  // tiles of 16 query rows of a wave
 constexpr int K4_CHUNK_ROWS = K8_WAVES * 16 * K4_TILES;
@@ -499,6 +509,9 @@ __device__ __forceinline__ void k4_chunk_block(const Kv8AttnArgs& a, int few, in
     typedef typename K4Lane<HD>::v vlane;
     typedef const __attribute__((address_space(1))) char* gptr;
     constexpr int DT = HD / 16, ROWS = K4_CHUNK_ROWS, NT = K4_TILES;
+    // Whether the sums, needed anyway, tell that the reference has to move, and the step's scores are then made again (four chunks of 2048 492 us,
+    // with their maximum looked at in every step 503; heads of 64: 6 chunks of 300 to 600 46 and 44).
+    constexpr bool REDO = HD == 128;
     constexpr size_t head_bytes = 16 * HD, head_scales = HD / 2 + 16;
     const int lane = threadIdx.x & 63, c = lane & 15, g = lane >> 4;
     const int group = GROUPS == 1 ? 0 : __builtin_amdgcn_readfirstlane(threadIdx.x / K8_THREADS);
@@ -588,6 +601,7 @@ __device__ __forceinline__ void k4_chunk_block(const Kv8AttnArgs& a, int few, in
         put(sh.stage[group][0]);
     }
     if (group) __builtin_amdgcn_s_setprio(1);  // (the groups meet at every barrier, and would else want the same units at the same times)
+    bool fresh = true;
     for (int st = 0; st < most; ++st) {
         const K4Stage<HD>& s = sh.stage[group][st & 1];
         now = map;
@@ -603,8 +617,25 @@ __device__ __forceinline__ void k4_chunk_block(const Kv8AttnArgs& a, int few, in
             asm("" : "+v"(ln));
             const uint32_t base = k4_lds_at(&s), s16 = base + 16 * ln, sk = HD == 128 ? s16 : base + 16 * (ln & 31);
             const uint32_t odd = s.odd[0] | s.odd[1] | s.odd[2] | s.odd[3];
-            float x[NT][32];
-            {
+            float x[NT][32], l[NT];
+            const auto mask = [&](int u) {
+                if (CAP) k8_cap(reinterpret_cast<float(&)[1][32]>(x[u]), so);
+                if (edge) {
+                    const int pp = sh.pos[wave][u][lane & 15];
+                    const int hi = min(pp, row.len - 1) - j0 - 4 * g, lo = (a.window ? k8_hidden(a.window, pp) : -1) - j0 - 4 * g;
+#pragma unroll
+                    for (int i = 0; i < 32; ++i) {
+                        const int at = 16 * (i >> 2) + (i & 3);
+                        x[u][i] = (now >> (i >> 2) & 1u) && at <= hi && at > lo ? x[u][i] : -__builtin_inff();
+                    }
+                }
+                if (__any(odd != 0)) {  // a value of V that is not finite: the columns that see it, and no other, become NaN
+#pragma unroll
+                    for (int i = 0; i < 32; ++i)
+                        x[u][i] = (s.odd[i >> 3] >> (4 * g) >> (16 * (i >> 2 & 1) + (i & 3)) & 1u) && x[u][i] != -__builtin_inff() ? __builtin_nanf("") : x[u][i];
+                }
+            };
+            for (bool move = fresh;; move = true) {
                 f32x4_k8 sc[NT][K4_STEP];
                 const u32x2_k8 ks = k4_lds<u32x2_k8>(base + SKS + 8 * ln);
                 uint32_t qs[NT];
@@ -658,28 +689,27 @@ __device__ __forceinline__ void k4_chunk_block(const Kv8AttnArgs& a, int few, in
 #pragma unroll
                     for (int i = 0; i < 32; ++i) x[u][i] = sc[u][i >> 2][i & 3];
                 }
+                __builtin_amdgcn_sched_barrier(0);
+                if (!REDO) break;
+#pragma unroll
+                for (int u = 0; u < NT; ++u) {
+                    mask(u);
+                    if (move) k4_move<HD>(k4_most(x[u]), so.f, acc[u]);
+                    l[u] = k4_exp(x[u], so.f, acc[u].m);
+                }
+                if (move || !__any(l[0] > 0.5f || l[1] > 0.5f)) break;
             }
+            fresh = false;
             i32x6_k4 p[NT][2];
             uint32_t ps[NT];
-            __builtin_amdgcn_sched_barrier(0);
 #pragma unroll
             for (int u = 0; u < NT; ++u) {
-                if (CAP) k8_cap(reinterpret_cast<float(&)[1][32]>(x[u]), so);
-                if (edge) {
-                    const int pp = sh.pos[wave][u][lane & 15];
-                    const int hi = min(pp, row.len - 1) - j0 - 4 * g, lo = (a.window ? k8_hidden(a.window, pp) : -1) - j0 - 4 * g;
-#pragma unroll
-                    for (int i = 0; i < 32; ++i) {
-                        const int at = 16 * (i >> 2) + (i & 3);
-                        x[u][i] = (now >> (i >> 2) & 1u) && at <= hi && at > lo ? x[u][i] : -__builtin_inff();
-                    }
+                if (REDO) {
+                    acc[u].l += l[u];
+                } else {
+                    mask(u);
+                    k4_probs<HD>(x[u], so.f, acc[u]);
                 }
-                if (__any(odd != 0)) {  // a value of V that is not finite: the columns that see it, and no other, become NaN
-#pragma unroll
-                    for (int i = 0; i < 32; ++i)
-                        x[u][i] = (s.odd[i >> 3] >> (4 * g) >> (16 * (i >> 2 & 1) + (i & 3)) & 1u) && x[u][i] != -__builtin_inff() ? __builtin_nanf("") : x[u][i];
-                }
-                k4_probs<HD>(x[u], so.f, acc[u]);
                 f32x16_k4 y[2];
                 float top = 0.0f;
 #pragma unroll
