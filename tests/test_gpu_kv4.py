@@ -259,6 +259,22 @@ def test_large_scores(new):
     Batch(np.add([300, 70], new), new, 8, 2, 64, seed=15, std=40.0).check()
 
 
+@pytest.mark.parametrize("hd", [64, 128])
+@pytest.mark.parametrize("window", [0, 300])
+@pytest.mark.parametrize("new", [[1, 1], [90, 40]])
+@pytest.mark.parametrize("to", [0.02, 30.0])
+def test_scores_that_rise_and_fall_over_the_positions(hd, window, new, to):
+    """Keys that grow (or shrink) by a power over the positions, so that the reference moves in some steps and for some rows only."""
+    b = Batch(np.add([1500, 700], new), new, 8, 2, hd, seed=29)
+    rng = np.random.RandomState(31)
+    for r, n in enumerate(b.lens):
+        j = np.arange(n)
+        slots = b.table[r, j // 16] * 16 + j % 16
+        k = rows(rng, (n, 2, hd)) * torch.as_tensor(to ** (j / n)[:, None, None]).to(torch.bfloat16)
+        mg.kv4_append(b.codes, b.scales, k.cuda(), rows(rng, (n, 2, hd)).cuda(), dev_i32(slots))
+    b.check(window=window)
+
+
 @pytest.mark.parametrize("new", [[1, 1, 1, 1], [20, 2, 33, 4]])
 def test_rows_that_see_nothing(new):
     """No positions, fewer positions than tokens, all pages unmapped, lengths past the table."""
