@@ -10,7 +10,7 @@
 //
 // What bounds it: the logits' bytes where rows are many (2001 rows of 152064 bf16 with 8 alternatives 128 us, 4.75 TB/s, 2001 of
 // 32000 fp32 with 20 49.7 us, 5.2 TB/s; a large read reaches 6.1), and where they are few the chain of load, floor, list, join and the second
-// launch (one row of 128256 fp32 with 5 alternatives 10.6 us, the join alone 4; 64 rows with 20 16.8 us, 9.1 without alternatives).
+// launch (one row of 128256 fp32 with 5 alternatives 9.7 us, the join alone 3; 64 rows with 20 16.1 us, 9.2 without alternatives).
 // Exponentials take the logits' differences from the reference in 32 bits; nothing is rounded to fewer.
 #include <algorithm>
 
@@ -25,8 +25,8 @@ constexpr int LP_THREADS = 64 * LP_WAVES;
 constexpr int LP_PER = 32;              // logits of a lane
 constexpr int LP_SUB = 64 * LP_PER;     // and of a wave at a time
 constexpr int LP_MAX_SEGS = 64;
-// A row is cut into segments until so many blocks a CU are there: 64 rows of 128256 fp32 logits with 20 alternatives take 16.8 us with 4 and
-// 17.9 with 2, 256 such rows 35.4 and 34.6, one row 10.6 either way.
+// A row is cut into segments until so many blocks a CU are there: 64 rows of 128256 fp32 logits with 20 alternatives take 16.0 us with 4 and
+// 17.1 with 2, 256 such rows 34.2 and 34.1, one row 9.7 either way.
 constexpr int LP_BLOCKS_PER_CU = 4;
 constexpr float LP_NONE = -__builtin_inff();
 
@@ -76,7 +76,7 @@ __device__ __forceinline__ float lp_wave_max(float v) {
 // A candidate: value and index.  a before b: the larger value, the lower index among equal ones.
 __device__ __forceinline__ bool lp_before(float av, int ai, float bv, int bi) { return av > bv || (av == bv && ai < bi); }
 
-// The lists of a wave: lane i the i-th candidate.
+// A list over lanes: lane i the i-th candidate.
 struct LpList {
     float v;
     int i;
@@ -90,18 +90,22 @@ __device__ __forceinline__ void lp_order(LpList& a) {  // the lane without bit O
         a.i = i;
     }
 }
-// the 64 first of two sorted lists, sorted; (rv, ri): the other list from its end
+// Lists of up to 32, one in each half of a wave: the 32 first of a list and another one, (rv, ri) from its end, sorted
+static_assert(LOGP_MAX_TOP <= 32, "a list fits half a wave");
 __device__ __forceinline__ void lp_merge(LpList& a, float rv, int ri) {
     if (lp_before(rv, ri, a.v, a.i)) {
         a.v = rv;
         a.i = ri;
     }
-    lp_order<32>(a);
     lp_order<16>(a);
     lp_order<8>(a);
     lp_order<4>(a);
     lp_order<2>(a);
     lp_order<1>(a);
+}
+// and of the two halves' lists
+__device__ __forceinline__ void lp_merge_halves(LpList& a) {
+    lp_merge(a, __shfl_xor(a.v, 63, 64), __shfl_xor(a.i, 63, 64));
 }
 // A number that at least k lanes' values reach, close below the k-th largest of them (-inf if fewer than k are above): by halving
 // an interval of the floats' order, which a count of lanes decides and scalar instructions carry.
@@ -224,8 +228,8 @@ __device__ __forceinline__ void lp_finish(const LogpArgs& a, int64_t row, const 
 // its state and list.
 template <bool BF16, bool TOP>
 __global__ __launch_bounds__(LP_THREADS) void logprobs_kernel(LogpArgs a, int segs) {
-    __shared__ float sv[LP_WAVES][64], sm[LP_WAVES][3], sf[LP_WAVES];
-    __shared__ int si[LP_WAVES][64];
+    __shared__ float sv[LP_WAVES][32], sm[LP_WAVES][3], sf[LP_WAVES];
+    __shared__ int si[LP_WAVES][32];
     const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
     const int64_t row = blockIdx.x / segs;
     const int seg = blockIdx.x % segs;
@@ -305,7 +309,7 @@ __global__ __launch_bounds__(LP_THREADS) void logprobs_kernel(LogpArgs a, int se
         sm[wave][1] = st.S;
         sm[wave][2] = st.T;
     }
-    if (TOP) {
+    if (TOP && lane < 32) {
         sv[wave][lane] = lane < a.top ? list.v : LP_NONE;
         si[wave][lane] = lane < a.top ? list.i : 0x7fffffff;
     }
@@ -323,9 +327,11 @@ __global__ __launch_bounds__(LP_THREADS) void logprobs_kernel(LogpArgs a, int se
         sum.T += o.T;
     }
     if (TOP) {
-        list = LpList{sv[0][lane], si[0][lane]};
-#pragma unroll
-        for (int w = 1; w < LP_WAVES; ++w) lp_merge(list, sv[w][63 - lane], si[w][63 - lane]);
+        static_assert(LP_WAVES == 4, "two lists a half");
+        const int h = lane >> 5, i = lane & 31;
+        list = LpList{sv[h][i], si[h][i]};
+        lp_merge(list, sv[h + 2][31 - i], si[h + 2][31 - i]);
+        lp_merge_halves(list);
     }
     if (segs == 1) {
         lp_finish<BF16>(a, row, sum, list, own);
@@ -339,12 +345,12 @@ __global__ __launch_bounds__(LP_THREADS) void logprobs_kernel(LogpArgs a, int se
     }
 }
 
-// One block a row: its segments' states and lists join, a wave a list and then the waves pairwise.
-constexpr int LP_JOIN_WAVES = 8;
+// One block a row: its segments' states and lists join, half a wave a list, then the halves and the waves.
+constexpr int LP_JOIN_WAVES = 4;
 template <bool BF16, bool TOP>
 __global__ __launch_bounds__(64 * LP_JOIN_WAVES) void logprobs_join_kernel(LogpArgs a, int segs) {
-    __shared__ float sv[LP_JOIN_WAVES][64];
-    __shared__ int si[LP_JOIN_WAVES][64];
+    __shared__ float sv[LP_JOIN_WAVES][32];
+    __shared__ int si[LP_JOIN_WAVES][32];
     const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
     const int64_t row = blockIdx.x;
     const int width = lp_width(a.top);
@@ -357,25 +363,34 @@ __global__ __launch_bounds__(64 * LP_JOIN_WAVES) void logprobs_join_kernel(LogpA
     }
     LpList list{LP_NONE, 0x7fffffff};
     if (TOP) {
-        // a wave's first list as it is, the others from their ends
-        if (lane < a.top && wave < segs) {
-            const float* q = part + (int64_t)wave * width + 4;
-            list = LpList{q[lane], reinterpret_cast<const int*>(q)[a.top + lane]};
-        }
-        const int r = 63 - lane;
-        for (int s = wave + LP_JOIN_WAVES; s < segs; s += LP_JOIN_WAVES) {
-            const float* q = part + (int64_t)s * width + 4;
-            lp_merge(list, r < a.top ? q[r] : LP_NONE, r < a.top ? reinterpret_cast<const int*>(q)[a.top + r] : 0x7fffffff);
-        }
-#pragma unroll
-        for (int o = LP_JOIN_WAVES / 2; o >= 1; o >>= 1) {
-            if (wave >= o && wave < 2 * o) {
-                sv[wave][lane] = list.v;
-                si[wave][lane] = list.i;
+        // a half's first list as it is, the others from their ends
+        const int h = lane >> 5, i = lane & 31;
+        for (int s = 2 * wave; s < segs; s += 2 * LP_JOIN_WAVES) {
+            const bool first = s == 2 * wave;
+            const int j = first ? i : 31 - i;
+            float v = LP_NONE;
+            int id = 0x7fffffff;
+            if (s + h < segs && j < a.top) {
+                const float* q = part + (int64_t)(s + h) * width + 4;
+                v = q[j];
+                id = reinterpret_cast<const int*>(q)[a.top + j];
             }
-            __syncthreads();
-            if (wave < o) lp_merge(list, sv[wave + o][63 - lane], si[wave + o][63 - lane]);
+            if (first)
+                list = LpList{v, id};
+            else
+                lp_merge(list, v, id);
         }
+        lp_merge_halves(list);
+        if (h == 0) {
+            sv[wave][i] = list.v;
+            si[wave][i] = list.i;
+        }
+        __syncthreads();
+        if (wave) return;
+        static_assert(LP_JOIN_WAVES == 4, "two lists a half");
+        list = LpList{sv[h][i], si[h][i]};
+        lp_merge(list, sv[h + 2][31 - i], si[h + 2][31 - i]);
+        lp_merge_halves(list);
     }
     if (wave) return;
     lp_move(st, wave_max(st.m));
