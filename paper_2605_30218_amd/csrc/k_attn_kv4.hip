@@ -97,7 +97,7 @@ __device__ __forceinline__ uint32_t k4_pair(f32x16_k4& even, f32x16_k4& odd, flo
 
 // Query rows rr0 + 16 u + c of a row's KV head (row rr: token rr / G, head rr % G of the group) as B operands in LDS (registers are
 // what bounds a wave's tiles), and the positions of their tokens; columns past the row's last repeat its first.  Three terms of a
-// value: exact but for what is below 2^-7 of the largest of its 32 features, which is off by 2^-15 of that at most.  HD 128: an
+// value: exact but for what is below 2^-6 of the largest of its 32 features, which is off by 2^-14 of that at most.  HD 128: an
 // operand a term.  HD 64: the first two terms share one (lanes 0..31 and 32..63, against K's features twice), the third has
 // one with zeros.
 template <int HD>

@@ -112,8 +112,9 @@ def attention(cache, q, table, lens, cu, scale, window=0, softcap=0.0):
     """(out, bound) in float64: the definition's result for q [T][Hq][hd], and how far a bf16 result may be from it.  With w the
     softmax weights and A = sum_j w_j |v_j| the bound adds
       the output's rounding, half a step of bf16: 2^-8 |out|;
-      a query value's three 6-bit terms: below 2^-7 of the largest of its 32 features it is off by 2^-15 of that at most, so a
-        score by 2^-15 * scale * sum (largest of the block) |k|;
+      a query value's three 6-bit terms under S, S / 32, S / 1024 with the block's largest in [S, 2 S): their steps are an eighth of these, so a
+        value from S / 64 up, a multiple of S / 8192 in bf16, is exact, and one below is off by half a step, S / 16384, at most: a
+        score by 2^-14 * scale * sum (largest of the block) |k|;
       fp32 scores: hd + 16 roundings of 2^-24 relative to scale * sum |q k| (a capped score: 2^-20 of the largest score more), and exp's argument,
         rounded once relative to the largest score; each weight moves by at most 2 (E + 2^-23 max|s|) of itself, twice for the quotient;
       a probability times its value's scale as two 6-bit terms, for each code, under s and s / 32 with the largest of its 32 positions from
@@ -153,7 +154,7 @@ def attention(cache, q, table, lens, cu, scale, window=0, softcap=0.0):
             s = x @ k.T * scale
             E = (hd + 16) * 2.0 ** -24 * scale * np.where(see, np.abs(x) @ np.abs(k).T, 0.0).max(1)
             xb = np.repeat(np.abs(x).reshape(len(x), -1, 32).max(2), 32, 1)
-            E += 2.0 ** -15 * scale * np.where(see, xb @ np.abs(k).T, 0.0).max(1)
+            E += 2.0 ** -14 * scale * np.where(see, xb @ np.abs(k).T, 0.0).max(1)
             if softcap:
                 s = softcap * np.tanh(s / softcap)
                 E = E + 2.0 ** -20 * np.where(see, np.abs(s), 0.0).max(1)
