@@ -57,11 +57,22 @@ __device__ __forceinline__ i32x6_k4 k4_block(const f32x16_k4& even, const f32x16
 // Three terms of 32 query values under scales s, s / 32, s / 1024, with s the power of two under which the largest (`top`, float bits, finite) is
 // below 2: a term is off by 1/16 of its scale at most, and 32 times that is at most 2 again, so s / 16384 or 2^-14 of the largest is left in the end.
 // What a term leaves is found by adding and taking away a number whose last bit is an eighth of its scale, which rounds as the conversion does.
+// That number would be infinite from s = 2^108 on, so values of blocks from 2^64 up are taken 2^64 lower first (exact but for what is below 2^-126 of
+// the largest); the scales' bytes are those of the values as they were.
 __device__ __forceinline__ uint32_t k4_triple(f32x16_k4& even, f32x16_k4& odd, uint32_t top, i32x6_k4 (&t)[3]) {
     const uint32_t scale = max(top & 0x7f800000u, 12u << 23);  // (the third's is a normal number)
+    uint32_t at = scale;
+    if (scale >= (127u + 64u) << 23) {
+        at -= 64u << 23;
+#pragma unroll
+        for (int i = 0; i < 16; ++i) {
+            even[i] *= 0x1p-64f;
+            odd[i] *= 0x1p-64f;
+        }
+    }
 #pragma unroll
     for (int k = 0; k < 3; ++k) {
-        const float s = __uint_as_float(scale - k * (5u << 23)), M = s * 0x1.8p+20f;
+        const float s = __uint_as_float(at - k * (5u << 23)), M = s * 0x1.8p+20f;
         t[k] = k4_block(even, odd, s);
         if (k == 2) break;
 #pragma unroll
