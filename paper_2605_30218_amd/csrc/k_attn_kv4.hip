@@ -167,25 +167,35 @@ __device__ __forceinline__ i32x6_k4 k4_operand(const K4Query<HD>& q, int k) {
 
 template <int HD>
 struct K4Acc {
-    float m, l;  // reference of the exponents (log2 units); sum over the lane's positions
+    float m, l;  // the score (as x below, before the factor f) that the exponents refer to; sum over the lane's positions
     f32x4_k8 o[HD / 16];
     __device__ __forceinline__ void clear() {
-        // below every finite score, and finite: exp2(masked - m) is 0 where nothing was seen yet
-        m = -3.0e38f;
+        // no score is below it, and it is finite: exp2 of a masked score's difference is 0 where nothing was seen yet
+        m = -3.402823466e38f;
         l = 0.0f;
 #pragma unroll
         for (int d = 0; d < HD / 16; ++d) o[d] = f32x4_k8{0.f, 0.f, 0.f, 0.f};
     }
 };
 
-// A step's scores x (position 16 i + 4 g + r at x[4 i + r]) become its probabilities, of at most 1/2: the reference is K4_FOLD above the scores that
-// moved it last, so that a probability times a value's scale, up to 2^126, is finite.  It moves only when a score of the step passes it
-// by -1: exchanges between lanes and rescaled outputs are rare.
+// A step's scores x (position 16 i + 4 g + r at x[4 i + r]) become its probabilities, of at most some 1/2: 2^((x - m) f - K4_FOLD), with m the score that
+// moved the reference last, so that a probability times a value's scale, up to 2^126, is finite.  m moves only when a score of the step passes it
+// by 12 / f: exchanges between lanes and rescaled outputs are rare.
+// The exponent is x f - (m f + K4_FOLD) with one rounding, relative to the rounded second term; that rounding is the same for all scores, but from
+// |m f| of some 2^30 on it is larger than what exp2 takes.  So references beyond K4_FAR take x - m first (an instruction a score, in rare steps).
 constexpr float K4_FOLD = 13.0f;
+constexpr float K4_FAR = 4096.0f;
+__device__ __forceinline__ float k4_at(float m, float f) { return fmaxf(__builtin_fmaf(m, f, K4_FOLD), -3.0e38f); }
+__device__ __forceinline__ bool k4_far(float at) { return __builtin_fabsf(at) > K4_FAR; }
+// the factor of what was summed under reference m where the reference becomes `to`, at least m
+__device__ __forceinline__ float k4_rescale(float m, float to, float f) {
+    const float a = k4_at(m, f), b = k4_at(to, f);
+    return __builtin_amdgcn_exp2f(k4_far(a) || k4_far(b) ? (m - to) * f : a - b);
+}
 template <int HD>
 __device__ __forceinline__ void k4_move(float mx, float f, K4Acc<HD>& acc) {
-    const float mn = fmaxf(acc.m, __builtin_fmaf(k8_col_max(mx), f, K4_FOLD));
-    const float al = __builtin_amdgcn_exp2f(acc.m - mn);
+    const float mn = fmaxf(acc.m, k8_col_max(mx));
+    const float al = k4_rescale(acc.m, mn, f);
     acc.m = mn;
     acc.l *= al;
 #pragma unroll
@@ -199,10 +209,17 @@ __device__ __forceinline__ float k4_most(const float (&x)[32]) {
 }
 // the exponentials in place; returned: their sum
 __device__ __forceinline__ float k4_exp(float (&x)[32], float f, float m) {
+    float at = k4_at(m, f);
+    if (__any(k4_far(at))) {
+        const float sub = k4_far(at) ? m : 0.0f;
+#pragma unroll
+        for (int i = 0; i < 32; ++i) x[i] -= sub;
+        at = k4_far(at) ? K4_FOLD : at;
+    }
     float s[4];
 #pragma unroll
     for (int i = 0; i < 32; ++i) {
-        x[i] = __builtin_amdgcn_exp2f(__builtin_fmaf(x[i], f, -m));
+        x[i] = __builtin_amdgcn_exp2f(__builtin_fmaf(x[i], f, -at));
         s[i & 3] = i < 4 ? x[i] : s[i & 3] + x[i];
     }
     return (s[0] + s[1]) + (s[2] + s[3]);
@@ -210,7 +227,7 @@ __device__ __forceinline__ float k4_exp(float (&x)[32], float f, float m) {
 template <int HD>
 __device__ __forceinline__ void k4_probs(float (&x)[32], float f, K4Acc<HD>& acc) {
     const float mx = k4_most(x);
-    if (__any(__builtin_fmaf(mx, f, -acc.m) > -1.0f)) k4_move(mx, f, acc);
+    if (__any((mx - acc.m) * f > 12.0f)) k4_move(mx, f, acc);
     acc.l += k4_exp(x, f, acc.m);
 }
 
@@ -413,6 +430,7 @@ __device__ __forceinline__ void k4_few_block(const Kv8AttnArgs& a, const K8Few& 
     for (int d = 0; d < DT; ++d) *reinterpret_cast<f32x4_k8*>(&sh.o[wave][c][16 * d + 4 * g]) = acc.o[d];
     __syncthreads();
     const int live = row.n * a.G;
+    const float unit = k8_soft(a).f;
     for (int i = threadIdx.x; i < live * (HD / 4); i += 64 * WAVES) {
         const int rr = i / (HD / 4), d = i % (HD / 4) * 4;
         const int w0 = rr / 16, rc = rr % 16;
@@ -423,7 +441,7 @@ __device__ __forceinline__ void k4_few_block(const Kv8AttnArgs& a, const K8Few& 
         f32x4_k8 O = f32x4_k8{0.f, 0.f, 0.f, 0.f};
 #pragma unroll
         for (int w = 0; w < WAVES / NT; ++w) {
-            const float f = __builtin_amdgcn_exp2f(sh.m[w0 + w * NT][rc] - M);
+            const float f = k4_rescale(sh.m[w0 + w * NT][rc], M, unit);
             L += f * sh.l[w0 + w * NT][rc];
             O += f * *reinterpret_cast<const f32x4_k8*>(&sh.o[w0 + w * NT][rc][d]);
         }
@@ -471,7 +489,9 @@ __device__ __forceinline__ void k4_few_join(const Kv8AttnArgs& a, const K8Few& f
     const int nsplit = few.most;
     const size_t first = ((size_t)r * a.c.Hkv + kh) * nsplit * (16 * NT) + rr;
     const float* ml = a.part + (size_t)a.B * a.c.Hkv * nsplit * (16 * NT) * HD;
-    k8_join<HD>(a.part + first * HD, (size_t)(16 * NT) * HD, ml + 2 * first, 2 * 16 * NT, act, k8_out(a, row, kh, rr));
+    const float unit = k8_soft(a).f;
+    k8_join<HD>(a.part + first * HD, (size_t)(16 * NT) * HD, ml + 2 * first, 2 * 16 * NT, act, k8_out(a, row, kh, rr),
+                [unit](float m, float M) { return k4_rescale(m, M, unit); });
 }
 template <int HD, int NT, bool EVEN>
 __global__ __launch_bounds__(K8_THREADS) void attn_kv4_join_kernel(Kv8AttnArgs a, K8Few few, int rowb) {
@@ -767,7 +787,7 @@ __device__ __forceinline__ void k4_chunk_block(const Kv8AttnArgs& a, int few, in
 #pragma unroll
         for (int u = 0; u < NT; ++u) {
             const float m1 = other_ml[2 * u * 64], M = fmaxf(acc[u].m, m1);
-            const float f0 = __builtin_amdgcn_exp2f(acc[u].m - M), f1 = __builtin_amdgcn_exp2f(m1 - M);
+            const float f0 = k4_rescale(acc[u].m, M, so.f), f1 = k4_rescale(m1, M, so.f);
             acc[u].m = M;
             acc[u].l = acc[u].l * f0 + other_ml[(2 * u + 1) * 64] * f1;
 #pragma unroll
@@ -836,7 +856,9 @@ __global__ __launch_bounds__(K8_THREADS) void attn_kv4_mixed_join_kernel(Kv8Attn
     if (act == 1) return;
     const size_t first = (size_t)at * csplit * ROWS + i;
     const float* ml = cpart + (size_t)tiles * a.c.Hkv * csplit * ROWS * HD;
-    k8_join<HD>(cpart + first * HD, (size_t)ROWS * HD, ml + 2 * first, 2 * ROWS, act, k8_out(a, row, kh, rr));
+    const float unit = k8_soft(a).f;
+    k8_join<HD>(cpart + first * HD, (size_t)ROWS * HD, ml + 2 * first, 2 * ROWS, act, k8_out(a, row, kh, rr),
+                [unit](float m, float M) { return k4_rescale(m, M, unit); });
 }
 
 // The launch.

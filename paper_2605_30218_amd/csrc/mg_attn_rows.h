@@ -152,10 +152,14 @@ __device__ __forceinline__ void k8_cap(float (&x)[NT][N], const K8Soft& so) {
         }
 }
 
+// The factor of what was summed under an exponents' reference m (log2 units) where the reference is M.
+struct K8Weight {
+    __device__ __forceinline__ float operator()(float m, float M) const { return __builtin_amdgcn_exp2f(m - M); }
+};
 // One query row's splits joined in their order by a wave: outputs at po + s * so, reference and sum of split s in lane s's
-// ml (act <= 64).
-template <int HD>
-__device__ __forceinline__ void k8_join(const float* po, size_t so, const float* pml, size_t sml, int act, uint16_t* out) {
+// ml (act <= 64); weight: as K8Weight.
+template <int HD, class Weight = K8Weight>
+__device__ __forceinline__ void k8_join(const float* po, size_t so, const float* pml, size_t sml, int act, uint16_t* out, Weight weight = Weight{}) {
     constexpr int PL = HD / 64;  // consecutive features of a lane
     constexpr int AHEAD = 8;     // splits whose outputs are requested together, the first before their weights are known
     const int lane = threadIdx.x & 63;
@@ -166,7 +170,7 @@ __device__ __forceinline__ void k8_join(const float* po, size_t so, const float*
 #pragma unroll
     for (int k = 0; k < AHEAD; ++k) v[k] = *reinterpret_cast<const vec*>(po + (size_t)min(k, act - 1) * so);
     const float M = wave_max(ml.x);
-    const float f = lane < act ? __builtin_amdgcn_exp2f(ml.x - M) : 0.0f;
+    const float f = lane < act ? weight(ml.x, M) : 0.0f;
     const float L = wave_sum_fast(lane < act ? f * ml.y : 0.0f);
     const float inv = L == 0.0f ? 0.0f : ieee_div(1.0f, L);
     float O[PL];
