@@ -391,8 +391,9 @@ mg_status mg_kv4_read(const mg_kv4_cache* cache, int n, const int32_t* slots, ui
  * A value of K or V that is NaN (a scale byte of 255) makes the outputs of the tokens that see it NaN, of V in all features; so do a
  * query value that is not finite and sums past fp32, which are reached where |v| passes some 2^100.  Query values enter as three 6-bit terms
  * under the scale of 32 features: exact but for those below 2^-6 of their block's largest, which are off by at most 2^-14 of that.
- * A probability times its value's scale enters the product with V as two such terms: off by at most 2^-8 of itself or 1/1920 of the largest of
- * 32 positions, whichever is more (and by some 2^-116: where all |v| of a row are below some 2^-100 its outputs lose bits). */
+ * A probability times its value's scale enters the product with V as two such terms, or more where 32 positions' scales are more than 2^2 apart: a
+ * probability is off by at most 2^-8 of itself or 1/480 of the largest of 32 positions, whichever is more, whatever the sizes of their values (and by some
+ * 2^-116 over its value's scale: where all |v| of a row are below some 2^-100 its outputs lose bits). */
 size_t mg_kv4_attention_workspace_bytes(const mg_kv4_cache* cache, const mg_kv8_attn_args* args);
 mg_status mg_kv4_attention(const mg_kv4_cache* cache, const mg_kv8_attn_args* args, void* workspace,
                            size_t workspace_bytes, void* stream);

@@ -105,6 +105,60 @@ __device__ __forceinline__ uint32_t k4_pair(f32x16_k4& even, f32x16_k4& odd, flo
     t[1] = k4_block(even, odd, __uint_as_float(scale - (5u << 23)));
     return (scale >> 23) * 0x101u - 0x500u;
 }
+// The 1/1920 is of the largest weight times scale.  Where scales of V differ, a position of a small one beside a large one would lose as much, though the
+// large one has no part in the features that its codes leave 0: beside scales 2^5, 2^7, 2^9 times theirs such features were off by 0.008, 0.03, 0.12, with
+// bf16 weights by 0.0014, with two terms and scales within 2^2 by 0.0009 to 0.0014.  So a block takes one more term, under a 32nd of the scale before it,
+// for each 2^5 that its scales are further apart: a weight is off by 2^-8 of itself or 1/480 of the block's largest, whatever the scales of V.
+// To look at the scales costs steps that need no further term 4 % in chunks (four of 2048 500 -> 522 us) and nothing that shows in rows of few
+// query rows; with a further term in all steps four chunks take 652 us, 64 rows 15.9 instead of 13.7, 32 long rows 87 instead of 81.
+constexpr uint32_t K4_NEAR = 2;
+// Positions that hold nothing, what is not finite (both 0 here) or the least scale have a part in no distance.
+constexpr uint32_t K4_EMPTY = 16;
+__device__ __forceinline__ uint32_t k4_counted(uint32_t b) { return b > K4_EMPTY ? b : 255u; }
+// terms of a block whose scales' bytes are from lo to hi (0: k4_pair's)
+__device__ __forceinline__ int k4_terms(uint32_t lo, uint32_t hi) { return hi > lo + K4_NEAR ? (int)(hi - lo + 4 - K4_NEAR) / 5 : 0; }
+// the most of a wave's lanes
+__device__ __forceinline__ int k4_wave_most(int n) {
+    int most = 0;
+    while (__any(n > most)) ++most;
+    return most;
+}
+// n terms after the second of k4_pair, which left even and odd and the scales' bytes ps: add(term, its scale's byte) for each.
+// (Scales stay normal numbers: what is below some 2^-120 is lost.)
+// What a term leaves is found by making it again and converting it back (BACK), or, with 32 registers less and some 300 cycles more, by rounding to eighths of
+// its scale: so for numbers up to twice that; larger ones were 2 s or more, the second term left 2^-8 of them at most, and they need no more.
+template <bool BACK, class Add>
+__device__ __forceinline__ void k4_more(f32x16_k4& even, f32x16_k4& odd, uint32_t ps, int n, const Add& add) {
+    uint32_t b = max(ps >> 8 & 0xffu, 5u);
+#pragma unroll 1
+    for (int k = 0; k < n; ++k) {
+        if constexpr (BACK) {
+            const float s = __uint_as_float(b << 23);
+            const i32x6_k4 t = k4_block(even, odd, s);
+            f32x32_k4 y = __builtin_amdgcn_cvt_scalef32_pk32_f32_fp6(__builtin_bit_cast(u32x6_k4, t), s);
+            asm volatile("" : "+v"(y) : "v"(t), "v"(s));
+#pragma unroll
+            for (int i = 0; i < 16; ++i) {
+                even[i] -= y[2 * i];
+                odd[i] -= y[2 * i + 1];
+            }
+        } else {
+            const float to = __uint_as_float((257u - b) << 23), by = __uint_as_float(b << 23) * 0.125f;  // 8 / s, s / 8
+            const auto rest = [&](float x) {
+                const float y = x * to;
+                return __builtin_fabsf(y) <= 16.0f ? __builtin_fmaf(-__builtin_rintf(y), by, x) : 0.0f;
+            };
+#pragma unroll
+            for (int i = 0; i < 16; ++i) {
+                even[i] = rest(even[i]);
+                odd[i] = rest(odd[i]);
+                __builtin_amdgcn_sched_barrier(0);
+            }
+        }
+        b = max(b, 10u) - 5u;
+        add(k4_block(even, odd, __uint_as_float(b << 23)), b);
+    }
+}
 
 // Query rows rr0 + 16 u + c of a row's KV head (row rr: token rr / G, head rr % G of the group) as B operands in LDS (registers are
 // what bounds a wave's tiles), and the positions of their tokens; columns past the row's last repeat its first.  Three terms of a
@@ -351,21 +405,47 @@ __device__ __forceinline__ void k4_walk(const Kv8AttnArgs& a, const K8Row& row, 
             k4_probs<HD>(x, so.f, acc);
             f32x16_k4 y[2];
             float top = 0.0f;
+            uint32_t hi = 0, lo = 255;  // of the scales' bytes
 #pragma unroll
             for (int i = 0; i < 32; ++i) {
-                y[i & 1][i >> 1] = x[i] * __uint_as_float((vs[i >> 2] >> (8 * (i & 3)) & 0xffu) << 23);
+                const uint32_t b = vs[i >> 2] >> (8 * (i & 3)) & 0xffu;
+                hi = max(hi, b);
+                lo = min(lo, b);
+                y[i & 1][i >> 1] = x[i] * __uint_as_float(b << 23);
                 top = fmaxf(top, y[i & 1][i >> 1]);
+            }
+            const auto values = [&](int d) {
+                u32x4_k8 A;
+#pragma unroll
+                for (int e = 0; e < 4; ++e) A[e] = __builtin_amdgcn_perm(vb[2 * e + 1][d / 2], vb[2 * e][d / 2], d & 1 ? 0x07060302u : 0x05040100u);
+                return A;
+            };
+            int terms = 0;
+            if (__any(hi > lo + K4_NEAR)) {
+                lo = 255;
+#pragma unroll
+                for (int i = 0; i < 32; ++i) lo = min(lo, k4_counted(vs[i >> 2] >> (8 * (i & 3)) & 0xffu));
+                terms = k4_wave_most(k4_terms(lo, hi));
             }
             i32x6_k4 p[2];
             const uint32_t ps = k4_pair(y[0], y[1], top, p);
 #pragma unroll
             for (int d = 0; d < DT; ++d) {
-                u32x4_k8 A;
-#pragma unroll
-                for (int e = 0; e < 4; ++e)
-                    A[e] = __builtin_amdgcn_perm(vb[2 * e + 1][d / 2], vb[2 * e][d / 2], d & 1 ? 0x07060302u : 0x05040100u);
+                const u32x4_k8 A = values(d);
                 acc.o[d] = k4_mfma<0, 0>(A, 127u, p[0], ps, acc.o[d]);
                 acc.o[d] = k4_mfma<0, 1>(A, 127u, p[1], ps, acc.o[d]);
+            }
+            if (terms) {
+                __builtin_amdgcn_sched_barrier(0);
+                k4_more<HD == 64>(y[0], y[1], ps, terms, [&](const i32x6_k4& t, uint32_t b) {
+#pragma unroll
+                    for (int e = 0; e < K4_STEP; ++e) asm volatile("" : "+v"(vb[e]));  // (operands are made in each turn, not held in registers)
+#pragma unroll
+                    for (int d = 0; d < DT; ++d) {
+                        acc.o[d] = k4_mfma<0, 0>(values(d), 127u, t, b, acc.o[d]);
+                        __builtin_amdgcn_sched_barrier(0);
+                    }
+                });
             }
             __builtin_amdgcn_sched_barrier(0);
             if (more) fetch_v(s + stride);
@@ -511,6 +591,15 @@ constexpr int K4_TILES = 2;  // tiles of 16 query rows of a wave
 constexpr int K4_CHUNK_ROWS = K8_WAVES * 16 * K4_TILES;
 constexpr int K4_MIN_STAGES = 4;  // steps that a split of a tile takes at least
 static_assert(K4_STEP == 2 * K8_WAVES, "a wave stages two pages");
+// the largest of a row of 16 lanes
+template <int CTRL>
+__device__ __forceinline__ uint32_t k4_max_of(uint32_t x) { return max(x, (uint32_t)__builtin_amdgcn_update_dpp(0, (int)x, CTRL, 0xf, 0xf, true)); }
+__device__ __forceinline__ uint32_t k4_row_most(uint32_t x) {
+    x = k4_max_of<0xB1>(x);   // (lanes 1 0 3 2)
+    x = k4_max_of<0x4E>(x);   // (2 3 0 1)
+    x = k4_max_of<0x141>(x);  // (7 .. 0)
+    return k4_max_of<0x140>(x);  // (15 .. 0)
+}
 // values at a byte address of LDS: a register and a constant each, so that neighbouring reads share the register
 template <class T>
 __device__ __forceinline__ T k4_lds(uint32_t at) {
@@ -527,6 +616,7 @@ struct K4Stage {
     uint8_t ks[64][K4_STEP];         // a lane's scale bytes of K, page by page
     float vs[K4_STEP][16];           // V's scales (0 where the value is not finite)
     uint32_t odd[K8_WAVES];          // bit 16 e + t: position t of page 2 word + e of V is not finite
+    uint32_t span[K8_WAVES];         // of V's scale bytes of these two pages (0 where not finite): the largest, and 255 less the least, 16 bits each
 };
 template <int HD, int GROUPS>
 struct K4ChunkShared {
@@ -543,6 +633,8 @@ __device__ __forceinline__ void k4_chunk_block(const Kv8AttnArgs& a, int few, in
     // Whether the sums, needed anyway, tell that the reference has to move, and the step's scores are then made again (four chunks of 2048 492 us,
     // with their maximum looked at in every step 503; heads of 64: 6 chunks of 300 to 600 46 and 44).
     constexpr bool REDO = HD == 128;
+    // Where the weights' further terms are made: behind all else of a step, or (with fewer registers held) behind their tile's first two
+    constexpr bool LATE = HD == 128;
     constexpr size_t head_bytes = 16 * HD, head_scales = HD / 2 + 16;
     const int lane = threadIdx.x & 63, c = lane & 15, g = lane >> 4;
     const int group = GROUPS == 1 ? 0 : __builtin_amdgcn_readfirstlane(threadIdx.x / K8_THREADS);
@@ -619,8 +711,16 @@ __device__ __forceinline__ void k4_chunk_block(const Kv8AttnArgs& a, int few, in
 #pragma unroll
         for (int d = 0; d < DT; ++d) s.v[d][lane][wave] = __builtin_amdgcn_perm(nv[1][d / 2], nv[0][d / 2], d & 1 ? 0x07060302u : 0x05040100u);
         const unsigned long long odd = __ballot(nvs == 255u);
-        if (lane < 32) s.vs[2 * wave + (lane >> 4)][lane & 15] = __uint_as_float(nvs == 255u ? 0u : nvs << 23);
-        if (lane == 0) s.odd[wave] = (uint32_t)odd;
+        const uint32_t b = nvs == 255u ? 0u : nvs;
+        if (lane < 32) s.vs[2 * wave + (lane >> 4)][lane & 15] = __uint_as_float(b << 23);
+        // (both halves of the wave have these bytes: one takes the largest, the other the least)
+        const uint32_t m = k4_row_most(lane < 32 ? b : 255u - b);
+        const auto of = [&](int at) { return (uint32_t)__builtin_amdgcn_readlane((int)m, at); };
+        const uint32_t span = max(of(0), of(16)) | max(of(32), of(48)) << 16;
+        if (lane == 0) {
+            s.odd[wave] = (uint32_t)odd;
+            s.span[wave] = span;
+        }
     };
 
     // a lane's places in LDS
@@ -731,8 +831,40 @@ __device__ __forceinline__ void k4_chunk_block(const Kv8AttnArgs& a, int few, in
                 if (move || !__any(l[0] > 0.5f || l[1] > 0.5f)) break;
             }
             fresh = false;
+            int terms = 0;  // of the weights (0: two)
+            {
+                uint32_t hi = 0, low = 0;  // (255 less the least)
+#pragma unroll
+                for (int w = 0; w < K8_WAVES; ++w) {
+                    const uint32_t span = (uint32_t)__builtin_amdgcn_readfirstlane((int)s.span[w]);
+                    hi = max(hi, span & 0xffffu);
+                    low = max(low, span >> 16);
+                }
+                uint32_t lo = 255u - low;
+                if (hi > lo + K4_NEAR) {
+                    if (lo <= K4_EMPTY) {
+                        lo = 255;
+#pragma unroll 1
+                        for (int e = 0; e < K4_STEP; ++e)
+#pragma unroll
+                            for (int i = 0; i < 4; ++i) lo = min(lo, k4_counted(__float_as_uint(s.vs[e][4 * g + i]) >> 23));
+                    }
+                    terms = k4_wave_most(k4_terms(lo, hi));
+                }
+            }
+            f32x16_k4 y[NT][2];
             i32x6_k4 p[NT][2];
             uint32_t ps[NT];
+            const auto more = [&](int u) {
+                k4_more<true>(y[u][0], y[u][1], ps[u], terms, [&](const i32x6_k4& t, uint32_t b) {
+                    asm volatile("" ::: "memory");  // (operands are read in each turn, not held in registers)
+#pragma unroll
+                    for (int d = 0; d < DT; ++d) {
+                        acc[u].o[d] = k4_mfma<0, 0>(k4_lds<u32x4_k8>(s16 + SV + d * 1024), 127u, t, b, acc[u].o[d]);
+                        __builtin_amdgcn_sched_barrier(0);
+                    }
+                });
+            };
 #pragma unroll
             for (int u = 0; u < NT; ++u) {
                 if (REDO) {
@@ -741,18 +873,18 @@ __device__ __forceinline__ void k4_chunk_block(const Kv8AttnArgs& a, int few, in
                     mask(u);
                     k4_probs<HD>(x[u], so.f, acc[u]);
                 }
-                f32x16_k4 y[2];
                 float top = 0.0f;
 #pragma unroll
                 for (int e = 0; e < K4_STEP; ++e) {
                     const f32x4_k8 v = k4_lds<f32x4_k8>(base + SVS + 64 * e + 16 * g);
 #pragma unroll
                     for (int i = 0; i < 4; ++i) {
-                        y[i & 1][2 * e + (i >> 1)] = x[u][4 * e + i] * v[i];
-                        top = fmaxf(top, y[i & 1][2 * e + (i >> 1)]);
+                        y[u][i & 1][2 * e + (i >> 1)] = x[u][4 * e + i] * v[i];
+                        top = fmaxf(top, y[u][i & 1][2 * e + (i >> 1)]);
                     }
                 }
-                ps[u] = k4_pair(y[0], y[1], top, p[u]);
+                ps[u] = k4_pair(y[u][0], y[u][1], top, p[u]);
+                if (!LATE && terms) more(u);
             }
 #pragma unroll
             for (int d = 0; d < DT; ++d) {
@@ -762,6 +894,11 @@ __device__ __forceinline__ void k4_chunk_block(const Kv8AttnArgs& a, int few, in
                     acc[u].o[d] = k4_mfma<0, 0>(A, 127u, p[u][0], ps[u], acc[u].o[d]);
                     acc[u].o[d] = k4_mfma<0, 1>(A, 127u, p[u][1], ps[u], acc[u].o[d]);
                 }
+            }
+            if (LATE && terms) {
+                __builtin_amdgcn_sched_barrier(0);
+#pragma unroll
+                for (int u = 0; u < NT; ++u) more(u);
             }
         }
         if (st + 1 < steps) put(sh.stage[group][(st + 1) & 1]);
