@@ -409,7 +409,7 @@ mg_status mg_kv4_attention(const mg_kv4_cache* cache, const mg_kv8_attn_args* ar
  * Logits of -inf are masked: they have no part in the sums.  A row that is masked whole has log probabilities of -inf and an
  * entropy of 0.  A NaN or +inf in a row makes its log probabilities and entropy NaN; NaN is never among the top tokens.
  * logits fp32 (logits_bf16 = 0) or bf16, row stride `stride` values (>= vocab, any alignment of a value); 1 <= vocab <= 2^30,
- * 0 <= top <= 32, top <= vocab, n <= 2^24.  logprob, entropy [n], top_tokens, top_logprobs [n][top]: any may be NULL (with
+ * 0 <= top <= 32, top <= vocab, n < 2^24.  logprob, entropy [n], top_tokens, top_logprobs [n][top]: any may be NULL (with
  * logprob NULL tokens are not read).  No output may overlap the logits or tokens.  The workspace holds nothing between calls; the
  * same call gives the same bits. */
 size_t mg_token_logprobs_workspace_bytes(int n, int vocab, int top);

@@ -7,7 +7,8 @@ using namespace mg;
 namespace {
 
 bool sizes_ok(int n, int vocab, int top) {
-    return n >= 0 && n <= (1 << 24) && vocab >= 1 && vocab <= (1 << 30) && top >= 0 && top <= LOGP_MAX_TOP && top <= vocab;
+    // (a block of 256 threads a row, and a launch takes fewer than 2^32)
+    return n >= 0 && n < (1 << 24) && vocab >= 1 && vocab <= (1 << 30) && top >= 0 && top <= LOGP_MAX_TOP && top <= vocab;
 }
 
 }  // namespace

@@ -1,0 +1,14 @@
+"""The largest calls of the 4-bit K/V cache and of token log probabilities (CPU): what a launch cannot take is refused before any work is enqueued.  The
+pointers of the refused calls are never followed."""
+from paper_2605_30218_amd import mg
+
+ARG = -1
+P = 1 << 20  # an aligned address that no refused call reads
+
+
+def test_log_probabilities_of_more_rows_than_a_launch_takes():
+    """A row has a block of 256 threads, and 2^24 of these are the 2^32 threads that no launch has."""
+    lib = mg.load()
+    call = lambda n: lib.mg_token_logprobs(n, 2, P, 0, 2, P, 1, 2 * P, 3 * P, 4 * P, 5 * P, 6 * P, 1 << 40, None)  # noqa: E731
+    assert call(1 << 24) == ARG and call((1 << 24) + 1) == ARG
+    assert lib.mg_token_logprobs_workspace_bytes(1 << 24, 128256, 5) == 0
