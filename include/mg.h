@@ -363,8 +363,8 @@ size_t mg_kv4_scale_bytes(int n_pages, int n_kv_heads, int head_dim);
  * mg_batch_plan lists them: else the values (not the keys) of these four positions are undefined.  Two tokens with the same slot
  * leave its key undefined, and its value is the later token's (if they stand so).
  * q, k, v, q_out bf16 [n][heads][hd], 16-byte aligned, strides in values, multiples of 8 and >= heads * hd.  q_out may be q
- * itself (with q's stride); else no written row may overlap a row of q, k or v: MG_ERR_ARG.  At most 2^26 (token, head) pairs of q and k a
- * call.  slots, positions int32 [n]; rope fp32 [n_positions][hd], 16-byte aligned. */
+ * itself (with q's stride); else no written row may overlap a row of q, k or v: MG_ERR_ARG.  At most 2^25 tokens and
+ * 2^26 (token, head) pairs of q and k a call.  slots, positions int32 [n]; rope fp32 [n_positions][hd], 16-byte aligned. */
 typedef struct {
     int32_t n_tokens;
     int32_t n_q_heads;         /* 0..4096 */

@@ -20,6 +20,9 @@ mg_status attn_args(const mg_kv4_cache* c, const mg_kv8_attn_args* g, Kv8AttnArg
 }
 
 constexpr int64_t MOST_PAIRS = 1 << 26;
+// of an append: a token's values take 64 threads for each four KV heads, its heads at most 4 each, and a launch takes fewer than 2^32
+constexpr int64_t MOST_TOKENS = 1 << 25;
+static_assert(16 * (MOST_PAIRS + 3 * MOST_TOKENS) + 4 * (MOST_PAIRS + MOST_TOKENS) + 512 < 1ll << 32, "an append is one launch");
 
 // n rows of `width` bf16 values
 struct Rows {
@@ -53,7 +56,7 @@ mg_status mg_kv4_append(const mg_kv4_cache* cache, const mg_kv4_append_args* g, 
     if (st != MG_OK) return st;
     if (!g || g->n_tokens < 0) return MG_ERR_ARG;
     if (g->n_q_heads < 0 || g->n_q_heads > 4096) return MG_ERR_SHAPE;
-    if ((int64_t)g->n_tokens * (g->n_q_heads + cache->n_kv_heads) > MOST_PAIRS) return MG_ERR_ARG;
+    if (g->n_tokens > MOST_TOKENS || (int64_t)g->n_tokens * (g->n_q_heads + cache->n_kv_heads) > MOST_PAIRS) return MG_ERR_ARG;
     if (g->n_tokens == 0) return MG_OK;
     const int64_t hd = cache->head_dim, kw = hd * cache->n_kv_heads, qw = hd * g->n_q_heads;
     if (!g->k || !g->v || !g->slots || !rows_ok(g->k, g->k_stride, kw) || !rows_ok(g->v, g->v_stride, kw)) return MG_ERR_ARG;

@@ -1,5 +1,9 @@
 """The largest calls of the 4-bit K/V cache and of token log probabilities (CPU): what a launch cannot take is refused before any work is enqueued.  The
 pointers of the refused calls are never followed."""
+import ctypes as C
+
+import pytest
+
 from paper_2605_30218_amd import mg
 
 ARG = -1
@@ -12,3 +16,12 @@ def test_log_probabilities_of_more_rows_than_a_launch_takes():
     call = lambda n: lib.mg_token_logprobs(n, 2, P, 0, 2, P, 1, 2 * P, 3 * P, 4 * P, 5 * P, 6 * P, 1 << 40, None)  # noqa: E731
     assert call(1 << 24) == ARG and call((1 << 24) + 1) == ARG
     assert lib.mg_token_logprobs_workspace_bytes(1 << 24, 128256, 5) == 0
+
+
+@pytest.mark.parametrize("hd", [64, 128])
+@pytest.mark.parametrize("n", [(1 << 25) + 1, 59700000, 63200000, 1 << 26])
+def test_appends_of_more_tokens_than_a_launch_takes(n, hd):
+    """A token's values take 64 threads whatever its heads, so pairs alone do not bound a call of one KV head and no queries."""
+    c = mg.MgKv4Cache(P, P, 8, 1, hd)
+    a = mg.MgKv4AppendArgs(n, 0, None, 0, None, 0, 2 * P, hd, 3 * P, hd, P, None, None, 0)
+    assert mg.load().mg_kv4_append(C.byref(c), C.byref(a), None) == ARG
