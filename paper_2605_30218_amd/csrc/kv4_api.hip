@@ -6,11 +6,14 @@ using namespace mg;
 
 namespace {
 
+// (a page of a head has a number of 31 bits: 2 TiB of codes)
+bool dims_ok(int n_pages, int n_kv_heads, int head_dim) {
+    return cache_dims_ok(n_pages, n_kv_heads, head_dim) && (int64_t)n_pages * n_kv_heads < (1ll << 31);
+}
 // MG_OK, or why the cache is refused
 mg_status cache_status(const mg_kv4_cache* c) {
     if (!c || !c->codes || !c->scales || !aligned(c->codes, 16) || !aligned(c->scales, 4)) return MG_ERR_ARG;
-    // (a page of a head has a number of 31 bits: 2 TiB of codes)
-    return cache_dims_ok(c->n_pages, c->n_kv_heads, c->head_dim) && (int64_t)c->n_pages * c->n_kv_heads < (1ll << 31) ? MG_OK : MG_ERR_SHAPE;
+    return dims_ok(c->n_pages, c->n_kv_heads, c->head_dim) ? MG_OK : MG_ERR_SHAPE;
 }
 Kv8 view(const mg_kv4_cache* c) { return Kv8{c->codes, c->scales, c->n_pages, c->n_kv_heads, c->head_dim}; }
 // the checked arguments of an attention call as the kernels take them
@@ -44,11 +47,11 @@ struct Rows {
 extern "C" {
 
 size_t mg_kv4_code_bytes(int n_pages, int n_kv_heads, int head_dim) {
-    return cache_dims_ok(n_pages, n_kv_heads, head_dim) ? (size_t)n_pages * n_kv_heads * 2 * 8 * head_dim : 0;
+    return dims_ok(n_pages, n_kv_heads, head_dim) ? (size_t)n_pages * n_kv_heads * 2 * 8 * head_dim : 0;
 }
 
 size_t mg_kv4_scale_bytes(int n_pages, int n_kv_heads, int head_dim) {
-    return cache_dims_ok(n_pages, n_kv_heads, head_dim) ? (size_t)n_pages * n_kv_heads * (head_dim / 2 + 16) : 0;
+    return dims_ok(n_pages, n_kv_heads, head_dim) ? (size_t)n_pages * n_kv_heads * (head_dim / 2 + 16) : 0;
 }
 
 mg_status mg_kv4_append(const mg_kv4_cache* cache, const mg_kv4_append_args* g, void* stream) {

@@ -6,7 +6,7 @@ import pytest
 
 from paper_2605_30218_amd import mg
 
-ARG = -1
+ARG, SHAPE = -1, -2
 P = 1 << 20  # an aligned address that no refused call reads
 
 
@@ -25,3 +25,16 @@ def test_appends_of_more_tokens_than_a_launch_takes(n, hd):
     c = mg.MgKv4Cache(P, P, 8, 1, hd)
     a = mg.MgKv4AppendArgs(n, 0, None, 0, None, 0, 2 * P, hd, 3 * P, hd, P, None, None, 0)
     assert mg.load().mg_kv4_append(C.byref(c), C.byref(a), None) == ARG
+
+
+@pytest.mark.parametrize("n_pages,hkv", [((1 << 27) - 1, 1024), (1 << 21, 1024), (1 << 26, 32)])
+def test_sizes_of_caches_that_the_calls_refuse_are_zero(n_pages, hkv):
+    """A page of a head has a number of 31 bits."""
+    lib = mg.load()
+    for hd in (64, 128):
+        c = mg.MgKv4Cache(P, P, n_pages, hkv, hd)
+        assert lib.mg_kv4_read(C.byref(c), 1, P, P, hkv * hd, P, hkv * hd, None) == SHAPE
+        assert lib.mg_kv4_code_bytes(n_pages, hkv, hd) == 0 and lib.mg_kv4_scale_bytes(n_pages, hkv, hd) == 0
+        assert lib.mg_kv4_code_bytes((1 << 31) // hkv - 1, hkv, hd) == ((1 << 31) // hkv - 1) * hkv * 16 * hd
+    with pytest.raises(mg.MgError):
+        mg.kv4_empty(n_pages, hkv, 128, device="cpu")
