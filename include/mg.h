@@ -359,9 +359,9 @@ size_t mg_kv4_scale_bytes(int n_pages, int n_kv_heads, int head_dim);
  * rotated (rope is not read; q is copied to q_out).
  * Tokens with a negative position are left out: nothing is written for them.  A slot outside the cache stores nothing (its q is
  * rotated).  A position of n_positions or more has no angle: its q_out and key become NaN.
- * The tokens of four aligned positions of a page (4 g .. 4 g + 3) stand within four consecutive tokens of the call, as
- * mg_batch_plan lists them: else the values (not the keys) of these four positions are undefined.  Two tokens with the same slot
- * leave its key undefined, and its value is the later token's (if they stand so).
+ * Tokens may stand in any order (the plan's, where neighbouring positions are neighbours, is the fastest), and positions that the call has no token for are
+ * left as they were.  Two tokens with the same slot leave its key undefined; its value is the later one's where they stand within four consecutive
+ * tokens, else the values of its four aligned positions (4 g .. 4 g + 3 of a page) are undefined.
  * q, k, v, q_out bf16 [n][heads][hd], 16-byte aligned, strides in values, multiples of 8 and >= heads * hd.  q_out may be q
  * itself (with q's stride); else no written row may overlap a row of q, k or v: MG_ERR_ARG.  At most 2^25 tokens and
  * 2^26 (token, head) pairs of q and k a call.  slots, positions int32 [n]; rope fp32 [n_positions][hd], 16-byte aligned. */

@@ -134,35 +134,41 @@ __device__ __forceinline__ void k4_rotate(const Kv4AppendArgs& a, int block) {
     }
 }
 
-// Values: two positions share a byte, and four stand in 16 (HD 128) or 8 bytes of a lane, so the first token of the call at four
-// aligned positions of a page writes for all of them (within four tokens of the call), and keeps what they do not cover.  16 lanes
-// a head, lane m with features 16 c + m.
+// Values: two positions share a byte, and four stand in 16 (HD 128) or 8 bytes of a lane.  Tokens that stand together in the call and in four aligned
+// positions of a page (up to four of a row, as a batch plan lists them) are written by the first of them: by plain stores where they are all
+// four, else by changing their own bits alone, as other tokens of the call may change the others at the same time.  Of two tokens with the same slot within
+// four the earlier one is left out.  16 lanes a head, lane m with features 16 c + m.  (The neighbours' slots by a lane each and all that follows from them in
+// scalar registers: 64 tokens 4.5 us, with the loads and comparisons in every lane 5.4; plain stores where no other token can be near: no gain.)
 template <int HD>
 __device__ __forceinline__ void k4_values(const Kv4AppendArgs& a, int block) {
     constexpr int C = HD / 16;
     const int m = threadIdx.x & 15;
     const int64_t task = ((int64_t)block * K4_THREADS + threadIdx.x) >> 4;
     const int groups = (a.c.Hkv + 3) / 4;  // (a wave's four heads are one token's)
-    const int tok = (int)(task / 4 / groups), h = (int)(task / 4 % groups * 4 + task % 4);
+    const int tok = __builtin_amdgcn_readfirstlane((int)(task / 4 / groups)), h = (int)(task / 4 % groups * 4 + task % 4);
     if (tok >= a.n || h >= a.c.Hkv) return;
-    int slot[7], pos[7];  // of the tokens from tok - 3 to tok + 3, all requested at once
+    int near[8];  // slots of the tokens from tok - 1 to tok + 6 (-1: nothing is stored), a lane each
+    {
+        const int o = tok - 1 + (int)(threadIdx.x & 7), in = min(max(o, 0), a.n - 1);
+        const int slot = a.slots[in], pos = a.positions ? a.positions[in] : 0;
+        const int own = k4_at(a, slot, o == in ? pos : -1).page < 0 ? -1 : slot;
 #pragma unroll
-    for (int i = 0; i < 7; ++i) {
-        const int o = min(max(tok + i - 3, 0), a.n - 1);
-        slot[i] = a.slots[o];
-        pos[i] = a.positions ? a.positions[o] : 0;
+        for (int i = 0; i < 8; ++i) near[i] = __builtin_amdgcn_readlane(own, i);
     }
-    const K4At at = k4_at(a, slot[3], pos[3]);
-    if (at.page < 0) return;
+    // whether neighbour i is of the four positions of tok's, and none of the three behind it has its slot
+    const auto here = [&](int i) {
+        return near[i] >> 2 == near[1] >> 2 && near[i] != near[i + 1] && near[i] != near[i + 2] && near[i] != near[i + 3];
+    };
+    if (near[1] < 0 || !here(1) || here(0)) return;
+    const K4At at{near[1] >> 4, near[1] & 15};
     int src[4] = {-1, -1, -1, -1};  // the token at each of the four positions
+    bool run = true;
 #pragma unroll
-    for (int i = 0; i < 7; ++i) {
-        const K4At o = k4_at(a, slot[i], pos[i]);
-        const bool here = tok + i - 3 >= 0 && tok + i - 3 < a.n && o.page == at.page && (o.t >> 2) == (at.t >> 2);
-        if (i < 3 && here) return;
+    for (int i = 1; i < 5; ++i) {
+        run = run && here(i);
 #pragma unroll
         for (int j = 0; j < 4; ++j)
-            if (i >= 3 && here && (o.t & 3) == j) src[j] = tok + i - 3;
+            if (run && (near[i] & 3) == j) src[j] = tok + i - 1;
     }
     uint32_t keep = 0;  // the nibbles of the positions that have none
 #pragma unroll
@@ -203,12 +209,17 @@ __device__ __forceinline__ void k4_values(const Kv4AppendArgs& a, int block) {
         n = k4_codes<1>(n, bf2f(x[2][2 * i]) * u[2], bf2f(x[3][2 * i]) * u[3]);
         n = k4_codes<2>(n, bf2f(x[0][2 * i + 1]) * u[0], bf2f(x[1][2 * i + 1]) * u[1]);
         n = k4_codes<3>(n, bf2f(x[2][2 * i + 1]) * u[2], bf2f(x[3][2 * i + 1]) * u[3]);
-        w[i] = keep ? (n & ~keep) | (w[i] & keep) : n;
+        w[i] = keep ? (n ^ w[i]) & ~keep : n;  // (what changes)
     }
-    if constexpr (C == 8)
+    if (keep) {
+#pragma unroll
+        for (int i = 0; i < C / 2; i += 2)
+            atomicXor(reinterpret_cast<unsigned long long*>(codes) + i / 2, w[i] | (unsigned long long)w[i + 1] << 32);
+    } else if constexpr (C == 8) {
         *reinterpret_cast<uint4*>(codes) = make_uint4(w[0], w[1], w[2], w[3]);
-    else
+    } else {
         *reinterpret_cast<uint2*>(codes) = make_uint2(w[0], w[1]);
+    }
 }
 
 template <int HD, int U>

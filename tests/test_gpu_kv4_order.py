@@ -1,0 +1,99 @@
+"""Appends to the 4-bit K/V cache (GPU) with tokens in any order: positions that share bytes of the cache, wherever in the call they stand."""
+import numpy as np
+import pytest
+import torch
+
+import _kv4_ref as ref
+from _gpu_common import dev_i32
+from _kv8_ref import bf16
+from paper_2605_30218_amd import mg
+from test_gpu_kv4 import check_append, rows, table_of
+
+pytestmark = pytest.mark.gpu
+
+
+def filled(n_pages, hkv, hd, seed=0):
+    """A cache whose pages hold other values, and what stands for it."""
+    rng = np.random.RandomState(seed)
+    cache, want = mg.kv4_empty(n_pages, hkv, hd), ref.RefCache(n_pages, hkv, hd)
+    n = 16 * n_pages
+    check_append(cache, want, rows(rng, (n, hkv, hd)), rows(rng, (n, hkv, hd), 3.0), np.arange(n))
+    return cache, want
+
+
+def append(cache, want, slots, seed=1, **kw):
+    rng = np.random.RandomState(seed)
+    shape = (len(slots), want.val.shape[1], want.val.shape[-1])
+    check_append(cache, want, rows(rng, shape, 2.0), rows(rng, shape), np.asarray(slots), **kw)
+
+
+@pytest.mark.parametrize("hkv,hd", [(1, 64), (8, 128), (5, 64)])
+@pytest.mark.parametrize("part", [0.1, 0.5, 1.0])
+def test_any_order(hkv, hd, part):
+    """Random slots in a random order, forwards and backwards."""
+    n_pages = 40
+    for seed in range(3):
+        cache, want = filled(n_pages, hkv, hd, seed)
+        s = np.random.RandomState(seed).permutation(16 * n_pages)[:int(part * 16 * n_pages)]
+        for order in (s, np.sort(s), np.sort(s)[::-1]):
+            append(cache, want, order, seed)
+
+
+@pytest.mark.parametrize("hd", [64, 128])
+@pytest.mark.parametrize("rows_", [2, 5, 64])
+def test_tokens_ordered_by_position_over_the_rows(hd, rows_):
+    """Each row's next tokens, position by position: neighbours of a row are `rows_` tokens apart, positions rotated on the way."""
+    rng = np.random.RandomState(rows_)
+    cache, want = filled(2 * rows_, 2, hd)
+    first = rng.randint(0, 20, rows_)
+    pos = (first[None] + np.arange(11)[:, None]).reshape(-1)
+    page = rng.permutation(2 * rows_).reshape(rows_, 2)
+    slots = (page[np.arange(rows_)[None], (first[None] + np.arange(11)[:, None]) // 16]).reshape(-1) * 16 + pos % 16
+    append(cache, want, slots, pos=pos, table=table_of(64, hd))
+
+
+@pytest.mark.parametrize("hd", [64, 128])
+def test_groups_that_are_cut(hd):
+    """Tokens of four positions with others, absent ones and ones left out between them, and in chains of small distances."""
+    cache, want = filled(6, 3, hd)
+    append(cache, want, [0, 40, 41, 1, 50, 2])         # 0 . . 1 . 2
+    append(cache, want, [4, 60, 5, 61, 6, 62, 7, 63])  # two groups, turn by turn
+    append(cache, want, [11, -1, 10, -1, 9, 200, 8])
+    append(cache, want, [13, 12, 15, 14])
+    append(cache, want, [16, 17, 18, 19, 20, 21], pos=np.array([0, -1, 2, 3, -1, 5]), table=table_of(64, hd))
+    append(cache, want, [35, 32, 80, 81, 82, 83, 84, 85, 86, 34, 33])
+
+
+@pytest.mark.parametrize("hd", [64, 128])
+@pytest.mark.parametrize("slots", [[0, 0, 1, 2, 3], [0, 1, 2, 0, 3], [5, 5, 5, 5], [8, 40, 8, 9, 10, 11], [12, 13, 14, 15, 15], [17, 18, 17, 18, 19]])
+def test_a_slot_twice_within_four_tokens_has_the_later_value(hd, slots):
+    """The other positions keep theirs; keys of such slots are undefined."""
+    cache, want = filled(3, 2, hd)
+    rng = np.random.RandomState(2)
+    k, v = (rows(rng, (len(slots), 2, hd)) for _ in range(2))
+    mg.kv4_append(*cache, k.cuda(), v.cuda(), dev_i32(slots))
+    want.append(bf16(k), bf16(v), np.array(slots))
+    got = ref.unpack(*cache)[0]
+    np.testing.assert_array_equal(got[:, :, 1], want.val[:, :, 1])
+    twice = [s for s in set(slots) if slots.count(s) > 1]
+    one = np.ones((3, 16), bool)
+    for s in twice:
+        one[s // 16, s % 16] = False
+    np.testing.assert_array_equal(got[:, :, 0].transpose(0, 2, 1, 3)[one], want.val[:, :, 0].transpose(0, 2, 1, 3)[one])
+
+
+def test_orders_give_the_same_bits():
+    """The same tokens in two orders leave the same bytes, many times over."""
+    n_pages, hkv, hd = 300, 8, 128
+    rng = np.random.RandomState(4)
+    s = rng.permutation(16 * n_pages)[:3000]
+    k, v = (rows(rng, (len(s), hkv, hd)) for _ in range(2))
+    by = np.argsort(s)
+    one = mg.kv4_empty(n_pages, hkv, hd)
+    mg.kv4_append(*one, k[by].cuda(), v[by].cuda(), dev_i32(s[by]))
+    for i in range(10):
+        p = rng.permutation(len(s))
+        two = mg.kv4_empty(n_pages, hkv, hd)
+        mg.kv4_append(*two, k[p].cuda(), v[p].cuda(), dev_i32(s[p]))
+        for a, b in zip(one, two):
+            assert torch.equal(a, b), i
