@@ -296,7 +296,8 @@ mg_status mg_kv8_read(const mg_kv8_cache* cache, int n, const int32_t* slots, ui
  * it, NaN and infinity among it; a value of V that reads as NaN or infinity makes its feature NaN or infinity
  * in the tokens that see it.  Query head h reads KV head h / (Hq / Hkv).  Rows without tokens and rows of out behind
  * the last token are left as they were.
- * Sums are fp32 of terms up to 2^9 above their weights on average, so features overflow where |v| passes some
+ * Scores are fp32 numbers; they have to stay within 2^23 of zero (the exponents' reference is rounded with them: from some 2^30 on a row's
+ * outputs become NaN or zeros).  Sums are fp32 of terms up to 2^9 above their weights on average, so features overflow where |v| passes some
  * 2^116 / (positions seen); a probability enters the product with V as two bf16 terms (16 bits) where a row has
  * few query rows (tokens times query heads of a KV head: up to 16, or 32 where no row of the call has
  * more), and as one (8 bits, as an output's) in longer chunks.  The order of a row's sums follows the
@@ -393,7 +394,7 @@ mg_status mg_kv4_read(const mg_kv4_cache* cache, int n, const int32_t* slots, ui
  * under the scale of 32 features: exact but for those below 2^-6 of their block's largest, which are off by at most 2^-14 of that.
  * A probability times its value's scale enters the product with V as two such terms, or more where 32 positions' scales are more than 2^2 apart: a
  * probability is off by at most 2^-8 of itself or 1/480 of the largest of 32 positions, whichever is more, whatever the sizes of their values (and by some
- * 2^-116 over its value's scale: where all |v| of a row are below some 2^-100 its outputs lose bits). */
+ * 2^-116 over its value's scale: where all |v| of a row are below some 2^-100 its outputs lose bits).  Scores may be any fp32 numbers. */
 size_t mg_kv4_attention_workspace_bytes(const mg_kv4_cache* cache, const mg_kv8_attn_args* args);
 mg_status mg_kv4_attention(const mg_kv4_cache* cache, const mg_kv8_attn_args* args, void* workspace,
                            size_t workspace_bytes, void* stream);
