@@ -14,7 +14,6 @@ namespace mg {
 namespace {
 
 typedef uint32_t u32x4_k4 __attribute__((ext_vector_type(4)));
-typedef uint32_t u32x2_k4 __attribute__((ext_vector_type(2)));
 typedef __bf16 bf16x2_k4 __attribute__((ext_vector_type(2)));
 
 constexpr int K4_THREADS = 256;

@@ -97,3 +97,12 @@ def test_orders_give_the_same_bits():
         mg.kv4_append(*two, k[p].cuda(), v[p].cuda(), dev_i32(s[p]))
         for a, b in zip(one, two):
             assert torch.equal(a, b), i
+
+
+def test_positions_behind_the_table_are_seen_in_the_cache():
+    """Keys of positions that the table has no angle for read as NaN, their values as they are, and no other position is touched."""
+    cache, want = filled(3, 2, 128)
+    append(cache, want, [5, 6, 20, 21], pos=np.array([10, 63, 64, 2 ** 31 - 1]), table=table_of(64, 128))
+    got = ref.unpack(*cache)[0]
+    assert np.isnan(got[1, :, 0, 4:6]).all() and np.isnan(got).sum() == 2 * 2 * 128
+    assert np.isfinite(got[1, :, 1, 4:6]).all()
