@@ -112,9 +112,16 @@ __device__ __forceinline__ uint32_t k4_pair(f32x16_k4& even, f32x16_k4& odd, flo
 // To look at the scales costs steps that need no further term 4 % in chunks (four of 2048 500 -> 522 us) and nothing that shows in rows of few
 // query rows; with a further term in all steps four chunks take 652 us, 64 rows 15.9 instead of 13.7, 32 long rows 87 instead of 81.
 constexpr uint32_t K4_NEAR = 2;
-// Positions that hold nothing, what is not finite (both 0 here) or the least scale have a part in no distance.
+// Positions that are not seen, that hold nothing, what is not finite (both bytes of 0 here) or the least scale have a part in no distance.
 constexpr uint32_t K4_EMPTY = 16;
-__device__ __forceinline__ uint32_t k4_counted(uint32_t b) { return b > K4_EMPTY ? b : 255u; }
+struct K4Apart {
+    uint32_t lo = 255, hi = 0;
+    __device__ __forceinline__ void add(uint32_t b, bool seen) {
+        const bool part = seen && b > K4_EMPTY;
+        hi = max(hi, part ? b : 0u);
+        lo = min(lo, part ? b : 255u);
+    }
+};
 // terms of a block whose scales' bytes are from lo to hi (0: k4_pair's)
 __device__ __forceinline__ int k4_terms(uint32_t lo, uint32_t hi) { return hi > lo + K4_NEAR ? (int)(hi - lo + 4 - K4_NEAR) / 5 : 0; }
 // the most of a wave's lanes
@@ -123,12 +130,13 @@ __device__ __forceinline__ int k4_wave_most(int n) {
     while (__any(n > most)) ++most;
     return most;
 }
-// n terms after the second of k4_pair, which left even and odd and the scales' bytes ps: add(term, its scale's byte) for each.
+// n terms after the second of k4_pair, which left even and odd and the scales' bytes ps, of which the lane's block takes `own`: add(term, its scale's byte)
+// for each.
 // (Scales stay normal numbers: what is below some 2^-120 is lost.)
 // What a term leaves is found by making it again and converting it back (BACK), or, with 32 registers less and some 300 cycles more, by rounding to eighths of
 // its scale: so for numbers up to twice that; larger ones were 2 s or more, the second term left 2^-8 of them at most, and they need no more.
 template <bool BACK, class Add>
-__device__ __forceinline__ void k4_more(f32x16_k4& even, f32x16_k4& odd, uint32_t ps, int n, const Add& add) {
+__device__ __forceinline__ void k4_more(f32x16_k4& even, f32x16_k4& odd, uint32_t ps, int own, int n, const Add& add) {
     uint32_t b = max(ps >> 8 & 0xffu, 5u);
 #pragma unroll 1
     for (int k = 0; k < n; ++k) {
@@ -156,7 +164,10 @@ __device__ __forceinline__ void k4_more(f32x16_k4& even, f32x16_k4& odd, uint32_
             }
         }
         b = max(b, 10u) - 5u;
-        add(k4_block(even, odd, __uint_as_float(b << 23)), b);
+        i32x6_k4 t = k4_block(even, odd, __uint_as_float(b << 23));
+#pragma unroll
+        for (int i = 0; i < 6; ++i) t[i] = k < own ? t[i] : 0;
+        add(t, b);
     }
 }
 
@@ -420,12 +431,13 @@ __device__ __forceinline__ void k4_walk(const Kv8AttnArgs& a, const K8Row& row, 
                 for (int e = 0; e < 4; ++e) A[e] = __builtin_amdgcn_perm(vb[2 * e + 1][d / 2], vb[2 * e][d / 2], d & 1 ? 0x07060302u : 0x05040100u);
                 return A;
             };
-            int terms = 0;
+            int own = 0, terms = 0;  // past two: the lane's, the most of the wave's
             if (__any(hi > lo + K4_NEAR)) {
-                lo = 255;
+                K4Apart d;
 #pragma unroll
-                for (int i = 0; i < 32; ++i) lo = min(lo, k4_counted(vs[i >> 2] >> (8 * (i & 3)) & 0xffu));
-                terms = k4_wave_most(k4_terms(lo, hi));
+                for (int i = 0; i < 32; ++i) d.add(vs[i >> 2] >> (8 * (i & 3)) & 0xffu, y[i & 1][i >> 1] > 0.0f);
+                own = k4_terms(d.lo, d.hi);
+                terms = k4_wave_most(own);
             }
             i32x6_k4 p[2];
             const uint32_t ps = k4_pair(y[0], y[1], top, p);
@@ -437,7 +449,7 @@ __device__ __forceinline__ void k4_walk(const Kv8AttnArgs& a, const K8Row& row, 
             }
             if (terms) {
                 __builtin_amdgcn_sched_barrier(0);
-                k4_more<HD == 64>(y[0], y[1], ps, terms, [&](const i32x6_k4& t, uint32_t b) {
+                k4_more<HD == 64>(y[0], y[1], ps, own, terms, [&](const i32x6_k4& t, uint32_t b) {
 #pragma unroll
                     for (int e = 0; e < K4_STEP; ++e) asm volatile("" : "+v"(vb[e]));  // (operands are made in each turn, not held in registers)
 #pragma unroll
@@ -634,7 +646,7 @@ __device__ __forceinline__ void k4_chunk_block(const Kv8AttnArgs& a, int few, in
     // with their maximum looked at in every step 503; heads of 64: 6 chunks of 300 to 600 46 and 44).
     constexpr bool REDO = HD == 128;
     // Where the weights' further terms are made: behind all else of a step, or (with fewer registers held) behind their tile's first two
-    constexpr bool LATE = HD == 128;
+    constexpr bool LATE = REDO;
     constexpr size_t head_bytes = 16 * HD, head_scales = HD / 2 + 16;
     const int lane = threadIdx.x & 63, c = lane & 15, g = lane >> 4;
     const int group = GROUPS == 1 ? 0 : __builtin_amdgcn_readfirstlane(threadIdx.x / K8_THREADS);
@@ -831,7 +843,7 @@ __device__ __forceinline__ void k4_chunk_block(const Kv8AttnArgs& a, int few, in
                 if (move || !__any(l[0] > 0.5f || l[1] > 0.5f)) break;
             }
             fresh = false;
-            int terms = 0;  // of the weights (0: two)
+            int terms = 0;  // of the weights past two
             {
                 uint32_t hi = 0, low = 0;  // (255 less the least)
 #pragma unroll
@@ -840,23 +852,27 @@ __device__ __forceinline__ void k4_chunk_block(const Kv8AttnArgs& a, int few, in
                     hi = max(hi, span & 0xffffu);
                     low = max(low, span >> 16);
                 }
-                uint32_t lo = 255u - low;
-                if (hi > lo + K4_NEAR) {
-                    if (lo <= K4_EMPTY) {
-                        lo = 255;
+                K4Apart d;
+                d.lo = 255u - low;
+                d.hi = hi;
+                if (d.hi > d.lo + K4_NEAR) {
+                    if (edge || d.lo <= K4_EMPTY) {  // of what some token of the wave sees
+                        d = K4Apart{};
+                        const int last = min(wp1, row.len - 1) - j0 - 4 * g, first = (a.window ? k8_hidden(a.window, wp0) : -1) - j0 - 4 * g;
 #pragma unroll 1
                         for (int e = 0; e < K4_STEP; ++e)
 #pragma unroll
-                            for (int i = 0; i < 4; ++i) lo = min(lo, k4_counted(__float_as_uint(s.vs[e][4 * g + i]) >> 23));
+                            for (int i = 0; i < 4; ++i)
+                                d.add(__float_as_uint(s.vs[e][4 * g + i]) >> 23, (now >> e & 1u) && 16 * e + i <= last && 16 * e + i > first);
                     }
-                    terms = k4_wave_most(k4_terms(lo, hi));
+                    terms = k4_wave_most(k4_terms(d.lo, d.hi));
                 }
             }
             f32x16_k4 y[NT][2];
             i32x6_k4 p[NT][2];
             uint32_t ps[NT];
             const auto more = [&](int u) {
-                k4_more<true>(y[u][0], y[u][1], ps[u], terms, [&](const i32x6_k4& t, uint32_t b) {
+                k4_more<true>(y[u][0], y[u][1], ps[u], terms, terms, [&](const i32x6_k4& t, uint32_t b) {
                     asm volatile("" ::: "memory");  // (operands are read in each turn, not held in registers)
 #pragma unroll
                     for (int d = 0; d < DT; ++d) {

@@ -105,3 +105,27 @@ def test_ordinary_steps_beside_others():
     keep[row:int(b.cu[2])] = False
     np.testing.assert_array_equal(got[keep], clean[keep])
     assert (got[~keep] != clean[~keep]).any()
+
+
+@pytest.mark.parametrize("hd", [64, 128])
+@pytest.mark.parametrize("window", [0, 70])
+@pytest.mark.parametrize("new", KINDS)
+def test_what_no_token_sees_changes_no_bit(new, hd, window):
+    """Positions behind the lengths, before the window, on unmapped pages and in the pages that holes stand for: scales and codes of any kind."""
+    b = batch(new, hd, "flat", seed=13)
+    put_values(b, lambda rng, v: v * 2.0 ** rng.uniform(-2, 2, v.shape[:2])[..., None], seed=4)
+    b.table[1, 20:23] = -1
+    seen = np.zeros((len(b.codes), 16), bool)
+    for r, n in enumerate(b.lens):
+        j = np.arange(max(0, n - b.new[r] - window + 1) if window else 0, n)
+        j = j[b.table[r, j // 16] >= 0]
+        seen[b.table[r, j // 16], j % 16] = True
+    clean = bf16(b.run(window=window))
+    assert np.isfinite(clean).all()
+    rng = np.random.RandomState(17)
+    for kind in range(3):
+        sc = b.scales.cpu().numpy()
+        s = sc[:, :, hd // 2:].transpose(0, 2, 1)
+        s[~seen] = [rng.randint(0, 256, s[~seen].shape), 255, rng.choice([17, 250], s[~seen].shape)][kind]
+        b.scales.copy_(torch.as_tensor(sc))
+        np.testing.assert_array_equal(bf16(b.run(window=window)), clean)
