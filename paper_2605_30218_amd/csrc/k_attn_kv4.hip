@@ -88,8 +88,8 @@ __device__ __forceinline__ uint32_t k4_triple(f32x16_k4& even, f32x16_k4& odd, u
 // format and become 7.5.  So s / 64, s / 256, s / 512 are left: 2^-8 of a value, as a bf16 weight would be off, or 1/1920 of the largest, at most.
 // What the first leaves is found by converting it back, one instruction of some 70 cycles.
 // Chunks of 2048 tokens over 2048 to 8192 positions were off by 0.0039 of their outputs, the bf16 results' rounding, 0.0016, among it, with two terms
-// of which the first is held below 2 s as above, by 0.0020 with these, in the same time; three terms took 585 us instead of 510 there, and a step of 64
-// rows 14.6 us instead of 13.7, off by 0.0017.
+// of which the first is held below 2 s as above, by 0.0019 with these, in the same time; with a third term in every step four chunks take 656 us instead of
+// 522, a step of 64 rows 16.6 instead of 13.7.
 __device__ __forceinline__ uint32_t k4_pair(f32x16_k4& even, f32x16_k4& odd, float top, i32x6_k4 (&t)[2]) {
     constexpr uint32_t least = 7u << 23;  // (the second's is a normal number)
     const uint32_t scale = max(__float_as_uint(top * (16.0f / 15.0f)) & 0x7f800000u, least + (2u << 23)) - (2u << 23);
@@ -110,7 +110,7 @@ __device__ __forceinline__ uint32_t k4_pair(f32x16_k4& even, f32x16_k4& odd, flo
 // bf16 weights by 0.0014, with two terms and scales within 2^2 by 0.0009 to 0.0014.  So a block takes one more term, under a 32nd of the scale before it,
 // for each 2^5 that its scales are further apart: a weight is off by 2^-8 of itself or 1/480 of the block's largest, whatever the scales of V.
 // To look at the scales costs steps that need no further term 4 % in chunks (four of 2048 500 -> 522 us) and nothing that shows in rows of few
-// query rows; with a further term in all steps four chunks take 652 us, 64 rows 15.9 instead of 13.7, 32 long rows 87 instead of 81.
+// query rows; with one or two further terms in all steps four chunks take 656 and 807 us, 64 rows 16.6 and 18.2, 32 long rows 88 and 96 instead of 81.
 constexpr uint32_t K4_NEAR = 2;
 // Positions that are not seen, that hold nothing, what is not finite (both bytes of 0 here) or the least scale have a part in no distance.
 constexpr uint32_t K4_EMPTY = 16;
@@ -467,9 +467,10 @@ __device__ __forceinline__ void k4_walk(const Kv8AttnArgs& a, const K8Row& row, 
 
 // Rows of few query rows (tokens times query heads of a KV head <= 16 NT): one block per (row, KV head, split of the row's pages).
 // A wave has one of the NT tiles of 16 query rows, and the waves of a tile take its steps in turn.
-// Long rows are bound by the cache's bytes: 32 rows of 4096 to 16384 take 81 us, 4.3 TB/s, and 77 with the loads alone, as the scales' records of 80
-// bytes lie in lines of 128 that blocks on two XCDs fetch (without them 6.7 us less).  Shorter ones by what a step takes after its loads, some 2300 cycles
-// of matrix and vector instructions, which do not overlap, and by the chain of length, page ids, codes before: 64 rows of 640 13.7 us, one of 512 6.0.
+// Long rows are bound by the cache's bytes: 32 rows of 4096 to 16384 take 81 us one after the other in a graph, 4.3 TB/s, and 76 so with the loads
+// alone, as the scales' records of 80 bytes lie in lines of 128 that blocks on two XCDs fetch (71 without them).  Shorter ones by what a step takes after its
+// loads, some 2300 cycles of matrix and vector instructions, which do not overlap, and by the chain of length, page ids, codes before: 64 rows of
+// 640 13.7 us (10.4 with the loads alone), one of 512 6.1 (4.7).
 template <int HD, int WAVES>
 struct K4FewShared {
     float o[WAVES][16][HD + 4];  // (padded rows)
@@ -596,9 +597,9 @@ __global__ __launch_bounds__(K8_THREADS) void attn_kv4_join_kernel(Kv8AttnArgs a
 // numbers; one barrier a step parts the buffers.  GROUPS 2: the block has four waves more for the same query rows, and each group takes half of
 // its steps; their outputs join at the end.
 // Bound by issue: a tile's step is 40 matrix instructions (16 cycles each) and some 185 vector ones (32 exponentials among them), three conversions of
-// 70 cycles; counters show the two kinds' cycles add up to the time (matrix cores 26 % busy, vector units 68 %).  Four chunks of 2048 tokens behind
-// 0 to 6144 take 495 us, 1110 TFLOP/s of the definition's operations, where the 8-bit cache takes 581.  A barrier's wait is short; blocks in the order of
-// what they see over all rows instead of row by row: 505 us there, but 71 instead of 67 for two prompts of 1500.
+// 70 cycles; counters show the two kinds' cycles add up to the time (matrix cores 25 % busy, vector units 66 %).  Four chunks of 2048 tokens behind
+// 0 to 6144 take 522 us, 1050 TFLOP/s of the definition's operations, where the 8-bit cache takes 575.  A barrier's wait is short; blocks in the order of
+// what they see over all rows instead of row by row: 1 % less there, but 6 % more for two prompts of 1500.
 constexpr int K4_TILES = 2;  // tiles of 16 query rows of a wave
 constexpr int K4_CHUNK_ROWS = K8_WAVES * 16 * K4_TILES;
 constexpr int K4_MIN_STAGES = 4;  // steps that a split of a tile takes at least
@@ -642,8 +643,8 @@ __device__ __forceinline__ void k4_chunk_block(const Kv8AttnArgs& a, int few, in
     typedef typename K4Lane<HD>::v vlane;
     typedef const __attribute__((address_space(1))) char* gptr;
     constexpr int DT = HD / 16, ROWS = K4_CHUNK_ROWS, NT = K4_TILES;
-    // Whether the sums, needed anyway, tell that the reference has to move, and the step's scores are then made again (four chunks of 2048 492 us,
-    // with their maximum looked at in every step 503; heads of 64: 6 chunks of 300 to 600 46 and 44).
+    // Whether the sums, needed anyway, tell that the reference has to move, and the step's scores are then made again (heads of 64: 6 chunks of 300 to
+    // 600 48.2 us, with their maximum looked at in every step 46.8; heads of 128: the maximum leaves too few registers).
     constexpr bool REDO = HD == 128;
     // Where the weights' further terms are made: behind all else of a step, or (with fewer registers held) behind their tile's first two
     constexpr bool LATE = REDO;
@@ -1025,26 +1026,27 @@ struct K4Plan {
 };
 // Each choice with what was measured beside it (us; rows of one token with 32 query heads over 8 KV heads of 128, if not said otherwise):
 // Rows of few query rows are split until there are two blocks of four waves a CU, or one of eight, which is what the registers let reside (four:
-// 64 rows of 640 positions 19.5 instead of 13.7, 32 rows of 50 to 9000 45 instead of 41, 8 rows of 2000 the same; two of eight: 23 rows of four tokens
-// behind 300 to 5000, 28 heads over 4, 27.2 instead of 20.3, 8 of six tokens behind 1000 to 4000 22.9 instead of 16.4).
+// 64 rows of 640 positions 19.8 instead of 13.7, 32 rows of 50 to 9000 45 instead of 42, 8 rows of 2000 the same; two of eight: 23 rows of four tokens
+// behind 300 to 5000, 28 heads over 4, 27.2 instead of 20.0, 8 of six tokens behind 1000 to 4000 21.9 instead of 15.9).
 constexpr int K4_BLOCKS_PER_CU = 2;
-// Pages that a split takes at least: a step of every wave (half of that: one row of 512 8.3 instead of 6.0, for the join's launch, one of 16384 17.4
-// instead of 12.1; twice: 8 rows of 2000 12.1 instead of 10.4),
+// Pages that a split takes at least: a step of every wave (half of that: one row of 512 8.5 instead of 6.1, for the join's launch, one of 16384 17.3
+// instead of 12.5; twice: 8 rows of 2000 11.4 instead of 10.0),
 constexpr int K4_MIN_PAGES = K4_STEP * K8_WAVES;
-// and at most (256: 32 rows of 4096 to 16384 89.6 instead of 83.7),
+// and at most (256: 32 rows of 4096 to 16384 86.7 instead of 81.5),
 constexpr int K4_MAX_PAGES = 1024;
-// and beside longer rows, whose blocks take longer (64, 256, 1024: 10 rows of 2000 to 15000 beside two chunks 250, 241, 237 in all; 1024: three
-// of 16000 beside a chunk of 40 67 instead of 57).
+// and beside longer rows, whose blocks take longer (64, 256, 512, 1024: 10 rows of 2000 to 15000 beside two chunks 247, 238, 238, 235 in all, three
+// of 16000 beside a chunk of 40 59, 57, 57, 67, 20 rows of 40 to 4000 with a window of 1024 beside four 42.5, 38.9, 38.8, 38.9).
 constexpr int K4_MIXED_PAGES = 512;
 constexpr int K4_MAX_SPLITS = 64;
-// From splits of so many pages on, the blocks find from all lengths how few pages a split may take (never: 32 rows of 4096 to 16384 87.5 instead of 80.3, of
-// 50 to 9000 47.8 instead of 41.3; from 16 pages on: 8 rows of 2000 14.3 instead of 10.4, for the lengths that every block then reads).
+// From splits of so many pages on, the blocks find from all lengths how few pages a split may take (never: 32 rows of 4096 to 16384 88.3 instead of 81.5, of
+// 50 to 9000 48.6 instead of 41.6; from 16 pages on: 8 rows of 2000 12.6 instead of 10.0, for the lengths that every block then reads).
 constexpr int K4_EVEN_PAGES = 64;
-// Longer rows: tiles are split while they leave CUs without a block (two blocks a CU: a prompt of 1000 45 instead of 26, as the splits' outputs are
-// written and joined). Splits of 2 and of 8 steps at least were as fast as of 4.
+// Longer rows: tiles are split while they leave CUs without a block (two blocks a CU: a prompt of 1000 46 instead of 26, a chunk of 300 behind 8000 77
+// instead of 66, as the splits' outputs are written and joined; a chunk of 40 beside three rows of 16000 46 instead of 57). Splits of 2 and of 8 steps at least
+// were as fast as of 4.
 constexpr int K4_CHUNK_BLOCKS_PER_CU = 1;
-// A block has two groups of waves up to so many blocks a CU (always: four chunks of 2048 588 instead of 505; never: a prompt of 2001 57 instead
-// of 50, the mixed batch of 20 tokens and 4 chunks 46 instead of 39).
+// A block has two groups of waves up to so many blocks a CU (always: four chunks of 2048 588 instead of 522; never: a prompt of 2001 59 instead
+// of 51, the mixed batch of 20 tokens and 4 chunks 48 instead of 39).
 constexpr int K4_GROUP_BLOCKS_PER_CU = 2;
 // pages that a group of `tokens` neighbouring tokens of a row sees at most, by the host's bounds
 int64_t pages_seen(const Kv8AttnArgs& a, int64_t tokens) {

@@ -5,8 +5,8 @@
 // value) becomes e2m1 codes under the least power of two whose sevenfold holds its largest magnitude: dividing by it is exact, so a
 // code is the nearest one whatever the scale, and nothing written before is rounded again.
 //
-// Many tokens are bound by bytes: 12000 of 28 query heads over 4 of 128 take 39.8 us, 203 MB at 5.1 TB/s (a copy of 200 MiB: 5.4), the read
-// of them 8.2 us; few by the chain of slot, row, maximum, code: 64 tokens of 32 heads over 8 4.8 us, their read 2.8, a launch that does nothing 1.6.
+// Many tokens are bound by bytes: 12000 of 28 query heads over 4 of 128 take 37.6 us, 203 MB at 5.4 TB/s (as a copy of 200 MiB), the read
+// of them 8.1 us; few by the chain of slot, row, maximum, code: 64 tokens of 32 heads over 8 4.5 us, their read 2.9, a launch that does nothing 1.6.
 #include "mg_device.h"
 #include "mg_kernels.h"
 
@@ -286,8 +286,8 @@ __global__ __launch_bounds__(K4_THREADS) void kv4_read_kernel(Kv8 c, int n, cons
 template <int HD>
 void append(const Kv4AppendArgs& a, hipStream_t s) {
     const int heads = a.Hq + a.c.Hkv;
-    // (heads of a lane: with 1, 2, 4, 8 of them 64 tokens of 40 heads take 4.8, 4.8, 5.8, 9.0 us, 12000 of 32 41.3, 39.7, 40.2, 42.1, 12000 of 40
-    // 62, 59, 58, 62)
+    // (heads of a lane: with 1, 2, 4, 8 of them 64 tokens of 40 heads take 4.4, 4.4, 5.8, 9.0 us, 12000 of 32 39.5, 37.6, 37.8, 38.7, 12000 of 40
+    // 56, 54, 53, 55)
     constexpr int U = 2;
     const int64_t lanes = (int64_t)a.n * ((heads + U - 1) / U) * (HD / 16);
     const int64_t rot = (lanes + K4_THREADS - 1) / K4_THREADS;
