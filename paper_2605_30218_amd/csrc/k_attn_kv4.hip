@@ -130,13 +130,12 @@ __device__ __forceinline__ int k4_wave_most(int n) {
     while (__any(n > most)) ++most;
     return most;
 }
-// n terms after the second of k4_pair, which left even and odd and the scales' bytes ps, of which the lane's block takes `own`: add(term, its scale's byte)
-// for each.
+// n terms after the second of k4_pair, which left even and odd and the scales' bytes ps: add(term, its scale's byte) for each.
 // (Scales stay normal numbers: what is below some 2^-120 is lost.)
 // What a term leaves is found by making it again and converting it back (BACK), or, with 32 registers less and some 300 cycles more, by rounding to eighths of
 // its scale: so for numbers up to twice that; larger ones were 2 s or more, the second term left 2^-8 of them at most, and they need no more.
 template <bool BACK, class Add>
-__device__ __forceinline__ void k4_more(f32x16_k4& even, f32x16_k4& odd, uint32_t ps, int own, int n, const Add& add) {
+__device__ __forceinline__ void k4_more(f32x16_k4& even, f32x16_k4& odd, uint32_t ps, int n, const Add& add) {
     uint32_t b = max(ps >> 8 & 0xffu, 5u);
 #pragma unroll 1
     for (int k = 0; k < n; ++k) {
@@ -164,10 +163,7 @@ __device__ __forceinline__ void k4_more(f32x16_k4& even, f32x16_k4& odd, uint32_
             }
         }
         b = max(b, 10u) - 5u;
-        i32x6_k4 t = k4_block(even, odd, __uint_as_float(b << 23));
-#pragma unroll
-        for (int i = 0; i < 6; ++i) t[i] = k < own ? t[i] : 0;
-        add(t, b);
+        add(k4_block(even, odd, __uint_as_float(b << 23)), b);
     }
 }
 
@@ -331,8 +327,9 @@ __device__ __forceinline__ void k4_walk(const Kv8AttnArgs& a, const K8Row& row, 
         uint32_t ks[K4_STEP], vs[K4_STEP];
         auto fetch_k = [&](int s) {
             // (made anew: a load then takes its page's address from scalar registers, and nothing of it is held meanwhile)
-            uint32_t k_lane = HD == 128 ? lane : lane & 31, at = place;
+            uint32_t k_lane = threadIdx.x, at = place;
             asm volatile("" : "+v"(k_lane), "+v"(at));
+            k_lane &= HD == 128 ? 63 : 31;
             const uint32_t k_at = k_lane * 16u;
 #pragma unroll
             for (int e = 0; e < K4_STEP; ++e) {
@@ -345,8 +342,9 @@ __device__ __forceinline__ void k4_walk(const Kv8AttnArgs& a, const K8Row& row, 
             }
         };
         auto fetch_v = [&](int s) {
-            uint32_t v_lane = lane, at = place;
+            uint32_t v_lane = threadIdx.x, at = place;
             asm volatile("" : "+v"(v_lane), "+v"(at));
+            v_lane &= 63;
             const uint32_t v_at = v_lane * (uint32_t)sizeof(vlane), vs_at = v_lane >> 4 << 2;
 #pragma unroll
             for (int e = 0; e < K4_STEP; ++e) {
@@ -370,6 +368,26 @@ __device__ __forceinline__ void k4_walk(const Kv8AttnArgs& a, const K8Row& row, 
 #pragma unroll
             for (int e = 0; e < K4_STEP; ++e) odd |= vs[e] & ((vs[e] & 0x7f7f7f7fu) + 0x01010101u) & 0x80808080u;
             const bool any_odd = __any(odd != 0);
+            // terms of the weights past two
+            const auto look = [&]() {
+                uint32_t hi = 0, lo = 255;  // of the scales' bytes
+#pragma unroll
+                for (int i = 0; i < 32; ++i) {
+                    const uint32_t b = vs[i >> 2] >> (8 * (i & 3)) & 0xffu;
+                    hi = max(hi, b);
+                    lo = min(lo, b);
+                }
+                if (!__any(hi > lo + K4_NEAR)) return 0;
+                K4Apart d;  // of what some token sees
+                const int last = min(p_hi, row.len - 1) - j0 - 4 * g, first = (a.window ? k8_hidden(a.window, p_lo) : -1) - j0 - 4 * g;
+#pragma unroll
+                for (int i = 0; i < 32; ++i) {
+                    const int at = 16 * (i >> 2) + (i & 3);
+                    d.add(vs[i >> 2] >> (8 * (i & 3)) & 0xffu, (mapped >> (i >> 2) & 1u) && at <= last && at > first);
+                }
+                return k4_wave_most(k4_terms(d.lo, d.hi));
+            };
+            int terms = CAP ? look() : 0;  // (behind the scores 3 % shorter, but a cap leaves no registers for it there)
             float x[32];
             {
                 asm volatile("" ::: "memory");  // (the queries are read anew, not held in registers)
@@ -416,29 +434,18 @@ __device__ __forceinline__ void k4_walk(const Kv8AttnArgs& a, const K8Row& row, 
             k4_probs<HD>(x, so.f, acc);
             f32x16_k4 y[2];
             float top = 0.0f;
-            uint32_t hi = 0, lo = 255;  // of the scales' bytes
 #pragma unroll
             for (int i = 0; i < 32; ++i) {
-                const uint32_t b = vs[i >> 2] >> (8 * (i & 3)) & 0xffu;
-                hi = max(hi, b);
-                lo = min(lo, b);
-                y[i & 1][i >> 1] = x[i] * __uint_as_float(b << 23);
+                y[i & 1][i >> 1] = x[i] * __uint_as_float((vs[i >> 2] >> (8 * (i & 3)) & 0xffu) << 23);
                 top = fmaxf(top, y[i & 1][i >> 1]);
             }
+            if (!CAP) terms = look();
             const auto values = [&](int d) {
                 u32x4_k8 A;
 #pragma unroll
                 for (int e = 0; e < 4; ++e) A[e] = __builtin_amdgcn_perm(vb[2 * e + 1][d / 2], vb[2 * e][d / 2], d & 1 ? 0x07060302u : 0x05040100u);
                 return A;
             };
-            int own = 0, terms = 0;  // past two: the lane's, the most of the wave's
-            if (__any(hi > lo + K4_NEAR)) {
-                K4Apart d;
-#pragma unroll
-                for (int i = 0; i < 32; ++i) d.add(vs[i >> 2] >> (8 * (i & 3)) & 0xffu, y[i & 1][i >> 1] > 0.0f);
-                own = k4_terms(d.lo, d.hi);
-                terms = k4_wave_most(own);
-            }
             i32x6_k4 p[2];
             const uint32_t ps = k4_pair(y[0], y[1], top, p);
 #pragma unroll
@@ -449,7 +456,7 @@ __device__ __forceinline__ void k4_walk(const Kv8AttnArgs& a, const K8Row& row, 
             }
             if (terms) {
                 __builtin_amdgcn_sched_barrier(0);
-                k4_more<HD == 64>(y[0], y[1], ps, own, terms, [&](const i32x6_k4& t, uint32_t b) {
+                k4_more<HD == 64>(y[0], y[1], ps, terms, [&](const i32x6_k4& t, uint32_t b) {
 #pragma unroll
                     for (int e = 0; e < K4_STEP; ++e) asm volatile("" : "+v"(vb[e]));  // (operands are made in each turn, not held in registers)
 #pragma unroll
@@ -480,7 +487,7 @@ struct K4FewShared {
 template <int HD, int NT, int WAVES, bool CAP, bool EVEN>
 __device__ __forceinline__ void k4_few_block(const Kv8AttnArgs& a, const K8Few& few, int block, K4FewShared<HD, WAVES>& sh) {
     constexpr int DT = HD / 16;
-    const int lane = threadIdx.x & 63, c = lane & 15, g = lane >> 4;
+    const int c = threadIdx.x & 15;
     const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
     const int kh = block % a.c.Hkv;
     int r = block / a.c.Hkv % a.B, split = block / a.c.Hkv / a.B, act;
@@ -513,18 +520,19 @@ __device__ __forceinline__ void k4_few_block(const Kv8AttnArgs& a, const K8Few& 
     if (16 * tile < row.n * a.G)
         k4_walk<HD, CAP, NT == 1>(a, row, r, kh, pg0, pg1, wave / NT, WAVES / NT, sh.q[wave], pos, row.p0 + row.n - 1, acc);
 
-    // the waves' shares join in LDS
+    // the waves' shares join in LDS (the lane's number is made again: it is not held over the walk)
+    const int ln = (int)__lane_id(), col = ln & 15, quarter = ln >> 4;
     const float ls = k8_col_sum(acc.l);
-    if (g == 0) {
-        sh.m[wave][c] = acc.m;
-        sh.l[wave][c] = ls;
+    if (quarter == 0) {
+        sh.m[wave][col] = acc.m;
+        sh.l[wave][col] = ls;
     }
 #pragma unroll
-    for (int d = 0; d < DT; ++d) *reinterpret_cast<f32x4_k8*>(&sh.o[wave][c][16 * d + 4 * g]) = acc.o[d];
+    for (int d = 0; d < DT; ++d) *reinterpret_cast<f32x4_k8*>(&sh.o[wave][col][16 * d + 4 * quarter]) = acc.o[d];
     __syncthreads();
     const int live = row.n * a.G;
     const float unit = k8_soft(a).f;
-    for (int i = threadIdx.x; i < live * (HD / 4); i += 64 * WAVES) {
+    for (int i = 64 * wave + ln; i < live * (HD / 4); i += 64 * WAVES) {
         const int rr = i / (HD / 4), d = i % (HD / 4) * 4;
         const int w0 = rr / 16, rc = rr % 16;
         float M = sh.m[w0][rc];
@@ -646,8 +654,8 @@ __device__ __forceinline__ void k4_chunk_block(const Kv8AttnArgs& a, int few, in
     // Whether the sums, needed anyway, tell that the reference has to move, and the step's scores are then made again (heads of 64: 6 chunks of 300 to
     // 600 48.2 us, with their maximum looked at in every step 46.8; heads of 128: the maximum leaves too few registers).
     constexpr bool REDO = HD == 128;
-    // Where the weights' further terms are made: behind all else of a step, or (with fewer registers held) behind their tile's first two
-    constexpr bool LATE = REDO;
+    // Where the weights' further terms are made: behind all else of a step, or (with fewer registers held, as caps need) behind their tile's first two
+    constexpr bool LATE = REDO && !CAP;
     constexpr size_t head_bytes = 16 * HD, head_scales = HD / 2 + 16;
     const int lane = threadIdx.x & 63, c = lane & 15, g = lane >> 4;
     const int group = GROUPS == 1 ? 0 : __builtin_amdgcn_readfirstlane(threadIdx.x / K8_THREADS);
@@ -873,7 +881,7 @@ __device__ __forceinline__ void k4_chunk_block(const Kv8AttnArgs& a, int few, in
             i32x6_k4 p[NT][2];
             uint32_t ps[NT];
             const auto more = [&](int u) {
-                k4_more<true>(y[u][0], y[u][1], ps[u], terms, terms, [&](const i32x6_k4& t, uint32_t b) {
+                k4_more<!CAP>(y[u][0], y[u][1], ps[u], terms, [&](const i32x6_k4& t, uint32_t b) {
                     asm volatile("" ::: "memory");  // (operands are read in each turn, not held in registers)
 #pragma unroll
                     for (int d = 0; d < DT; ++d) {
