@@ -15,7 +15,7 @@ pytestmark = pytest.mark.gpu
 
 # rows of single tokens, of a few, and chunks, over contexts that are split and that are not
 KINDS = [[1, 1, 1], [4, 2, 3], [90, 1, 40]]
-CTX = [30, 3000, 700]
+CTX = [30, 1300, 500]
 WHOLE = np.array([0, 1, 2, 3, 4, 6, -1, -2, -3, -4, -6.0])
 
 
@@ -50,7 +50,7 @@ def check(b, scale, got=None, **kw):
     assert worst <= 1.0, f"{worst} of the bound"
 
 
-@pytest.mark.parametrize("scale", [1e-3, 1.0, 7.0, 1e3, 1e9, 1e15])
+@pytest.mark.parametrize("scale", [1e-3, 7.0, 1e9, 1e15])
 @pytest.mark.parametrize("kind", ["flat", "rise", "fall", "negative"])
 @pytest.mark.parametrize("hd", [64, 128])
 @pytest.mark.parametrize("new", KINDS)
@@ -66,7 +66,7 @@ def test_scores_of_any_size_behind_a_window(new, hd, scale):
     check(batch(new, hd, "rise", seed=5), scale, window=100)
 
 
-@pytest.mark.parametrize("ctx,new", [([9000] * 3, [1] * 3), ([5000, 100, 4000, 20], [4] * 4), ([20, 2500], [2000, 300])])
+@pytest.mark.parametrize("ctx,new", [([9000, 20], [1, 1]), ([5000, 100, 20], [4] * 3), ([20, 1500], [600, 300])])
 def test_large_scores_of_long_rows(ctx, new):
     """Splits, rows of unequal length, and two groups of waves a block."""
     check(batch(new, 128, "flat", seed=9, ctx=ctx), 1e9)

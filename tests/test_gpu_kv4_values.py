@@ -33,7 +33,7 @@ def check(b, scale=0.01, **kw):
     assert worst <= 1.0, f"{worst} of the bound"
 
 
-@pytest.mark.parametrize("to", [3, 5, 9, 14, 30, 60])
+@pytest.mark.parametrize("to", [3, 9, 14, 60])
 @pytest.mark.parametrize("hd", [64, 128])
 @pytest.mark.parametrize("new", KINDS)
 def test_one_large_feature_of_one_position_in_32(new, hd, to):
@@ -48,7 +48,7 @@ def test_one_large_feature_of_one_position_in_32(new, hd, to):
     check(b)
 
 
-@pytest.mark.parametrize("spread", [1, 3, 6, 20, 50])
+@pytest.mark.parametrize("spread", [1, 6, 40])
 @pytest.mark.parametrize("hd", [64, 128])
 @pytest.mark.parametrize("new", KINDS)
 def test_sizes_of_every_kind(new, hd, spread):
@@ -78,7 +78,7 @@ def test_positions_that_hold_little_or_nothing(new, hd, window):
     check(b, window=window)
 
 
-@pytest.mark.parametrize("ctx,new", [([9000] * 3, [1] * 3), ([5000, 100, 4000, 20], [4] * 4), ([20, 2500], [2000, 300])])
+@pytest.mark.parametrize("ctx,new", [([9000, 20], [1, 1]), ([5000, 100, 20], [4] * 3), ([20, 1500], [600, 300])])
 def test_unequal_values_of_long_rows(ctx, new):
     """Splits, rows of unequal length, and two groups of waves a block."""
     b = batch(new, 128, "flat", seed=9, ctx=ctx)
