@@ -88,8 +88,8 @@ __device__ __forceinline__ uint32_t k4_triple(f32x16_k4& even, f32x16_k4& odd, u
 // format and become 7.5.  So s / 64, s / 256, s / 512 are left: 2^-8 of a value, as a bf16 weight would be off, or 1/1920 of the largest, at most.
 // What the first leaves is found by converting it back, one instruction of some 70 cycles.
 // Chunks of 2048 tokens over 2048 to 8192 positions were off by 0.0039 of their outputs, the bf16 results' rounding, 0.0016, among it, with two terms
-// of which the first is held below 2 s as above, by 0.0019 with these, in the same time; with a third term in every step four chunks take 656 us instead of
-// 522, a step of 64 rows 16.6 instead of 13.7.
+// of which the first is held below 2 s as above, by 0.0019 with these, in the same time; with a third term in every step four chunks take 667 us instead of
+// 525, a step of 64 rows 18.2 instead of 13.9.
 __device__ __forceinline__ uint32_t k4_pair(f32x16_k4& even, f32x16_k4& odd, float top, i32x6_k4 (&t)[2]) {
     constexpr uint32_t least = 7u << 23;  // (the second's is a normal number)
     const uint32_t scale = max(__float_as_uint(top * (16.0f / 15.0f)) & 0x7f800000u, least + (2u << 23)) - (2u << 23);
@@ -109,8 +109,8 @@ __device__ __forceinline__ uint32_t k4_pair(f32x16_k4& even, f32x16_k4& odd, flo
 // large one has no part in the features that its codes leave 0: beside scales 2^5, 2^7, 2^9 times theirs such features were off by 0.008, 0.03, 0.12, with
 // bf16 weights by 0.0014, with two terms and scales within 2^2 by 0.0009 to 0.0014.  So a block takes one more term, under a 32nd of the scale before it,
 // for each 2^5 that its scales are further apart: a weight is off by 2^-8 of itself or 1/480 of the block's largest, whatever the scales of V.
-// To look at the scales costs steps that need no further term 4 % in chunks (four of 2048 500 -> 522 us) and nothing that shows in rows of few
-// query rows; with one or two further terms in all steps four chunks take 656 and 807 us, 64 rows 16.6 and 18.2, 32 long rows 88 and 96 instead of 81.
+// To look at the scales costs steps that need no further term 4 % in chunks (four of 2048 500 -> 525 us) and next to nothing in rows of few
+// query rows; with one or two further terms in all steps four chunks take 667 and 811 us, 64 rows 18.2 and 19.7, 32 long rows 94 and 102 instead of 82.
 constexpr uint32_t K4_NEAR = 2;
 // Positions that are not seen, that hold nothing, what is not finite (both bytes of 0 here) or the least scale have a part in no distance.
 constexpr uint32_t K4_EMPTY = 16;
@@ -474,10 +474,10 @@ __device__ __forceinline__ void k4_walk(const Kv8AttnArgs& a, const K8Row& row, 
 
 // Rows of few query rows (tokens times query heads of a KV head <= 16 NT): one block per (row, KV head, split of the row's pages).
 // A wave has one of the NT tiles of 16 query rows, and the waves of a tile take its steps in turn.
-// Long rows are bound by the cache's bytes: 32 rows of 4096 to 16384 take 81 us one after the other in a graph, 4.3 TB/s, and 76 so with the loads
+// Long rows are bound by the cache's bytes: 32 rows of 4096 to 16384 take 82 us one after the other in a graph, 4.2 TB/s, and 76 so with the loads
 // alone, as the scales' records of 80 bytes lie in lines of 128 that blocks on two XCDs fetch (71 without them).  Shorter ones by what a step takes after its
 // loads, some 2300 cycles of matrix and vector instructions, which do not overlap, and by the chain of length, page ids, codes before: 64 rows of
-// 640 13.7 us (10.4 with the loads alone), one of 512 6.1 (4.7).
+// 640 13.9 us (10.4 with the loads alone), one of 512 6.2 (4.7).
 template <int HD, int WAVES>
 struct K4FewShared {
     float o[WAVES][16][HD + 4];  // (padded rows)
@@ -606,7 +606,7 @@ __global__ __launch_bounds__(K8_THREADS) void attn_kv4_join_kernel(Kv8AttnArgs a
 // its steps; their outputs join at the end.
 // Bound by issue: a tile's step is 40 matrix instructions (16 cycles each) and some 185 vector ones (32 exponentials among them), three conversions of
 // 70 cycles; counters show the two kinds' cycles add up to the time (matrix cores 25 % busy, vector units 66 %).  Four chunks of 2048 tokens behind
-// 0 to 6144 take 522 us, 1050 TFLOP/s of the definition's operations, where the 8-bit cache takes 575.  A barrier's wait is short; blocks in the order of
+// 0 to 6144 take 525 us, 1045 TFLOP/s of the definition's operations, where the 8-bit cache takes 575.  A barrier's wait is short; blocks in the order of
 // what they see over all rows instead of row by row: 1 % less there, but 6 % more for two prompts of 1500.
 constexpr int K4_TILES = 2;  // tiles of 16 query rows of a wave
 constexpr int K4_CHUNK_ROWS = K8_WAVES * 16 * K4_TILES;
