@@ -112,12 +112,12 @@ __device__ __forceinline__ uint32_t k4_pair(f32x16_k4& even, f32x16_k4& odd, flo
 // To look at the scales costs steps that need no further term 4 % in chunks (four of 2048 500 -> 525 us) and next to nothing in rows of few
 // query rows; with one or two further terms in all steps four chunks take 667 and 811 us, 64 rows 18.2 and 19.7, 32 long rows 94 and 102 instead of 82.
 constexpr uint32_t K4_NEAR = 2;
-// Positions that are not seen, that hold nothing, what is not finite (both bytes of 0 here) or the least scale have a part in no distance.
+// Positions that are not seen, that hold nothing (0), what is not finite (255, or 0 where that was noted) or the least scale have a part in no distance.
 constexpr uint32_t K4_EMPTY = 16;
 struct K4Apart {
     uint32_t lo = 255, hi = 0;
     __device__ __forceinline__ void add(uint32_t b, bool seen) {
-        const bool part = seen && b > K4_EMPTY;
+        const bool part = seen && b > K4_EMPTY && b < 255u;
         hi = max(hi, part ? b : 0u);
         lo = min(lo, part ? b : 255u);
     }

@@ -129,3 +129,22 @@ def test_what_no_token_sees_changes_no_bit(new, hd, window):
         s[~seen] = [rng.randint(0, 256, s[~seen].shape), 255, rng.choice([17, 250], s[~seen].shape)][kind]
         b.scales.copy_(torch.as_tensor(sc))
         np.testing.assert_array_equal(bf16(b.run(window=window)), clean)
+
+
+@pytest.mark.parametrize("cap", [0.0, 20.0])
+@pytest.mark.parametrize("hd", [64, 128])
+@pytest.mark.parametrize("new", [[4, 2, 3], [40, 30, 60]])
+def test_a_value_that_is_not_finite_is_no_large_one(new, hd, cap):
+    """A row's last position holds infinity: the row's last token is NaN, and the others, which do not see it, keep every bit."""
+    b = batch(new, hd, "flat", seed=23)
+    clean = bf16(b.run(softcap=cap))
+    for r, n in enumerate(b.lens):
+        slot = dev_i32([b.table[r, (n - 1) // 16] * 16 + (n - 1) % 16])
+        k, v = mg.kv4_read(b.codes, b.scales, slot)
+        v[:, :, 5] = np.inf
+        mg.kv4_append(b.codes, b.scales, k, v, slot)
+    got = bf16(b.run(softcap=cap))
+    last = np.zeros(len(got), bool)
+    last[b.cu[1:] - 1] = True
+    assert np.isnan(got[last]).all()
+    np.testing.assert_array_equal(got[~last], clean[~last])
